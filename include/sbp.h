@@ -51,7 +51,13 @@ typedef int32_t sbp_t;
 #define SBP_AUTO    ((sbp_t)-100)   /* sbp_matmul only: "whatever Table 1 says" */
 
 /* ---- element types --------------------------------------------------------*/
-enum { SBP_F32 = 0, SBP_BF16 = 1, SBP_I32 = 2 /* class labels of sbp_xent_* only */ };
+enum {
+    SBP_F32 = 0,
+    SBP_BF16 = 1,
+    SBP_I32 = 2,      /* class labels of sbp_xent_* only */
+    SBP_F8E4M3 = 3,   /* 8 bits next to scales (sbp_scales_t): largest value 448, no infinity   */
+    SBP_F8E5M2 = 4    /*                                       largest value 57344              */
+};
 
 /* ---- status codes ---------------------------------------------------------*/
 enum {
@@ -73,7 +79,7 @@ enum {
 typedef struct sbp_tensor {
     void* const* shard; /* host array [k] of device pointers                          */
     int64_t rows, cols; /* GLOBAL shape; vectors are [n, 1]                           */
-    int32_t dtype;      /* SBP_F32 | SBP_BF16 (SBP_I32 for label vectors)             */
+    int32_t dtype;      /* SBP_F32 | SBP_BF16 (SBP_I32 for label vectors; SBP_F8* with scales) */
     int32_t trans;      /* 0: shards hold the local tensor; 1: its transpose          */
     int64_t ld;         /* row pitch of every stored local buffer in elements, 0 = dense
                            (the stored row length).  Must be at least the longest stored row of
@@ -84,9 +90,22 @@ typedef struct sbp_tensor {
                            128 bytes keeps every row on cache-line boundaries (the classifier's
                            125000-column logits shards: pitch 125056).  Accepted by sbp_matmul,
                            sbp_matmul_ex, sbp_matmul_rowmax, sbp_matmul_2d, sbp_row_max,
-                           sbp_row_sumexp, sbp_xent_loss and sbp_xent_grad; the boxing entry
+                           sbp_row_sumexp, sbp_xent_loss and sbp_xent_grad, and for the activations,
+                           their gradients and the matrices of the operators on 8-bit tensors and of
+                           layer normalisation; the boxing entry
                            points take dense tensors only (SBP_ERR_UNSUPPORTED).                */
 } sbp_tensor_t;
+
+/* ---- the scales of an 8-bit tensor ----------------------------------------
+ * An 8-bit tensor (SBP_F8E4M3, SBP_F8E5M2) is its values and one power of two for every 128
+ * consecutive values of a stored row: the value stands for itself times that power.  Shard i's scales
+ * are bytes [stored rows][ceil(stored row length / 128)] of the LOCAL tensor as it is stored (trans
+ * included), counted from the row's start; byte b stands for 2^(b - 127).  255 is no scale. */
+#define SBP_F8_BLOCK 128
+typedef struct sbp_scales {
+    void* const* shard; /* host array [k] of device pointers, 16-byte aligned            */
+    int64_t ld;         /* pitch of a row of scales in bytes, 0 = dense                  */
+} sbp_scales_t;
 
 /* ---- epilogues of sbp_matmul_ex -------------------------------------------*/
 enum {
@@ -256,6 +275,67 @@ int32_t sbp_xent_loss(const sbp_tensor_t* logits, sbp_t sbp_l, const sbp_tensor_
 int32_t sbp_xent_grad(const sbp_tensor_t* logits, sbp_t sbp_l, const sbp_tensor_t* labels, const sbp_tensor_t* gmax,
                       const sbp_tensor_t* denom, const sbp_tensor_t* grad, const sbp_tensor_t* dlogits, int32_t k,
                       void* stream);
+
+/* Layer normalisation over the rows of x [R,C], S(0) or B, on the devices that hold them:
+ *   y = (x - mean) * rstd * gamma + beta,  mean the row's, rstd = 1 / sqrt(variance + eps)
+ * (the variance over C, computed from the distances to the mean).  x SBP_F32 or SBP_BF16; y under x's
+ * signature, in any of the two or in 8 bits (with y_scales, NULL else); gamma, beta [C,1] of one type,
+ * SBP_F32 or SBP_BF16, B, or NULL (ones, zeros); mean, rstd [R,1] SBP_F32 under x's signature, or both
+ * NULL.  Everything is computed in fp32; y is rounded once.  At most 32 devices and rows of 16384
+ * elements, and no S(1) (SBP_ERR_UNSUPPORTED); a P tensor is SBP_ERR_SIGNATURE. */
+int32_t sbp_layernorm(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_tensor_t* gamma, const sbp_tensor_t* beta, float eps,
+                      const sbp_tensor_t* y, const sbp_scales_t* y_scales, const sbp_tensor_t* mean,
+                      const sbp_tensor_t* rstd, int32_t k, void* stream);
+
+/* Its gradient from x, or from x kept in 8 bits (with x_scales; NULL else), and the forward pass's mean
+ * and rstd: with xhat = (x - mean) * rstd and g = dy * gamma,
+ *   dx = rstd * (g - sum(g) / C - xhat * sum(g * xhat) / C)        dtype of dy, under x's signature
+ *   dgamma = sum over the device's rows of dy * xhat,  dbeta = that of dy      [C,1] SBP_F32
+ * dgamma and dbeta hold a whole vector on every device: P(sum) for x S(0), B for x B.  Both may be NULL.
+ * Sums are made in fp32 in an order that depends on the sizes alone.  workspace: device memory of
+ * sbp_layernorm_grad_workspace() bytes, 16-byte aligned, whose contents do not matter before or after the
+ * call (NULL where that is 0 or dgamma is NULL; SBP_ERR_SHAPE if workspace_bytes is too little).  Calls
+ * that may overlap in time need one each. */
+int32_t sbp_layernorm_grad(const sbp_tensor_t* x, const sbp_scales_t* x_scales, sbp_t sbp_x, const sbp_tensor_t* gamma,
+                           const sbp_tensor_t* mean, const sbp_tensor_t* rstd, const sbp_tensor_t* dy,
+                           const sbp_tensor_t* dx, const sbp_tensor_t* dgamma, const sbp_tensor_t* dbeta, void* workspace,
+                           int64_t workspace_bytes, int32_t k, void* stream);
+int32_t sbp_layernorm_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_x, int32_t k, int64_t* bytes);
+
+/* An activation into 8 bits (SBP_F8E4M3 or SBP_F8E5M2 and scales), S or B, and back.
+ * sbp_quantize: q = round(v / 2^e) to nearest even, v = x (SBP_F32 or SBP_BF16) or gelu(x), e for every
+ *   block of 128 the smallest integer >= -127 with max|v| / 2^e within q's type, so that nothing saturates.
+ *   The maximum is over the finite values; NaN stays NaN, infinity becomes NaN in SBP_F8E4M3 and stays in
+ *   SBP_F8E5M2.  The scales are outputs.  q.trans = 1 stores the transpose, blocks along x's rows: the
+ *   operand of a weight's gradient.
+ * sbp_dequantize: x (SBP_F32 or SBP_BF16) = the values q stands for, or gelu of them.  Without GeLU exact
+ *   in fp32, and in bf16 down to 2^-126 (2^128, to which the largest fp32 numbers round, is infinity).  q.trans as above, x.trans = 0.
+ * epilogue: SBP_EPI_NONE or SBP_EPI_GELU (to 2.2e-5 of its value before rounding; 1e-7 for fp32 results). */
+int32_t sbp_quantize(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_tensor_t* q, const sbp_scales_t* q_scales, int32_t k,
+                     void* stream, int32_t epilogue);
+int32_t sbp_dequantize(const sbp_tensor_t* q, const sbp_scales_t* q_scales, sbp_t sbp_q, const sbp_tensor_t* x, int32_t k,
+                       void* stream, int32_t epilogue);
+
+/* The gradient of GeLU (exact erf form): da = dh * (Phi(a) + a phi(a)), Phi and phi the normal
+ * distribution and its density, evaluated in fp32 to 5e-7 before the single rounding.  a: the pre-activation, SBP_F32,
+ * SBP_BF16 or in 8 bits (with a_scales; NULL else); dh and da SBP_F32 or SBP_BF16, one type; all
+ * S or B under one signature (a nonlinear function of a partial is SBP_ERR_SIGNATURE). */
+int32_t sbp_gelu_grad(const sbp_tensor_t* a, const sbp_scales_t* a_scales, sbp_t sbp_a, const sbp_tensor_t* dh,
+                      const sbp_tensor_t* da, int32_t k, void* stream);
+
+/* Y = XW of 8-bit tensors under SBP: sbp_matmul_ex for X [M,K] and W [K,N] in SBP_F8E4M3 or SBP_F8E5M2
+ * (each its own) with scales.  Signatures as in Table 1 without its P rows (a partial is not in 8 bits:
+ * SBP_ERR_DTYPE).  Both operands have to be stored with the reduction index contiguous, so that the blocks of 128
+ * run along it: x.trans = 0, w.trans = 1 (SBP_ERR_UNSUPPORTED else); sbp_quantize stores either way.
+ * y SBP_BF16 or SBP_F32, SBP_F32 where it is P(sum), trans = 0.
+ *   fp32 results: exact products, summed in fp32.
+ *   bf16 results: on the 8-bit matrix instruction, which aligns a group of products to the largest of
+ *   them and drops what lies some 2^-12 below: an error of about 2^-16 of a typical result and at most
+ *   2^-11 of the sum of the products' magnitudes, next to the rounding to bf16 of up to 2^-8 of the result.
+ * At most 32 devices. */
+int32_t sbp_matmul_f8(const sbp_tensor_t* x, const sbp_scales_t* x_scales, sbp_t sbp_x, const sbp_tensor_t* w,
+                      const sbp_scales_t* w_scales, sbp_t sbp_w, const sbp_tensor_t* y, sbp_t sbp_y, int32_t k, void* stream,
+                      int32_t epilogue);
 
 /* Tuning knobs; they never change what is computed beyond the order of fp32 sums inside a GEMM tile
  * and, for fp32 operands, whether a product is formed by the fp32 instruction or from bf16 terms

@@ -20,6 +20,8 @@ AUTO = -100
 F32 = 0
 BF16 = 1
 I32 = 2
+F8E4M3 = 3
+F8E5M2 = 4
 # epilogues
 EPI_NONE = 0
 EPI_GELU = 1
@@ -31,13 +33,18 @@ KNOB_BOX_REDUCE = 2
 #: every symbol include/sbp.h declares
 EXPORTS = ("sbp_infer_matmul", "sbp_local_shape", "sbp_matmul", "sbp_matmul_ex", "sbp_matmul_rowmax", "sbp_boxing", "sbp_boxing_across", "sbp_boxing_cast",
            "sbp_infer_matmul_2d", "sbp_local_shape_2d", "sbp_matmul_2d", "sbp_boxing_2d",
-           "sbp_row_max", "sbp_row_sumexp", "sbp_xent_loss", "sbp_xent_grad", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
+           "sbp_row_max", "sbp_row_sumexp", "sbp_xent_loss", "sbp_xent_grad",
+           "sbp_layernorm", "sbp_layernorm_grad", "sbp_layernorm_grad_workspace", "sbp_quantize", "sbp_dequantize", "sbp_gelu_grad", "sbp_matmul_f8", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
 
 
 class _CTensor(ctypes.Structure):
     _fields_ = [("shard", ctypes.POINTER(ctypes.c_void_p)),
                 ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("dtype", ctypes.c_int32), ("trans", ctypes.c_int32), ("ld", ctypes.c_int64)]
+
+
+class _CScales(ctypes.Structure):
+    _fields_ = [("shard", ctypes.POINTER(ctypes.c_void_p)), ("ld", ctypes.c_int64)]
 
 
 class SbpError(RuntimeError):
@@ -87,6 +94,14 @@ def lib() -> ctypes.CDLL:
         L.sbp_row_sumexp.argtypes = [T, i32, T, T, i32, vp]
         L.sbp_xent_loss.argtypes = [T, i32, T, T, T, T, i32, vp]
         L.sbp_xent_grad.argtypes = [T, i32, T, T, T, T, T, i32, vp]
+        C, f32 = ctypes.POINTER(_CScales), ctypes.c_float
+        L.sbp_layernorm.argtypes = [T, i32, T, T, f32, T, C, T, T, i32, vp]
+        L.sbp_layernorm_grad.argtypes = [T, C, i32, T, T, T, T, T, T, T, vp, i64, i32, vp]
+        L.sbp_layernorm_grad_workspace.argtypes = [i64, i64, i32, i32, ctypes.POINTER(i64)]
+        L.sbp_quantize.argtypes = [T, i32, T, C, i32, vp, i32]
+        L.sbp_dequantize.argtypes = [T, C, i32, T, i32, vp, i32]
+        L.sbp_gelu_grad.argtypes = [T, C, i32, T, T, i32, vp]
+        L.sbp_matmul_f8.argtypes = [T, C, i32, T, C, i32, T, i32, i32, vp, i32]
         L.sbp_set_knob.argtypes = [i32, i32]
         L.sbp_probe_mfma.argtypes = [i32, i32, i32, vp, vp]
         L.sbp_probe_mfma_static.argtypes = [i32, i32, i32, vp, vp]
@@ -114,6 +129,25 @@ class SbpTensor:
 
     def ref(self):
         return ctypes.byref(self.c)
+
+
+class SbpScales:
+    """The scales of an 8-bit tensor: k device pointers to bytes (b stands for 2^(b - 127)), one for every 128 values of
+    a stored row, rows `ld` bytes apart (0 = dense).  Shards as for SbpTensor."""
+
+    def __init__(self, shards: Sequence, ld: int = 0):
+        self.keep = list(shards)
+        ptrs = [s if isinstance(s, int) or s is None else s.data_ptr() for s in shards]
+        self.k = len(ptrs)
+        self._arr = (ctypes.c_void_p * max(1, self.k))(*ptrs)
+        self.c = _CScales(ctypes.cast(self._arr, ctypes.POINTER(ctypes.c_void_p)), ld)
+
+    def ref(self):
+        return ctypes.byref(self.c)
+
+
+def _ref(t):
+    return None if t is None else t.ref()
 
 
 _raw_stream = None   # (current device, its current stream) of torch, looked up at the first call
@@ -259,6 +293,50 @@ def sbp_xent_grad(logits: SbpTensor, sbp_l: int, labels: SbpTensor, gmax: SbpTen
     _need(k, logits, labels, gmax, denom, grad, dlogits)
     _check(lib().sbp_xent_grad(logits.ref(), sbp_l, labels.ref(), gmax.ref(), denom.ref(), grad.ref(), dlogits.ref(), k,
                                _stream_ptr(stream)), "sbp_xent_grad")
+
+
+def sbp_layernorm(x: SbpTensor, sbp_x: int, gamma: SbpTensor | None, beta: SbpTensor | None, eps: float, y: SbpTensor, y_scales: SbpScales | None,
+                  mean: SbpTensor | None, rstd: SbpTensor | None, k: int, stream=None) -> None:
+    _need(k, x, gamma, beta, y, y_scales, mean, rstd)
+    _check(lib().sbp_layernorm(x.ref(), sbp_x, _ref(gamma), _ref(beta), eps, y.ref(), _ref(y_scales), _ref(mean), _ref(rstd), k, _stream_ptr(stream)),
+           "sbp_layernorm")
+
+
+def sbp_layernorm_grad_workspace(rows: int, cols: int, sbp_x: int, k: int) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sbp_layernorm_grad_workspace(rows, cols, sbp_x, k, ctypes.byref(out)), "sbp_layernorm_grad_workspace")
+    return out.value
+
+
+def sbp_layernorm_grad(x: SbpTensor, x_scales: SbpScales | None, sbp_x: int, gamma: SbpTensor | None, mean: SbpTensor, rstd: SbpTensor, dy: SbpTensor,
+                       dx: SbpTensor, dgamma: SbpTensor | None, dbeta: SbpTensor | None, workspace, k: int, stream=None) -> None:
+    """workspace: a device buffer of sbp_layernorm_grad_workspace() bytes (a torch tensor), or None where none is needed."""
+    _need(k, x, x_scales, gamma, mean, rstd, dy, dx, dgamma, dbeta)
+    room = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(lib().sbp_layernorm_grad(x.ref(), _ref(x_scales), sbp_x, _ref(gamma), mean.ref(), rstd.ref(), dy.ref(), dx.ref(), _ref(dgamma), _ref(dbeta),
+                                    ctypes.c_void_p(workspace.data_ptr() if room else 0), room, k, _stream_ptr(stream)), "sbp_layernorm_grad")
+
+
+def sbp_quantize(x: SbpTensor, sbp_x: int, q: SbpTensor, q_scales: SbpScales, k: int, stream=None, epilogue: int = EPI_NONE) -> None:
+    _need(k, x, q, q_scales)
+    _check(lib().sbp_quantize(x.ref(), sbp_x, q.ref(), _ref(q_scales), k, _stream_ptr(stream), epilogue), "sbp_quantize")
+
+
+def sbp_dequantize(q: SbpTensor, q_scales: SbpScales, sbp_q: int, x: SbpTensor, k: int, stream=None, epilogue: int = EPI_NONE) -> None:
+    _need(k, q, q_scales, x)
+    _check(lib().sbp_dequantize(q.ref(), _ref(q_scales), sbp_q, x.ref(), k, _stream_ptr(stream), epilogue), "sbp_dequantize")
+
+
+def sbp_gelu_grad(a: SbpTensor, a_scales: SbpScales | None, sbp_a: int, dh: SbpTensor, da: SbpTensor, k: int, stream=None) -> None:
+    _need(k, a, a_scales, dh, da)
+    _check(lib().sbp_gelu_grad(a.ref(), _ref(a_scales), sbp_a, dh.ref(), da.ref(), k, _stream_ptr(stream)), "sbp_gelu_grad")
+
+
+def sbp_matmul_f8(x: SbpTensor, x_scales: SbpScales, sbp_x: int, w: SbpTensor, w_scales: SbpScales, sbp_w: int, y: SbpTensor, sbp_y: int, k: int,
+                  stream=None, epilogue: int = EPI_NONE) -> None:
+    _need(k, x, x_scales, w, w_scales, y)
+    _check(lib().sbp_matmul_f8(x.ref(), _ref(x_scales), sbp_x, w.ref(), _ref(w_scales), sbp_w, y.ref(), sbp_y, k, _stream_ptr(stream), epilogue),
+           "sbp_matmul_f8")
 
 
 def sbp_probe_mfma(mode: int, iters: int, zero_operands: int, scratch, stream=None) -> None:

@@ -1,0 +1,223 @@
+// Device-side building blocks of 8-bit tensors (values with one power of two for every 128 of a stored row) and of row kernels that
+// read and write eight consecutive elements a lane at any alignment.  Everything is internal (anonymous namespace).
+#pragma once
+#include "gemm_device.h"
+
+namespace sbp {
+namespace {
+
+typedef u32x2 __attribute__((aligned(1))) u32x2_any;
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+
+// element types as template arguments
+enum ElemType : int { T_F32 = SBP_F32, T_BF16 = SBP_BF16, T_E4M3 = SBP_F8E4M3, T_E5M2 = SBP_F8E5M2 };
+template <int T>
+constexpr int bytes_of = T == T_F32 ? 4 : T == T_BF16 ? 2 : 1;
+
+// Eight consecutive elements as they are stored.
+template <int T>
+struct Raw8;
+template <>
+struct Raw8<T_F32> {
+    f32x4 a, b;
+};
+template <>
+struct Raw8<T_BF16> {
+    u32x4 w;
+};
+template <>
+struct Raw8<T_E4M3> {
+    u32x2 w;
+};
+template <>
+struct Raw8<T_E5M2> {
+    u32x2 w;
+};
+
+// `valid` of eight elements at `at` exist (8 and more: all, none: 0 and less); the others are zero and not read.
+template <int T>
+__device__ inline Raw8<T> load8(const void* at, int valid) {
+    Raw8<T> r{};
+    const char* p = static_cast<const char*>(at);
+    if (valid >= 8) {
+        if constexpr (T == T_F32) {
+            r.a = *reinterpret_cast<const f32x4_any*>(p);
+            r.b = *reinterpret_cast<const f32x4_any*>(p + 16);
+        } else if constexpr (T == T_BF16) r.w = *reinterpret_cast<const u32x4_any*>(p);
+        else r.w = *reinterpret_cast<const u32x2_any*>(p);
+    } else if (valid > 0) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < valid) {
+                if constexpr (T == T_F32) {
+                    const float v = reinterpret_cast<const float*>(p)[e];
+                    if (e < 4) r.a[e] = v;
+                    else r.b[e - 4] = v;
+                } else if constexpr (T == T_BF16) r.w[e >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
+                else r.w[e >> 2] |= (uint32_t) reinterpret_cast<const uint8_t*>(p)[e] << (8 * (e & 3));
+            }
+    }
+    return r;
+}
+template <int T>
+__device__ inline void store8(void* at, const Raw8<T> r, int valid) {
+    char* p = static_cast<char*>(at);
+    if (valid >= 8) {
+        if constexpr (T == T_F32) {
+            *reinterpret_cast<f32x4_any*>(p) = r.a;
+            *reinterpret_cast<f32x4_any*>(p + 16) = r.b;
+        } else if constexpr (T == T_BF16) *reinterpret_cast<u32x4_any*>(p) = r.w;
+        else *reinterpret_cast<u32x2_any*>(p) = r.w;
+    } else if (valid > 0) {
+#pragma unroll
+        for (int e = 0; e < 7; ++e)
+            if (e < valid) {
+                if constexpr (T == T_F32) reinterpret_cast<float*>(p)[e] = e < 4 ? r.a[e] : r.b[e - 4];
+                else if constexpr (T == T_BF16) reinterpret_cast<uint16_t*>(p)[e] = (uint16_t)(r.w[e >> 1] >> (16 * (e & 1)));
+                else reinterpret_cast<uint8_t*>(p)[e] = (uint8_t)(r.w[e >> 2] >> (8 * (e & 3)));
+            }
+    }
+}
+
+// A scale byte b stands for 2^(b - 127).  The conversions below take a power of two as the exponent field of an fp32 number, 0 there
+// standing for 2^-127.
+__device__ inline float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }
+
+// Widening: exact (an 8-bit value times a power of two is an fp32 number).  `scale`: scale_of() for 8-bit types, not looked at else.
+template <int T>
+__device__ inline void widen(const Raw8<T> r, float scale, float (&v)[8]) {
+    if constexpr (T == T_F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = r.a[e];
+            v[e + 4] = r.b[e];
+        }
+    } else if constexpr (T == T_BF16) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[2 * e] = __uint_as_float(r.w[e] << 16);
+            v[2 * e + 1] = __uint_as_float(r.w[e] & 0xFFFF0000u);
+        }
+    } else {
+#pragma unroll
+        for (int d = 0; d < 2; ++d) {
+            f32x2 lo, hi;
+            if constexpr (T == T_E4M3) {
+                lo = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(r.w[d], scale, false);
+                hi = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(r.w[d], scale, true);
+            } else {
+                lo = __builtin_amdgcn_cvt_scalef32_pk_f32_bf8(r.w[d], scale, false);
+                hi = __builtin_amdgcn_cvt_scalef32_pk_f32_bf8(r.w[d], scale, true);
+            }
+            v[4 * d] = lo[0];
+            v[4 * d + 1] = lo[1];
+            v[4 * d + 2] = hi[0];
+            v[4 * d + 3] = hi[1];
+        }
+    }
+}
+
+// Rounding to the nearest, ties to even.
+template <int T>
+__device__ inline Raw8<T> narrow(const float (&v)[8]) {
+    static_assert(T == T_F32 || T == T_BF16, "8-bit types need a scale");
+    Raw8<T> r;
+    if constexpr (T == T_F32) {
+        r.a = f32x4{v[0], v[1], v[2], v[3]};
+        r.b = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+#pragma unroll
+        for (int d = 0; d < 4; ++d) r.w[d] = f32_to_bf16x2(v[2 * d], v[2 * d + 1]);
+    }
+    return r;
+}
+// four values over 2^e, rounded to nearest even; NaN stays NaN, infinity becomes NaN (e4m3 has none) or stays (e5m2)
+template <int T>
+__device__ inline uint32_t narrow4(float a, float b, float c, float d, float scale) {
+    s16x2 r = {0, 0};
+    if constexpr (T == T_E4M3) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, a, b, scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(r, c, d, scale, true);
+    } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, a, b, scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_f32(r, c, d, scale, true);
+    }
+    return __builtin_bit_cast(uint32_t, r);
+}
+// four bf16 values
+template <int T>
+__device__ inline uint32_t narrow4(uint32_t lo, uint32_t hi, float scale) {
+    s16x2 r = {0, 0};
+    if constexpr (T == T_E4M3) {
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, lo), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, hi), scale, true);
+    } else {
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, __builtin_bit_cast(bf16x2, lo), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, __builtin_bit_cast(bf16x2, hi), scale, true);
+    }
+    return __builtin_bit_cast(uint32_t, r);
+}
+
+// The scale byte of a block whose largest finite magnitude is `most`: the smallest e >= -127 with most / 2^e within the type, whose
+// largest value is 1.75 * 2^8 (e4m3) or 1.75 * 2^15 (e5m2), so nothing saturates.  On the bits: the exponent, one more where the
+// fraction passes 0.75.
+template <int T>
+__device__ inline uint32_t scale_byte(float most) {
+    const int e = (int)((__float_as_uint(most) + 0x1FFFFFu) >> 23) - (T == T_E4M3 ? 8 : 15);
+    return (uint32_t)(e > 0 ? e : 0);
+}
+
+// Sums and maxima over the lanes of a wave.  The first four steps stay inside rows of 16 lanes (DPP: neighbours, pairs, mirrored halves,
+// mirrored row), which is one block of 128 values at eight a lane.
+template <int CTRL>
+__device__ inline uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
+}
+template <int CTRL>
+__device__ inline float dpp(float v) {
+    return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
+}
+__device__ inline float max_row16(float v) {
+    v = fmaxf(v, dpp<0xB1>(v));
+    v = fmaxf(v, dpp<0x4E>(v));
+    v = fmaxf(v, dpp<0x141>(v));
+    return fmaxf(v, dpp<0x140>(v));
+}
+__device__ inline float sum_wave(float v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    v += dpp<0x141>(v);
+    v += dpp<0x140>(v);
+    auto h = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(h[0]) + __uint_as_float(h[1]);
+    h = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(h[0]) + __uint_as_float(h[1]);
+}
+
+// Largest finite magnitude of the 128 values that 16 lanes hold eight each.  A NaN is passed over by the maximum; a block with an
+// infinity is gone through again without it.
+__device__ inline float most_of_block(const float (&v)[8]) {
+    float m = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))), fmaxf(fmaxf(fabsf(v[4]), fabsf(v[5])), fmaxf(fabsf(v[6]), fabsf(v[7]))));
+    m = max_row16(m);
+    if (m == INFINITY) {   // the 16 lanes of a block go here together
+        m = 0.0f;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]) < INFINITY ? fabsf(v[e]) : 0.0f);
+        m = max_row16(m);
+    }
+    return m == m ? m : 0.0f;   // all NaN
+}
+
+// 8-bit form of the values that 16 lanes hold eight each, and their block's scale byte.
+template <int T>
+__device__ inline Raw8<T> narrow_block(const float (&v)[8], uint32_t& byte) {
+    byte = scale_byte<T>(most_of_block(v));
+    const float s = scale_of(byte);
+    Raw8<T> r;
+    r.w[0] = narrow4<T>(v[0], v[1], v[2], v[3], s);
+    r.w[1] = narrow4<T>(v[4], v[5], v[6], v[7], s);
+    return r;
+}
+
+}  // namespace
+}  // namespace sbp

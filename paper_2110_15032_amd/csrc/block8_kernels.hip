@@ -1,0 +1,333 @@
+// Activations in 8 bits: saving them, restoring them, and the gradient of GeLU from a saved pre-activation.
+//
+// An 8-bit tensor is e4m3 or e5m2 values and, for every 128 consecutive ones of a stored row, a power of two 2^e, e the smallest integer
+// >= -127 with max|x| / 2^e within the type; value = round(x / 2^e).  A power of two, because the division and the way back are then
+// exact (one rounding in all, the way back to bf16 none) and the matrix instruction takes it as it is.
+#include "block8_device.h"
+
+namespace sbp {
+namespace {
+
+constexpr int NT = 256;
+
+// The blocks of 128 of a row-major tensor, 16 lanes to a block: (row, block) by one division, then advanced by the grid stride with adds.
+struct BlockWalk {
+    uint32_t nb, dr, db, b;
+    int64_t r;
+    __device__ BlockWalk(int cols, int64_t first, int64_t stride) {
+        nb = (uint32_t)((cols + F8_BLOCK - 1) / F8_BLOCK);
+        if (first < UINT32_MAX && stride < UINT32_MAX) {
+            dr = (uint32_t)stride / nb;
+            db = (uint32_t)stride % nb;
+            r = (uint32_t)first / nb;
+            b = (uint32_t)first % nb;
+        } else {
+            dr = (uint32_t)(stride / nb);
+            db = (uint32_t)(stride % nb);
+            r = first / nb;
+            b = (uint32_t)(first % nb);
+        }
+    }
+    __device__ void next() {
+        r += dr;
+        b += db;
+        if (b >= nb) {
+            b -= nb;
+            ++r;
+        }
+    }
+};
+
+// Rounding to 8 bits makes GeLU's fit to 2.2e-5 as good as an exact one; so does rounding to bf16.
+template <bool FAST>
+__device__ inline float gelu_of(float x) {
+    if constexpr (FAST) return gelu_fast(x);
+    else return gelu_erf(x);
+}
+
+template <int XT, int QT, bool GELU>
+__global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
+    const Block8Shard& s = p.s[blockIdx.y];
+    if (s.rows == 0 || s.cols == 0) return;
+    const int lane = threadIdx.x & 15;
+    const int64_t stride = (int64_t)gridDim.x * (NT / 16);
+    BlockWalk w(s.cols, (int64_t)blockIdx.x * (NT / 16) + (threadIdx.x >> 4), stride);
+    for (; w.r < s.rows; w.next()) {
+        const int c = (int)w.b * F8_BLOCK + lane * 8;
+        const Raw8<XT> raw = load8<XT>(static_cast<const char*>(s.x) + (w.r * s.ldx + c) * bytes_of<XT>, s.cols - c);
+        float v[8];
+        widen<XT>(raw, 1.0f, v);
+        if constexpr (GELU) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gelu_of<true>(v[e]);
+        }
+        uint32_t byte;
+        const Raw8<QT> q = narrow_block<QT>(v, byte);
+        store8<QT>(static_cast<char*>(s.out) + w.r * s.ldo + c, q, s.cols - c);
+        if (lane == 0) static_cast<uint8_t*>(s.scales)[w.r * s.lds + w.b] = (uint8_t)byte;
+    }
+}
+
+// Transposed: the block runs along the rows.  A workgroup takes 128 rows by 64 columns; thread t holds rows 4 (t / 8) .. + 3 of the eight
+// columns 8 (t % 8), the column maxima meet over the lanes of a wave and over the waves in LDS, the bytes turn in LDS.
+constexpr int TC = 64;
+constexpr int QPITCH = F8_BLOCK + 16;   // bytes of one column in LDS
+template <int XT, int QT, bool GELU>
+__global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, int tiles_r, int tiles_c) {
+    const Block8Shard& s = p.s[blockIdx.y];
+    __shared__ float most[4][TC];
+    __shared__ __attribute__((aligned(16))) char turn[TC * QPITCH];
+    const int t = threadIdx.x, wave = t >> 6, co = t & 7, rg = t >> 3;
+    for (int64_t tile = blockIdx.x; tile < (int64_t)tiles_r * tiles_c; tile += gridDim.x) {
+        const int tr = (int)(tile / tiles_c), tc = (int)(tile % tiles_c);
+        const int64_t r0 = (int64_t)tr * F8_BLOCK;
+        const int64_t c0 = (int64_t)tc * TC;
+        if (r0 >= s.rows || c0 >= s.cols) continue;
+        const int64_t c = c0 + co * 8;
+        Raw8<XT> raw[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = r0 + rg * 4 + i;
+            raw[i] = load8<XT>(static_cast<const char*>(s.x) + (r * s.ldx + c) * bytes_of<XT>, r < s.rows ? (int)(c < s.cols ? s.cols - c : 0) : 0);
+        }
+        float v[4][8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            widen<XT>(raw[i], 1.0f, v[i]);
+            if constexpr (GELU) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[i][e] = gelu_of<true>(v[i][e]);
+            }
+        }
+        float m[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) m[e] = fmaxf(m[e], fabsf(v[i][e]) < INFINITY ? fabsf(v[i][e]) : 0.0f);
+            m[e] = fmaxf(m[e], dpp<0x128>(m[e]));   // eight lanes on in the row of 16
+            auto h = __builtin_amdgcn_permlane16_swap(__float_as_uint(m[e]), __float_as_uint(m[e]), false, false);
+            m[e] = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+            h = __builtin_amdgcn_permlane32_swap(__float_as_uint(m[e]), __float_as_uint(m[e]), false, false);
+            m[e] = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+        }
+        if ((t & 63) < 8) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) most[wave][co * 8 + e] = m[e];
+        }
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const int j = co * 8 + e;
+            const uint32_t byte = scale_byte<QT>(fmaxf(fmaxf(most[0][j], most[1][j]), fmaxf(most[2][j], most[3][j])));
+            *reinterpret_cast<uint32_t*>(turn + j * QPITCH + rg * 4) = narrow4<QT>(v[0][e], v[1][e], v[2][e], v[3][e], scale_of(byte));
+            if (rg == 0 && c + e < s.cols) static_cast<uint8_t*>(s.scales)[(c + e) * s.lds + tr] = (uint8_t)byte;
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < TC * 8 / NT; ++i) {
+            const int j = (i * NT + t) >> 3, at = ((i * NT + t) & 7) * 16;
+            const int64_t r = r0 + at;
+            if (c0 + j >= s.cols || r >= s.rows) continue;
+            const u32x4 w = *reinterpret_cast<const u32x4*>(turn + j * QPITCH + at);
+            char* dst = static_cast<char*>(s.out) + (c0 + j) * (int64_t)s.ldo + r;
+            if (r + 16 <= s.rows) {
+                __builtin_memcpy(dst, &w, 16);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 15; ++e)
+                    if (r + e < s.rows) dst[e] = (char)(w[e >> 2] >> (8 * (e & 3)));
+            }
+        }
+        // the next tile's maxima are written before the barrier that follows these reads of the turned bytes, its bytes after it
+    }
+}
+
+template <int QT, int YT, bool GELU>
+__global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
+    const Block8Shard& s = p.s[blockIdx.y];
+    if (s.rows == 0 || s.cols == 0) return;
+    const int lane = threadIdx.x & 15;
+    const int64_t stride = (int64_t)gridDim.x * (NT / 16);
+    BlockWalk w(s.cols, (int64_t)blockIdx.x * (NT / 16) + (threadIdx.x >> 4), stride);
+    for (; w.r < s.rows; w.next()) {
+        const int c = (int)w.b * F8_BLOCK + lane * 8;
+        const Raw8<QT> raw = load8<QT>(static_cast<const char*>(s.x) + w.r * s.ldx + c, s.cols - c);
+        const float scale = scale_of(static_cast<const uint8_t*>(s.scales)[w.r * s.lds + w.b]);
+        float v[8];
+        widen<QT>(raw, scale, v);
+        if constexpr (GELU) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gelu_of<YT == T_BF16>(v[e]);
+        }
+        store8<YT>(static_cast<char*>(s.out) + (w.r * s.ldo + c) * bytes_of<YT>, narrow<YT>(v), s.cols - c);
+    }
+}
+
+// Restoring a tensor that was saved transposed: 128 saved bytes (128 rows of the result) of 64 saved rows (its columns) turn in LDS.
+template <int QT, int YT, bool GELU>
+__global__ __launch_bounds__(NT) void dequantize_transposed_kernel(Block8Plan p, int tiles_r, int tiles_c) {
+    const Block8Shard& s = p.s[blockIdx.y];
+    __shared__ __attribute__((aligned(16))) char turn[TC * QPITCH];
+    __shared__ float scale[TC];
+    const int t = threadIdx.x, co = t & 7, rg = t >> 3;
+    for (int64_t tile = blockIdx.x; tile < (int64_t)tiles_r * tiles_c; tile += gridDim.x) {
+        const int tr = (int)(tile / tiles_c), tc = (int)(tile % tiles_c);
+        const int64_t r0 = (int64_t)tr * F8_BLOCK, c0 = (int64_t)tc * TC;
+        if (r0 >= s.rows || c0 >= s.cols) continue;
+        __syncthreads();   // the tile before has been read
+#pragma unroll
+        for (int i = 0; i < TC * 16 / NT; ++i) {
+            const int j = (i * NT + t) >> 4, at = ((i * NT + t) & 15) * 8;
+            const int64_t left = c0 + j < s.cols ? s.rows - (r0 + at) : 0;
+            const Raw8<QT> raw = load8<QT>(static_cast<const char*>(s.x) + (c0 + j) * (int64_t)s.ldx + r0 + at, (int)(left < 8 ? left : 8));
+            *reinterpret_cast<u32x2*>(turn + j * QPITCH + at) = raw.w;
+        }
+        if (t < TC) scale[t] = c0 + t < s.cols ? scale_of(static_cast<const uint8_t*>(s.scales)[(c0 + t) * s.lds + tr]) : 0.0f;
+        __syncthreads();
+        const int64_t c = c0 + co * 8;
+        uint32_t four[8];   // rows 4 rg .. + 3 of each column
+#pragma unroll
+        for (int e = 0; e < 8; ++e) four[e] = *reinterpret_cast<const uint32_t*>(turn + (co * 8 + e) * QPITCH + rg * 4);
+        float v[4][8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            Raw8<QT> raw{};
+            raw.w[0] = four[e];
+            float u[8];
+            widen<QT>(raw, scale[co * 8 + e], u);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i][e] = GELU ? gelu_of<YT == T_BF16>(u[i]) : u[i];
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t r = r0 + rg * 4 + i;
+            if (r < s.rows) store8<YT>(static_cast<char*>(s.out) + (r * s.ldo + c) * bytes_of<YT>, narrow<YT>(v[i]), (int)(c < s.cols ? s.cols - c : 0));
+        }
+    }
+}
+
+// gelu'(a) = Phi(a) + a phi(a), with the upper tail of Phi as phi(|a|)'s exponential times a polynomial in t = 1 / (1 + p |a| / sqrt 2):
+// Abramowitz and Stegun 7.1.26, erf to 1.5e-7.  One exponential serves both terms.  Past |a| = 14 both tails are below fp32's range (the
+// clamp keeps infinity times zero out); NaN stays NaN.
+__device__ inline float gelu_slope(float a) {
+    const float x = __builtin_amdgcn_fmed3f(a, -14.0f, 14.0f);
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), 0.3275911f * 0.70710678118654752f, 1.0f));
+    const float w = x * 0.84932180028801905f;   // sqrt(log2(e) / 2)
+    const float e = __builtin_amdgcn_exp2f(-w * w);
+    float q = 0.5f * 1.061405429f;
+    q = fmaf(q, t, 0.5f * -1.453152027f);
+    q = fmaf(q, t, 0.5f * 1.421413741f);
+    q = fmaf(q, t, 0.5f * -0.284496736f);
+    q = fmaf(q, t, 0.5f * 0.254829592f);
+    const float tail = q * t * e;   // 1 - Phi(|x|)
+    const float cdf = x < 0.0f ? tail : 1.0f - tail;
+    return a == a ? fmaf(x * 0.39894228040143268f, e, cdf) : a;
+}
+
+// da = dh gelu'(a).  AT: the pre-activation's type, 8 bits or as it was.
+template <int AT, int YT>
+__global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
+    const Block8Shard& s = p.s[blockIdx.y];
+    if (s.rows == 0 || s.cols == 0) return;
+    const int lane = threadIdx.x & 15;
+    const int64_t stride = (int64_t)gridDim.x * (NT / 16);
+    BlockWalk w(s.cols, (int64_t)blockIdx.x * (NT / 16) + (threadIdx.x >> 4), stride);
+    for (; w.r < s.rows; w.next()) {
+        const int c = (int)w.b * F8_BLOCK + lane * 8;
+        const Raw8<AT> ra = load8<AT>(static_cast<const char*>(s.x) + (w.r * s.ldx + c) * bytes_of<AT>, s.cols - c);
+        const Raw8<YT> rh = load8<YT>(static_cast<const char*>(s.dh) + (w.r * s.lddh + c) * bytes_of<YT>, s.cols - c);
+        float scale = 1.0f;
+        if constexpr (bytes_of<AT> == 1) scale = scale_of(static_cast<const uint8_t*>(s.scales)[w.r * s.lds + w.b]);
+        float a[8], h[8];
+        widen<AT>(ra, scale, a);
+        widen<YT>(rh, 1.0f, h);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] *= gelu_slope(a[e]);
+        store8<YT>(static_cast<char*>(s.out) + (w.r * s.ldo + c) * bytes_of<YT>, narrow<YT>(h), s.cols - c);
+    }
+}
+
+// grid of the kernels that walk blocks of 128
+dim3 walk_grid(const Block8Plan& plan) {
+    int64_t most = 0;
+    for (int i = 0; i < plan.k; ++i) most = std::max(most, plan.s[i].rows * f8_blocks(plan.s[i].cols));
+    int64_t bx = (most + NT / 16 - 1) / (NT / 16);
+    bx = std::min<int64_t>(bx, (1 << 16) / plan.k);
+    return dim3((uint32_t)std::max<int64_t>(bx, 1), (uint32_t)plan.k);
+}
+struct TileGrid {
+    dim3 grid;
+    int rows, cols;
+};
+TileGrid tile_grid(const Block8Plan& plan) {
+    TileGrid g{};
+    for (int i = 0; i < plan.k; ++i) {
+        g.rows = std::max(g.rows, tiles_along(plan.s[i].rows, F8_BLOCK));
+        g.cols = std::max(g.cols, tiles_along(plan.s[i].cols, TC));
+    }
+    const int64_t bx = std::min<int64_t>((int64_t)g.rows * g.cols, (1 << 18) / plan.k);
+    g.grid = dim3((uint32_t)std::max<int64_t>(bx, 1), (uint32_t)plan.k);
+    return g;
+}
+
+template <typename F>
+void with_f8(int32_t f8, F&& f) {
+    if (f8 == SBP_F8E4M3) f(std::integral_constant<int, T_E4M3>{});
+    else f(std::integral_constant<int, T_E5M2>{});
+}
+template <typename F>
+void with_wide(int32_t dtype, F&& f) {
+    if (dtype == SBP_BF16) f(std::integral_constant<int, T_BF16>{});
+    else f(std::integral_constant<int, T_F32>{});
+}
+template <typename F>
+void with_bool(bool b, F&& f) {
+    if (b) f(std::true_type{});
+    else f(std::false_type{});
+}
+
+}  // namespace
+
+int32_t launch_quantize(const Block8Plan& plan, hipStream_t stream) {
+    with_f8(plan.f8, [&](auto q) {
+        with_wide(plan.dtype, [&](auto x) {
+            with_bool(plan.gelu != 0, [&](auto gelu) {
+                if (plan.trans) {
+                    const TileGrid g = tile_grid(plan);
+                    hipLaunchKernelGGL((quantize_transposed_kernel<x(), q(), gelu()>), g.grid, dim3(NT), 0, stream, plan, g.rows, g.cols);
+                } else {
+                    hipLaunchKernelGGL((quantize_kernel<x(), q(), gelu()>), walk_grid(plan), dim3(NT), 0, stream, plan);
+                }
+            });
+        });
+    });
+    return launch_status(__func__);
+}
+
+int32_t launch_dequantize(const Block8Plan& plan, hipStream_t stream) {
+    with_f8(plan.f8, [&](auto q) {
+        with_wide(plan.dtype, [&](auto y) {
+            with_bool(plan.gelu != 0, [&](auto gelu) {
+                if (plan.trans) {
+                    const TileGrid g = tile_grid(plan);
+                    hipLaunchKernelGGL((dequantize_transposed_kernel<q(), y(), gelu()>), g.grid, dim3(NT), 0, stream, plan, g.rows, g.cols);
+                } else {
+                    hipLaunchKernelGGL((dequantize_kernel<q(), y(), gelu()>), walk_grid(plan), dim3(NT), 0, stream, plan);
+                }
+            });
+        });
+    });
+    return launch_status(__func__);
+}
+
+int32_t launch_gelu_grad(const Block8Plan& plan, hipStream_t stream) {
+    with_wide(plan.dtype, [&](auto y) {
+        auto go = [&](auto a) { hipLaunchKernelGGL((gelu_grad_kernel<a(), y()>), walk_grid(plan), dim3(NT), 0, stream, plan); };
+        if (plan.f8 == SBP_F8E4M3 || plan.f8 == SBP_F8E5M2) with_f8(plan.f8, go);
+        else with_wide(plan.f8, go);
+    });
+    return launch_status(__func__);
+}
+
+}  // namespace sbp

@@ -1,0 +1,360 @@
+// Layer normalisation over rows and its gradient.
+//
+//   y = (x - mean) rstd gamma + beta,  mean = sum x / n,  rstd = 1 / sqrt(sum (x - mean)^2 / n + eps)
+//   xhat = (x - mean) rstd,  g = dy gamma,  dx = rstd (g - sum g / n - xhat sum (g xhat) / n),  dgamma = sum over rows dy xhat,  dbeta = sum dy
+//
+// Both are bound by HBM: a row is read once and stays in registers, TPR threads a row with V vectors of eight elements each.  A workgroup
+// walks over rows, so that gamma and beta are read once, and reads the next row before it works on this one.
+#include "block8_device.h"
+
+namespace sbp {
+namespace {
+
+// Workgroups of a launch: enough for every compute unit to have several.
+constexpr int NORM_BLOCKS = 2048, GRAD_BLOCKS = 512;
+constexpr int GRAD_NT = 512;
+
+template <int WT, int V, int TPR>
+__device__ inline void load_weight(const void* w, int t, int cols, float otherwise, float (&out)[V * 8]) {
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        const int c = (v * TPR + t) * 8;
+        float u[8];
+        if (w) {
+            widen<WT>(load8<WT>(static_cast<const char*>(w) + (int64_t)c * bytes_of<WT>, cols - c), 1.0f, u);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) u[e] = otherwise;
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[v * 8 + e] = u[e];
+    }
+}
+
+// The statistics are exact to fp32 sums whatever the row's offset: every wave sums its elements, then the squares of their distances from
+// its own mean, and the waves' pairs are joined with the distances of their means (one exchange for both).
+template <int XT, int YT, int WT, int TPR, int V>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p) {
+    constexpr int NT = TPR < 256 ? 256 : TPR, G = NT / TPR, NW = TPR / 64;
+    const NormShard& s = p.s[blockIdx.y];
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, wave = t >> 6, cols = p.cols;
+    __shared__ float2 part[2][NW];
+    float gamma[V * 8], beta[V * 8];
+    load_weight<WT, V, TPR>(s.gamma, t, cols, 1.0f, gamma);
+    load_weight<WT, V, TPR>(s.beta, t, cols, 0.0f, beta);
+    int have = 0;   // elements of this lane
+#pragma unroll
+    for (int v = 0; v < V; ++v) have += min(max(cols - (v * TPR + t) * 8, 0), 8);
+    const float of_wave = sum_wave((float)have), over_wave = of_wave > 0.0f ? 1.0f / of_wave : 0.0f, over = 1.0f / (float)cols;
+
+    const int step = gridDim.x * G;
+    Raw8<XT> next[V];
+    auto fetch = [&](int64_t row) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + t) * 8;
+            next[v] = load8<XT>(static_cast<const char*>(s.x) + (row * s.ldx + c) * bytes_of<XT>, row < s.rows ? cols - c : 0);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * G + group;
+    fetch(row);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * G; first < s.rows; first += step, row += step, turn ^= 1) {
+        float x[V * 8];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float u[8];
+            widen<XT>(next[v], 1.0f, u);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[v * 8 + e] = u[e];
+        }
+        fetch(row + step);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V * 8; ++i) sum += x[i];
+        sum = sum_wave(sum);
+        const float centre = sum * over_wave;
+        float sq = 0.0f;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int left = cols - (v * TPR + t) * 8;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float d = e < left ? x[v * 8 + e] - centre : 0.0f;
+                sq = fmaf(d, d, sq);
+            }
+        }
+        sq = sum_wave(sq);
+        float mean = centre, m2 = sq;
+        if constexpr (NW > 1) {
+            if ((threadIdx.x & 63) == 0) part[turn][wave] = float2{centre, sq};
+            __syncthreads();   // one a row: the other half is written next, and this one again only behind the next barrier
+            float of[NW];   // elements of each wave
+            mean = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                int n = 0;
+#pragma unroll
+                for (int v = 0; v < V; ++v) n += min(max(cols - (v * TPR + w * 64) * 8, 0), 512);
+                of[w] = (float)n;
+                mean = fmaf(of[w], part[turn][w].x, mean);
+            }
+            mean *= over;
+            m2 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                const float d = part[turn][w].x - mean;
+                m2 += fmaf(of[w] * d, d, part[turn][w].y);
+            }
+        }
+        const float rstd = 1.0f / sqrtf(fmaf(m2, over, p.eps));
+        if (row >= s.rows) continue;
+        if (t == 0 && s.mean) {
+            s.mean[row] = mean;
+            s.rstd[row] = rstd;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + t) * 8;
+            float y[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[e] = fmaf((x[v * 8 + e] - mean) * rstd, gamma[v * 8 + e], beta[v * 8 + e]);
+            char* dst = static_cast<char*>(s.y) + (row * s.ldy + c) * bytes_of<YT>;
+            if constexpr (bytes_of<YT> == 1) {
+                if (c / F8_BLOCK * F8_BLOCK >= cols) continue;   // no column of this lane's block exists
+#pragma unroll
+                for (int e = 0; e < 8; ++e) y[e] = c + e < cols ? y[e] : 0.0f;
+                uint32_t byte;
+                const Raw8<YT> q = narrow_block<YT>(y, byte);
+                store8<YT>(dst, q, cols - c);
+                if ((t & 15) == 0) static_cast<uint8_t*>(s.y_scales)[row * s.lds + c / F8_BLOCK] = (uint8_t)byte;
+            } else {
+                store8<YT>(dst, narrow<YT>(y), cols - c);
+            }
+        }
+    }
+}
+
+// One partial sum of the weights' gradients for every workgroup, in the order of its rows; where a shard has one workgroup, that is the result.
+// GROUPS rows of TPR threads side by side in a workgroup: their sums meet in LDS at the end, so that fewer partial sums go to memory.
+template <int XT, int YT, int WT, int TPR, int V>
+__global__ __launch_bounds__(GRAD_NT) void norm_grad_kernel(NormGradPlan p) {
+    constexpr int G = GRAD_NT / TPR, NW = TPR / 64, CAP = TPR * V * 8;
+    const NormGradShard& s = p.s[blockIdx.y];
+    if ((int)blockIdx.x >= s.blocks) return;
+    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, wave = t >> 6, cols = p.cols;
+    __shared__ float2 part[2][G][NW];
+    float gamma[V * 8], dgamma[V * 8], dbeta[V * 8];
+    load_weight<WT, V, TPR>(s.gamma, t, cols, 1.0f, gamma);
+#pragma unroll
+    for (int i = 0; i < V * 8; ++i) dgamma[i] = dbeta[i] = 0.0f;
+    const float over = 1.0f / (float)cols;
+
+    const int step = s.blocks * G;
+    Raw8<XT> next_x[V];
+    Raw8<YT> next_dy[V];
+    float next_scale[V], next_mean = 0.0f, next_rstd = 0.0f;
+    auto fetch = [&](int64_t row) {
+        const bool there = row < s.rows;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + t) * 8, left = there ? cols - c : 0;
+            next_x[v] = load8<XT>(static_cast<const char*>(s.x) + (row * s.ldx + c) * bytes_of<XT>, left);
+            next_dy[v] = load8<YT>(static_cast<const char*>(s.dy) + (row * s.lddy + c) * bytes_of<YT>, left);
+            next_scale[v] = 1.0f;
+            if constexpr (bytes_of<XT> == 1) next_scale[v] = left > 0 ? scale_of(static_cast<const uint8_t*>(s.x_scales)[row * s.lds + c / F8_BLOCK]) : 0.0f;
+        }
+        next_mean = there ? s.mean[row] : 0.0f;
+        next_rstd = there ? s.rstd[row] : 0.0f;
+    };
+    int64_t row = (int64_t)blockIdx.x * G + group;
+    fetch(row);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * G; first < s.rows; first += step, row += step, turn ^= 1) {
+        float xhat[V * 8], dy[V * 8];
+        const float mean = next_mean, rstd = next_rstd;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float u[8], w[8];
+            widen<XT>(next_x[v], next_scale[v], u);
+            widen<YT>(next_dy[v], 1.0f, w);
+            const int left = row < s.rows ? cols - (v * TPR + t) * 8 : 0;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                xhat[v * 8 + e] = e < left ? (u[e] - mean) * rstd : 0.0f;
+                dy[v * 8 + e] = w[e];
+            }
+        }
+        fetch(row + step);
+        float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+        for (int i = 0; i < V * 8; ++i) {
+            const float g = dy[i] * gamma[i];
+            s1 += g;
+            s2 = fmaf(g, xhat[i], s2);
+            dgamma[i] = fmaf(dy[i], xhat[i], dgamma[i]);
+            dbeta[i] += dy[i];
+        }
+        s1 = sum_wave(s1);
+        s2 = sum_wave(s2);
+        if constexpr (NW > 1) {
+            if ((threadIdx.x & 63) == 0) part[turn][group][wave] = float2{s1, s2};
+            __syncthreads();   // one a row, as in norm_kernel
+            s1 = s2 = 0.0f;
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                s1 += part[turn][group][w].x;
+                s2 += part[turn][group][w].y;
+            }
+        }
+        s1 *= over;
+        s2 *= over;
+        if (row >= s.rows) continue;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + t) * 8;
+            float d[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = v * 8 + e;
+                d[e] = rstd * (fmaf(dy[i], gamma[i], -s1) - xhat[i] * s2);
+            }
+            store8<YT>(static_cast<char*>(s.dx) + (row * s.lddx + c) * bytes_of<YT>, narrow<YT>(d), cols - c);
+        }
+    }
+    if (!s.dgamma) return;
+    float* const to_gamma = s.blocks > 1 ? s.part + (int64_t)blockIdx.x * 2 * cols : s.dgamma;
+    float* const to_beta = s.blocks > 1 ? to_gamma + cols : s.dbeta;
+    if constexpr (G > 1) {
+        __shared__ float sums[G][2][CAP];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                sums[group][0][(v * TPR + t) * 8 + e] = dgamma[v * 8 + e];
+                sums[group][1][(v * TPR + t) * 8 + e] = dbeta[v * 8 + e];
+            }
+        __syncthreads();
+        for (int c = threadIdx.x; c < cols; c += GRAD_NT) {
+            float a = 0.0f, b = 0.0f;
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                a += sums[g][0][c];
+                b += sums[g][1][c];
+            }
+            to_gamma[c] = a;
+            to_beta[c] = b;
+        }
+    } else {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + t) * 8;
+            Raw8<T_F32> a, b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a.a[e] = dgamma[v * 8 + e];
+                a.b[e] = dgamma[v * 8 + 4 + e];
+                b.a[e] = dbeta[v * 8 + e];
+                b.b[e] = dbeta[v * 8 + 4 + e];
+            }
+            store8<T_F32>(to_gamma + c, a, cols - c);
+            store8<T_F32>(to_beta + c, b, cols - c);
+        }
+    }
+}
+
+// The partial sums of a shard's workgroups joined in order: 32 columns a workgroup, eight runs of partial sums side by side.
+__global__ __launch_bounds__(256) void norm_grad_join_kernel(NormGradPlan p) {
+    const NormGradShard& s = p.s[blockIdx.y];
+    if (s.blocks <= 1) return;
+    __shared__ float sums[8][33];
+    const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, width = 2 * p.cols;
+    const int64_t c = (int64_t)blockIdx.x * 32 + lane;
+    float a = 0.0f;
+    if (c < width)
+        for (int b = run; b < s.blocks; b += 8) a += s.part[(int64_t)b * width + c];
+    sums[run][lane] = a;
+    __syncthreads();
+    if (run == 0 && c < width) {
+        a = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) a += sums[r][lane];
+        (c < p.cols ? s.dgamma : s.dbeta - p.cols)[c] = a;
+    }
+}
+
+template <typename F>
+void with_elem(int32_t dtype, F&& f) {
+    if (dtype == SBP_F32) f(std::integral_constant<int, T_F32>{});
+    else if (dtype == SBP_BF16) f(std::integral_constant<int, T_BF16>{});
+    else if (dtype == SBP_F8E4M3) f(std::integral_constant<int, T_E4M3>{});
+    else f(std::integral_constant<int, T_E5M2>{});
+}
+template <typename F>
+void with_wide(int32_t dtype, F&& f) {
+    if (dtype == SBP_F32) f(std::integral_constant<int, T_F32>{});
+    else f(std::integral_constant<int, T_BF16>{});
+}
+
+// threads of a row in the gradient: a vector a lane up to 512 columns, then two up to 4096
+int grad_tpr(int64_t cols) { return cols <= 512 ? 64 : cols <= 4096 ? 256 : 512; }
+
+}  // namespace
+
+int32_t launch_norm(const NormPlan& plan, hipStream_t stream) {
+    int64_t rows = 0;
+    for (int i = 0; i < plan.k; ++i) rows = std::max<int64_t>(rows, plan.s[i].rows);
+    with_wide(plan.x_dtype, [&](auto x) {
+        with_elem(plan.y_dtype, [&](auto y) {
+            with_wide(plan.w_dtype, [&](auto w) {
+                auto go = [&](auto tpr, auto v) {
+                    constexpr int NT = tpr() < 256 ? 256 : tpr(), G = NT / tpr();
+                    const int64_t bx = std::max<int64_t>(1, std::min<int64_t>((rows + G - 1) / G, NORM_BLOCKS * 256 / NT / plan.k));
+                    hipLaunchKernelGGL((norm_kernel<x(), y(), w(), tpr(), v()>), dim3((uint32_t)bx, (uint32_t)plan.k), dim3(NT), 0, stream, plan);
+                };
+                using std::integral_constant;
+                if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+                else if (plan.cols <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+                else go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+            });
+        });
+    });
+    return launch_status(__func__);
+}
+
+int32_t norm_grad_blocks(int64_t rows, int64_t cols, int32_t k) {
+    const int64_t g = GRAD_NT / grad_tpr(cols);
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + g - 1) / g, GRAD_BLOCKS / k));
+}
+
+int32_t launch_norm_grad(const NormGradPlan& plan, hipStream_t stream) {
+    int blocks = 1;
+    bool join = false;
+    for (int i = 0; i < plan.k; ++i) {
+        blocks = std::max(blocks, plan.s[i].blocks);
+        join = join || (plan.s[i].blocks > 1 && plan.s[i].dgamma);
+    }
+    with_elem(plan.x_dtype, [&](auto x) {
+        with_wide(plan.dy_dtype, [&](auto y) {
+            with_wide(plan.w_dtype, [&](auto w) {
+                auto go = [&](auto tpr, auto v) {
+                    hipLaunchKernelGGL((norm_grad_kernel<x(), y(), w(), tpr(), v()>), dim3((uint32_t)blocks, (uint32_t)plan.k), dim3(GRAD_NT), 0, stream, plan);
+                };
+                using std::integral_constant;
+                if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+                else if (plan.cols <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+                else go(integral_constant<int, 512>{}, integral_constant<int, 4>{});
+            });
+        });
+    });
+    int32_t st = launch_status(__func__);
+    if (st != SBP_OK || !join) return st;
+    hipLaunchKernelGGL(norm_grad_join_kernel, dim3((uint32_t)((2 * plan.cols + 31) / 32), (uint32_t)plan.k), dim3(256), 0, stream, plan);
+    return launch_status(__func__);
+}
+
+}  // namespace sbp

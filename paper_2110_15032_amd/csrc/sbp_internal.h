@@ -160,4 +160,97 @@ int32_t launch_xent_grad(const XentPlan& plan, hipStream_t stream);
 
 int32_t launch_row_stat(const RowStatPlan& plan, bool sumexp, hipStream_t stream);
 
+// ---------------------------------------------------------------------------------------------
+// 8-bit tensors: values and one power of two for every F8_BLOCK consecutive values of a stored row.
+// ---------------------------------------------------------------------------------------------
+constexpr int F8_BLOCK = 128;
+constexpr int64_t f8_blocks(int64_t n) { return (n + F8_BLOCK - 1) / F8_BLOCK; }
+
+// One shard of an elementwise pass over an 8-bit tensor.  rows and cols are the logical local shape; trans: the 8-bit tensor holds
+// its transpose.
+struct Block8Shard {
+    const void* x;     // saving: the tensor to save; restoring: the 8-bit values; GeLU's gradient: the pre-activation
+    void* scales;      // of the 8-bit tensor (written when saving)
+    const void* dh;    // GeLU's gradient only
+    void* out;
+    int32_t rows, cols;
+    int32_t ldx, lds, lddh, ldo;   // row pitches in elements
+};
+struct Block8Plan {
+    Block8Shard s[SBP_MAX_K];
+    int32_t k;
+    int32_t f8;      // SBP_F8E4M3 | SBP_F8E5M2, or a 16- or 32-bit pre-activation's type
+    int32_t dtype;   // of the other tensors
+    int32_t trans;
+    int32_t gelu;
+};
+int32_t launch_quantize(const Block8Plan& plan, hipStream_t stream);
+int32_t launch_dequantize(const Block8Plan& plan, hipStream_t stream);
+int32_t launch_gelu_grad(const Block8Plan& plan, hipStream_t stream);
+
+// ---------------------------------------------------------------------------------------------
+// Layer normalisation over rows.  Arrays sized for 32 shards keep the argument block small.
+// ---------------------------------------------------------------------------------------------
+constexpr int NORM_MAX_K = 32;
+constexpr int NORM_MAX_COLS = 16384;   // a row stays in the registers of one workgroup
+struct NormShard {
+    const void* x;
+    const void* gamma;   // null: ones
+    const void* beta;    // null: zeros
+    void* y;
+    void* y_scales;
+    float* mean;         // null: not wanted
+    float* rstd;
+    int32_t rows, ldx, ldy, lds;
+};
+struct NormPlan {
+    NormShard s[NORM_MAX_K];
+    int32_t k, cols;
+    int32_t x_dtype, y_dtype, w_dtype;
+    float eps;
+};
+struct NormGradShard {
+    const void* x;
+    const void* x_scales;
+    const void* gamma;
+    const float* mean;
+    const float* rstd;
+    const void* dy;
+    void* dx;
+    float* dgamma;       // null: neither is wanted
+    float* dbeta;
+    float* part;         // [blocks][2][cols], where blocks > 1
+    int32_t rows, ldx, lds, lddy, lddx, blocks;
+};
+struct NormGradPlan {
+    NormGradShard s[NORM_MAX_K];
+    int32_t k, cols;
+    int32_t x_dtype, dy_dtype, w_dtype;
+};
+// workgroups that launch_norm_grad gives a shard of so many rows, each of which leaves one partial sum of the weights' gradients
+int32_t norm_grad_blocks(int64_t rows, int64_t cols, int32_t k);
+int32_t launch_norm(const NormPlan& plan, hipStream_t stream);
+int32_t launch_norm_grad(const NormGradPlan& plan, hipStream_t stream);
+
+// ---------------------------------------------------------------------------------------------
+// Grouped product of 8-bit tensors: C_g[m, n] = sum over kk of A_g[m, kk] * B_g[n, kk], both with the reduction index contiguous.
+// ---------------------------------------------------------------------------------------------
+constexpr int GEMM_F8_MAX_K = 32;
+struct GemmF8Shard {
+    const uint8_t* a;
+    const uint8_t* a_scales;
+    const uint8_t* b;
+    const uint8_t* b_scales;
+    void* c;
+    int32_t m, n, kk;
+    int32_t lda, ldas, ldb, ldbs, ldc;   // row pitches in elements
+};
+struct GemmF8Plan {
+    GemmF8Shard s[GEMM_F8_MAX_K];
+    int32_t groups;
+    int32_t a_dtype, b_dtype, out_dtype;
+    int32_t epilogue;   // SBP_EPI_*
+};
+int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream);
+
 }  // namespace sbp
