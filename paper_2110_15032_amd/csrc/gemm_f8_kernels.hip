@@ -52,7 +52,7 @@ __device__ inline bf16x8 widen_frag(uint32_t a, uint32_t b, float scale) {
     return __builtin_bit_cast(bf16x8, u32x4{__builtin_bit_cast(uint32_t, v[0]), __builtin_bit_cast(uint32_t, v[1]), __builtin_bit_cast(uint32_t, v[2]), __builtin_bit_cast(uint32_t, v[3])});
 }
 
-// An operand's 32 values as the matrix instructions take them.
+// An operand's 32 values as the matrix instructions take them, with the scale in the low byte of `byte`.
 template <int T, bool EXACT>
 struct Operand;
 template <int T>
@@ -67,7 +67,7 @@ template <int T>
 struct Operand<T, true> {
     bf16x8 v[4];
     __device__ Operand(const Frag& f, uint32_t byte) {
-        const float s = scale_of(byte);
+        const float s = scale_of(byte & 255u);
         v[0] = widen_frag<T>(f.lo[0], f.lo[1], s);
         v[1] = widen_frag<T>(f.lo[2], f.lo[3], s);
         v[2] = widen_frag<T>(f.hi[0], f.hi[1], s);
@@ -116,6 +116,24 @@ __device__ inline void store4(const GemmF8Shard& s, int64_t m, int n, f32x4 v) {
     }
 }
 
+// sixteen that exist
+template <bool F32, bool GELU>
+__device__ inline void store16(const GemmF8Shard& s, int64_t m, int n, const f32x4 (&v)[4]) {
+    float u[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) u[e] = finish<F32, GELU>(v[e >> 2][e & 3]);
+    if constexpr (F32) {
+        float* dst = static_cast<float*>(s.c) + m * s.ldc + n;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) *reinterpret_cast<f32x4_any*>(dst + e) = f32x4{u[e], u[e + 1], u[e + 2], u[e + 3]};
+    } else {
+        uint16_t* dst = static_cast<uint16_t*>(s.c) + m * s.ldc + n;
+#pragma unroll
+        for (int e = 0; e < 16; e += 8)
+            *reinterpret_cast<u32x4_any*>(dst + e) = u32x4{f32_to_bf16x2(u[e], u[e + 1]), f32_to_bf16x2(u[e + 2], u[e + 3]), f32_to_bf16x2(u[e + 4], u[e + 5]), f32_to_bf16x2(u[e + 6], u[e + 7])};
+    }
+}
+
 // Few rows: the weights are the traffic, and every workgroup streams 16 of their rows past MB blocks of 16 rows of A, its four waves
 // taking every fourth block of the reduction.  No LDS before the sums meet; operands at any pitch.
 template <int AT, int BT, bool F32, bool GELU, int MB>
@@ -141,7 +159,6 @@ __global__ __launch_bounds__(256) void gemm_f8_stream_kernel(GemmF8Plan p, int t
 #pragma unroll
     for (int i = 0; i < MB; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
     const int whole = s.kk / F8_BLOCK, blocks = (s.kk + F8_BLOCK - 1) / F8_BLOCK;
-#pragma unroll 4
     for (int kb = wave; kb < whole; kb += 4) {
         const int64_t at = (int64_t)kb * F8_BLOCK;
         const Operand<BT, EXACT> ob(load_frag<true>(b + at, 128), bs[kb]);
@@ -167,6 +184,276 @@ __global__ __launch_bounds__(256) void gemm_f8_stream_kernel(GemmF8Plan p, int t
     }
 }
 
+// Tiles of WM MI 16 rows by WN 64 columns, one persistent workgroup a compute unit (or two of the smaller tile) that walks over its share of
+// the (shard, tile) list; a wave has MI 16 rows by 64 columns.  A step is a block of 128 of the reduction: one instruction deep, one cache line
+// of a row.  Two stages in LDS, and one barrier a step, behind which the stage before is free for the step after next: its loads (straight
+// into LDS) have a whole step to arrive.  The last two of the wave's MI row blocks are multiplied behind the barrier, underneath the reads of
+// the next step's first fragments.
+//
+// LDS image of an operand: rows of 128 bytes, 16-byte chunk c of a row at c ^ key(row), so that the 16 lanes of a read's pass fall on
+// different banks: row / 2 for A, whose fragment is 16 consecutive rows.  B's fragment j is rows 4 j + 0..3 of every 16 of the wave's 64, so that
+// a lane ends with 16 consecutive columns of a row of the result; its key is that place in the fragment over 2.
+template <int ROWS, int NT, bool B_SIDE>
+struct StageF8 {
+    static constexpr int PER = ROWS * 8 / NT;   // chunks of a thread
+    static constexpr int BYTES = ROWS * F8_BLOCK;
+    __device__ static int key(int row) { return B_SIDE ? ((row >> 4) & 3) << 1 | ((row >> 1) & 1) : (row >> 1) & 7; }
+    __device__ static int row_of(int p) { return p >> 3; }
+    __device__ static int chunk_of(int p) { return (p & 7) ^ key(p >> 3); }
+    // byte offset of chunk position p from the tile's first row; rows past the operand's end are its last one
+    __device__ static uint32_t offset(int p, int rows_left, int pitch) { return (uint32_t)min(row_of(p), rows_left - 1) * (uint32_t)pitch + (uint32_t)chunk_of(p) * 16u; }
+};
+
+template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, bool DIRECT>
+__global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Plan p, int tm, int tn, int order, int tiles) {
+    constexpr bool EXACT = F32;
+    constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * 64, NJ = 4;
+    using StA = StageF8<BM, NT, false>;
+    using StB = StageF8<BN, NT, true>;
+    constexpr int STAGE = StA::BYTES + StB::BYTES;
+    constexpr int SCALE_BLOCKS = 16, SCALE_BYTES = (BM + BN) * SCALE_BLOCKS;   // scales of 16 blocks, twice
+    constexpr int SCALE_ROWS = (BM + BN) / NT;                                // of a thread
+    static_assert((BM + BN) % NT == 0, "rows of scales divide over the workgroup");
+    __shared__ __attribute__((aligned(16))) char lds[2 * STAGE + 2 * SCALE_BYTES];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const int wm = wave / WN, wn = wave % WN;
+
+    // the tiles of this workgroup that exist, in order
+    struct At {
+        int id, g, m0, n0, steps;
+    };
+    auto settle = [&](int id) {   // the first tile of the walk from id on that lies in its shard; id >= tiles: none
+        At t{id, 0, 0, 0, 0};
+        for (; t.id < tiles; t.id += (int)gridDim.x) {
+            const TileCoord c = map_tile(t.id, (tiles + 7) & ~7, tm, tn, p.groups, order);
+            if (!c.valid) continue;
+            const GemmF8Shard& s = p.s[c.g];
+            if ((int64_t)c.tile_m * BM >= s.m || (int64_t)c.tile_n * BN >= s.n) continue;
+            t.g = c.g;
+            t.m0 = c.tile_m * BM;
+            t.n0 = c.tile_n * BN;
+            t.steps = (s.kk + F8_BLOCK - 1) / F8_BLOCK;
+            break;
+        }
+        return t;
+    };
+    At now = settle(blockIdx.x);
+    if (now.id >= tiles) return;
+
+    // ---- loads of stages: a cursor that runs ahead of the multiplication
+    At ahead = now;
+    int ahead_step = 0;
+    uint32_t off_a[StA::PER], off_b[StB::PER];
+    gbl_char *src_a, *src_b;
+    auto enter = [&]() {
+        const GemmF8Shard& s = p.s[ahead.g];
+        src_a = (gbl_char*)(s.a + (int64_t)ahead.m0 * s.lda);
+        src_b = (gbl_char*)(s.b + (int64_t)ahead.n0 * s.ldb);
+#pragma unroll
+        for (int i = 0; i < StA::PER; ++i) off_a[i] = StA::offset(i * NT + (int)threadIdx.x, s.m - ahead.m0, s.lda);
+#pragma unroll
+        for (int i = 0; i < StB::PER; ++i) off_b[i] = StB::offset(i * NT + (int)threadIdx.x, s.n - ahead.n0, s.ldb);
+    };
+    enter();
+    u32x4 held[DIRECT ? 1 : StA::PER + StB::PER];   // not DIRECT: a stage on its way
+    int arriving = F8_BLOCK;   // reduction elements from the start of the stage that was loaded last to the end
+    auto load_stage = [&](char* stage) {
+        if (ahead.id >= tiles) return;
+        const int left = p.s[ahead.g].kk - ahead_step * F8_BLOCK;
+        arriving = left;
+        if constexpr (DIRECT) {
+            // a chunk that starts behind the reduction's end is read from the last one that does not (put_stage clears both)
+            const int last = left < F8_BLOCK ? (left - 1) >> 4 : 7;
+            auto bring = [&](gbl_char* src, uint32_t off, uint32_t lds_at) {
+                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(src), "s"(lds_at) : "memory", "m0");
+            };
+            const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)stage;
+#pragma unroll
+            for (int i = 0; i < StA::PER; ++i) {
+                uint32_t off = off_a[i];
+                if (last < 7) off -= (uint32_t)max(StA::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
+                bring(src_a, off, __builtin_amdgcn_readfirstlane(base + (uint32_t)(i * NT + wave * 64) * 16u));
+            }
+#pragma unroll
+            for (int i = 0; i < StB::PER; ++i) {
+                uint32_t off = off_b[i];
+                if (last < 7) off -= (uint32_t)max(StB::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
+                bring(src_b, off, __builtin_amdgcn_readfirstlane(base + (uint32_t)(StA::BYTES + (i * NT + wave * 64) * 16)));
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < StA::PER; ++i) held[i] = load_some((const uint8_t*)src_a + off_a[i], left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+#pragma unroll
+            for (int i = 0; i < StB::PER; ++i) held[StA::PER + i] = load_some((const uint8_t*)src_b + off_b[i], left - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
+        }
+        src_a += F8_BLOCK;
+        src_b += F8_BLOCK;
+        if (++ahead_step == ahead.steps) {
+            ahead = settle(ahead.id + (int)gridDim.x);
+            ahead_step = 0;
+            if (ahead.id < tiles) enter();
+        }
+    };
+    // A stage that has arrived: what this thread brought of it, put in its place (not DIRECT), or cut off where the reduction ends.
+    auto put_stage = [&](char* stage) {
+        if constexpr (DIRECT) {
+            if (arriving >= F8_BLOCK) return;
+            auto cut = [&](char* at, int valid) {
+                u32x4 v = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) {
+                    const int n = valid - d * 4;
+                    v[d] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+                }
+                *reinterpret_cast<u32x4*>(at) = v;
+            };
+#pragma unroll
+            for (int i = 0; i < StA::PER; ++i) cut(stage + (i * NT + threadIdx.x) * 16, arriving - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+#pragma unroll
+            for (int i = 0; i < StB::PER; ++i) cut(stage + StA::BYTES + (i * NT + threadIdx.x) * 16, arriving - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
+        } else {
+#pragma unroll
+            for (int i = 0; i < StA::PER; ++i) *reinterpret_cast<u32x4*>(stage + (i * NT + threadIdx.x) * 16) = held[i];
+#pragma unroll
+            for (int i = 0; i < StB::PER; ++i) *reinterpret_cast<u32x4*>(stage + StA::BYTES + (i * NT + threadIdx.x) * 16) = held[StA::PER + i];
+        }
+    };
+    // ---- scales, 16 blocks of a row at a time
+    u32x4 scales[SCALE_ROWS];
+    auto load_scales = [&](const At& t, int step) {
+        if (t.id >= tiles) return;
+        const GemmF8Shard& s = p.s[t.g];
+#pragma unroll
+        for (int i = 0; i < SCALE_ROWS; ++i) {
+            const int row = i * NT + (int)threadIdx.x;
+            const uint8_t* at = row < BM ? s.a_scales + (int64_t)min(t.m0 + row, s.m - 1) * s.ldas : s.b_scales + (int64_t)min(t.n0 + row - BM, s.n - 1) * s.ldbs;
+            const int valid = t.steps - step;
+            if (valid >= SCALE_BLOCKS) {
+                scales[i] = *reinterpret_cast<const u32x4_byte*>(at + step);
+            } else {
+                uint64_t lo = 0, hi = 0;
+#pragma unroll 1
+                for (int e = valid - 1; e >= 0; --e) {
+                    const uint64_t b = at[step + e];
+                    hi = hi << 8 | lo >> 56;
+                    lo = lo << 8 | b;
+                }
+                scales[i] = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
+            }
+        }
+    };
+    auto put_scales = [&](char* to) {
+#pragma unroll
+        for (int i = 0; i < SCALE_ROWS; ++i) *reinterpret_cast<u32x4*>(to + (i * NT + threadIdx.x) * SCALE_BLOCKS) = scales[i];
+    };
+    char* const scale_lds = lds + 2 * STAGE;
+
+    // ---- fragments
+    const int a_row = wm * MI * 16 + r, b_row = wn * 64 + (r >> 2) * 16 + (r & 3);
+    const int a_lo = a_row * F8_BLOCK + ((g ^ StA::key(a_row)) << 4), b_lo = StA::BYTES + b_row * F8_BLOCK + ((g ^ StB::key(b_row)) << 4);
+    auto frag_a = [&](const char* stage, int i) {
+        return Frag{*reinterpret_cast<const u32x4*>(stage + a_lo + i * 16 * F8_BLOCK), *reinterpret_cast<const u32x4*>(stage + (a_lo ^ 64) + i * 16 * F8_BLOCK)};
+    };
+    auto frag_b = [&](const char* stage, int j) {
+        return Frag{*reinterpret_cast<const u32x4*>(stage + b_lo + j * 4 * F8_BLOCK), *reinterpret_cast<const u32x4*>(stage + (b_lo ^ 64) + j * 4 * F8_BLOCK)};
+    };
+    f32x4 acc[MI][NJ];
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+
+    load_stage(lds);
+    load_scales(now, 0);
+    put_scales(scale_lds);
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    put_stage(lds);
+    __syncthreads();
+    load_stage(lds + STAGE);
+
+    int cur = 0, scale_cur = 0;
+    uint32_t sa[MI], sb[NJ];
+    Frag fb[NJ], fa[2];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) fb[j] = frag_b(lds, j);
+    fa[0] = frag_a(lds, 0);
+    while (true) {
+        const GemmF8Shard& s = p.s[now.g];
+        const At next = settle(now.id + (int)gridDim.x);
+        for (int k = 0; k < now.steps; ++k) {
+            const char* const stage = lds + cur * STAGE;
+            char* const other = lds + (cur ^ 1) * STAGE;
+            const int in_chunk = k & (SCALE_BLOCKS - 1);
+            // the next 16 blocks' scales (or the next tile's) at the chunk's second step, its first where there is one only
+            const bool more = in_chunk == min(1, now.steps - 1 - (k - in_chunk));
+            if (more) {
+                const int to = k - in_chunk + SCALE_BLOCKS;
+                load_scales(to < now.steps ? now : next, to < now.steps ? to : 0);
+            }
+            if ((k & 3) == 0) {
+                const char* at = scale_lds + scale_cur * SCALE_BYTES + in_chunk;
+#pragma unroll
+                for (int i = 0; i < MI; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(at + (a_row + i * 16) * SCALE_BLOCKS);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(at + (BM + b_row + j * 4) * SCALE_BLOCKS);
+            }
+            auto row = [&](int i) {
+                const Operand<AT, EXACT> oa(fa[i & 1], sa[i]);
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) acc[i][j] = multiply<BT, AT>(Operand<BT, EXACT>(fb[j], sb[j]), oa, acc[i][j]);
+                // in its place: products put off to behind the barrier, or reads brought forward, keep more fragments than there are registers
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+            };
+#pragma unroll
+            for (int i = 0; i < MI - 2; ++i) {
+                fa[(i + 1) & 1] = frag_a(stage, i + 1);
+                __builtin_amdgcn_sched_barrier(0);   // the read first: it has this row's products to arrive
+                row(i);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            const Frag last = frag_a(stage, MI - 1);
+            // everything of this stage has been read, and the next one is there
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+            put_stage(other);
+            if (more) put_scales(scale_lds + (scale_cur ^ 1) * SCALE_BYTES);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            load_stage(lds + cur * STAGE);
+            row(MI - 2);
+            fa[(MI - 1) & 1] = last;
+            row(MI - 1);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) fb[j] = frag_b(other, j);
+            fa[0] = frag_a(other, 0);
+#pragma unroll
+            for (int i = 0; i < MI; ++i) sa[i] >>= 8;
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) sb[j] >>= 8;
+            cur ^= 1;
+            if (in_chunk == SCALE_BLOCKS - 1 || k + 1 == now.steps) scale_cur ^= 1;
+        }
+
+        // 16 consecutive columns of a row in every lane
+        const bool inside = now.m0 + BM <= s.m && now.n0 + BN <= s.n;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int64_t m = (int64_t)now.m0 + wm * MI * 16 + i * 16 + r;
+            const int n = now.n0 + wn * 64 + g * 16;
+            if (inside) store16<F32, GELU>(s, m, n, acc[i]);
+            else
+#pragma unroll
+                for (int j = 0; j < NJ; ++j) store4<F32, GELU>(s, m, n + j * 4, acc[i][j]);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        }
+        now = next;
+        if (now.id >= tiles) break;
+    }
+}
+
 }  // namespace
 
 int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
@@ -176,6 +463,13 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
         max_n = std::max(max_n, plan.s[g].n);
     }
     if (max_m == 0 || max_n == 0) return SBP_OK;
+    bool direct = true, empty = false;   // rows of both operands 16-byte aligned; a shard without anything to sum
+    for (int g = 0; g < plan.groups; ++g) {
+        const GemmF8Shard& s = plan.s[g];
+        if (s.lda % 16 || s.ldb % 16) direct = false;
+        empty = empty || s.kk == 0;
+        if (s.lda > (1 << 23) || s.ldb > (1 << 23)) empty = true;   // 256 rows of a tile are counted in 32 bits
+    }
     auto types = [&](auto f) {
         auto second = [&](auto a) {
             if (plan.b_dtype == SBP_F8E4M3) f(a, std::integral_constant<int, T_E4M3>{});
@@ -203,8 +497,27 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
                 }
                 hipLaunchKernelGGL((gemm_f8_stream_kernel<a(), b(), f32(), gelu(), mb()>), dim3((uint32_t)(tm * tn), (uint32_t)plan.groups), dim3(256), 0, stream, plan, tm);
             };
-            if (max_m <= 16) stream_rows(std::integral_constant<int, 1>{});
-            else stream_rows(std::integral_constant<int, 4>{});
+            auto tile = [&](auto wm, auto wn, auto mi, auto direct) {
+                constexpr int BM = wm() * mi() * 16, BN = wn() * 64;
+                const int tm = tiles_along(max_m, BM), tn = tiles_along(max_n, BN);
+                const int64_t tiles = (int64_t)tm * tn * plan.groups;
+                if (tiles > INT32_MAX - 65536) {
+                    st = SBP_ERR_UNSUPPORTED;
+                    return;
+                }
+                const int64_t at_once = (int64_t)compute_units() * (BM * BN > 128 * 128 ? 1 : 2), all = (tiles + 7) & ~7;
+                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), direct()>), dim3((uint32_t)std::min(all, at_once)),
+                                   dim3(wm() * wn() * 64), 0, stream, plan, tm, tn, tn > 8 ? 6 : 2, (int)all);
+            };
+            using std::integral_constant;
+            const auto i2 = integral_constant<int, 2>{};
+            const auto i4 = integral_constant<int, 4>{};
+            const int64_t large = (int64_t)tiles_along(max_m, 256) * tiles_along(max_n, 256) * plan.groups;
+            if (max_m <= 16) stream_rows(integral_constant<int, 1>{});
+            else if (max_m <= 64 || empty) stream_rows(i4);
+            else if (!direct) tile(i2, i2, i4, std::false_type{});
+            else if (large < compute_units()) tile(i2, i2, i4, std::true_type{});
+            else tile(i2, i4, integral_constant<int, 8>{}, std::true_type{});
         });
     });
     return st != SBP_OK ? st : launch_status(__func__);
