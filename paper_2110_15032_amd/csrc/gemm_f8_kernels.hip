@@ -59,6 +59,7 @@ template <int T>
 struct Operand<T, false> {
     i32x8 v;
     int scale;
+    Operand() = default;
     __device__ Operand(const Frag& f, uint32_t byte) : scale((int)byte) {
         v = i32x8{(int)f.lo[0], (int)f.lo[1], (int)f.lo[2], (int)f.lo[3], (int)f.hi[0], (int)f.hi[1], (int)f.hi[2], (int)f.hi[3]};
     }
@@ -66,6 +67,7 @@ struct Operand<T, false> {
 template <int T>
 struct Operand<T, true> {
     bf16x8 v[4];
+    Operand() = default;
     __device__ Operand(const Frag& f, uint32_t byte) {
         const float s = scale_of(byte & 255u);
         v[0] = widen_frag<T>(f.lo[0], f.lo[1], s);
@@ -186,9 +188,12 @@ __global__ __launch_bounds__(256) void gemm_f8_stream_kernel(GemmF8Plan p, int t
 
 // Tiles of WM MI 16 rows by WN 64 columns, one persistent workgroup a compute unit (or two of the smaller tile) that walks over its share of
 // the (shard, tile) list; a wave has MI 16 rows by 64 columns.  A step is a block of 128 of the reduction: one instruction deep, one cache line
-// of a row.  Two stages in LDS, and one barrier a step, behind which the stage before is free for the step after next: its loads (straight
-// into LDS) have a whole step to arrive.  The last two of the wave's MI row blocks are multiplied behind the barrier, underneath the reads of
-// the next step's first fragments.
+// of a row.
+//
+// Two stages in LDS, and two barriers a step, so that parts of a stage are free for the stage after next as soon as they have been read: B and the
+// first half of every wave's row blocks behind the first barrier, the other half behind the second.  Loads go straight into LDS and have a
+// step and a half to arrive (with one barrier and a step the loads alone took 467 us of the 515 of 8192 x 4096 x 16384).  The row blocks before a
+// barrier are multiplied behind it, underneath the reads of the next fragments.
 //
 // LDS image of an operand: rows of 128 bytes, 16-byte chunk c of a row at c ^ key(row), so that the 16 lanes of a read's pass fall on
 // different banks: row / 2 for A, whose fragment is 16 consecutive rows.  B's fragment j is rows 4 j + 0..3 of every 16 of the wave's 64, so that
@@ -204,16 +209,26 @@ struct StageF8 {
     __device__ static uint32_t offset(int p, int rows_left, int pitch) { return (uint32_t)min(row_of(p), rows_left - 1) * (uint32_t)pitch + (uint32_t)chunk_of(p) * 16u; }
 };
 
-template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, bool DIRECT>
+// an address that every lane has, in scalar registers
+__device__ inline gbl_char* uniform(gbl_char* at) {
+    const uint64_t v = (uint64_t)(uintptr_t)at;
+    return (gbl_char*)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v));
+}
+
+// SCALES4: rows of scales at pitches of 4 bytes, which go straight into LDS too; else through registers, byte by byte at their end.
+template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, bool DIRECT, bool SCALES4>
 __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Plan p, int tm, int tn, int order, int tiles) {
     constexpr bool EXACT = F32;
     constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * 64, NJ = 4;
     using StA = StageF8<BM, NT, false>;
     using StB = StageF8<BN, NT, true>;
     constexpr int STAGE = StA::BYTES + StB::BYTES;
-    constexpr int SCALE_BLOCKS = 16, SCALE_BYTES = (BM + BN) * SCALE_BLOCKS;   // scales of 16 blocks, twice
-    constexpr int SCALE_ROWS = (BM + BN) / NT;                                // of a thread
+    constexpr int SCALE_ROWS = (BM + BN) / NT;   // of a thread
     static_assert((BM + BN) % NT == 0, "rows of scales divide over the workgroup");
+    // chunk i of a thread lies in rows NT / 8 i + 0..: half a wave's rows, so that even chunks of A are first halves
+    static_assert(NT / 8 == MI * 8 && StA::PER == 2 * WM, "an operand's chunks fall into halves of the waves' rows");
+    // scales of 16 blocks of the reduction, twice: four planes of [row] dwords, four blocks each
+    constexpr int SCALE_PLANE = (BM + BN) * 4, SCALE_BYTES = 4 * SCALE_PLANE;
     __shared__ __attribute__((aligned(16))) char lds[2 * STAGE + 2 * SCALE_BYTES];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int wm = wave / WN, wn = wave % WN;
@@ -225,7 +240,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     auto settle = [&](int id) {   // the first tile of the walk from id on that lies in its shard; id >= tiles: none
         At t{id, 0, 0, 0, 0};
         for (; t.id < tiles; t.id += (int)gridDim.x) {
-            const TileCoord c = map_tile(t.id, (tiles + 7) & ~7, tm, tn, p.groups, order);
+            const TileCoord c = map_tile(t.id, tiles, tm, tn, p.groups, order);
             if (!c.valid) continue;
             const GemmF8Shard& s = p.s[c.g];
             if ((int64_t)c.tile_m * BM >= s.m || (int64_t)c.tile_n * BN >= s.n) continue;
@@ -240,111 +255,129 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     At now = settle(blockIdx.x);
     if (now.id >= tiles) return;
 
-    // ---- loads of stages: a cursor that runs ahead of the multiplication
+    // ---- loads of stages: a cursor that runs two steps ahead of the multiplication, and stays at the last stage of all (whose loads are then
+    // repeated into a stage that nobody reads: the waits can count on them)
+    constexpr int LOADS = StA::PER + StB::PER;   // instructions of a wave and stage
     At ahead = now;
-    int ahead_step = 0;
+    int ahead_left;   // reduction elements from the cursor's stage to the end
     uint32_t off_a[StA::PER], off_b[StB::PER];
     gbl_char *src_a, *src_b;
+    // A stage that the reduction ends in: a chunk that starts behind the end is read from the last one that does not (cut_* clears both).
+    auto shorten = [&]() {
+        if (!DIRECT || ahead_left >= F8_BLOCK) return;
+        const int last = (ahead_left - 1) >> 4;
+#pragma unroll
+        for (int i = 0; i < StA::PER; ++i) off_a[i] -= (uint32_t)max(StA::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
+#pragma unroll
+        for (int i = 0; i < StB::PER; ++i) off_b[i] -= (uint32_t)max(StB::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
+    };
     auto enter = [&]() {
         const GemmF8Shard& s = p.s[ahead.g];
+        ahead_left = s.kk;
         src_a = (gbl_char*)(s.a + (int64_t)ahead.m0 * s.lda);
         src_b = (gbl_char*)(s.b + (int64_t)ahead.n0 * s.ldb);
 #pragma unroll
         for (int i = 0; i < StA::PER; ++i) off_a[i] = StA::offset(i * NT + (int)threadIdx.x, s.m - ahead.m0, s.lda);
 #pragma unroll
         for (int i = 0; i < StB::PER; ++i) off_b[i] = StB::offset(i * NT + (int)threadIdx.x, s.n - ahead.n0, s.ldb);
+        shorten();
     };
     enter();
-    u32x4 held[DIRECT ? 1 : StA::PER + StB::PER];   // not DIRECT: a stage on its way
-    int arriving = F8_BLOCK;   // reduction elements from the start of the stage that was loaded last to the end
-    auto load_stage = [&](char* stage) {
-        if (ahead.id >= tiles) return;
-        const int left = p.s[ahead.g].kk - ahead_step * F8_BLOCK;
-        arriving = left;
-        if constexpr (DIRECT) {
-            // a chunk that starts behind the reduction's end is read from the last one that does not (put_stage clears both)
-            const int last = left < F8_BLOCK ? (left - 1) >> 4 : 7;
-            auto bring = [&](gbl_char* src, uint32_t off, uint32_t lds_at) {
-                asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(src), "s"(lds_at) : "memory", "m0");
-            };
-            const uint32_t base = (uint32_t)(uintptr_t)(lds_void*)stage;
-#pragma unroll
-            for (int i = 0; i < StA::PER; ++i) {
-                uint32_t off = off_a[i];
-                if (last < 7) off -= (uint32_t)max(StA::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
-                bring(src_a, off, __builtin_amdgcn_readfirstlane(base + (uint32_t)(i * NT + wave * 64) * 16u));
-            }
-#pragma unroll
-            for (int i = 0; i < StB::PER; ++i) {
-                uint32_t off = off_b[i];
-                if (last < 7) off -= (uint32_t)max(StB::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
-                bring(src_b, off, __builtin_amdgcn_readfirstlane(base + (uint32_t)(StA::BYTES + (i * NT + wave * 64) * 16)));
-            }
+    auto advance = [&]() {
+        if (ahead_left > F8_BLOCK) {
+            src_a += F8_BLOCK;
+            src_b += F8_BLOCK;
+            ahead_left -= F8_BLOCK;
+            shorten();
         } else {
-#pragma unroll
-            for (int i = 0; i < StA::PER; ++i) held[i] = load_some((const uint8_t*)src_a + off_a[i], left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
-#pragma unroll
-            for (int i = 0; i < StB::PER; ++i) held[StA::PER + i] = load_some((const uint8_t*)src_b + off_b[i], left - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
-        }
-        src_a += F8_BLOCK;
-        src_b += F8_BLOCK;
-        if (++ahead_step == ahead.steps) {
-            ahead = settle(ahead.id + (int)gridDim.x);
-            ahead_step = 0;
-            if (ahead.id < tiles) enter();
+            const At t = settle(ahead.id + (int)gridDim.x);
+            if (t.id < tiles) {
+                ahead = t;
+                enter();
+            }
         }
     };
-    // A stage that has arrived: what this thread brought of it, put in its place (not DIRECT), or cut off where the reduction ends.
-    auto put_stage = [&](char* stage) {
-        if constexpr (DIRECT) {
-            if (arriving >= F8_BLOCK) return;
-            auto cut = [&](char* at, int valid) {
-                u32x4 v = *reinterpret_cast<const u32x4*>(at);
+    // one chunk of a thread into the stage whose bytes for this wave start at `at` (uniform)
+    auto bring = [&](gbl_char* src, uint32_t off, uint32_t at, auto behind) {
+        asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(uniform(src)), "s"(at), "n"(behind()) : "memory", "m0", "scc");
+    };
+    auto bring_a = [&](uint32_t at, auto i) { bring(src_a, off_a[i()], at, std::integral_constant<int, i() * NT * 16>{}); };
+    auto bring_b = [&](uint32_t at, auto i) { bring(src_b, off_b[i()], at, std::integral_constant<int, StA::BYTES + i() * NT * 16>{}); };
+    const uint32_t lds_wave = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds + (uint32_t)wave * 1024u);
+    u32x4 held[DIRECT ? 1 : LOADS];   // not DIRECT: a stage on its way
+    auto hold = [&]() {
+        if constexpr (!DIRECT) {
 #pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    const int n = valid - d * 4;
-                    v[d] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
-                }
-                *reinterpret_cast<u32x4*>(at) = v;
-            };
+            for (int i = 0; i < StA::PER; ++i) held[i] = load_some((const uint8_t*)src_a + off_a[i], ahead_left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
 #pragma unroll
-            for (int i = 0; i < StA::PER; ++i) cut(stage + (i * NT + threadIdx.x) * 16, arriving - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
-#pragma unroll
-            for (int i = 0; i < StB::PER; ++i) cut(stage + StA::BYTES + (i * NT + threadIdx.x) * 16, arriving - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
-        } else {
+            for (int i = 0; i < StB::PER; ++i) held[StA::PER + i] = load_some((const uint8_t*)src_b + off_b[i], ahead_left - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
+        }
+    };
+    // B and the first halves of A, then the second halves
+    constexpr int FIRST = StB::PER + WM, SECOND = WM;
+    auto bring_first = [&](uint32_t at, auto n) {
+        if constexpr (n() < StB::PER) bring_b(at, n);
+        else bring_a(at, std::integral_constant<int, 2 * (n() - StB::PER)>{});
+    };
+    auto bring_second = [&](uint32_t at, auto n) { bring_a(at, std::integral_constant<int, 2 * n() + 1>{}); };
+    auto put_held = [&](char* stage) {
+        if constexpr (!DIRECT) {
 #pragma unroll
             for (int i = 0; i < StA::PER; ++i) *reinterpret_cast<u32x4*>(stage + (i * NT + threadIdx.x) * 16) = held[i];
 #pragma unroll
             for (int i = 0; i < StB::PER; ++i) *reinterpret_cast<u32x4*>(stage + StA::BYTES + (i * NT + threadIdx.x) * 16) = held[StA::PER + i];
         }
     };
+    // what this thread brought of a stage that the reduction ends in, `left` elements from its start: the bytes behind are cleared in LDS
+    auto cut = [&](char* at, int valid) {
+        u32x4 v = *reinterpret_cast<const u32x4*>(at);
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+            const int n = valid - d * 4;
+            v[d] &= n >= 4 ? 0xFFFFFFFFu : n <= 0 ? 0u : (1u << (8 * n)) - 1u;
+        }
+        *reinterpret_cast<u32x4*>(at) = v;
+    };
+    auto cut_first = [&](char* stage, int left) {
+        if (!DIRECT || left >= F8_BLOCK) return;
+#pragma unroll
+        for (int i = 0; i < StB::PER; ++i) cut(stage + StA::BYTES + (i * NT + threadIdx.x) * 16, left - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
+#pragma unroll
+        for (int i = 0; i < StA::PER; i += 2) cut(stage + (i * NT + threadIdx.x) * 16, left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+    };
+    auto cut_second = [&](char* stage, int left) {
+        if (!DIRECT || left >= F8_BLOCK) return;
+#pragma unroll
+        for (int i = 1; i < StA::PER; i += 2) cut(stage + (i * NT + threadIdx.x) * 16, left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+    };
+
     // ---- scales, 16 blocks of a row at a time
-    u32x4 scales[SCALE_ROWS];
-    auto load_scales = [&](const At& t, int step) {
-        if (t.id >= tiles) return;
+    constexpr int LOADS_SCALES = 4 * SCALE_ROWS;
+    auto load_scales = [&](const At t, int step, char* to) {
         const GemmF8Shard& s = p.s[t.g];
 #pragma unroll
         for (int i = 0; i < SCALE_ROWS; ++i) {
             const int row = i * NT + (int)threadIdx.x;
-            const uint8_t* at = row < BM ? s.a_scales + (int64_t)min(t.m0 + row, s.m - 1) * s.ldas : s.b_scales + (int64_t)min(t.n0 + row - BM, s.n - 1) * s.ldbs;
-            const int valid = t.steps - step;
-            if (valid >= SCALE_BLOCKS) {
-                scales[i] = *reinterpret_cast<const u32x4_byte*>(at + step);
-            } else {
-                uint64_t lo = 0, hi = 0;
-#pragma unroll 1
-                for (int e = valid - 1; e >= 0; --e) {
-                    const uint64_t b = at[step + e];
-                    hi = hi << 8 | lo >> 56;
-                    lo = lo << 8 | b;
+            const bool of_a = i * NT + wave * 64 < BM;   // whole waves: BM is a multiple of 64
+            const int first = of_a ? t.m0 : t.n0 - BM, last = (of_a ? s.m : s.n) - 1, pitch = of_a ? s.ldas : s.ldbs;
+            const uint8_t* const from = (of_a ? s.a_scales : s.b_scales) + (int64_t)min(first + row, last) * pitch;
+#pragma unroll
+            for (int d = 0; d < 4; ++d) {
+                char* const plane = to + d * SCALE_PLANE + (i * NT + wave * 64) * 4;
+                if constexpr (SCALES4) {
+                    // four blocks from the row's last four on are those again (a row ends with them, its pitch being whole dwords)
+                    const int b = min(step + 4 * d, (t.steps - 1) & ~3);
+                    const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)plane);
+                    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(from + b), "s"(lds_at) : "memory", "m0");
+                } else {
+                    uint32_t v = 0;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (step + 4 * d + e < t.steps) v |= (uint32_t)from[step + 4 * d + e] << (8 * e);
+                    *reinterpret_cast<uint32_t*>(plane + lane * 4) = v;
                 }
-                scales[i] = u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
             }
         }
-    };
-    auto put_scales = [&](char* to) {
-#pragma unroll
-        for (int i = 0; i < SCALE_ROWS; ++i) *reinterpret_cast<u32x4*>(to + (i * NT + threadIdx.x) * SCALE_BLOCKS) = scales[i];
     };
     char* const scale_lds = lds + 2 * STAGE;
 
@@ -357,19 +390,53 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     auto frag_b = [&](const char* stage, int j) {
         return Frag{*reinterpret_cast<const u32x4*>(stage + b_lo + j * 4 * F8_BLOCK), *reinterpret_cast<const u32x4*>(stage + (b_lo ^ 64) + j * 4 * F8_BLOCK)};
     };
+
     f32x4 acc[MI][NJ];
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
         for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 
-    load_stage(lds);
-    load_scales(now, 0);
-    put_scales(scale_lds);
+    // Loads are dealt out over a step's rows of products, one or two in the middle of each: all at once behind a barrier they hold every wave of
+    // the workgroup up, and the matrix pipe with them (8192 x 4096 x 16384: 591 us).  The second halves of the stage ahead go with the
+    // rows before the first barrier, the first loads of the one after with the others.
+    constexpr int ROWS_SECOND = MI / 2 - 1, ROWS_FIRST = MI - ROWS_SECOND;
+    // Waits.  Loads and stores share one in-order counter; the number is how many of the youngest may be on their way.  At the first barrier: all that
+    // was brought since the second halves of this stage; at the second: since the first part of the next one.  `stores`: waits that a whole
+    // tile's stores may be younger than what is waited for.
+    constexpr int BEFORE_SECOND_BARRIER = (ROWS_FIRST - 2) * FIRST / ROWS_FIRST;   // first loads that go with rows before it
+    constexpr int NSTORE = MI * (F32 ? 4 : 2);
+    int stores = 0;
+    auto wait = [&](auto youngest, bool scales_too, bool scales_now) {
+        if constexpr (!DIRECT) return;   // registers wait for themselves
+        if (scales_now) __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+        else if (stores > 0) __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest() + NSTORE));
+        else if (scales_too) __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest() + LOADS_SCALES));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest()));
+        if (stores > 0) --stores;
+    };
+    auto barrier = [&]() {
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wave read and wrote in LDS
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+    };
+
+    load_scales(now, 0, scale_lds);
+    const int left0 = ahead_left;
+    if constexpr (DIRECT) {
+        static_for<FIRST>([&](auto n) { bring_first(lds_wave, n); });
+        static_for<SECOND>([&](auto n) { bring_second(lds_wave, n); });
+        advance();
+        static_for<FIRST>([&](auto n) { bring_first(lds_wave + STAGE, n); });
+    } else {
+        hold();
+        put_held(lds);
+        advance();
+        hold();
+    }
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-    put_stage(lds);
-    __syncthreads();
-    load_stage(lds + STAGE);
+    cut_first(lds, left0);
+    barrier();
 
     int cur = 0, scale_cur = 0;
     uint32_t sa[MI], sb[NJ];
@@ -380,60 +447,94 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     while (true) {
         const GemmF8Shard& s = p.s[now.g];
         const At next = settle(now.id + (int)gridDim.x);
-        for (int k = 0; k < now.steps; ++k) {
-            const char* const stage = lds + cur * STAGE;
+        const int kk_next = next.id < tiles ? p.s[next.g].kk : F8_BLOCK;
+        int left = s.kk;
+        for (int k = 0; k < now.steps; ++k, left -= F8_BLOCK) {
+            char* const stage = lds + cur * STAGE;
             char* const other = lds + (cur ^ 1) * STAGE;
-            const int in_chunk = k & (SCALE_BLOCKS - 1);
-            // the next 16 blocks' scales (or the next tile's) at the chunk's second step, its first where there is one only
-            const bool more = in_chunk == min(1, now.steps - 1 - (k - in_chunk));
+            const uint32_t at = __builtin_amdgcn_readfirstlane(lds_wave + (uint32_t)cur * STAGE);
+            const int in_chunk = k & 15, last_of_chunk = min(15, now.steps - 1 - (k - in_chunk));
+            // the next 16 blocks' scales (or the next tile's; this one's again where there is none, which the waits count on) at the chunk's second
+            // step, its first where there is one only
+            const bool more = in_chunk == min(1, last_of_chunk);
             if (more) {
-                const int to = k - in_chunk + SCALE_BLOCKS;
-                load_scales(to < now.steps ? now : next, to < now.steps ? to : 0);
+                const int to = k - in_chunk + 16;
+                const bool here = to < now.steps || next.id >= tiles;
+                load_scales(At{0, here ? now.g : next.g, here ? now.m0 : next.m0, here ? now.n0 : next.n0, here ? now.steps : next.steps}, to < now.steps ? to : 0, scale_lds + (scale_cur ^ 1) * SCALE_BYTES);
             }
             if ((k & 3) == 0) {
-                const char* at = scale_lds + scale_cur * SCALE_BYTES + in_chunk;
+                const char* from = scale_lds + scale_cur * SCALE_BYTES + (in_chunk >> 2) * SCALE_PLANE;
 #pragma unroll
-                for (int i = 0; i < MI; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(at + (a_row + i * 16) * SCALE_BLOCKS);
+                for (int i = 0; i < MI; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(from + (a_row + i * 16) * 4);
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(at + (BM + b_row + j * 4) * SCALE_BLOCKS);
+                for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(from + (BM + b_row + j * 4) * 4);
             }
-            auto row = [&](int i) {
-                const Operand<AT, EXACT> oa(fa[i & 1], sa[i]);
+            Operand<BT, EXACT> ob[NJ];
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = multiply<BT, AT>(Operand<BT, EXACT>(fb[j], sb[j]), oa, acc[i][j]);
-                // in its place: products put off to behind the barrier, or reads brought forward, keep more fragments than there are registers
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) asm volatile("" : "+v"(acc[i][j]));
+            for (int j = 0; j < NJ; ++j) ob[j] = Operand<BT, EXACT>(fb[j], sb[j]);
+            auto product = [&](const Operand<AT, EXACT>& oa, int i, int j) {
+                acc[i][j] = multiply<BT, AT>(ob[j], oa, acc[i][j]);
+                // in its place: products put off to behind a barrier, or reads brought forward, keep more fragments than there are registers
+                asm volatile("" : "+v"(acc[i][j]));
             };
-#pragma unroll
-            for (int i = 0; i < MI - 2; ++i) {
-                fa[(i + 1) & 1] = frag_a(stage, i + 1);
-                __builtin_amdgcn_sched_barrier(0);   // the read first: it has this row's products to arrive
-                row(i);
+            const uint32_t at_other = __builtin_amdgcn_readfirstlane(lds_wave + (uint32_t)(cur ^ 1) * STAGE);
+            auto loads = [&](auto i) {
+                if constexpr (!DIRECT) return;
+                else if constexpr (i() < ROWS_SECOND) {
+                    static_for<SECOND>([&](auto n) { if constexpr (n() * ROWS_SECOND / SECOND == i()) bring_second(at_other, n); });
+                } else {
+                    static_for<FIRST>([&](auto n) { if constexpr (n() >= (i() - ROWS_SECOND) * FIRST / ROWS_FIRST && n() < (i() - ROWS_SECOND + 1) * FIRST / ROWS_FIRST) bring_first(at, n); });
+                }
+            };
+            auto row = [&](auto i) {
+                const Operand<AT, EXACT> oa(fa[i() & 1], sa[i()]);
+                static_for<NJ>([&](auto j) {
+                    product(oa, i(), j());
+                    if constexpr (j() == 1) loads(i);
+                });
                 __builtin_amdgcn_sched_barrier(0);
-            }
-            const Frag last = frag_a(stage, MI - 1);
-            // everything of this stage has been read, and the next one is there
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-            put_stage(other);
-            if (more) put_scales(scale_lds + (scale_cur ^ 1) * SCALE_BYTES);
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-            __builtin_amdgcn_s_barrier();
-            asm volatile("" ::: "memory");
-            load_stage(lds + cur * STAGE);
-            row(MI - 2);
-            fa[(MI - 1) & 1] = last;
-            row(MI - 1);
-#pragma unroll
-            for (int j = 0; j < NJ; ++j) fb[j] = frag_b(other, j);
-            fa[0] = frag_a(other, 0);
+            };
+            auto read_row = [&](int i) {   // before the row ahead of it is multiplied: it has those products to arrive
+                fa[i & 1] = frag_a(stage, i);
+                __builtin_amdgcn_sched_barrier(0);
+            };
+            static_for<MI / 2 - 1>([&](auto i) {
+                read_row(i() + 1);
+                row(i);
+            });
+            advance();
+            // B and the first halves have been read; the second halves are there
+            wait(std::integral_constant<int, LOADS>{}, more, false);
+            cut_second(stage, left);
+            barrier();
+            static_for<MI / 2 - 1>([&](auto i) {
+                read_row(i() + MI / 2);
+                row(std::integral_constant<int, i() + MI / 2 - 1>{});
+            });
+            read_row(MI - 1);
+            // the second halves have been read; B and the first halves of the next stage are there
+            wait(std::integral_constant<int, SECOND + BEFORE_SECOND_BARRIER>{}, more, more && in_chunk == last_of_chunk);
+            put_held(other);
+            cut_first(other, left > F8_BLOCK ? left - F8_BLOCK : kk_next);
+            barrier();
+            const Frag start = frag_a(other, 0);
+            const Operand<AT, EXACT> o0(fa[0], sa[MI - 2]), o1(fa[1], sa[MI - 1]);
+            static_for<NJ>([&](auto j) {
+                product(o0, MI - 2, j());
+                product(o1, MI - 1, j());
+                if constexpr (j() == 1) loads(std::integral_constant<int, MI - 2>{});
+                if constexpr (j() == 2) loads(std::integral_constant<int, MI - 1>{});
+                fb[j()] = frag_b(other, j());
+                __builtin_amdgcn_sched_barrier(0);
+            });
+            hold();
+            fa[0] = start;
 #pragma unroll
             for (int i = 0; i < MI; ++i) sa[i] >>= 8;
 #pragma unroll
             for (int j = 0; j < NJ; ++j) sb[j] >>= 8;
             cur ^= 1;
-            if (in_chunk == SCALE_BLOCKS - 1 || k + 1 == now.steps) scale_cur ^= 1;
+            if (in_chunk == last_of_chunk) scale_cur ^= 1;
         }
 
         // 16 consecutive columns of a row in every lane
@@ -449,9 +550,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
 #pragma unroll
             for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
+        if (inside) stores = 2;
         now = next;
         if (now.id >= tiles) break;
     }
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));   // nothing may come into LDS that another workgroup has by then
 }
 
 }  // namespace
@@ -463,10 +566,11 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
         max_n = std::max(max_n, plan.s[g].n);
     }
     if (max_m == 0 || max_n == 0) return SBP_OK;
-    bool direct = true, empty = false;   // rows of both operands 16-byte aligned; a shard without anything to sum
+    bool direct = true, scales4 = true, empty = false;   // rows of both operands 16-byte aligned, of their scales 4-byte; a shard without anything to sum
     for (int g = 0; g < plan.groups; ++g) {
         const GemmF8Shard& s = plan.s[g];
         if (s.lda % 16 || s.ldb % 16) direct = false;
+        if (s.ldas % 4 || s.ldbs % 4) scales4 = false;
         empty = empty || s.kk == 0;
         if (s.lda > (1 << 23) || s.ldb > (1 << 23)) empty = true;   // 256 rows of a tile are counted in 32 bits
     }
@@ -497,7 +601,7 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
                 }
                 hipLaunchKernelGGL((gemm_f8_stream_kernel<a(), b(), f32(), gelu(), mb()>), dim3((uint32_t)(tm * tn), (uint32_t)plan.groups), dim3(256), 0, stream, plan, tm);
             };
-            auto tile = [&](auto wm, auto wn, auto mi, auto direct) {
+            auto tile = [&](auto wm, auto wn, auto mi, auto direct, auto scales4) {
                 constexpr int BM = wm() * mi() * 16, BN = wn() * 64;
                 const int tm = tiles_along(max_m, BM), tn = tiles_along(max_n, BN);
                 const int64_t tiles = (int64_t)tm * tn * plan.groups;
@@ -505,19 +609,22 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
                     st = SBP_ERR_UNSUPPORTED;
                     return;
                 }
-                const int64_t at_once = (int64_t)compute_units() * (BM * BN > 128 * 128 ? 1 : 2), all = (tiles + 7) & ~7;
-                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), direct()>), dim3((uint32_t)std::min(all, at_once)),
+                const int64_t at_once = (int64_t)compute_units() * (wm() * wn() > 4 ? 1 : 2), all = (tiles + 7) & ~7;
+                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), direct(), scales4()>), dim3((uint32_t)std::min(all, at_once)),
                                    dim3(wm() * wn() * 64), 0, stream, plan, tm, tn, tn > 8 ? 6 : 2, (int)all);
             };
             using std::integral_constant;
             const auto i2 = integral_constant<int, 2>{};
             const auto i4 = integral_constant<int, 4>{};
+            const auto yes = std::true_type{};
+            const auto no = std::false_type{};
             const int64_t large = (int64_t)tiles_along(max_m, 256) * tiles_along(max_n, 256) * plan.groups;
             if (max_m <= 16) stream_rows(integral_constant<int, 1>{});
             else if (max_m <= 64 || empty) stream_rows(i4);
-            else if (!direct) tile(i2, i2, i4, std::false_type{});
-            else if (large < compute_units()) tile(i2, i2, i4, std::true_type{});
-            else tile(i2, i4, integral_constant<int, 8>{}, std::true_type{});
+            else if (!direct || !scales4) tile(i2, i2, i4, no, no);
+            else if (large < compute_units()) tile(i2, i2, i4, yes, yes);
+            else if constexpr (f32()) tile(i2, i2, i4, yes, yes);
+            else tile(i2, i4, integral_constant<int, 8>{}, yes, yes);
         });
     });
     return st != SBP_OK ? st : launch_status(__func__);
