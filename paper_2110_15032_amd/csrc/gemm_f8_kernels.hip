@@ -94,45 +94,31 @@ __device__ inline float finish(float v) {
     else return gelu_fast(v);
 }
 
-// four consecutive columns of a row, at any alignment
-template <bool F32, bool GELU>
-__device__ inline void store4(const GemmF8Shard& s, int64_t m, int n, f32x4 v) {
-    if (m >= s.m || n >= s.n) return;
+// N consecutive columns of a row, at any alignment; whole: all of them exist
+template <bool F32, bool GELU, int N>
+__device__ inline void store_row(const GemmF8Shard& s, int64_t m, int n, bool whole, const f32x4 (&v)[N / 4]) {
+    static_assert(F32 ? N == 4 : N == 4 || N == 8, "up to 16 bytes");
+    if (!whole && (m >= s.m || n >= s.n)) return;
+    float u[N];
 #pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = finish<F32, GELU>(v[e]);
+    for (int e = 0; e < N; ++e) u[e] = finish<F32, GELU>(v[e >> 2][e & 3]);
     if constexpr (F32) {
         float* dst = static_cast<float*>(s.c) + m * s.ldc + n;
-        if (n + 4 <= s.n) *reinterpret_cast<f32x4_any*>(dst) = v;
+        if (whole || n + N <= s.n) *reinterpret_cast<f32x4_any*>(dst) = f32x4{u[0], u[1], u[2], u[3]};
         else
 #pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (n + e < s.n) dst[e] = v[e];
+            for (int e = 0; e < N - 1; ++e)
+                if (n + e < s.n) dst[e] = u[e];
     } else {
         uint16_t* dst = static_cast<uint16_t*>(s.c) + m * s.ldc + n;
-        const u32x2 w = {f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3])};
-        if (n + 4 <= s.n) *reinterpret_cast<u32x2_half*>(dst) = w;
-        else
+        if (whole || n + N <= s.n) {
+            if constexpr (N == 8) *reinterpret_cast<u32x4_any*>(dst) = u32x4{f32_to_bf16x2(u[0], u[1]), f32_to_bf16x2(u[2], u[3]), f32_to_bf16x2(u[4], u[5]), f32_to_bf16x2(u[6], u[7])};
+            else *reinterpret_cast<u32x2_half*>(dst) = u32x2{f32_to_bf16x2(u[0], u[1]), f32_to_bf16x2(u[2], u[3])};
+        } else {
 #pragma unroll
-            for (int e = 0; e < 3; ++e)
-                if (n + e < s.n) dst[e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
-    }
-}
-
-// sixteen that exist
-template <bool F32, bool GELU>
-__device__ inline void store16(const GemmF8Shard& s, int64_t m, int n, const f32x4 (&v)[4]) {
-    float u[16];
-#pragma unroll
-    for (int e = 0; e < 16; ++e) u[e] = finish<F32, GELU>(v[e >> 2][e & 3]);
-    if constexpr (F32) {
-        float* dst = static_cast<float*>(s.c) + m * s.ldc + n;
-#pragma unroll
-        for (int e = 0; e < 16; e += 4) *reinterpret_cast<f32x4_any*>(dst + e) = f32x4{u[e], u[e + 1], u[e + 2], u[e + 3]};
-    } else {
-        uint16_t* dst = static_cast<uint16_t*>(s.c) + m * s.ldc + n;
-#pragma unroll
-        for (int e = 0; e < 16; e += 8)
-            *reinterpret_cast<u32x4_any*>(dst + e) = u32x4{f32_to_bf16x2(u[e], u[e + 1]), f32_to_bf16x2(u[e + 2], u[e + 3]), f32_to_bf16x2(u[e + 4], u[e + 5]), f32_to_bf16x2(u[e + 6], u[e + 7])};
+            for (int e = 0; e < N - 1; ++e)
+                if (n + e < s.n) dst[e] = f32_to_bf16(u[e]);
+        }
     }
 }
 
@@ -182,7 +168,7 @@ __global__ __launch_bounds__(256) void gemm_f8_stream_kernel(GemmF8Plan p, int t
         f32x4 v = sums[0][i][lane];
 #pragma unroll
         for (int w = 1; w < 4; ++w) v += sums[w][i][lane];
-        store4<F32, GELU>(s, m0 + i * 16 + r, (int)n0 + g * 4, v);
+        store_row<F32, GELU, 4>(s, m0 + i * 16 + r, (int)n0 + g * 4, false, {v});
     }
 }
 
@@ -196,13 +182,17 @@ __global__ __launch_bounds__(256) void gemm_f8_stream_kernel(GemmF8Plan p, int t
 // barrier are multiplied behind it, underneath the reads of the next fragments.
 //
 // LDS image of an operand: rows of 128 bytes, 16-byte chunk c of a row at c ^ key(row), so that the 16 lanes of a read's pass fall on
-// different banks: row / 2 for A, whose fragment is 16 consecutive rows.  B's fragment j is rows 4 j + 0..3 of every 16 of the wave's 64, so that
-// a lane ends with 16 consecutive columns of a row of the result; its key is that place in the fragment over 2.
-template <int ROWS, int NT, bool B_SIDE>
+// different banks: row / 2 where a fragment is 16 consecutive rows, as A's are, and B's for fp32 results.  For bf16 results (PAIRS) B's fragments
+// are taken in pairs, rows 8 i + 0..3 of 32 and rows 8 i + 4..7, so that a lane ends with eight consecutive columns of a row, and four lanes
+// store 64 consecutive bytes either way; the key is the place in the fragment over 2.
+template <int ROWS, int NT, bool PAIRS>
 struct StageF8 {
     static constexpr int PER = ROWS * 8 / NT;   // chunks of a thread
     static constexpr int BYTES = ROWS * F8_BLOCK;
-    __device__ static int key(int row) { return B_SIDE ? ((row >> 4) & 3) << 1 | ((row >> 1) & 1) : (row >> 1) & 7; }
+    __device__ static int key(int row) { return PAIRS ? ((row >> 3) & 3) << 1 | ((row >> 1) & 1) : (row >> 1) & 7; }
+    // row of place r in fragment j, and the byte offset of fragment j from fragment 0
+    __device__ static int fragment_row(int r) { return PAIRS ? (r >> 2) * 8 + (r & 3) : r; }
+    static constexpr int fragment(int j) { return (PAIRS ? (j >> 1) * 32 + (j & 1) * 4 : j * 16) * F8_BLOCK; }
     __device__ static int row_of(int p) { return p >> 3; }
     __device__ static int chunk_of(int p) { return (p & 7) ^ key(p >> 3); }
     // byte offset of chunk position p from the tile's first row; rows past the operand's end are its last one
@@ -221,7 +211,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     constexpr bool EXACT = F32;
     constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * 64, NJ = 4;
     using StA = StageF8<BM, NT, false>;
-    using StB = StageF8<BN, NT, true>;
+    using StB = StageF8<BN, NT, !F32>;
     constexpr int STAGE = StA::BYTES + StB::BYTES;
     constexpr int SCALE_ROWS = (BM + BN) / NT;   // of a thread
     static_assert((BM + BN) % NT == 0, "rows of scales divide over the workgroup");
@@ -262,14 +252,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     int ahead_left;   // reduction elements from the cursor's stage to the end
     uint32_t off_a[StA::PER], off_b[StB::PER];
     gbl_char *src_a, *src_b;
-    // A stage that the reduction ends in: a chunk that starts behind the end is read from the last one that does not (cut_* clears both).
+    // A stage that the reduction ends in: a chunk that starts behind the end is read from the last one that does not (cut_* clears both).  A
+    // thread's chunks of an operand lie at one place in their rows.
+    uint32_t less_a, less_b;
     auto shorten = [&]() {
-        if (!DIRECT || ahead_left >= F8_BLOCK) return;
-        const int last = (ahead_left - 1) >> 4;
-#pragma unroll
-        for (int i = 0; i < StA::PER; ++i) off_a[i] -= (uint32_t)max(StA::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
-#pragma unroll
-        for (int i = 0; i < StB::PER; ++i) off_b[i] -= (uint32_t)max(StB::chunk_of(i * NT + (int)threadIdx.x) - last, 0) * 16u;
+        const int last = min(ahead_left - 1, F8_BLOCK - 1) >> 4;
+        less_a = DIRECT ? (uint32_t)max(StA::chunk_of((int)threadIdx.x) - last, 0) * 16u : 0u;
+        less_b = DIRECT ? (uint32_t)max(StB::chunk_of((int)threadIdx.x) - last, 0) * 16u : 0u;
     };
     auto enter = [&]() {
         const GemmF8Shard& s = p.s[ahead.g];
@@ -288,7 +277,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
             src_a += F8_BLOCK;
             src_b += F8_BLOCK;
             ahead_left -= F8_BLOCK;
-            shorten();
+            if (ahead_left < F8_BLOCK) shorten();
         } else {
             const At t = settle(ahead.id + (int)gridDim.x);
             if (t.id < tiles) {
@@ -301,8 +290,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     auto bring = [&](gbl_char* src, uint32_t off, uint32_t at, auto behind) {
         asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(uniform(src)), "s"(at), "n"(behind()) : "memory", "m0", "scc");
     };
-    auto bring_a = [&](uint32_t at, auto i) { bring(src_a, off_a[i()], at, std::integral_constant<int, i() * NT * 16>{}); };
-    auto bring_b = [&](uint32_t at, auto i) { bring(src_b, off_b[i()], at, std::integral_constant<int, StA::BYTES + i() * NT * 16>{}); };
+    auto bring_a = [&](uint32_t at, auto i) { bring(src_a, off_a[i()] - less_a, at, std::integral_constant<int, i() * NT * 16>{}); };
+    auto bring_b = [&](uint32_t at, auto i) { bring(src_b, off_b[i()] - less_b, at, std::integral_constant<int, StA::BYTES + i() * NT * 16>{}); };
     const uint32_t lds_wave = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)lds + (uint32_t)wave * 1024u);
     u32x4 held[DIRECT ? 1 : LOADS];   // not DIRECT: a stage on its way
     auto hold = [&]() {
@@ -382,13 +371,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     char* const scale_lds = lds + 2 * STAGE;
 
     // ---- fragments
-    const int a_row = wm * MI * 16 + r, b_row = wn * 64 + (r >> 2) * 16 + (r & 3);
+    const int a_row = wm * MI * 16 + r, b_row = wn * 64 + StB::fragment_row(r);
     const int a_lo = a_row * F8_BLOCK + ((g ^ StA::key(a_row)) << 4), b_lo = StA::BYTES + b_row * F8_BLOCK + ((g ^ StB::key(b_row)) << 4);
     auto frag_a = [&](const char* stage, int i) {
         return Frag{*reinterpret_cast<const u32x4*>(stage + a_lo + i * 16 * F8_BLOCK), *reinterpret_cast<const u32x4*>(stage + (a_lo ^ 64) + i * 16 * F8_BLOCK)};
     };
     auto frag_b = [&](const char* stage, int j) {
-        return Frag{*reinterpret_cast<const u32x4*>(stage + b_lo + j * 4 * F8_BLOCK), *reinterpret_cast<const u32x4*>(stage + (b_lo ^ 64) + j * 4 * F8_BLOCK)};
+        return Frag{*reinterpret_cast<const u32x4*>(stage + b_lo + StB::fragment(j)), *reinterpret_cast<const u32x4*>(stage + (b_lo ^ 64) + StB::fragment(j))};
     };
 
     f32x4 acc[MI][NJ];
@@ -440,6 +429,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
 
     int cur = 0, scale_cur = 0;
     uint32_t sa[MI], sb[NJ];
+    auto read_scales = [&](int plane) {
+        const char* const from = scale_lds + scale_cur * SCALE_BYTES + plane * SCALE_PLANE;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(from + (a_row + i * 16) * 4);
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(from + (BM + b_row) * 4 + StB::fragment(j) / F8_BLOCK * 4);
+    };
+    read_scales(0);
     Frag fb[NJ], fa[2];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) fb[j] = frag_b(lds, j);
@@ -462,13 +459,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
                 const bool here = to < now.steps || next.id >= tiles;
                 load_scales(At{0, here ? now.g : next.g, here ? now.m0 : next.m0, here ? now.n0 : next.n0, here ? now.steps : next.steps}, to < now.steps ? to : 0, scale_lds + (scale_cur ^ 1) * SCALE_BYTES);
             }
-            if ((k & 3) == 0) {
-                const char* from = scale_lds + scale_cur * SCALE_BYTES + (in_chunk >> 2) * SCALE_PLANE;
-#pragma unroll
-                for (int i = 0; i < MI; ++i) sa[i] = *reinterpret_cast<const uint32_t*>(from + (a_row + i * 16) * 4);
-#pragma unroll
-                for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(from + (BM + b_row + j * 4) * 4);
-            }
+            __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0): what was read at the end of the last step, so that the reads below are not waited for
             Operand<BT, EXACT> ob[NJ];
 #pragma unroll
             for (int j = 0; j < NJ; ++j) ob[j] = Operand<BT, EXACT>(fb[j], sb[j]);
@@ -529,24 +520,32 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
             });
             hold();
             fa[0] = start;
+            // the next step's scales: the next bytes of these, or the next four blocks'
+            const bool chunk_ends = in_chunk == last_of_chunk;
+            if (chunk_ends) scale_cur ^= 1;
+            if (chunk_ends || (k & 3) == 3) {
+                read_scales(chunk_ends ? 0 : (in_chunk + 1) >> 2);
+            } else {
 #pragma unroll
-            for (int i = 0; i < MI; ++i) sa[i] >>= 8;
+                for (int i = 0; i < MI; ++i) sa[i] >>= 8;
 #pragma unroll
-            for (int j = 0; j < NJ; ++j) sb[j] >>= 8;
+                for (int j = 0; j < NJ; ++j) sb[j] >>= 8;
+            }
             cur ^= 1;
-            if (in_chunk == last_of_chunk) scale_cur ^= 1;
         }
 
-        // 16 consecutive columns of a row in every lane
         const bool inside = now.m0 + BM <= s.m && now.n0 + BN <= s.n;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int64_t m = (int64_t)now.m0 + wm * MI * 16 + i * 16 + r;
-            const int n = now.n0 + wn * 64 + g * 16;
-            if (inside) store16<F32, GELU>(s, m, n, acc[i]);
-            else
+            const int n = now.n0 + wn * 64;
+            if constexpr (F32) {
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) store4<F32, GELU>(s, m, n + j * 4, acc[i][j]);
+                for (int j = 0; j < NJ; ++j) store_row<F32, GELU, 4>(s, m, n + j * 16 + g * 4, inside, {acc[i][j]});
+            } else {
+#pragma unroll
+                for (int j = 0; j < NJ; j += 2) store_row<F32, GELU, 8>(s, m, n + j * 16 + g * 8, inside, {acc[i][j], acc[i][j + 1]});
+            }
 #pragma unroll
             for (int j = 0; j < NJ; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
         }
