@@ -248,6 +248,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     // ---- loads of stages: a cursor that runs two steps ahead of the multiplication, and stays at the last stage of all (whose loads are then
     // repeated into a stage that nobody reads: the waits can count on them)
     constexpr int LOADS = StA::PER + StB::PER;   // instructions of a wave and stage
+    constexpr int DEPTH = MI >= 8 ? 2 : 1;       // rows of products ahead of which a fragment of A is read: one is short where the other wave waits
     At ahead = now;
     int ahead_left;   // reduction elements from the cursor's stage to the end
     uint32_t off_a[StA::PER], off_b[StB::PER];
@@ -389,7 +390,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     // Loads are dealt out over a step's rows of products, one or two in the middle of each: all at once behind a barrier they hold every wave of
     // the workgroup up, and the matrix pipe with them (8192 x 4096 x 16384: 591 us).  The second halves of the stage ahead go with the
     // rows before the first barrier, the first loads of the one after with the others.
-    constexpr int ROWS_SECOND = MI / 2 - 1, ROWS_FIRST = MI - ROWS_SECOND;
+    constexpr int ROWS_SECOND = MI / 2 - DEPTH, ROWS_FIRST = MI - ROWS_SECOND;
     // Waits.  Loads and stores share one in-order counter; the number is how many of the youngest may be on their way.  At the first barrier: all that
     // was brought since the second halves of this stage; at the second: since the first part of the next one.  `stores`: waits that a whole
     // tile's stores may be younger than what is waited for.
@@ -437,10 +438,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
         for (int j = 0; j < NJ; ++j) sb[j] = *reinterpret_cast<const uint32_t*>(from + (BM + b_row) * 4 + StB::fragment(j) / F8_BLOCK * 4);
     };
     read_scales(0);
-    Frag fb[NJ], fa[2];
+    Frag fb[NJ], fa[DEPTH + 1];
 #pragma unroll
     for (int j = 0; j < NJ; ++j) fb[j] = frag_b(lds, j);
-    fa[0] = frag_a(lds, 0);
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i) fa[i] = frag_a(lds, i);
     while (true) {
         const GemmF8Shard& s = p.s[now.g];
         const At next = settle(now.id + (int)gridDim.x);
@@ -478,7 +480,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
                 }
             };
             auto row = [&](auto i) {
-                const Operand<AT, EXACT> oa(fa[i() & 1], sa[i()]);
+                const Operand<AT, EXACT> oa(fa[i() % (DEPTH + 1)], sa[i()]);
                 static_for<NJ>([&](auto j) {
                     product(oa, i(), j());
                     if constexpr (j() == 1) loads(i);
@@ -486,11 +488,11 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
                 __builtin_amdgcn_sched_barrier(0);
             };
             auto read_row = [&](int i) {   // before the row ahead of it is multiplied: it has those products to arrive
-                fa[i & 1] = frag_a(stage, i);
+                fa[i % (DEPTH + 1)] = frag_a(stage, i);
                 __builtin_amdgcn_sched_barrier(0);
             };
-            static_for<MI / 2 - 1>([&](auto i) {
-                read_row(i() + 1);
+            static_for<ROWS_SECOND>([&](auto i) {
+                read_row(i() + DEPTH);
                 row(i);
             });
             advance();
@@ -498,18 +500,18 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
             wait(std::integral_constant<int, LOADS>{}, more, false);
             cut_second(stage, left);
             barrier();
-            static_for<MI / 2 - 1>([&](auto i) {
+            static_for<ROWS_FIRST - 2>([&](auto i) {
                 read_row(i() + MI / 2);
-                row(std::integral_constant<int, i() + MI / 2 - 1>{});
+                row(std::integral_constant<int, i() + ROWS_SECOND>{});
             });
-            read_row(MI - 1);
+            if constexpr (DEPTH == 1) read_row(MI - 1);
             // the second halves have been read; B and the first halves of the next stage are there
             wait(std::integral_constant<int, SECOND + BEFORE_SECOND_BARRIER>{}, more, more && in_chunk == last_of_chunk);
             put_held(other);
             cut_first(other, left > F8_BLOCK ? left - F8_BLOCK : kk_next);
             barrier();
             const Frag start = frag_a(other, 0);
-            const Operand<AT, EXACT> o0(fa[0], sa[MI - 2]), o1(fa[1], sa[MI - 1]);
+            const Operand<AT, EXACT> o0(fa[(MI - 2) % (DEPTH + 1)], sa[MI - 2]), o1(fa[(MI - 1) % (DEPTH + 1)], sa[MI - 1]);
             static_for<NJ>([&](auto j) {
                 product(o0, MI - 2, j());
                 product(o1, MI - 1, j());
@@ -520,6 +522,8 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
             });
             hold();
             fa[0] = start;
+#pragma unroll
+            for (int i = 1; i < DEPTH; ++i) fa[i] = frag_a(other, i);
             // the next step's scales: the next bytes of these, or the next four blocks'
             const bool chunk_ends = in_chunk == last_of_chunk;
             if (chunk_ends) scale_cur ^= 1;
