@@ -21,19 +21,29 @@ typedef u32x2 __attribute__((aligned(2))) u32x2_half;
 struct Frag {
     u32x4 lo, hi;
 };
-__device__ inline u32x4 load_some(const uint8_t* at, int valid) {
+// 16 bytes at `at`, those from `valid` on zero; `before` bytes of the row lie in front.  Nothing outside the row is read: where it ends among the 16,
+// its last 16 are read and shifted.
+__device__ inline u32x4 load_some(const uint8_t* at, int valid, int before) {
     u32x4 v = {0u, 0u, 0u, 0u};
     if (valid >= 16) return *reinterpret_cast<const u32x4_byte*>(at);
-#pragma unroll
-    for (int e = 0; e < 15; ++e)
-        if (e < valid) v[e >> 2] |= (uint32_t)at[e] << (8 * (e & 3));
-    return v;
+    if (valid <= 0) return v;
+    if (before + valid >= 16) {
+        const int gone = 16 - valid;   // bytes to shift out, 1 .. 15
+        const u32x4 w = *reinterpret_cast<const u32x4_byte*>(at - gone);
+        const uint64_t lo = (uint64_t)w[1] << 32 | w[0], hi = (uint64_t)w[3] << 32 | w[2];
+        const int bits = gone * 8 & 63;
+        const uint64_t a = gone >= 8 ? hi >> bits : bits ? lo >> bits | hi << (64 - bits) : lo, b = gone >= 8 ? 0 : hi >> bits;
+        return u32x4{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    }
+    uint64_t lo = 0, hi = 0;   // a row of fewer than 16
+#pragma unroll 1
+    for (int e = valid - 1; e >= 0; --e) {
+        hi = hi << 8 | lo >> 56;
+        lo = lo << 8 | at[e];
+    }
+    return u32x4{(uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32)};
 }
-template <bool WHOLE>
-__device__ inline Frag load_frag(const uint8_t* at, int valid) {
-    if constexpr (WHOLE) return {*reinterpret_cast<const u32x4_byte*>(at), *reinterpret_cast<const u32x4_byte*>(at + 64)};
-    else return {load_some(at, valid), load_some(at + 64, valid - 64)};
-}
+__device__ inline Frag load_frag(const uint8_t* at) { return {*reinterpret_cast<const u32x4_byte*>(at), *reinterpret_cast<const u32x4_byte*>(at + 64)}; }
 
 template <int T>
 __device__ inline bf16x8 widen_frag(uint32_t a, uint32_t b, float scale) {
@@ -122,53 +132,109 @@ __device__ inline void store_row(const GemmF8Shard& s, int64_t m, int n, bool wh
     }
 }
 
-// Few rows: the weights are the traffic, and every workgroup streams 16 of their rows past MB blocks of 16 rows of A, its four waves
-// taking every fourth block of the reduction.  No LDS before the sums meet; operands at any pitch.
-template <int AT, int BT, bool F32, bool GELU, int MB>
-__global__ __launch_bounds__(256) void gemm_f8_stream_kernel(GemmF8Plan p, int tiles_m) {
+// Tiles of MB 16 rows by NB 16 columns whose NW waves take every NW-th block of the reduction, straight from memory into registers: for few rows,
+// where the weights are the traffic and a stage in LDS would only be on their way, and for few tiles.  U blocks at a time, the next ones on their
+// way while these are multiplied; no LDS before the waves' sums meet, in order.  Operands at any pitch.
+template <int AT, int BT, bool F32, bool GELU, int MB, int NB, int NW>
+__global__ __launch_bounds__(NW * 64) void gemm_f8_wave_kernel(GemmF8Plan p, int tm, int tn, int order) {
     constexpr bool EXACT = F32;
-    const GemmF8Shard& s = p.s[blockIdx.y];
-    const int tn = blockIdx.x / tiles_m, tm = blockIdx.x % tiles_m;
-    const int64_t n0 = (int64_t)tn * 16, m0 = (int64_t)tm * (16 * MB);
-    if (n0 >= s.n || m0 >= s.m) return;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 15, g = lane >> 4;
-    const int64_t n = min(n0 + r, (int64_t)s.n - 1);
-    const uint8_t* const b = s.b + n * s.ldb + g * 16;
-    const uint8_t* const bs = s.b_scales + n * s.ldbs;
-    const uint8_t* a[MB];
-    const uint8_t* as[MB];
+    // twice U blocks' registers next to the sums: waves of 16 have 128 each, the others up to 256
+    constexpr int U = std::max(1, (NW == 16 ? 60 : 150 - MB * NB * 4) / (18 * (MB + NB)));
+    const TileCoord t = map_tile(blockIdx.x, gridDim.x, tm, tn, p.groups, order);
+    if (!t.valid) return;
+    const GemmF8Shard& s = p.s[t.g];
+    const int64_t m0 = (int64_t)t.tile_m * (MB * 16), n0 = (int64_t)t.tile_n * (NB * 16);
+    if (m0 >= s.m || n0 >= s.n) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
+    const uint8_t *const a = s.a + m0 * s.lda, *const as = s.a_scales + m0 * s.ldas, *const b = s.b + n0 * s.ldb, *const bs = s.b_scales + n0 * s.ldbs;
+    uint32_t a_row[MB], as_row[MB], b_row[NB], bs_row[NB];   // of this lane's rows, from the tile's first
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
-        const int64_t m = min(m0 + i * 16 + r, (int64_t)s.m - 1);
-        a[i] = s.a + m * s.lda + g * 16;
-        as[i] = s.a_scales + m * s.ldas;
+        const uint32_t m = min((uint32_t)(i * 16 + r), (uint32_t)(s.m - 1 - (int)m0));
+        a_row[i] = m * (uint32_t)s.lda + g * 16;
+        as_row[i] = m * (uint32_t)s.ldas;
     }
-    f32x4 acc[MB];
 #pragma unroll
-    for (int i = 0; i < MB; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    const int whole = s.kk / F8_BLOCK, blocks = (s.kk + F8_BLOCK - 1) / F8_BLOCK;
-    for (int kb = wave; kb < whole; kb += 4) {
-        const int64_t at = (int64_t)kb * F8_BLOCK;
-        const Operand<BT, EXACT> ob(load_frag<true>(b + at, 128), bs[kb]);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) acc[i] = multiply<BT, AT>(ob, Operand<AT, EXACT>(load_frag<true>(a[i] + at, 128), as[i][kb]), acc[i]);
+    for (int j = 0; j < NB; ++j) {
+        const uint32_t n = min((uint32_t)(j * 16 + r), (uint32_t)(s.n - 1 - (int)n0));
+        b_row[j] = n * (uint32_t)s.ldb + g * 16;
+        bs_row[j] = n * (uint32_t)s.ldbs;
     }
-    if (whole < blocks && wave == (whole & 3)) {
-        const int64_t at = (int64_t)whole * F8_BLOCK;
-        const int valid = s.kk - whole * F8_BLOCK - g * 16;
-        const Operand<BT, EXACT> ob(load_frag<false>(b + at, valid), bs[whole]);
+    f32x4 acc[MB][NB];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) acc[i] = multiply<BT, AT>(ob, Operand<AT, EXACT>(load_frag<false>(a[i] + at, valid), as[i][whole]), acc[i]);
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    struct Block {
+        Frag a[MB], b[NB];
+        uint32_t as[MB], bs[NB];
+    };
+    auto scales = [&](Block& o, int kb) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j) o.bs[j] = (bs + kb)[bs_row[j]];
+#pragma unroll
+        for (int i = 0; i < MB; ++i) o.as[i] = (as + kb)[as_row[i]];
+    };
+    auto work = [&](const Block& o) {
+        Operand<BT, EXACT> ob[NB];
+#pragma unroll
+        for (int j = 0; j < NB; ++j) ob[j] = Operand<BT, EXACT>(o.b[j], o.bs[j]);
+#pragma unroll
+        for (int i = 0; i < MB; ++i) {
+            const Operand<AT, EXACT> oa(o.a[i], o.as[i]);
+#pragma unroll
+            for (int j = 0; j < NB; ++j) acc[i][j] = multiply<BT, AT>(ob[j], oa, acc[i][j]);
+        }
+    };
+    // this wave's whole blocks, U at a time
+    const int whole = s.kk / F8_BLOCK, mine = (whole - wave + NW - 1) / NW;
+    auto load = [&](Block (&o)[U], int first) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (first + u < mine) {
+                const int kb = wave + (first + u) * NW;
+                const int64_t at = (int64_t)kb * F8_BLOCK;
+#pragma unroll
+                for (int j = 0; j < NB; ++j) o[u].b[j] = load_frag(b + at + b_row[j]);
+#pragma unroll
+                for (int i = 0; i < MB; ++i) o[u].a[i] = load_frag(a + at + a_row[i]);
+                scales(o[u], kb);
+            }
+    };
+    auto multiply_all = [&](const Block (&o)[U], int first) {
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (first + u < mine) work(o[u]);
+    };
+    Block even[U], odd[U];
+    load(even, 0);
+    for (int first = 0; first < mine; first += 2 * U) {
+        load(odd, first + U);
+        multiply_all(even, first);
+        load(even, first + 2 * U);
+        multiply_all(odd, first + U);
     }
-    __shared__ f32x4 sums[4][MB][64];
+    if (whole * F8_BLOCK < s.kk && wave == whole % NW) {   // the block that the reduction ends in
+        Block last;
+        const int at = whole * F8_BLOCK, left = s.kk - at - g * 16, before = at + g * 16;
 #pragma unroll
-    for (int i = 0; i < MB; ++i) sums[wave][i][lane] = acc[i];
+        for (int j = 0; j < NB; ++j) last.b[j] = {load_some(b + at + b_row[j], left, before), load_some(b + at + b_row[j] + 64, left - 64, before + 64)};
+#pragma unroll
+        for (int i = 0; i < MB; ++i) last.a[i] = {load_some(a + at + a_row[i], left, before), load_some(a + at + a_row[i] + 64, left - 64, before + 64)};
+        scales(last, whole);
+        work(last);
+    }
+    __shared__ f32x4 sums[NW][MB * NB][64];
+#pragma unroll
+    for (int i = 0; i < MB; ++i)
+#pragma unroll
+        for (int j = 0; j < NB; ++j) sums[wave][i * NB + j][lane] = acc[i][j];
     __syncthreads();
-    for (int i = wave; i < MB; i += 4) {
-        f32x4 v = sums[0][i][lane];
+    for (int q = wave; q < MB * NB; q += NW) {
+        f32x4 v = sums[0][q][lane];
 #pragma unroll
-        for (int w = 1; w < 4; ++w) v += sums[w][i][lane];
-        store_row<F32, GELU, 4>(s, m0 + i * 16 + r, (int)n0 + g * 4, false, {v});
+        for (int w = 1; w < NW; ++w) v += sums[w][q][lane];
+        store_row<F32, GELU, 4>(s, m0 + q / NB * 16 + r, (int)n0 + q % NB * 16 + g * 4, false, {v});
     }
 }
 
@@ -297,10 +363,13 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     u32x4 held[DIRECT ? 1 : LOADS];   // not DIRECT: a stage on its way
     auto hold = [&]() {
         if constexpr (!DIRECT) {
+            const int ahead_done = p.s[ahead.g].kk - ahead_left;
+            int at = StA::chunk_of((int)threadIdx.x) * 16;
 #pragma unroll
-            for (int i = 0; i < StA::PER; ++i) held[i] = load_some((const uint8_t*)src_a + off_a[i], ahead_left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+            for (int i = 0; i < StA::PER; ++i) held[i] = load_some((const uint8_t*)src_a + off_a[i], ahead_left - at, ahead_done + at);
+            at = StB::chunk_of((int)threadIdx.x) * 16;
 #pragma unroll
-            for (int i = 0; i < StB::PER; ++i) held[StA::PER + i] = load_some((const uint8_t*)src_b + off_b[i], ahead_left - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
+            for (int i = 0; i < StB::PER; ++i) held[StA::PER + i] = load_some((const uint8_t*)src_b + off_b[i], ahead_left - at, ahead_done + at);
         }
     };
     // B and the first halves of A, then the second halves
@@ -575,7 +644,7 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
         if (s.lda % 16 || s.ldb % 16) direct = false;
         if (s.ldas % 4 || s.ldbs % 4) scales4 = false;
         empty = empty || s.kk == 0;
-        if (s.lda > (1 << 23) || s.ldb > (1 << 23)) empty = true;   // 256 rows of a tile are counted in 32 bits
+        if (s.lda > GEMM_F8_MAX_PITCH || s.ldb > GEMM_F8_MAX_PITCH || s.ldas > GEMM_F8_MAX_PITCH || s.ldbs > GEMM_F8_MAX_PITCH) return SBP_ERR_UNSUPPORTED;
     }
     auto types = [&](auto f) {
         auto second = [&](auto a) {
@@ -596,13 +665,14 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
     int32_t st = SBP_OK;
     types([&](auto a, auto b) {
         results([&](auto f32, auto gelu) {
-            auto stream_rows = [&](auto mb) {
-                const int tm = tiles_along(max_m, 16 * mb()), tn = tiles_along(max_n, 16);
-                if (!grid_fits((int64_t)tm * tn, 256)) {
+            auto by_waves = [&](auto mb, auto nb, auto nw) {
+                const int tm = tiles_along(max_m, 16 * mb()), tn = tiles_along(max_n, 16 * nb());
+                const int64_t all = ((int64_t)tm * tn * plan.groups + 7) & ~7ll;
+                if (!grid_fits(all, 64 * nw())) {
                     st = SBP_ERR_UNSUPPORTED;
                     return;
                 }
-                hipLaunchKernelGGL((gemm_f8_stream_kernel<a(), b(), f32(), gelu(), mb()>), dim3((uint32_t)(tm * tn), (uint32_t)plan.groups), dim3(256), 0, stream, plan, tm);
+                hipLaunchKernelGGL((gemm_f8_wave_kernel<a(), b(), f32(), gelu(), mb(), nb(), nw()>), dim3((uint32_t)all), dim3(64 * nw()), 0, stream, plan, tm, tn, 4);
             };
             auto tile = [&](auto wm, auto wn, auto mi, auto direct, auto scales4) {
                 constexpr int BM = wm() * mi() * 16, BN = wn() * 64;
@@ -621,11 +691,22 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
             const auto i4 = integral_constant<int, 4>{};
             const auto yes = std::true_type{};
             const auto no = std::false_type{};
-            const int64_t large = (int64_t)tiles_along(max_m, 256) * tiles_along(max_n, 256) * plan.groups;
-            if (max_m <= 16) stream_rows(integral_constant<int, 1>{});
-            else if (max_m <= 64 || empty) stream_rows(i4);
+            const auto i1 = integral_constant<int, 1>{};
+            auto tiles_of = [&](int bm, int bn) { return (int64_t)tiles_along(max_m, bm) * tiles_along(max_n, bn) * plan.groups; };
+            const int cu = compute_units();
+            // Few rows or few tiles: as many columns a tile as leave every compute unit one.  us, 64, 32 or 16 columns: 32 rows, 4096 x 16384 on
+            // eight devices 19.7 / 24.1 / 34.1, 4096 x 4096 19.1 / 13.5 / 10.8; 128 rows, 4096 x 4096 25.1 / 19.3 / 30.8 (tiles through LDS
+            // 26.7), 1024 cubed 8.6 / 11.8 / - (10.2); 2048 cubed 47.7 (17.2).
+            auto by_columns = [&](auto mb) {
+                if (tiles_of(16 * mb(), 64) >= cu) by_waves(mb, i4, i4);
+                else if (tiles_of(16 * mb(), 32) >= cu) by_waves(mb, i2, i4);
+                else by_waves(mb, i1, i4);
+            };
+            if (max_m <= 16) by_columns(i1);
+            else if (max_m <= 32) by_columns(i2);
+            else if (tiles_of(64, 64) <= cu || empty) by_columns(i4);
             else if (!direct || !scales4) tile(i2, i2, i4, no, no);
-            else if (large < compute_units()) tile(i2, i2, i4, yes, yes);
+            else if (tiles_of(256, 256) < cu) tile(i2, i2, i4, yes, yes);
             else if constexpr (f32()) tile(i2, i2, i4, yes, yes);
             else tile(i2, i4, integral_constant<int, 8>{}, yes, yes);
         });

@@ -236,6 +236,7 @@ int32_t launch_norm_grad(const NormGradPlan& plan, hipStream_t stream);
 // Grouped product of 8-bit tensors: C_g[m, n] = sum over kk of A_g[m, kk] * B_g[n, kk], both with the reduction index contiguous.
 // ---------------------------------------------------------------------------------------------
 constexpr int GEMM_F8_MAX_K = 32;
+constexpr int GEMM_F8_MAX_PITCH = 1 << 23;   // 256 rows of a tile are counted in 32 bits
 struct GemmF8Shard {
     const uint8_t* a;
     const uint8_t* a_scales;
