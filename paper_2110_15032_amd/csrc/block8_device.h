@@ -177,11 +177,12 @@ template <int CTRL>
 __device__ inline float dpp(float v) {
     return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
 }
-__device__ inline float max_row16(float v) {
-    v = fmaxf(v, dpp<0xB1>(v));
-    v = fmaxf(v, dpp<0x4E>(v));
-    v = fmaxf(v, dpp<0x141>(v));
-    return fmaxf(v, dpp<0x140>(v));
+// of magnitudes as bits: unsigned maxima need no canonical operands, and anything not finite ends up on top
+__device__ inline uint32_t max_row16(uint32_t v) {
+    v = max(v, dpp<0xB1>(v));
+    v = max(v, dpp<0x4E>(v));
+    v = max(v, dpp<0x141>(v));
+    return max(v, dpp<0x140>(v));
 }
 __device__ inline float sum_wave(float v) {
     v += dpp<0xB1>(v);
@@ -194,18 +195,32 @@ __device__ inline float sum_wave(float v) {
     return __uint_as_float(h[0]) + __uint_as_float(h[1]);
 }
 
-// Largest finite magnitude of the 128 values that 16 lanes hold eight each.  A NaN is passed over by the maximum; a block with an
-// infinity is gone through again without it.
-__device__ inline float most_of_block(const float (&v)[8]) {
-    float m = fmaxf(fmaxf(fmaxf(fabsf(v[0]), fabsf(v[1])), fmaxf(fabsf(v[2]), fabsf(v[3]))), fmaxf(fmaxf(fabsf(v[4]), fabsf(v[5])), fmaxf(fabsf(v[6]), fabsf(v[7]))));
-    m = max_row16(m);
-    if (m == INFINITY) {   // the 16 lanes of a block go here together
-        m = 0.0f;
+// max(|a|, |b|, |c|), a NaN passed over next to a number (as assembly: fmaxf would make its operands canonical first)
+__device__ inline float max3_abs(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, |%1|, |%2|, |%3|" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+__device__ inline float most_of_8(const float (&v)[8]) {
+    const float m = max3_abs(v[0], v[1], v[2]);
+    return max3_abs(max3_abs(m, v[3], v[4]), v[5], max3_abs(v[6], v[7], v[7]));
+}
+__device__ inline float most_finite_of_8(const float (&v)[8]) {
+    uint32_t m = 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) m = fmaxf(m, fabsf(v[e]) < INFINITY ? fabsf(v[e]) : 0.0f);
-        m = max_row16(m);
+    for (int e = 0; e < 8; ++e) {
+        const uint32_t u = __float_as_uint(v[e]) & 0x7FFFFFFFu;
+        m = max(m, u < 0x7F800000u ? u : 0u);
     }
-    return m == m ? m : 0.0f;   // all NaN
+    return __uint_as_float(m);
+}
+
+// Largest finite magnitude of the 128 values that 16 lanes hold eight each.  A block with an infinity (or of NaN alone) is gone through again
+// without it; its 16 lanes go there together.
+__device__ inline float most_of_block(const float (&v)[8]) {
+    uint32_t m = max_row16(__float_as_uint(most_of_8(v)));
+    if (m >= 0x7F800000u) m = max_row16(__float_as_uint(most_finite_of_8(v)));
+    return __uint_as_float(m);
 }
 
 // 8-bit form of the values that 16 lanes hold eight each, and their block's scale byte.

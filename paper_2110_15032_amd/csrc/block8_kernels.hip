@@ -10,32 +10,28 @@ namespace {
 
 constexpr int NT = 256;
 
-// The blocks of 128 of a row-major tensor, 16 lanes to a block: (row, block) by one division, then advanced by the grid stride with adds.
-struct BlockWalk {
-    uint32_t nb, dr, db, b;
-    int64_t r;
-    __device__ BlockWalk(int cols, int64_t first, int64_t stride) {
-        nb = (uint32_t)((cols + F8_BLOCK - 1) / F8_BLOCK);
-        if (first < UINT32_MAX && stride < UINT32_MAX) {
-            dr = (uint32_t)stride / nb;
-            db = (uint32_t)stride % nb;
-            r = (uint32_t)first / nb;
-            b = (uint32_t)first % nb;
-        } else {
-            dr = (uint32_t)(stride / nb);
-            db = (uint32_t)(stride % nb);
-            r = first / nb;
-            b = (uint32_t)(first % nb);
-        }
+// Pairs of blocks of 128 of a row-major tensor, 16 lanes to a pair with eight elements of either block each (one address for both, and whole cache
+// lines a load): (row, pair) by one division, then advanced by the grid stride with adds.
+constexpr int UNIT = 2 * F8_BLOCK;
+struct UnitWalk {
+    uint32_t per_row, dr, db, b, r;
+    __device__ UnitWalk(int cols) {
+        per_row = (uint32_t)((cols + UNIT - 1) / UNIT);
+        const uint32_t stride = gridDim.x * (NT / 16), first = blockIdx.x * (NT / 16) + (threadIdx.x >> 4);   // a grid is at most 2^16 workgroups
+        dr = stride / per_row;
+        db = stride % per_row;
+        r = first / per_row;
+        b = first % per_row;
     }
     __device__ void next() {
         r += dr;
         b += db;
-        if (b >= nb) {
-            b -= nb;
+        if (b >= per_row) {
+            b -= per_row;
             ++r;
         }
     }
+    __device__ int64_t at(int ld) const { return (int64_t)((uint64_t)r * (uint32_t)ld); }
 };
 
 // Rounding to 8 bits makes GeLU's fit to 2.2e-5 as good as an exact one; so does rounding to bf16.
@@ -50,32 +46,42 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
     if (s.rows == 0 || s.cols == 0) return;
     const int lane = threadIdx.x & 15;
-    const int64_t stride = (int64_t)gridDim.x * (NT / 16);
-    BlockWalk w(s.cols, (int64_t)blockIdx.x * (NT / 16) + (threadIdx.x >> 4), stride);
-    for (; w.r < s.rows; w.next()) {
-        const int c = (int)w.b * F8_BLOCK + lane * 8;
-        const Raw8<XT> raw = load8<XT>(static_cast<const char*>(s.x) + (w.r * s.ldx + c) * bytes_of<XT>, s.cols - c);
-        float v[8];
-        widen<XT>(raw, 1.0f, v);
-        if constexpr (GELU) {
+    for (UnitWalk w(s.cols); w.r < (uint32_t)s.rows; w.next()) {
+        const int c = (int)w.b * UNIT + lane * 8;
+        const char* const from = static_cast<const char*>(s.x) + (w.at(s.ldx) + c) * bytes_of<XT>;
+        char* const to = static_cast<char*>(s.out) + w.at(s.ldo) + c;
+        uint8_t* const scales = static_cast<uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
+        Raw8<XT> raw[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = gelu_of<true>(v[e]);
+        for (int u = 0; u < 2; ++u) raw[u] = load8<XT>(from + u * F8_BLOCK * bytes_of<XT>, s.cols - c - u * F8_BLOCK);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float v[8];
+            widen<XT>(raw[u], 1.0f, v);
+            if constexpr (GELU) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = gelu_of<true>(v[e]);
+            }
+            uint32_t byte;
+            const Raw8<QT> q = narrow_block<QT>(v, byte);
+            store8<QT>(to + u * F8_BLOCK, q, s.cols - c - u * F8_BLOCK);
+            if (lane == 0 && c + u * F8_BLOCK < s.cols) scales[u] = (uint8_t)byte;
         }
-        uint32_t byte;
-        const Raw8<QT> q = narrow_block<QT>(v, byte);
-        store8<QT>(static_cast<char*>(s.out) + w.r * s.ldo + c, q, s.cols - c);
-        if (lane == 0) static_cast<uint8_t*>(s.scales)[w.r * s.lds + w.b] = (uint8_t)byte;
     }
 }
 
 // Transposed: the block runs along the rows.  A workgroup takes 128 rows by 64 columns; thread t holds rows 4 (t / 8) .. + 3 of the eight
 // columns 8 (t % 8), the column maxima meet over the lanes of a wave and over the waves in LDS, the bytes turn in LDS.
 constexpr int TC = 64;
-constexpr int QPITCH = F8_BLOCK + 16;   // bytes of one column in LDS
+// Bytes of one column in LDS.  Its 4-byte words are permuted by XOR with turn_key(column / 8), a multiple of four: the eight columns 8 co + e that a
+// wave's lanes write at once (eight consecutive words each) fall on different banks.
+constexpr int QPITCH = F8_BLOCK + 16;
+__device__ inline int turn_key(int co) { return (co >> 1 & 3) * 8; }
 template <int XT, int QT, bool GELU>
 __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, int tiles_r, int tiles_c) {
     const Block8Shard& s = p.s[blockIdx.y];
-    __shared__ float most[4][TC];
+    __shared__ uint32_t most[4][TC];
+    __shared__ __attribute__((aligned(16))) float scale[TC];
     __shared__ __attribute__((aligned(16))) char turn[TC * QPITCH];
     const int t = threadIdx.x, wave = t >> 6, co = t & 7, rg = t >> 3;
     for (int64_t tile = blockIdx.x; tile < (int64_t)tiles_r * tiles_c; tile += gridDim.x) {
@@ -99,37 +105,54 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
                 for (int e = 0; e < 8; ++e) v[i][e] = gelu_of<true>(v[i][e]);
             }
         }
-        float m[8];
+        uint32_t m[8];
+        bool finite = true;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            m[e] = 0.0f;
+            m[e] = __float_as_uint(max3_abs(max3_abs(v[0][e], v[1][e], v[2][e]), v[3][e], v[3][e]));
+            finite = finite && m[e] < 0x7F800000u;
+        }
+        if (!finite) {   // infinities, or NaN alone
 #pragma unroll
-            for (int i = 0; i < 4; ++i) m[e] = fmaxf(m[e], fabsf(v[i][e]) < INFINITY ? fabsf(v[i][e]) : 0.0f);
-            m[e] = fmaxf(m[e], dpp<0x128>(m[e]));   // eight lanes on in the row of 16
-            auto h = __builtin_amdgcn_permlane16_swap(__float_as_uint(m[e]), __float_as_uint(m[e]), false, false);
-            m[e] = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
-            h = __builtin_amdgcn_permlane32_swap(__float_as_uint(m[e]), __float_as_uint(m[e]), false, false);
-            m[e] = fmaxf(__uint_as_float(h[0]), __uint_as_float(h[1]));
+            for (int e = 0; e < 8; ++e) {
+                m[e] = 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t u = __float_as_uint(v[i][e]) & 0x7FFFFFFFu;
+                    m[e] = max(m[e], u < 0x7F800000u ? u : 0u);
+                }
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            m[e] = max(m[e], dpp<0x128>(m[e]));   // eight lanes on in the row of 16
+            auto h = __builtin_amdgcn_permlane16_swap(m[e], m[e], false, false);
+            m[e] = max((uint32_t)h[0], (uint32_t)h[1]);
+            h = __builtin_amdgcn_permlane32_swap(m[e], m[e], false, false);
+            m[e] = max((uint32_t)h[0], (uint32_t)h[1]);
         }
         if ((t & 63) < 8) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) most[wave][co * 8 + e] = m[e];
         }
         __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int j = co * 8 + e;
-            const uint32_t byte = scale_byte<QT>(fmaxf(fmaxf(most[0][j], most[1][j]), fmaxf(most[2][j], most[3][j])));
-            *reinterpret_cast<uint32_t*>(turn + j * QPITCH + rg * 4) = narrow4<QT>(v[0][e], v[1][e], v[2][e], v[3][e], scale_of(byte));
-            if (rg == 0 && c + e < s.cols) static_cast<uint8_t*>(s.scales)[(c + e) * s.lds + tr] = (uint8_t)byte;
+        if (t < TC) {
+            const uint32_t byte = scale_byte<QT>(__uint_as_float(max(max(most[0][t], most[1][t]), max(most[2][t], most[3][t]))));
+            scale[t] = scale_of(byte);
+            if (c0 + t < s.cols) static_cast<uint8_t*>(s.scales)[(c0 + t) * s.lds + tr] = (uint8_t)byte;
         }
+        __syncthreads();
+        const f32x4 s0 = *reinterpret_cast<const f32x4*>(scale + co * 8), s1 = *reinterpret_cast<const f32x4*>(scale + co * 8 + 4);
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+            *reinterpret_cast<uint32_t*>(turn + (co * 8 + e) * QPITCH + (rg ^ turn_key(co)) * 4) = narrow4<QT>(v[0][e], v[1][e], v[2][e], v[3][e], e < 4 ? s0[e] : s1[e - 4]);
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < TC * 8 / NT; ++i) {
             const int j = (i * NT + t) >> 3, at = ((i * NT + t) & 7) * 16;
             const int64_t r = r0 + at;
             if (c0 + j >= s.cols || r >= s.rows) continue;
-            const u32x4 w = *reinterpret_cast<const u32x4*>(turn + j * QPITCH + at);
+            const u32x4 w = *reinterpret_cast<const u32x4*>(turn + j * QPITCH + (at ^ turn_key(j >> 3) * 4));
             char* dst = static_cast<char*>(s.out) + (c0 + j) * (int64_t)s.ldo + r;
             if (r + 16 <= s.rows) {
                 __builtin_memcpy(dst, &w, 16);
@@ -148,19 +171,28 @@ __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
     if (s.rows == 0 || s.cols == 0) return;
     const int lane = threadIdx.x & 15;
-    const int64_t stride = (int64_t)gridDim.x * (NT / 16);
-    BlockWalk w(s.cols, (int64_t)blockIdx.x * (NT / 16) + (threadIdx.x >> 4), stride);
-    for (; w.r < s.rows; w.next()) {
-        const int c = (int)w.b * F8_BLOCK + lane * 8;
-        const Raw8<QT> raw = load8<QT>(static_cast<const char*>(s.x) + w.r * s.ldx + c, s.cols - c);
-        const float scale = scale_of(static_cast<const uint8_t*>(s.scales)[w.r * s.lds + w.b]);
-        float v[8];
-        widen<QT>(raw, scale, v);
-        if constexpr (GELU) {
+    for (UnitWalk w(s.cols); w.r < (uint32_t)s.rows; w.next()) {
+        const int c = (int)w.b * UNIT + lane * 8;
+        const char* const from = static_cast<const char*>(s.x) + w.at(s.ldx) + c;
+        char* const to = static_cast<char*>(s.out) + (w.at(s.ldo) + c) * bytes_of<YT>;
+        const uint8_t* const scales = static_cast<const uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
+        Raw8<QT> raw[2];
+        uint32_t byte[2];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = gelu_of<YT == T_BF16>(v[e]);
+        for (int u = 0; u < 2; ++u) {
+            raw[u] = load8<QT>(from + u * F8_BLOCK, s.cols - c - u * F8_BLOCK);
+            byte[u] = scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0];
         }
-        store8<YT>(static_cast<char*>(s.out) + (w.r * s.ldo + c) * bytes_of<YT>, narrow<YT>(v), s.cols - c);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float v[8];
+            widen<QT>(raw[u], scale_of(byte[u]), v);
+            if constexpr (GELU) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = gelu_of<YT == T_BF16>(v[e]);
+            }
+            store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(v), s.cols - c - u * F8_BLOCK);
+        }
     }
 }
 
@@ -231,27 +263,39 @@ __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
     if (s.rows == 0 || s.cols == 0) return;
     const int lane = threadIdx.x & 15;
-    const int64_t stride = (int64_t)gridDim.x * (NT / 16);
-    BlockWalk w(s.cols, (int64_t)blockIdx.x * (NT / 16) + (threadIdx.x >> 4), stride);
-    for (; w.r < s.rows; w.next()) {
-        const int c = (int)w.b * F8_BLOCK + lane * 8;
-        const Raw8<AT> ra = load8<AT>(static_cast<const char*>(s.x) + (w.r * s.ldx + c) * bytes_of<AT>, s.cols - c);
-        const Raw8<YT> rh = load8<YT>(static_cast<const char*>(s.dh) + (w.r * s.lddh + c) * bytes_of<YT>, s.cols - c);
-        float scale = 1.0f;
-        if constexpr (bytes_of<AT> == 1) scale = scale_of(static_cast<const uint8_t*>(s.scales)[w.r * s.lds + w.b]);
-        float a[8], h[8];
-        widen<AT>(ra, scale, a);
-        widen<YT>(rh, 1.0f, h);
+    for (UnitWalk w(s.cols); w.r < (uint32_t)s.rows; w.next()) {
+        const int c = (int)w.b * UNIT + lane * 8;
+        const char* const from_a = static_cast<const char*>(s.x) + (w.at(s.ldx) + c) * bytes_of<AT>;
+        const char* const from_h = static_cast<const char*>(s.dh) + (w.at(s.lddh) + c) * bytes_of<YT>;
+        char* const to = static_cast<char*>(s.out) + (w.at(s.ldo) + c) * bytes_of<YT>;
+        Raw8<AT> ra[2];
+        Raw8<YT> rh[2];
+        float scale[2] = {1.0f, 1.0f};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) h[e] *= gelu_slope(a[e]);
-        store8<YT>(static_cast<char*>(s.out) + (w.r * s.ldo + c) * bytes_of<YT>, narrow<YT>(h), s.cols - c);
+        for (int u = 0; u < 2; ++u) {
+            ra[u] = load8<AT>(from_a + u * F8_BLOCK * bytes_of<AT>, s.cols - c - u * F8_BLOCK);
+            rh[u] = load8<YT>(from_h + u * F8_BLOCK * bytes_of<YT>, s.cols - c - u * F8_BLOCK);
+            if constexpr (bytes_of<AT> == 1) {
+                const uint8_t* const scales = static_cast<const uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
+                scale[u] = scale_of(scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            float a[8], h[8];
+            widen<AT>(ra[u], scale[u], a);
+            widen<YT>(rh[u], 1.0f, h);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) h[e] *= gelu_slope(a[e]);
+            store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(h), s.cols - c - u * F8_BLOCK);
+        }
     }
 }
 
-// grid of the kernels that walk blocks of 128
+// grid of the kernels that walk pairs of blocks
 dim3 walk_grid(const Block8Plan& plan) {
     int64_t most = 0;
-    for (int i = 0; i < plan.k; ++i) most = std::max(most, plan.s[i].rows * f8_blocks(plan.s[i].cols));
+    for (int i = 0; i < plan.k; ++i) most = std::max(most, plan.s[i].rows * (((int64_t)plan.s[i].cols + UNIT - 1) / UNIT));
     int64_t bx = (most + NT / 16 - 1) / (NT / 16);
     bx = std::min<int64_t>(bx, (1 << 16) / plan.k);
     return dim3((uint32_t)std::max<int64_t>(bx, 1), (uint32_t)plan.k);

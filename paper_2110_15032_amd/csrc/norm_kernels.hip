@@ -24,7 +24,7 @@ __device__ inline void load_weight(const void* w, int t, int cols, float otherwi
             widen<WT>(load8<WT>(static_cast<const char*>(w) + (int64_t)c * bytes_of<WT>, cols - c), 1.0f, u);
         } else {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = otherwise;
+            for (int e = 0; e < 8; ++e) u[e] = c + e < cols ? otherwise : 0.0f;   // zeros behind the row's end, as load8 gives
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) out[v * 8 + e] = u[e];
@@ -45,6 +45,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
     int have = 0;   // elements of this lane
 #pragma unroll
     for (int v = 0; v < V; ++v) have += min(max(cols - (v * TPR + t) * 8, 0), 8);
+    const bool whole = cols == TPR * V * 8;   // no lane is without elements
     const float of_wave = sum_wave((float)have), over_wave = of_wave > 0.0f ? 1.0f / of_wave : 0.0f, over = 1.0f / (float)cols;
 
     const int step = gridDim.x * G;
@@ -75,13 +76,21 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
         sum = sum_wave(sum);
         const float centre = sum * over_wave;
         float sq = 0.0f;
+        if (whole) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int left = cols - (v * TPR + t) * 8;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float d = e < left ? x[v * 8 + e] - centre : 0.0f;
+            for (int i = 0; i < V * 8; ++i) {
+                const float d = x[i] - centre;
                 sq = fmaf(d, d, sq);
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int left = cols - (v * TPR + t) * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float d = e < left ? x[v * 8 + e] - centre : 0.0f;
+                    sq = fmaf(d, d, sq);
+                }
             }
         }
         sq = sum_wave(sq);
@@ -107,7 +116,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
                 m2 += fmaf(of[w] * d, d, part[turn][w].y);
             }
         }
-        const float rstd = 1.0f / sqrtf(fmaf(m2, over, p.eps));
+        const float rstd = 1.0f / sqrtf(fmaf(m2, over, p.eps)), shift = -mean * rstd;
         if (row >= s.rows) continue;
         if (t == 0 && s.mean) {
             s.mean[row] = mean;
@@ -118,12 +127,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
             const int c = (v * TPR + t) * 8;
             float y[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = fmaf((x[v * 8 + e] - mean) * rstd, gamma[v * 8 + e], beta[v * 8 + e]);
+            for (int e = 0; e < 8; ++e) y[e] = fmaf(fmaf(x[v * 8 + e], rstd, shift), gamma[v * 8 + e], beta[v * 8 + e]);
             char* dst = static_cast<char*>(s.y) + (row * s.ldy + c) * bytes_of<YT>;
             if constexpr (bytes_of<YT> == 1) {
-                if (c / F8_BLOCK * F8_BLOCK >= cols) continue;   // no column of this lane's block exists
-#pragma unroll
-                for (int e = 0; e < 8; ++e) y[e] = c + e < cols ? y[e] : 0.0f;
+                if (c / F8_BLOCK * F8_BLOCK >= cols) continue;   // no column of this lane's block exists; behind the row's end gamma and beta are 0, and y is
                 uint32_t byte;
                 const Raw8<YT> q = narrow_block<YT>(y, byte);
                 store8<YT>(dst, q, cols - c);
@@ -138,7 +145,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
 // One partial sum of the weights' gradients for every workgroup, in the order of its rows; where a shard has one workgroup, that is the result.
 // GROUPS rows of TPR threads side by side in a workgroup: their sums meet in LDS at the end, so that fewer partial sums go to memory.
 template <int XT, int YT, int WT, int TPR, int V>
-__global__ __launch_bounds__(GRAD_NT) void norm_grad_kernel(NormGradPlan p) {
+__global__ __launch_bounds__(GRAD_NT, TPR == 512 ? 2 : 4) void norm_grad_kernel(NormGradPlan p) {
     constexpr int G = GRAD_NT / TPR, NW = TPR / 64, CAP = TPR * V * 8;
     const NormGradShard& s = p.s[blockIdx.y];
     if ((int)blockIdx.x >= s.blocks) return;
@@ -178,10 +185,9 @@ __global__ __launch_bounds__(GRAD_NT) void norm_grad_kernel(NormGradPlan p) {
             float u[8], w[8];
             widen<XT>(next_x[v], next_scale[v], u);
             widen<YT>(next_dy[v], 1.0f, w);
-            const int left = row < s.rows ? cols - (v * TPR + t) * 8 : 0;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                xhat[v * 8 + e] = e < left ? (u[e] - mean) * rstd : 0.0f;
+            for (int e = 0; e < 8; ++e) {   // dy is 0 where there is no element, mean and rstd where there is no row
+                xhat[v * 8 + e] = (u[e] - mean) * rstd;
                 dy[v * 8 + e] = w[e];
             }
         }
@@ -271,8 +277,18 @@ __global__ __launch_bounds__(256) void norm_grad_join_kernel(NormGradPlan p) {
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, width = 2 * p.cols;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float a = 0.0f;
-    if (c < width)
-        for (int b = run; b < s.blocks; b += 8) a += s.part[(int64_t)b * width + c];
+    if (c < width) {
+        const float* part = s.part + c;
+        int b = run;
+        for (; b + 56 < s.blocks; b += 64) {   // eight on their way
+            float v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) v[u] = part[(int64_t)(b + 8 * u) * width];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) a += v[u];
+        }
+        for (; b < s.blocks; b += 8) a += part[(int64_t)b * width];
+    }
     sums[run][lane] = a;
     __syncthreads();
     if (run == 0 && c < width) {
@@ -296,8 +312,8 @@ void with_wide(int32_t dtype, F&& f) {
     else f(std::integral_constant<int, T_BF16>{});
 }
 
-// threads of a row in the gradient: a vector a lane up to 512 columns, then two up to 4096
-int grad_tpr(int64_t cols) { return cols <= 512 ? 64 : cols <= 4096 ? 256 : 512; }
+// threads of a row in the gradient
+int grad_tpr(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 4096 ? 256 : 512; }
 
 }  // namespace
 
@@ -314,6 +330,7 @@ int32_t launch_norm(const NormPlan& plan, hipStream_t stream) {
                 };
                 using std::integral_constant;
                 if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
                 else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
                 else if (plan.cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
                 else if (plan.cols <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
@@ -344,6 +361,8 @@ int32_t launch_norm_grad(const NormGradPlan& plan, hipStream_t stream) {
                 };
                 using std::integral_constant;
                 if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+                else if (plan.cols <= 1024) go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
                 else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
                 else if (plan.cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
                 else if (plan.cols <= 8192) go(integral_constant<int, 512>{}, integral_constant<int, 2>{});
