@@ -34,30 +34,54 @@ struct Raw8<T_E5M2> {
     u32x2 w;
 };
 
-// `valid` of eight elements at `at` exist (8 and more: all, none: 0 and less); the others are zero and not read.
+// Eight elements of a row from column c on, those behind its end (`cols`) as whatever settle8 makes zero: where the row ends among them its last
+// eight are read, and nothing outside the row.  The loads are all that happens here, so that a row can be on its way while another is worked on
+// (only a row shorter than eight is put together at once).
 template <int T>
-__device__ inline Raw8<T> load8(const void* at, int valid) {
+__device__ inline Raw8<T> load8(const char* row, int c, int cols) {
     Raw8<T> r{};
-    const char* p = static_cast<const char*>(at);
-    if (valid >= 8) {
+    if (c >= cols) return r;
+    if (cols >= 8) {
+        const char* const p = row + (int64_t)min(c, cols - 8) * bytes_of<T>;
         if constexpr (T == T_F32) {
             r.a = *reinterpret_cast<const f32x4_any*>(p);
             r.b = *reinterpret_cast<const f32x4_any*>(p + 16);
         } else if constexpr (T == T_BF16) r.w = *reinterpret_cast<const u32x4_any*>(p);
         else r.w = *reinterpret_cast<const u32x2_any*>(p);
-    } else if (valid > 0) {
+    } else {   // c is 0
 #pragma unroll
         for (int e = 0; e < 7; ++e)
-            if (e < valid) {
+            if (e < cols) {
                 if constexpr (T == T_F32) {
-                    const float v = reinterpret_cast<const float*>(p)[e];
+                    const float v = reinterpret_cast<const float*>(row)[e];
                     if (e < 4) r.a[e] = v;
                     else r.b[e - 4] = v;
-                } else if constexpr (T == T_BF16) r.w[e >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(p)[e] << (16 * (e & 1));
-                else r.w[e >> 2] |= (uint32_t) reinterpret_cast<const uint8_t*>(p)[e] << (8 * (e & 3));
+                } else if constexpr (T == T_BF16) r.w[e >> 1] |= (uint32_t) reinterpret_cast<const uint16_t*>(row)[e] << (16 * (e & 1));
+                else r.w[e >> 2] |= (uint32_t) reinterpret_cast<const uint8_t*>(row)[e] << (8 * (e & 3));
             }
     }
     return r;
+}
+template <int T>
+__device__ inline Raw8<T> settle8(Raw8<T> r, int c, int cols) {
+    const int gone = c + 8 - cols;   // 1 .. 7: that many elements in front belong to the lane before
+    if (gone <= 0 || gone >= 8 || cols < 8) return r;
+    if constexpr (T == T_F32) {
+        float v[8] = {r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
+#pragma unroll
+        for (int by = 4; by > 0; by >>= 1)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gone & by ? (e + by < 8 ? v[e + by] : 0.0f) : v[e];
+        return {f32x4{v[0], v[1], v[2], v[3]}, f32x4{v[4], v[5], v[6], v[7]}};
+    } else if constexpr (T == T_BF16) {
+        const uint64_t lo = (uint64_t)r.w[1] << 32 | r.w[0], hi = (uint64_t)r.w[3] << 32 | r.w[2];
+        const int bits = gone * 16 & 63;
+        const uint64_t x = gone >= 4 ? hi >> bits : lo >> bits | hi << (64 - bits), y = gone >= 4 ? 0 : hi >> bits;
+        return {u32x4{(uint32_t)x, (uint32_t)(x >> 32), (uint32_t)y, (uint32_t)(y >> 32)}};
+    } else {
+        const uint64_t x = ((uint64_t)r.w[1] << 32 | r.w[0]) >> (gone * 8);
+        return {u32x2{(uint32_t)x, (uint32_t)(x >> 32)}};
+    }
 }
 template <int T>
 __device__ inline void store8(void* at, const Raw8<T> r, int valid) {

@@ -48,16 +48,16 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
     const int lane = threadIdx.x & 15;
     for (UnitWalk w(s.cols); w.r < (uint32_t)s.rows; w.next()) {
         const int c = (int)w.b * UNIT + lane * 8;
-        const char* const from = static_cast<const char*>(s.x) + (w.at(s.ldx) + c) * bytes_of<XT>;
+        const char* const from = static_cast<const char*>(s.x) + w.at(s.ldx) * bytes_of<XT>;
         char* const to = static_cast<char*>(s.out) + w.at(s.ldo) + c;
         uint8_t* const scales = static_cast<uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
         Raw8<XT> raw[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) raw[u] = load8<XT>(from + u * F8_BLOCK * bytes_of<XT>, s.cols - c - u * F8_BLOCK);
+        for (int u = 0; u < 2; ++u) raw[u] = load8<XT>(from, c + u * F8_BLOCK, s.cols);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float v[8];
-            widen<XT>(raw[u], 1.0f, v);
+            widen<XT>(settle8<XT>(raw[u], c + u * F8_BLOCK, s.cols), 1.0f, v);
             if constexpr (GELU) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = gelu_of<true>(v[e]);
@@ -89,17 +89,17 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
         const int64_t r0 = (int64_t)tr * F8_BLOCK;
         const int64_t c0 = (int64_t)tc * TC;
         if (r0 >= s.rows || c0 >= s.cols) continue;
-        const int64_t c = c0 + co * 8;
+        const int c = (int)c0 + co * 8;
         Raw8<XT> raw[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t r = r0 + rg * 4 + i;
-            raw[i] = load8<XT>(static_cast<const char*>(s.x) + (r * s.ldx + c) * bytes_of<XT>, r < s.rows ? (int)(c < s.cols ? s.cols - c : 0) : 0);
+            raw[i] = load8<XT>(static_cast<const char*>(s.x) + r * s.ldx * bytes_of<XT>, c, r < s.rows ? s.cols : 0);
         }
         float v[4][8];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            widen<XT>(raw[i], 1.0f, v[i]);
+            widen<XT>(settle8<XT>(raw[i], c, r0 + rg * 4 + i < s.rows ? s.cols : 0), 1.0f, v[i]);
             if constexpr (GELU) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[i][e] = gelu_of<true>(v[i][e]);
@@ -173,20 +173,20 @@ __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
     const int lane = threadIdx.x & 15;
     for (UnitWalk w(s.cols); w.r < (uint32_t)s.rows; w.next()) {
         const int c = (int)w.b * UNIT + lane * 8;
-        const char* const from = static_cast<const char*>(s.x) + w.at(s.ldx) + c;
+        const char* const from = static_cast<const char*>(s.x) + w.at(s.ldx);
         char* const to = static_cast<char*>(s.out) + (w.at(s.ldo) + c) * bytes_of<YT>;
         const uint8_t* const scales = static_cast<const uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
         Raw8<QT> raw[2];
         uint32_t byte[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            raw[u] = load8<QT>(from + u * F8_BLOCK, s.cols - c - u * F8_BLOCK);
+            raw[u] = load8<QT>(from, c + u * F8_BLOCK, s.cols);
             byte[u] = scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0];
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float v[8];
-            widen<QT>(raw[u], scale_of(byte[u]), v);
+            widen<QT>(settle8<QT>(raw[u], c + u * F8_BLOCK, s.cols), scale_of(byte[u]), v);
             if constexpr (GELU) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = gelu_of<YT == T_BF16>(v[e]);
@@ -211,9 +211,9 @@ __global__ __launch_bounds__(NT) void dequantize_transposed_kernel(Block8Plan p,
 #pragma unroll
         for (int i = 0; i < TC * 16 / NT; ++i) {
             const int j = (i * NT + t) >> 4, at = ((i * NT + t) & 15) * 8;
-            const int64_t left = c0 + j < s.cols ? s.rows - (r0 + at) : 0;
-            const Raw8<QT> raw = load8<QT>(static_cast<const char*>(s.x) + (c0 + j) * (int64_t)s.ldx + r0 + at, (int)(left < 8 ? left : 8));
-            *reinterpret_cast<u32x2*>(turn + j * QPITCH + at) = raw.w;
+            const int r = (int)r0 + at, rows = c0 + j < s.cols ? s.rows : 0;
+            const Raw8<QT> raw = load8<QT>(static_cast<const char*>(s.x) + (c0 + j) * (int64_t)s.ldx, r, rows);
+            *reinterpret_cast<u32x2*>(turn + j * QPITCH + at) = settle8<QT>(raw, r, rows).w;
         }
         if (t < TC) scale[t] = c0 + t < s.cols ? scale_of(static_cast<const uint8_t*>(s.scales)[(c0 + t) * s.lds + tr]) : 0.0f;
         __syncthreads();
@@ -265,26 +265,26 @@ __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
     const int lane = threadIdx.x & 15;
     for (UnitWalk w(s.cols); w.r < (uint32_t)s.rows; w.next()) {
         const int c = (int)w.b * UNIT + lane * 8;
-        const char* const from_a = static_cast<const char*>(s.x) + (w.at(s.ldx) + c) * bytes_of<AT>;
-        const char* const from_h = static_cast<const char*>(s.dh) + (w.at(s.lddh) + c) * bytes_of<YT>;
+        const char* const from_a = static_cast<const char*>(s.x) + w.at(s.ldx) * bytes_of<AT>;
+        const char* const from_h = static_cast<const char*>(s.dh) + w.at(s.lddh) * bytes_of<YT>;
         char* const to = static_cast<char*>(s.out) + (w.at(s.ldo) + c) * bytes_of<YT>;
         Raw8<AT> ra[2];
         Raw8<YT> rh[2];
-        float scale[2] = {1.0f, 1.0f};
+        uint32_t byte[2] = {127, 127};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            ra[u] = load8<AT>(from_a + u * F8_BLOCK * bytes_of<AT>, s.cols - c - u * F8_BLOCK);
-            rh[u] = load8<YT>(from_h + u * F8_BLOCK * bytes_of<YT>, s.cols - c - u * F8_BLOCK);
+            ra[u] = load8<AT>(from_a, c + u * F8_BLOCK, s.cols);
+            rh[u] = load8<YT>(from_h, c + u * F8_BLOCK, s.cols);
             if constexpr (bytes_of<AT> == 1) {
                 const uint8_t* const scales = static_cast<const uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
-                scale[u] = scale_of(scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0]);
+                byte[u] = scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0];
             }
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             float a[8], h[8];
-            widen<AT>(ra[u], scale[u], a);
-            widen<YT>(rh[u], 1.0f, h);
+            widen<AT>(settle8<AT>(ra[u], c + u * F8_BLOCK, s.cols), scale_of(byte[u]), a);
+            widen<YT>(settle8<YT>(rh[u], c + u * F8_BLOCK, s.cols), 1.0f, h);
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[e] *= gelu_slope(a[e]);
             store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(h), s.cols - c - u * F8_BLOCK);

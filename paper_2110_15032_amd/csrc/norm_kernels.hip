@@ -21,7 +21,7 @@ __device__ inline void load_weight(const void* w, int t, int cols, float otherwi
         const int c = (v * TPR + t) * 8;
         float u[8];
         if (w) {
-            widen<WT>(load8<WT>(static_cast<const char*>(w) + (int64_t)c * bytes_of<WT>, cols - c), 1.0f, u);
+            widen<WT>(settle8<WT>(load8<WT>(static_cast<const char*>(w), c, cols), c, cols), 1.0f, u);
         } else {
 #pragma unroll
             for (int e = 0; e < 8; ++e) u[e] = c + e < cols ? otherwise : 0.0f;   // zeros behind the row's end, as load8 gives
@@ -48,28 +48,30 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
     const bool whole = cols == TPR * V * 8;   // no lane is without elements
     const float of_wave = sum_wave((float)have), over_wave = of_wave > 0.0f ? 1.0f / of_wave : 0.0f, over = 1.0f / (float)cols;
 
+    // AHEAD rows on their way
+    constexpr int AHEAD = XT == T_F32 ? 1 : 2;
     const int step = gridDim.x * G;
-    Raw8<XT> next[V];
-    auto fetch = [&](int64_t row) {
+    Raw8<XT> next[AHEAD][V];
+    auto fetch = [&](Raw8<XT> (&to)[V], int64_t row) {
+        const char* const from = static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>;
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * TPR + t) * 8;
-            next[v] = load8<XT>(static_cast<const char*>(s.x) + (row * s.ldx + c) * bytes_of<XT>, row < s.rows ? cols - c : 0);
-        }
+        for (int v = 0; v < V; ++v) to[v] = load8<XT>(from, (v * TPR + t) * 8, row < s.rows ? cols : 0);
     };
     int64_t row = (int64_t)blockIdx.x * G + group;
-    fetch(row);
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) fetch(next[a], row + a * step);
     int turn = 0;
-    for (int64_t first = (int64_t)blockIdx.x * G; first < s.rows; first += step, row += step, turn ^= 1) {
+    auto work = [&](Raw8<XT> (&raw)[V]) {   // one row of every group, and the row AHEAD of it on its way
         float x[V * 8];
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float u[8];
-            widen<XT>(next[v], 1.0f, u);
+            const int c = (v * TPR + t) * 8;
+            widen<XT>(whole ? raw[v] : settle8<XT>(raw[v], c, row < s.rows ? cols : 0), 1.0f, u);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x[v * 8 + e] = u[e];
         }
-        fetch(row + step);
+        fetch(raw, row + AHEAD * step);
         float sum = 0.0f;
 #pragma unroll
         for (int i = 0; i < V * 8; ++i) sum += x[i];
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
             }
         }
         const float rstd = 1.0f / sqrtf(fmaf(m2, over, p.eps)), shift = -mean * rstd;
-        if (row >= s.rows) continue;
+        if (row >= s.rows) return;
         if (t == 0 && s.mean) {
             s.mean[row] = mean;
             s.rstd[row] = rstd;
@@ -138,6 +140,16 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
             } else {
                 store8<YT>(dst, narrow<YT>(y), cols - c);
             }
+        }
+    };
+    for (int64_t first = (int64_t)blockIdx.x * G; first < s.rows;) {
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) {
+            if (first >= s.rows) break;
+            work(next[a]);
+            first += step;
+            row += step;
+            turn ^= 1;
         }
     }
 }
@@ -160,16 +172,21 @@ __global__ __launch_bounds__(GRAD_NT, TPR == 512 ? 2 : 4) void norm_grad_kernel(
     const int step = s.blocks * G;
     Raw8<XT> next_x[V];
     Raw8<YT> next_dy[V];
-    float next_scale[V], next_mean = 0.0f, next_rstd = 0.0f;
+    uint32_t next_byte[V];
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    const bool whole = cols == TPR * V * 8;   // no lane is without elements
     auto fetch = [&](int64_t row) {
         const bool there = row < s.rows;
+        const char* const from_x = static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>;
+        const char* const from_dy = static_cast<const char*>(s.dy) + row * s.lddy * bytes_of<YT>;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int c = (v * TPR + t) * 8, left = there ? cols - c : 0;
-            next_x[v] = load8<XT>(static_cast<const char*>(s.x) + (row * s.ldx + c) * bytes_of<XT>, left);
-            next_dy[v] = load8<YT>(static_cast<const char*>(s.dy) + (row * s.lddy + c) * bytes_of<YT>, left);
-            next_scale[v] = 1.0f;
-            if constexpr (bytes_of<XT> == 1) next_scale[v] = left > 0 ? scale_of(static_cast<const uint8_t*>(s.x_scales)[row * s.lds + c / F8_BLOCK]) : 0.0f;
+            const int c = (v * TPR + t) * 8;
+            next_x[v] = load8<XT>(from_x, c, there ? cols : 0);
+            next_dy[v] = load8<YT>(from_dy, c, there ? cols : 0);
+            next_byte[v] = 127;
+            if constexpr (bytes_of<XT> == 1)
+                if (there && c < cols) next_byte[v] = static_cast<const uint8_t*>(s.x_scales)[row * s.lds + c / F8_BLOCK];
         }
         next_mean = there ? s.mean[row] : 0.0f;
         next_rstd = there ? s.rstd[row] : 0.0f;
@@ -183,8 +200,9 @@ __global__ __launch_bounds__(GRAD_NT, TPR == 512 ? 2 : 4) void norm_grad_kernel(
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float u[8], w[8];
-            widen<XT>(next_x[v], next_scale[v], u);
-            widen<YT>(next_dy[v], 1.0f, w);
+            const int c = (v * TPR + t) * 8, there = row < s.rows ? cols : 0;
+            widen<XT>(whole ? next_x[v] : settle8<XT>(next_x[v], c, there), scale_of(next_byte[v]), u);
+            widen<YT>(whole ? next_dy[v] : settle8<YT>(next_dy[v], c, there), 1.0f, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {   // dy is 0 where there is no element, mean and rstd where there is no row
                 xhat[v * 8 + e] = (u[e] - mean) * rstd;
