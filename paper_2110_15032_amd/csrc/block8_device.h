@@ -192,7 +192,8 @@ __device__ inline uint32_t scale_byte(float most) {
 }
 
 // Sums and maxima over the lanes of a wave.  The first four steps stay inside rows of 16 lanes (DPP: neighbours, pairs, mirrored halves,
-// mirrored row), which is one block of 128 values at eight a lane.
+// mirrored row), which is one block of 128 values at eight a lane.  Maxima are taken of magnitudes as bits: unsigned ones need no canonical
+// operands, and whatever is not finite ends up on top.
 template <int CTRL>
 __device__ inline uint32_t dpp(uint32_t v) {
     return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, CTRL, 0xF, 0xF, true);
@@ -200,13 +201,6 @@ __device__ inline uint32_t dpp(uint32_t v) {
 template <int CTRL>
 __device__ inline float dpp(float v) {
     return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
-}
-// of magnitudes as bits: unsigned maxima need no canonical operands, and anything not finite ends up on top
-__device__ inline uint32_t max_row16(uint32_t v) {
-    v = max(v, dpp<0xB1>(v));
-    v = max(v, dpp<0x4E>(v));
-    v = max(v, dpp<0x141>(v));
-    return max(v, dpp<0x140>(v));
 }
 __device__ inline float sum_wave(float v) {
     v += dpp<0xB1>(v);
@@ -239,23 +233,41 @@ __device__ inline float most_finite_of_8(const float (&v)[8]) {
     return __uint_as_float(m);
 }
 
-// Largest finite magnitude of the 128 values that 16 lanes hold eight each.  A block with an infinity (or of NaN alone) is gone through again
-// without it; its 16 lanes go there together.
-__device__ inline float most_of_block(const float (&v)[8]) {
-    uint32_t m = max_row16(__float_as_uint(most_of_8(v)));
-    if (m >= 0x7F800000u) m = max_row16(__float_as_uint(most_finite_of_8(v)));
-    return __uint_as_float(m);
-}
-
-// 8-bit form of the values that 16 lanes hold eight each, and their block's scale byte.
-template <int T>
-__device__ inline Raw8<T> narrow_block(const float (&v)[8], uint32_t& byte) {
-    byte = scale_byte<T>(most_of_block(v));
-    const float s = scale_of(byte);
-    Raw8<T> r;
-    r.w[0] = narrow4<T>(v[0], v[1], v[2], v[3], s);
-    r.w[1] = narrow4<T>(v[4], v[5], v[6], v[7], s);
-    return r;
+// 8-bit form of N times eight values, 16 lanes to a block of 128, and the blocks' scale bytes.  The largest finite magnitude counts: a NaN is passed over
+// by the maximum, and blocks with an infinity (or of NaN alone) are gone through again; the lanes of a block go there together.  The N
+// chains over lanes are written side by side, each step of one fills the wait of the others.
+template <int T, int N>
+__device__ inline void narrow_blocks(const float (&v)[N][8], Raw8<T> (&q)[N], uint32_t (&byte)[N]) {
+    uint32_t m[N];
+    bool finite = true;
+#pragma unroll
+    for (int n = 0; n < N; ++n) m[n] = __float_as_uint(most_of_8(v[n]));
+    auto over_rows = [&]() {
+#pragma unroll
+        for (int n = 0; n < N; ++n) m[n] = max(m[n], dpp<0xB1>(m[n]));
+#pragma unroll
+        for (int n = 0; n < N; ++n) m[n] = max(m[n], dpp<0x4E>(m[n]));
+#pragma unroll
+        for (int n = 0; n < N; ++n) m[n] = max(m[n], dpp<0x141>(m[n]));
+#pragma unroll
+        for (int n = 0; n < N; ++n) m[n] = max(m[n], dpp<0x140>(m[n]));
+    };
+    over_rows();
+#pragma unroll
+    for (int n = 0; n < N; ++n) finite = finite && m[n] < 0x7F800000u;
+    if (!finite) {
+        asm volatile("");   // or it would be worked out always, and chosen from
+#pragma unroll
+        for (int n = 0; n < N; ++n) m[n] = __float_as_uint(most_finite_of_8(v[n]));
+        over_rows();
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        byte[n] = scale_byte<T>(__uint_as_float(m[n]));
+        const float s = scale_of(byte[n]);
+        q[n].w[0] = narrow4<T>(v[n][0], v[n][1], v[n][2], v[n][3], s);
+        q[n].w[1] = narrow4<T>(v[n][4], v[n][5], v[n][6], v[n][7], s);
+    }
 }
 
 }  // namespace

@@ -54,18 +54,22 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
         Raw8<XT> raw[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) raw[u] = load8<XT>(from, c + u * F8_BLOCK, s.cols);
+        float v[2][8];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            float v[8];
-            widen<XT>(settle8<XT>(raw[u], c + u * F8_BLOCK, s.cols), 1.0f, v);
+            widen<XT>(settle8<XT>(raw[u], c + u * F8_BLOCK, s.cols), 1.0f, v[u]);
             if constexpr (GELU) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = gelu_of<true>(v[e]);
+                for (int e = 0; e < 8; ++e) v[u][e] = gelu_of<true>(v[u][e]);
             }
-            uint32_t byte;
-            const Raw8<QT> q = narrow_block<QT>(v, byte);
-            store8<QT>(to + u * F8_BLOCK, q, s.cols - c - u * F8_BLOCK);
-            if (lane == 0 && c + u * F8_BLOCK < s.cols) scales[u] = (uint8_t)byte;
+        }
+        Raw8<QT> q[2];
+        uint32_t byte[2];
+        narrow_blocks<QT>(v, q, byte);
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            store8<QT>(to + u * F8_BLOCK, q[u], s.cols - c - u * F8_BLOCK);
+            if (lane == 0 && c + u * F8_BLOCK < s.cols) scales[u] = (uint8_t)byte[u];
         }
     }
 }
@@ -113,6 +117,7 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
             finite = finite && m[e] < 0x7F800000u;
         }
         if (!finite) {   // infinities, or NaN alone
+            asm volatile("");   // or it would be worked out always, and chosen from
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 m[e] = 0;

@@ -31,13 +31,22 @@ __device__ inline void load_weight(const void* w, int t, int cols, float otherwi
     }
 }
 
+// 1 / sqrt: the hardware's, to a unit in the last place, which takes subnormal numbers for zero
+__device__ inline float inverse_root(float v) {
+    if (v < 1e-37f) {
+        asm volatile("");
+        return 1.0f / sqrtf(v);
+    }
+    return __builtin_amdgcn_rsqf(v);
+}
+
 // The statistics are exact to fp32 sums whatever the row's offset: every wave sums its elements, then the squares of their distances from
 // its own mean, and the waves' pairs are joined with the distances of their means (one exchange for both).
 template <int XT, int YT, int WT, int TPR, int V>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p) {
     constexpr int NT = TPR < 256 ? 256 : TPR, G = NT / TPR, NW = TPR / 64;
     const NormShard& s = p.s[blockIdx.y];
-    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, wave = t >> 6, cols = p.cols;
+    const int t = threadIdx.x % TPR, group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0, wave = t >> 6, cols = p.cols;   // whole waves
     __shared__ float2 part[2][NW];
     float gamma[V * 8], beta[V * 8];
     load_weight<WT, V, TPR>(s.gamma, t, cols, 1.0f, gamma);
@@ -85,6 +94,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
                 sq = fmaf(d, d, sq);
             }
         } else {
+            asm volatile("");   // or both would be worked out, and one chosen
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int left = cols - (v * TPR + t) * 8;
@@ -118,27 +128,33 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
                 m2 += fmaf(of[w] * d, d, part[turn][w].y);
             }
         }
-        const float rstd = 1.0f / sqrtf(fmaf(m2, over, p.eps)), shift = -mean * rstd;
+        const float rstd = inverse_root(fmaf(m2, over, p.eps)), shift = -mean * rstd;
         if (row >= s.rows) return;
         if (t == 0 && s.mean) {
             s.mean[row] = mean;
             s.rstd[row] = rstd;
         }
+        float y[V][8];   // behind the row's end gamma and beta are 0, and y is
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int c = (v * TPR + t) * 8;
-            float y[8];
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[e] = fmaf(fmaf(x[v * 8 + e], rstd, shift), gamma[v * 8 + e], beta[v * 8 + e]);
-            char* dst = static_cast<char*>(s.y) + (row * s.ldy + c) * bytes_of<YT>;
-            if constexpr (bytes_of<YT> == 1) {
-                if (c / F8_BLOCK * F8_BLOCK >= cols) continue;   // no column of this lane's block exists; behind the row's end gamma and beta are 0, and y is
-                uint32_t byte;
-                const Raw8<YT> q = narrow_block<YT>(y, byte);
-                store8<YT>(dst, q, cols - c);
-                if ((t & 15) == 0) static_cast<uint8_t*>(s.y_scales)[row * s.lds + c / F8_BLOCK] = (uint8_t)byte;
-            } else {
-                store8<YT>(dst, narrow<YT>(y), cols - c);
+            for (int e = 0; e < 8; ++e) y[v][e] = fmaf(fmaf(x[v * 8 + e], rstd, shift), gamma[v * 8 + e], beta[v * 8 + e]);
+        char* const to = static_cast<char*>(s.y) + row * s.ldy * bytes_of<YT>;
+        if constexpr (bytes_of<YT> == 1) {
+            Raw8<YT> q[V];
+            uint32_t byte[V];
+            narrow_blocks<YT>(y, q, byte);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                store8<YT>(to + c, q[v], cols - c);
+                if ((t & 15) == 0 && c < cols) static_cast<uint8_t*>(s.y_scales)[row * s.lds + c / F8_BLOCK] = (uint8_t)byte[v];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                store8<YT>(to + c * bytes_of<YT>, narrow<YT>(y[v]), cols - c);
             }
         }
     };
@@ -161,7 +177,7 @@ __global__ __launch_bounds__(GRAD_NT, TPR == 512 ? 2 : 4) void norm_grad_kernel(
     constexpr int G = GRAD_NT / TPR, NW = TPR / 64, CAP = TPR * V * 8;
     const NormGradShard& s = p.s[blockIdx.y];
     if ((int)blockIdx.x >= s.blocks) return;
-    const int t = threadIdx.x % TPR, group = threadIdx.x / TPR, wave = t >> 6, cols = p.cols;
+    const int t = threadIdx.x % TPR, group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0, wave = t >> 6, cols = p.cols;   // whole waves
     __shared__ float2 part[2][G][NW];
     float gamma[V * 8], dgamma[V * 8], dbeta[V * 8];
     load_weight<WT, V, TPR>(s.gamma, t, cols, 1.0f, gamma);
@@ -379,7 +395,6 @@ int32_t launch_norm_grad(const NormGradPlan& plan, hipStream_t stream) {
                 };
                 using std::integral_constant;
                 if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-                else if (plan.cols <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
                 else if (plan.cols <= 1024) go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
                 else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
                 else if (plan.cols <= 4096) go(integral_constant<int, 256>{}, integral_constant<int, 2>{});
