@@ -7,6 +7,7 @@ namespace sbp {
 namespace {
 
 typedef u32x2 __attribute__((aligned(1))) u32x2_any;
+typedef u32x4 __attribute__((aligned(1))) u32x4_byte;
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 
 // element types as template arguments
@@ -36,18 +37,27 @@ struct Raw8<T_E5M2> {
 
 // Eight elements of a row from column c on, those behind its end (`cols`) as whatever settle8 makes zero: where the row ends among them its last
 // eight are read, and nothing outside the row.  The loads are all that happens here, so that a row can be on its way while another is worked on
-// (only a row shorter than eight is put together at once).
-template <int T>
+// (only a row shorter than eight is put together at once).  STREAM: past the caches (a
+// template argument, since the compiler takes the two forms of a load in two branches for one).
+template <int T, bool STREAM = false>
 __device__ inline Raw8<T> load8(const char* row, int c, int cols) {
     Raw8<T> r{};
     if (c >= cols) return r;
     if (cols >= 8) {
         const char* const p = row + (int64_t)min(c, cols - 8) * bytes_of<T>;
-        if constexpr (T == T_F32) {
-            r.a = *reinterpret_cast<const f32x4_any*>(p);
-            r.b = *reinterpret_cast<const f32x4_any*>(p + 16);
-        } else if constexpr (T == T_BF16) r.w = *reinterpret_cast<const u32x4_any*>(p);
-        else r.w = *reinterpret_cast<const u32x2_any*>(p);
+        if constexpr (STREAM) {
+            if constexpr (T == T_F32) {
+                r.a = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p));
+                r.b = __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p + 16));
+            } else if constexpr (T == T_BF16) r.w = __builtin_nontemporal_load(reinterpret_cast<const u32x4_any*>(p));
+            else r.w = __builtin_nontemporal_load(reinterpret_cast<const u32x2_any*>(p));
+        } else {
+            if constexpr (T == T_F32) {
+                r.a = *reinterpret_cast<const f32x4_any*>(p);
+                r.b = *reinterpret_cast<const f32x4_any*>(p + 16);
+            } else if constexpr (T == T_BF16) r.w = *reinterpret_cast<const u32x4_any*>(p);
+            else r.w = *reinterpret_cast<const u32x2_any*>(p);
+        }
     } else {   // c is 0
 #pragma unroll
         for (int e = 0; e < 7; ++e)
@@ -84,9 +94,15 @@ __device__ inline Raw8<T> settle8(Raw8<T> r, int c, int cols) {
     }
 }
 template <int T>
-__device__ inline void store8(void* at, const Raw8<T> r, int valid) {
+__device__ inline void store8(void* at, const Raw8<T> r, int valid, bool stream = false) {
     char* p = static_cast<char*>(at);
-    if (valid >= 8) {
+    if (valid >= 8 && stream) {
+        if constexpr (T == T_F32) {
+            __builtin_nontemporal_store(r.a, reinterpret_cast<f32x4_any*>(p));
+            __builtin_nontemporal_store(r.b, reinterpret_cast<f32x4_any*>(p + 16));
+        } else if constexpr (T == T_BF16) __builtin_nontemporal_store(r.w, reinterpret_cast<u32x4_any*>(p));
+        else __builtin_nontemporal_store(r.w, reinterpret_cast<u32x2_any*>(p));
+    } else if (valid >= 8) {
         if constexpr (T == T_F32) {
             *reinterpret_cast<f32x4_any*>(p) = r.a;
             *reinterpret_cast<f32x4_any*>(p + 16) = r.b;
@@ -101,6 +117,17 @@ __device__ inline void store8(void* at, const Raw8<T> r, int valid) {
                 else reinterpret_cast<uint8_t*>(p)[e] = (uint8_t)(r.w[e >> 2] >> (8 * (e & 3)));
             }
     }
+}
+
+// Which of a pass's tensors go past the caches.  Results: as much as the L2 caches of all XCDs hold and more, in rows that start on cache lines (else neighbouring
+// waves share lines, which L2 has to keep for both).  Inputs: when the pass has more than the memory-side cache holds.  us, cached / results past
+// them / inputs too: 8192 x 8192 from 8 bits to bf16 38.2 / 29.3 / 34.7, 16384 x 16384 bytes of GeLU's gradient (672 MB) 120.7 / 113.0 /
+// 110.0, 8192 x 16384 into 8 bits (404 MB) 69.5 / 67.2 / 63.2, normalising 8192 x 4096 in bf16 26.9 / 22.8 / 27.2, 8192 x 4097 in
+// fp32 58.1 / 58.8 / 56.6.
+enum Streams : int32_t { STREAM_OUT = 1, STREAM_IN = 2 };
+// fp32 results stay cached, as a lane stores its eight in two pieces (8192 x 4096 of GeLU's gradient 69.6, past the caches 72.8).
+inline int32_t streams_of(int64_t read, int64_t wrote, bool on_lines, int32_t out_dtype) {
+    return (wrote >= (int64_t)32 << 20 && on_lines && out_dtype != SBP_F32 ? STREAM_OUT : 0) | (read + wrote > (int64_t)256 << 20 ? STREAM_IN : 0);
 }
 
 // A scale byte b stands for 2^(b - 127).  The conversions below take a power of two as the exponent field of an fp32 number, 0 there

@@ -41,7 +41,8 @@ __device__ inline float gelu_of(float x) {
     else return gelu_erf(x);
 }
 
-template <int XT, int QT, bool GELU>
+// IN: inputs past the caches
+template <int XT, int QT, bool GELU, bool IN>
 __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
     if (s.rows == 0 || s.cols == 0) return;
@@ -53,7 +54,7 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
         uint8_t* const scales = static_cast<uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
         Raw8<XT> raw[2];
 #pragma unroll
-        for (int u = 0; u < 2; ++u) raw[u] = load8<XT>(from, c + u * F8_BLOCK, s.cols);
+        for (int u = 0; u < 2; ++u) raw[u] = load8<XT, IN>(from, c + u * F8_BLOCK, s.cols);
         float v[2][8];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -68,7 +69,7 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
         narrow_blocks<QT>(v, q, byte);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            store8<QT>(to + u * F8_BLOCK, q[u], s.cols - c - u * F8_BLOCK);
+            store8<QT>(to + u * F8_BLOCK, q[u], s.cols - c - u * F8_BLOCK, p.streams & STREAM_OUT);
             if (lane == 0 && c + u * F8_BLOCK < s.cols) scales[u] = (uint8_t)byte[u];
         }
     }
@@ -160,7 +161,8 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
             const u32x4 w = *reinterpret_cast<const u32x4*>(turn + j * QPITCH + (at ^ turn_key(j >> 3) * 4));
             char* dst = static_cast<char*>(s.out) + (c0 + j) * (int64_t)s.ldo + r;
             if (r + 16 <= s.rows) {
-                __builtin_memcpy(dst, &w, 16);
+                if (p.streams & STREAM_OUT) __builtin_nontemporal_store(w, reinterpret_cast<u32x4_byte*>(dst));
+                else *reinterpret_cast<u32x4_byte*>(dst) = w;
             } else {
 #pragma unroll
                 for (int e = 0; e < 15; ++e)
@@ -171,7 +173,7 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
     }
 }
 
-template <int QT, int YT, bool GELU>
+template <int QT, int YT, bool GELU, bool IN>
 __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
     if (s.rows == 0 || s.cols == 0) return;
@@ -185,7 +187,7 @@ __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
         uint32_t byte[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            raw[u] = load8<QT>(from, c + u * F8_BLOCK, s.cols);
+            raw[u] = load8<QT, IN>(from, c + u * F8_BLOCK, s.cols);
             byte[u] = scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0];
         }
 #pragma unroll
@@ -196,7 +198,7 @@ __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = gelu_of<YT == T_BF16>(v[e]);
             }
-            store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(v), s.cols - c - u * F8_BLOCK);
+            store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(v), s.cols - c - u * F8_BLOCK, p.streams & STREAM_OUT);
         }
     }
 }
@@ -239,7 +241,7 @@ __global__ __launch_bounds__(NT) void dequantize_transposed_kernel(Block8Plan p,
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int64_t r = r0 + rg * 4 + i;
-            if (r < s.rows) store8<YT>(static_cast<char*>(s.out) + (r * s.ldo + c) * bytes_of<YT>, narrow<YT>(v[i]), (int)(c < s.cols ? s.cols - c : 0));
+            if (r < s.rows) store8<YT>(static_cast<char*>(s.out) + (r * s.ldo + c) * bytes_of<YT>, narrow<YT>(v[i]), (int)(c < s.cols ? s.cols - c : 0), p.streams & STREAM_OUT);
         }
     }
 }
@@ -263,7 +265,7 @@ __device__ inline float gelu_slope(float a) {
 }
 
 // da = dh gelu'(a).  AT: the pre-activation's type, 8 bits or as it was.
-template <int AT, int YT>
+template <int AT, int YT, bool IN>
 __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
     if (s.rows == 0 || s.cols == 0) return;
@@ -278,8 +280,8 @@ __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
         uint32_t byte[2] = {127, 127};
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            ra[u] = load8<AT>(from_a, c + u * F8_BLOCK, s.cols);
-            rh[u] = load8<YT>(from_h, c + u * F8_BLOCK, s.cols);
+            ra[u] = load8<AT, IN>(from_a, c + u * F8_BLOCK, s.cols);
+            rh[u] = load8<YT, IN>(from_h, c + u * F8_BLOCK, s.cols);
             if constexpr (bytes_of<AT> == 1) {
                 const uint8_t* const scales = static_cast<const uint8_t*>(s.scales) + w.at(s.lds) + w.b * 2;
                 byte[u] = scales[(int)w.b * UNIT + u * F8_BLOCK < s.cols ? u : 0];
@@ -292,7 +294,7 @@ __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
             widen<YT>(settle8<YT>(rh[u], c + u * F8_BLOCK, s.cols), 1.0f, h);
 #pragma unroll
             for (int e = 0; e < 8; ++e) h[e] *= gelu_slope(a[e]);
-            store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(h), s.cols - c - u * F8_BLOCK);
+            store8<YT>(to + u * F8_BLOCK * bytes_of<YT>, narrow<YT>(h), s.cols - c - u * F8_BLOCK, p.streams & STREAM_OUT);
         }
     }
 }
@@ -336,9 +338,25 @@ void with_bool(bool b, F&& f) {
     else f(std::false_type{});
 }
 
+int bytes_each(int32_t dtype) { return dtype == SBP_F32 ? 4 : dtype == SBP_BF16 ? 2 : 1; }
+// in: bytes of an element read; out_dtype: of the results
+Block8Plan with_streams(Block8Plan plan, int in, int32_t out_dtype) {
+    const int out = bytes_each(out_dtype);
+    int64_t elements = 0;
+    bool on_lines = true;
+    for (int i = 0; i < plan.k; ++i) {
+        const Block8Shard& s = plan.s[i];
+        elements += (int64_t)s.rows * s.cols;
+        if ((int64_t)s.ldo * out % 128 || reinterpret_cast<uintptr_t>(s.out) % 128) on_lines = false;
+    }
+    plan.streams = streams_of(elements * in, elements * out, on_lines, out_dtype);
+    return plan;
+}
+
 }  // namespace
 
-int32_t launch_quantize(const Block8Plan& plan, hipStream_t stream) {
+int32_t launch_quantize(const Block8Plan& given, hipStream_t stream) {
+    const Block8Plan plan = with_streams(given, bytes_each(given.dtype), given.f8);
     with_f8(plan.f8, [&](auto q) {
         with_wide(plan.dtype, [&](auto x) {
             with_bool(plan.gelu != 0, [&](auto gelu) {
@@ -346,7 +364,7 @@ int32_t launch_quantize(const Block8Plan& plan, hipStream_t stream) {
                     const TileGrid g = tile_grid(plan);
                     hipLaunchKernelGGL((quantize_transposed_kernel<x(), q(), gelu()>), g.grid, dim3(NT), 0, stream, plan, g.rows, g.cols);
                 } else {
-                    hipLaunchKernelGGL((quantize_kernel<x(), q(), gelu()>), walk_grid(plan), dim3(NT), 0, stream, plan);
+                    with_bool(plan.streams & STREAM_IN, [&](auto in) { hipLaunchKernelGGL((quantize_kernel<x(), q(), gelu(), in()>), walk_grid(plan), dim3(NT), 0, stream, plan); });
                 }
             });
         });
@@ -354,7 +372,8 @@ int32_t launch_quantize(const Block8Plan& plan, hipStream_t stream) {
     return launch_status(__func__);
 }
 
-int32_t launch_dequantize(const Block8Plan& plan, hipStream_t stream) {
+int32_t launch_dequantize(const Block8Plan& given, hipStream_t stream) {
+    const Block8Plan plan = with_streams(given, 1, given.dtype);
     with_f8(plan.f8, [&](auto q) {
         with_wide(plan.dtype, [&](auto y) {
             with_bool(plan.gelu != 0, [&](auto gelu) {
@@ -362,7 +381,7 @@ int32_t launch_dequantize(const Block8Plan& plan, hipStream_t stream) {
                     const TileGrid g = tile_grid(plan);
                     hipLaunchKernelGGL((dequantize_transposed_kernel<q(), y(), gelu()>), g.grid, dim3(NT), 0, stream, plan, g.rows, g.cols);
                 } else {
-                    hipLaunchKernelGGL((dequantize_kernel<q(), y(), gelu()>), walk_grid(plan), dim3(NT), 0, stream, plan);
+                    with_bool(plan.streams & STREAM_IN, [&](auto in) { hipLaunchKernelGGL((dequantize_kernel<q(), y(), gelu(), in()>), walk_grid(plan), dim3(NT), 0, stream, plan); });
                 }
             });
         });
@@ -370,9 +389,12 @@ int32_t launch_dequantize(const Block8Plan& plan, hipStream_t stream) {
     return launch_status(__func__);
 }
 
-int32_t launch_gelu_grad(const Block8Plan& plan, hipStream_t stream) {
+int32_t launch_gelu_grad(const Block8Plan& given, hipStream_t stream) {
+    const Block8Plan plan = with_streams(given, bytes_each(given.f8) + bytes_each(given.dtype), given.dtype);
     with_wide(plan.dtype, [&](auto y) {
-        auto go = [&](auto a) { hipLaunchKernelGGL((gelu_grad_kernel<a(), y()>), walk_grid(plan), dim3(NT), 0, stream, plan); };
+        auto go = [&](auto a) {
+            with_bool(plan.streams & STREAM_IN, [&](auto in) { hipLaunchKernelGGL((gelu_grad_kernel<a(), y(), in()>), walk_grid(plan), dim3(NT), 0, stream, plan); });
+        };
         if (plan.f8 == SBP_F8E4M3 || plan.f8 == SBP_F8E5M2) with_f8(plan.f8, go);
         else with_wide(plan.f8, go);
     });

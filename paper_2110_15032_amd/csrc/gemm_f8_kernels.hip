@@ -12,7 +12,6 @@ namespace sbp {
 namespace {
 
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef u32x4 __attribute__((aligned(1))) u32x4_byte;
 typedef f32x4 __attribute__((aligned(4))) f32x4_any;
 typedef u32x2 __attribute__((aligned(2))) u32x2_half;
 

@@ -11,7 +11,7 @@ namespace sbp {
 namespace {
 
 // Workgroups of a launch: enough for every compute unit to have several.
-constexpr int NORM_BLOCKS = 2048, GRAD_BLOCKS = 512;
+constexpr int NORM_BLOCKS = 1024, GRAD_BLOCKS = 512;
 constexpr int GRAD_NT = 512;
 
 template <int WT, int V, int TPR>
@@ -147,14 +147,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int c = (v * TPR + t) * 8;
-                store8<YT>(to + c, q[v], cols - c);
+                store8<YT>(to + c, q[v], cols - c, p.streams & STREAM_OUT);
                 if ((t & 15) == 0 && c < cols) static_cast<uint8_t*>(s.y_scales)[row * s.lds + c / F8_BLOCK] = (uint8_t)byte[v];
             }
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int c = (v * TPR + t) * 8;
-                store8<YT>(to + c * bytes_of<YT>, narrow<YT>(y[v]), cols - c);
+                store8<YT>(to + c * bytes_of<YT>, narrow<YT>(y[v]), cols - c, p.streams & STREAM_OUT);
             }
         }
     };
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(GRAD_NT, TPR == 512 ? 2 : 4) void norm_grad_kernel(
                 const int i = v * 8 + e;
                 d[e] = rstd * (fmaf(dy[i], gamma[i], -s1) - xhat[i] * s2);
             }
-            store8<YT>(static_cast<char*>(s.dx) + (row * s.lddx + c) * bytes_of<YT>, narrow<YT>(d), cols - c);
+            store8<YT>(static_cast<char*>(s.dx) + (row * s.lddx + c) * bytes_of<YT>, narrow<YT>(d), cols - c, p.streams & STREAM_OUT);
         }
     }
     if (!s.dgamma) return;
@@ -346,14 +346,23 @@ void with_wide(int32_t dtype, F&& f) {
     else f(std::integral_constant<int, T_BF16>{});
 }
 
+int bytes_each(int32_t dtype) { return dtype == SBP_F32 ? 4 : dtype == SBP_BF16 ? 2 : 1; }
+
 // threads of a row in the gradient
 int grad_tpr(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 4096 ? 256 : 512; }
 
 }  // namespace
 
-int32_t launch_norm(const NormPlan& plan, hipStream_t stream) {
-    int64_t rows = 0;
-    for (int i = 0; i < plan.k; ++i) rows = std::max<int64_t>(rows, plan.s[i].rows);
+int32_t launch_norm(const NormPlan& given, hipStream_t stream) {
+    NormPlan plan = given;
+    int64_t rows = 0, all = 0;
+    bool on_lines = true;
+    for (int i = 0; i < plan.k; ++i) {
+        rows = std::max<int64_t>(rows, plan.s[i].rows);
+        all += plan.s[i].rows;
+        if ((int64_t)plan.s[i].ldy * bytes_each(plan.y_dtype) % 128 || reinterpret_cast<uintptr_t>(plan.s[i].y) % 128) on_lines = false;
+    }
+    plan.streams = streams_of(all * plan.cols * bytes_each(plan.x_dtype), all * plan.cols * bytes_each(plan.y_dtype), on_lines, plan.y_dtype);
     with_wide(plan.x_dtype, [&](auto x) {
         with_elem(plan.y_dtype, [&](auto y) {
             with_wide(plan.w_dtype, [&](auto w) {
@@ -380,13 +389,18 @@ int32_t norm_grad_blocks(int64_t rows, int64_t cols, int32_t k) {
     return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + g - 1) / g, GRAD_BLOCKS / k));
 }
 
-int32_t launch_norm_grad(const NormGradPlan& plan, hipStream_t stream) {
+int32_t launch_norm_grad(const NormGradPlan& given, hipStream_t stream) {
+    NormGradPlan plan = given;
     int blocks = 1;
-    bool join = false;
+    bool join = false, on_lines = true;
+    int64_t all = 0;
     for (int i = 0; i < plan.k; ++i) {
+        all += plan.s[i].rows;
+        if ((int64_t)plan.s[i].lddx * bytes_each(plan.dy_dtype) % 128 || reinterpret_cast<uintptr_t>(plan.s[i].dx) % 128) on_lines = false;
         blocks = std::max(blocks, plan.s[i].blocks);
         join = join || (plan.s[i].blocks > 1 && plan.s[i].dgamma);
     }
+    plan.streams = streams_of(all * plan.cols * (bytes_each(plan.x_dtype) + bytes_each(plan.dy_dtype)), all * plan.cols * bytes_each(plan.dy_dtype), on_lines, plan.dy_dtype);
     with_elem(plan.x_dtype, [&](auto x) {
         with_wide(plan.dy_dtype, [&](auto y) {
             with_wide(plan.w_dtype, [&](auto w) {

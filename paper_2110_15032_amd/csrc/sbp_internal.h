@@ -183,6 +183,7 @@ struct Block8Plan {
     int32_t dtype;   // of the other tensors
     int32_t trans;
     int32_t gelu;
+    int32_t streams;   // of block8_device.h, chosen at the launch
 };
 int32_t launch_quantize(const Block8Plan& plan, hipStream_t stream);
 int32_t launch_dequantize(const Block8Plan& plan, hipStream_t stream);
@@ -208,6 +209,7 @@ struct NormPlan {
     int32_t k, cols;
     int32_t x_dtype, y_dtype, w_dtype;
     float eps;
+    int32_t streams;
 };
 struct NormGradShard {
     const void* x;
@@ -226,6 +228,7 @@ struct NormGradPlan {
     NormGradShard s[NORM_MAX_K];
     int32_t k, cols;
     int32_t x_dtype, dy_dtype, w_dtype;
+    int32_t streams;
 };
 // workgroups that launch_norm_grad gives a shard of so many rows, each of which leaves one partial sum of the weights' gradients
 int32_t norm_grad_blocks(int64_t rows, int64_t cols, int32_t k);
