@@ -126,9 +126,10 @@ class SbpTensor:
         self.k = len(ptrs)
         self._arr = (ctypes.c_void_p * max(1, self.k))(*ptrs)
         self.c = _CTensor(ctypes.cast(self._arr, ctypes.POINTER(ctypes.c_void_p)), rows, cols, dtype, trans, ld)
+        self._ref = ctypes.byref(self.c)
 
     def ref(self):
-        return ctypes.byref(self.c)
+        return self._ref
 
 
 class SbpScales:
@@ -141,9 +142,10 @@ class SbpScales:
         self.k = len(ptrs)
         self._arr = (ctypes.c_void_p * max(1, self.k))(*ptrs)
         self.c = _CScales(ctypes.cast(self._arr, ctypes.POINTER(ctypes.c_void_p)), ld)
+        self._ref = ctypes.byref(self.c)
 
     def ref(self):
-        return ctypes.byref(self.c)
+        return self._ref
 
 
 def _ref(t):

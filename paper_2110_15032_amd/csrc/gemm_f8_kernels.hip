@@ -131,14 +131,36 @@ __device__ inline void store_row(const GemmF8Shard& s, int64_t m, int n, bool wh
     }
 }
 
-// Tiles of MB 16 rows by NB 16 columns whose NW waves take every NW-th block of the reduction, straight from memory into registers: for few rows,
-// where the weights are the traffic and a stage in LDS would only be on their way, and for few tiles.  U blocks at a time, the next ones on their
-// way while these are multiplied; no LDS before the waves' sums meet, in order.  Operands at any pitch.
-template <int AT, int BT, bool F32, bool GELU, int MB, int NB, int NW>
-__global__ __launch_bounds__(NW * 64) void gemm_f8_wave_kernel(GemmF8Plan p, int tm, int tn, int order) {
+// an address that every lane has, in scalar registers
+__device__ inline gbl_char* uniform(gbl_char* at) {
+    const uint64_t v = (uint64_t)(uintptr_t)at;
+    return (gbl_char*)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v));
+}
+
+// The last, cut block of a reduction, on the wave whose turn it is: straight from memory, at any pitch.
+template <int AT, int BT, bool EXACT, int MB, int NB>
+__device__ inline void multiply_cut_block(const uint8_t* a, const uint32_t (&a_row)[MB], const uint32_t (&as)[MB], const uint8_t* b, const uint32_t (&b_row)[NB],
+                                          const uint32_t (&bs)[NB], int left, int before, f32x4 (&acc)[MB][NB]) {
+    Operand<BT, EXACT> ob[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) ob[j] = Operand<BT, EXACT>({load_some(b + b_row[j], left, before), load_some(b + b_row[j] + 64, left - 64, before + 64)}, bs[j]);
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const Operand<AT, EXACT> oa({load_some(a + a_row[i], left, before), load_some(a + a_row[i] + 64, left - 64, before + 64)}, as[i]);
+#pragma unroll
+        for (int j = 0; j < NB; ++j) acc[i][j] = multiply<BT, AT>(ob[j], oa, acc[i][j]);
+    }
+}
+
+// Tiles of MB 16 rows by NB 16 columns whose four waves take every fourth block of the reduction: for few rows, where the weights are the traffic,
+// and for few tiles.  The waves' sums meet in LDS, in order.
+// RING: every wave brings its blocks into LDS of its own, DEPTH of them on their way: a load takes whole cache lines of eight rows, where one into
+// registers takes halves of sixteen (see choose_tile), and what is on its way costs no registers.  Nobody else reads it, so there is no
+// barrier before the sums.  Needs rows 16-byte and scales 4-byte aligned; else (any pitch) two sets of registers, U blocks each.
+template <int AT, int BT, bool F32, bool GELU, int MB, int NB, bool RING>
+__global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm, int tn, int order) {
     constexpr bool EXACT = F32;
-    // twice U blocks' registers next to the sums: waves of 16 have 128 each, the others up to 256
-    constexpr int U = std::max(1, (NW == 16 ? 60 : 150 - MB * NB * 4) / (18 * (MB + NB)));
+    constexpr int NW = 4;
     const TileCoord t = map_tile(blockIdx.x, gridDim.x, tm, tn, p.groups, order);
     if (!t.valid) return;
     const GemmF8Shard& s = p.s[t.g];
@@ -146,16 +168,17 @@ __global__ __launch_bounds__(NW * 64) void gemm_f8_wave_kernel(GemmF8Plan p, int
     if (m0 >= s.m || n0 >= s.n) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const uint8_t *const a = s.a + m0 * s.lda, *const as = s.a_scales + m0 * s.ldas, *const b = s.b + n0 * s.ldb, *const bs = s.b_scales + n0 * s.ldbs;
+    const uint32_t last_m = (uint32_t)(s.m - 1 - (int)m0), last_n = (uint32_t)(s.n - 1 - (int)n0);   // rows past an operand's end are its last one
     uint32_t a_row[MB], as_row[MB], b_row[NB], bs_row[NB];   // of this lane's rows, from the tile's first
 #pragma unroll
     for (int i = 0; i < MB; ++i) {
-        const uint32_t m = min((uint32_t)(i * 16 + r), (uint32_t)(s.m - 1 - (int)m0));
+        const uint32_t m = min((uint32_t)(i * 16 + r), last_m);
         a_row[i] = m * (uint32_t)s.lda + g * 16;
         as_row[i] = m * (uint32_t)s.ldas;
     }
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
-        const uint32_t n = min((uint32_t)(j * 16 + r), (uint32_t)(s.n - 1 - (int)n0));
+        const uint32_t n = min((uint32_t)(j * 16 + r), last_n);
         b_row[j] = n * (uint32_t)s.ldb + g * 16;
         bs_row[j] = n * (uint32_t)s.ldbs;
     }
@@ -164,75 +187,147 @@ __global__ __launch_bounds__(NW * 64) void gemm_f8_wave_kernel(GemmF8Plan p, int
     for (int i = 0; i < MB; ++i)
 #pragma unroll
         for (int j = 0; j < NB; ++j) acc[i][j] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    struct Block {
-        Frag a[MB], b[NB];
-        uint32_t as[MB], bs[NB];
-    };
-    auto scales = [&](Block& o, int kb) {
+    const int whole = s.kk / F8_BLOCK, mine = (whole - wave + NW - 1) / NW;   // this wave's whole blocks
+
+    // ring: a stage is 2 KB for each 16 rows (A's, then B's) and a dword of scales for each row
+    constexpr int BLOCKS = MB + NB, SCALE_LOADS = (BLOCKS * 16 + 63) / 64, LOADS = 2 * BLOCKS + SCALE_LOADS, STAGE = BLOCKS * 2048 + SCALE_LOADS * 256;
+    constexpr int DEPTH = std::max(2, std::min(4, 72 * 1024 / (NW * STAGE)));
+    constexpr int SUMS = NW * MB * NB * 1024;
+    __shared__ __attribute__((aligned(16))) char lds[RING ? std::max(NW * DEPTH * STAGE, SUMS) : SUMS];
+    if constexpr (RING) {
+        char* const ring = lds + wave * (DEPTH * STAGE);
+        const uint32_t ring_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)ring);
+        // load h of a block of 16 rows: row 8 h + lane / 8, chunk lane % 8 permuted by row / 2 (see StageF8)
+        uint32_t from[2 * BLOCKS], scales_from[SCALE_LOADS];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) o.bs[j] = (bs + kb)[bs_row[j]];
-#pragma unroll
-        for (int i = 0; i < MB; ++i) o.as[i] = (as + kb)[as_row[i]];
-    };
-    auto work = [&](const Block& o) {
-        Operand<BT, EXACT> ob[NB];
-#pragma unroll
-        for (int j = 0; j < NB; ++j) ob[j] = Operand<BT, EXACT>(o.b[j], o.bs[j]);
-#pragma unroll
-        for (int i = 0; i < MB; ++i) {
-            const Operand<AT, EXACT> oa(o.a[i], o.as[i]);
-#pragma unroll
-            for (int j = 0; j < NB; ++j) acc[i][j] = multiply<BT, AT>(ob[j], oa, acc[i][j]);
+        for (int l = 0; l < 2 * BLOCKS; ++l) {
+            const int row = (l & 1) * 8 + (lane >> 3), chunk = (lane & 7) ^ ((row >> 1) & 7);
+            const bool of_a = l < 2 * MB;
+            from[l] = min((uint32_t)((of_a ? l : l - 2 * MB) / 2 * 16 + row), of_a ? last_m : last_n) * (uint32_t)(of_a ? s.lda : s.ldb) + chunk * 16;
         }
-    };
-    // this wave's whole blocks, U at a time
-    const int whole = s.kk / F8_BLOCK, mine = (whole - wave + NW - 1) / NW;
-    auto load = [&](Block (&o)[U], int first) {
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (first + u < mine) {
-                const int kb = wave + (first + u) * NW;
-                const int64_t at = (int64_t)kb * F8_BLOCK;
-#pragma unroll
-                for (int j = 0; j < NB; ++j) o[u].b[j] = load_frag(b + at + b_row[j]);
-#pragma unroll
-                for (int i = 0; i < MB; ++i) o[u].a[i] = load_frag(a + at + a_row[i]);
-                scales(o[u], kb);
+        for (int l = 0; l < SCALE_LOADS; ++l) {   // rows of A, then of B, one a lane
+            const int row = l * 64 + lane;
+            scales_from[l] = row < MB * 16 ? min((uint32_t)row, last_m) * (uint32_t)s.ldas : min((uint32_t)min(row - MB * 16, NB * 16 - 1), last_n) * (uint32_t)s.ldbs;
+        }
+        auto bring = [&](int i, int slot) {
+            const int kb = wave + i * NW;
+            gbl_char *const at_a = (gbl_char*)(a + (int64_t)kb * F8_BLOCK), *const at_b = (gbl_char*)(b + (int64_t)kb * F8_BLOCK);
+            const uint32_t to = __builtin_amdgcn_readfirstlane(ring_at + (uint32_t)slot * STAGE);
+            static_for<2 * BLOCKS>([&](auto l) {
+                gbl_char* const src = uniform(l() < 2 * MB ? at_a : at_b);
+                const uint32_t off = from[l()], into = to;
+                asm volatile("s_add_u32 m0, %2, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" : : "v"(off), "s"(src), "s"(into), "n"(l() * 1024) : "memory", "m0", "scc");
+            });
+            static_for<SCALE_LOADS>([&](auto l) {
+                const uint8_t* const src = (l() * 64 + lane < MB * 16 ? as : bs) + (kb & ~3) + scales_from[l()];
+                const uint32_t into = to;
+                asm volatile("s_add_u32 m0, %1, %2\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" : : "v"(src), "s"(into), "n"(BLOCKS * 2048 + l() * 256) : "memory", "m0", "scc");
+            });
+        };
+        const int at = r * F8_BLOCK + ((g ^ (r >> 1)) << 4);
+        auto frag = [&](const char* stage, int block) {
+            return Frag{*reinterpret_cast<const u32x4*>(stage + block * 2048 + at), *reinterpret_cast<const u32x4*>(stage + block * 2048 + (at ^ 64))};
+        };
+        for (int i = 0; i < DEPTH - 1; ++i)
+            if (i < mine) bring(i, i);
+        int slot = 0;
+        for (int i = 0; i < mine; ++i) {
+            const int into = slot == 0 ? DEPTH - 1 : slot - 1;   // what was multiplied last
+            if (i + DEPTH - 1 < mine) {
+                bring(i + DEPTH - 1, into);
+                __builtin_amdgcn_s_waitcnt(vmcnt_only((DEPTH - 1) * LOADS));
+            } else {
+                __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
             }
-    };
-    auto multiply_all = [&](const Block (&o)[U], int first) {
+            asm volatile("" ::: "memory");
+            const char* const stage = ring + slot * STAGE;
+            const int shift = ((wave + i * NW) & 3) * 8;
+            const uint32_t* const scale = reinterpret_cast<const uint32_t*>(stage + BLOCKS * 2048) + r;
+            Operand<BT, EXACT> ob[NB];
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-            if (first + u < mine) work(o[u]);
-    };
-    Block even[U], odd[U];
-    load(even, 0);
-    for (int first = 0; first < mine; first += 2 * U) {
-        load(odd, first + U);
-        multiply_all(even, first);
-        load(even, first + 2 * U);
-        multiply_all(odd, first + U);
+            for (int j = 0; j < NB; ++j) ob[j] = Operand<BT, EXACT>(frag(stage, MB + j), scale[(MB + j) * 16] >> shift);
+#pragma unroll
+            for (int m = 0; m < MB; ++m) {
+                const Operand<AT, EXACT> oa(frag(stage, m), scale[m * 16] >> shift);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) {
+                    acc[m][j] = multiply<BT, AT>(ob[j], oa, acc[m][j]);
+                    asm volatile("" : "+v"(acc[m][j]));   // in its place, ahead of the loads into this slot
+                }
+            }
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            slot = slot == DEPTH - 1 ? 0 : slot + 1;
+        }
+    } else {
+        struct Block {
+            Frag a[MB], b[NB];
+            uint32_t as[MB], bs[NB];
+        };
+        auto work = [&](const Block& o) {
+            Operand<BT, EXACT> ob[NB];
+#pragma unroll
+            for (int j = 0; j < NB; ++j) ob[j] = Operand<BT, EXACT>(o.b[j], o.bs[j]);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) {
+                const Operand<AT, EXACT> oa(o.a[i], o.as[i]);
+#pragma unroll
+                for (int j = 0; j < NB; ++j) acc[i][j] = multiply<BT, AT>(ob[j], oa, acc[i][j]);
+            }
+        };
+        constexpr int U = std::max(1, (150 - MB * NB * 4) / (18 * BLOCKS));   // twice U blocks' registers next to the sums
+        auto load = [&](Block (&o)[U], int first) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (first + u < mine) {
+                    const int kb = wave + (first + u) * NW;
+                    const int64_t at = (int64_t)kb * F8_BLOCK;
+#pragma unroll
+                    for (int j = 0; j < NB; ++j) {
+                        o[u].b[j] = load_frag(b + at + b_row[j]);
+                        o[u].bs[j] = (bs + kb)[bs_row[j]];
+                    }
+#pragma unroll
+                    for (int i = 0; i < MB; ++i) {
+                        o[u].a[i] = load_frag(a + at + a_row[i]);
+                        o[u].as[i] = (as + kb)[as_row[i]];
+                    }
+                }
+        };
+        auto multiply_all = [&](const Block (&o)[U], int first) {
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (first + u < mine) work(o[u]);
+        };
+        Block even[U], odd[U];
+        load(even, 0);
+        for (int first = 0; first < mine; first += 2 * U) {
+            load(odd, first + U);
+            multiply_all(even, first);
+            load(even, first + 2 * U);
+            multiply_all(odd, first + U);
+        }
     }
     if (whole * F8_BLOCK < s.kk && wave == whole % NW) {   // the block that the reduction ends in
-        Block last;
-        const int at = whole * F8_BLOCK, left = s.kk - at - g * 16, before = at + g * 16;
+        uint32_t sa[MB], sb[NB];
 #pragma unroll
-        for (int j = 0; j < NB; ++j) last.b[j] = {load_some(b + at + b_row[j], left, before), load_some(b + at + b_row[j] + 64, left - 64, before + 64)};
+        for (int i = 0; i < MB; ++i) sa[i] = (as + whole)[as_row[i]];
 #pragma unroll
-        for (int i = 0; i < MB; ++i) last.a[i] = {load_some(a + at + a_row[i], left, before), load_some(a + at + a_row[i] + 64, left - 64, before + 64)};
-        scales(last, whole);
-        work(last);
+        for (int j = 0; j < NB; ++j) sb[j] = (bs + whole)[bs_row[j]];
+        const int64_t at = (int64_t)whole * F8_BLOCK;
+        multiply_cut_block<AT, BT, EXACT>(a + at, a_row, sa, b + at, b_row, sb, s.kk - (int)at - g * 16, (int)at + g * 16, acc);
     }
-    __shared__ f32x4 sums[NW][MB * NB][64];
+    if constexpr (RING) __syncthreads();   // the rings are free
+    f32x4* const sums = reinterpret_cast<f32x4*>(lds);
 #pragma unroll
     for (int i = 0; i < MB; ++i)
 #pragma unroll
-        for (int j = 0; j < NB; ++j) sums[wave][i * NB + j][lane] = acc[i][j];
+        for (int j = 0; j < NB; ++j) sums[(wave * MB * NB + i * NB + j) * 64 + lane] = acc[i][j];
     __syncthreads();
     for (int q = wave; q < MB * NB; q += NW) {
-        f32x4 v = sums[0][q][lane];
+        f32x4 v = sums[q * 64 + lane];
 #pragma unroll
-        for (int w = 1; w < NW; ++w) v += sums[w][q][lane];
+        for (int w = 1; w < NW; ++w) v += sums[(w * MB * NB + q) * 64 + lane];
         store_row<F32, GELU, 4>(s, m0 + q / NB * 16 + r, (int)n0 + q % NB * 16 + g * 4, false, {v});
     }
 }
@@ -263,12 +358,6 @@ struct StageF8 {
     // byte offset of chunk position p from the tile's first row; rows past the operand's end are its last one
     __device__ static uint32_t offset(int p, int rows_left, int pitch) { return (uint32_t)min(row_of(p), rows_left - 1) * (uint32_t)pitch + (uint32_t)chunk_of(p) * 16u; }
 };
-
-// an address that every lane has, in scalar registers
-__device__ inline gbl_char* uniform(gbl_char* at) {
-    const uint64_t v = (uint64_t)(uintptr_t)at;
-    return (gbl_char*)(uintptr_t)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)(v >> 32)) << 32 | (uint32_t)__builtin_amdgcn_readfirstlane((uint32_t)v));
-}
 
 // SCALES4: rows of scales at pitches of 4 bytes, which go straight into LDS too; else through registers, byte by byte at their end.
 template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, bool DIRECT, bool SCALES4>
@@ -664,14 +753,18 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
     int32_t st = SBP_OK;
     types([&](auto a, auto b) {
         results([&](auto f32, auto gelu) {
-            auto by_waves = [&](auto mb, auto nb, auto nw) {
+            auto by_waves = [&](auto mb, auto nb) {
                 const int tm = tiles_along(max_m, 16 * mb()), tn = tiles_along(max_n, 16 * nb());
                 const int64_t all = ((int64_t)tm * tn * plan.groups + 7) & ~7ll;
-                if (!grid_fits(all, 64 * nw())) {
+                if (!grid_fits(all, 256)) {
                     st = SBP_ERR_UNSUPPORTED;
                     return;
                 }
-                hipLaunchKernelGGL((gemm_f8_wave_kernel<a(), b(), f32(), gelu(), mb(), nb(), nw()>), dim3((uint32_t)all), dim3(64 * nw()), 0, stream, plan, tm, tn, 4);
+                auto go = [&](auto ring) {
+                    hipLaunchKernelGGL((gemm_f8_wave_kernel<a(), b(), f32(), gelu(), mb(), nb(), ring()>), dim3((uint32_t)all), dim3(256), 0, stream, plan, tm, tn, 4);
+                };
+                if (direct && scales4) go(std::true_type{});
+                else go(std::false_type{});
             };
             auto tile = [&](auto wm, auto wn, auto mi, auto direct, auto scales4) {
                 constexpr int BM = wm() * mi() * 16, BN = wn() * 64;
@@ -697,9 +790,9 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
             // eight devices 19.7 / 24.1 / 34.1, 4096 x 4096 19.1 / 13.5 / 10.8; 128 rows, 4096 x 4096 25.1 / 19.3 / 30.8 (tiles through LDS
             // 26.7), 1024 cubed 8.6 / 11.8 / - (10.2); 2048 cubed 47.7 (17.2).
             auto by_columns = [&](auto mb) {
-                if (tiles_of(16 * mb(), 64) >= cu) by_waves(mb, i4, i4);
-                else if (tiles_of(16 * mb(), 32) >= cu) by_waves(mb, i2, i4);
-                else by_waves(mb, i1, i4);
+                if (tiles_of(16 * mb(), 64) >= cu) by_waves(mb, i4);
+                else if (tiles_of(16 * mb(), 32) >= cu) by_waves(mb, i2);
+                else by_waves(mb, i1);
             };
             if (max_m <= 16) by_columns(i1);
             else if (max_m <= 32) by_columns(i2);
