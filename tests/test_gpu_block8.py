@@ -436,7 +436,7 @@ def test_layernorm_grad(rows, cols, k, sig, xk, yk, wk):
 
 
 # ------------------------------------------------------------------ products
-def matmul_case(rng, M, K, N, k, sig, xk, wk, yk, gelu=False, dense=False, special=None):
+def matmul_case(rng, M, K, N, k, sig, xk, wk, yk, gelu=False, dense=False, special=None, aligned=False):
     x, w = activations(rng, M, K), rng.normal(size=(N, K)) * 0.05     # w as it is stored: [N, K]
     if special is not None:
         special(x, w)
@@ -445,6 +445,7 @@ def matmul_case(rng, M, K, N, k, sig, xk, wk, yk, gelu=False, dense=False, speci
     kl, r16 = max(s.shape[1] for s in xs), lambda n: -(-n // 16) * 16  # noqa: E731
     ldx, ldw = (0, 0) if dense else (r16(kl) + 16 * int(rng.integers(0, 3)), r16(kl) + 16 * int(rng.integers(0, 3)))
     lds = 0 if dense else blocks(kl) + int(rng.integers(0, 6))
+    lds = -(-blocks(kl) // 4) * 4 if aligned else lds
     bx, bxs, vx = quantized(xs, xk, ldx, lds)
     bw, bws, vw = quantized(ws, wk, ldw, lds)
     a_sig, b_sig, y_sig = {"S0": (sbp.S(0), sbp.B, sbp.S(0)), "S1": (sbp.B, sbp.S(1), sbp.S(1)), "P": (sbp.S(1), sbp.S(0), sbp.P_SUM), "B": (sbp.B,) * 3}[sig]
@@ -479,6 +480,16 @@ def matmul_case(rng, M, K, N, k, sig, xk, wk, yk, gelu=False, dense=False, speci
 def test_matmul_f8(M, K, N, sig, k, yk):
     for dense in (False, True):
         matmul_case(np.random.default_rng(M + K + N), M, K, N, k, sig, "e4m3", "e4m3", yk, dense=dense)
+
+
+@pytest.mark.parametrize("aligned", [True, False])
+@pytest.mark.parametrize("yk", ["bf16", "f32"])
+@pytest.mark.parametrize("M,K,N", [(9, 300, 9), (3, 650, 4200), (2, 520, 8300), (4200, 300, 7), (300, 1700, 500), (30, 300, 8300), (8300, 300, 5), (8300, 140, 30), (40, 1040, 8300),
+                                   (200, 129, 9000), (3000, 2200, 2900), (4200, 2250, 4300), (7900, 300, 3900)])
+def test_matmul_f8_every_tile(M, K, N, yk, aligned):
+    """few rows, few columns, few and many of either: with 256 compute units each size has another tile, the last ones more tiles than workgroups; rows
+    of operands and scales aligned for loads into shared memory, and not"""
+    matmul_case(np.random.default_rng(M + K + N), M, K, N, 1, "B", "e4m3", "e4m3", yk, dense=not aligned, aligned=aligned)
 
 
 @pytest.mark.parametrize("xk,wk", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
