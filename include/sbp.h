@@ -100,7 +100,10 @@ typedef struct sbp_tensor {
  * An 8-bit tensor (SBP_F8E4M3, SBP_F8E5M2) is its values and one power of two for every 128
  * consecutive values of a stored row: the value stands for itself times that power.  Shard i's scales
  * are bytes [stored rows][ceil(stored row length / 128)] of the LOCAL tensor as it is stored (trans
- * included), counted from the row's start; byte b stands for 2^(b - 127).  255 is no scale. */
+ * included), counted from the row's start; byte b stands for 2^(b - 127).  255 is no scale.  A kernel may
+ * read the bytes behind a row of scales up to the next multiple of 4; their values never reach a result.
+ * Every operator on 8-bit tensors and layer normalisation takes at most 2^31 - 257 rows and columns
+ * (SBP_ERR_UNSUPPORTED). */
 #define SBP_F8_BLOCK 128
 typedef struct sbp_scales {
     void* const* shard; /* host array [k] of device pointers, 16-byte aligned            */
@@ -328,7 +331,8 @@ int32_t sbp_gelu_grad(const sbp_tensor_t* a, const sbp_scales_t* a_scales, sbp_t
  * SBP_ERR_DTYPE).  Both operands have to be stored with the reduction index contiguous, so that the blocks of 128
  * run along it: x.trans = 0, w.trans = 1 (SBP_ERR_UNSUPPORTED else); sbp_quantize stores either way.
  * y SBP_BF16 or SBP_F32, SBP_F32 where it is P(sum), trans = 0.
- *   fp32 results: exact products, summed in fp32.
+ *   fp32 results: exact products (of values between 2^-126 and bf16's largest, beyond which scales far
+ *   from 1 can take them), summed in fp32.
  *   bf16 results: on the 8-bit matrix instruction, which aligns a group of products to the largest of
  *   them and drops what lies some 2^-12 below: an error of about 2^-16 of a typical result and at most
  *   2^-11 of the sum of the products' magnitudes, next to the rounding to bf16 of up to 2^-8 of the result.

@@ -53,8 +53,9 @@ void Buffers::add(bool out, const sbp_tensor_t* t, const sbp_scales_t* scales, s
 // A tensor with its scales where it is in 8 bits, and none where it is not.
 int32_t check_block8(const sbp_tensor_t* t, const sbp_scales_t* scales, sbp_t s, int32_t k, bool f8 = true) {
     if (!t) return SBP_ERR_NULL;
-    // before anything is multiplied
-    if (t->rows > INT32_MAX || t->cols > INT32_MAX) return SBP_ERR_UNSUPPORTED;
+    // before anything is multiplied; kernels count up to the end of a tile of 256 behind a tensor's last row or column in 32 bits
+    constexpr int64_t MOST = INT32_MAX - 256;
+    if (t->rows > MOST || t->cols > MOST) return SBP_ERR_UNSUPPORTED;
     const int32_t st = check_tensor(t, s, k, true, f8);
     if (st != SBP_OK) return st;
     if (!is_f8(t->dtype)) return scales ? SBP_ERR_DTYPE : SBP_OK;

@@ -46,6 +46,8 @@ def test_quantize_refusals():
     same = sbp.SbpTensor([0x300000000] * 2, 64, 256, sbp.F8E4M3)
     assert quantize(sx=sbp.B, q=same, s=SC(2, 4)) == ALIAS
     assert quantize(x=T(2, 2 ** 31, 8), q=T(2, 2 ** 31, 8, sbp.F8E4M3, 1)) == UNSUPPORTED
+    for rows, cols in ((2 ** 31 - 1, 8), (8, 2 ** 31 - 1), (8, 2 ** 31 - 256)):      # the last tile's end would not be a 32-bit number
+        assert quantize(x=T(2, rows, cols), q=T(2, rows, cols, sbp.F8E4M3, 1)) == UNSUPPORTED
     with pytest.raises(ValueError):
         sbp.sbp_quantize(T(1, 64, 256), sbp.S(0), T(2, 64, 256, sbp.F8E4M3, 1), SC(2, 2), 2, STREAM)
 
