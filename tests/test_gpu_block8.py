@@ -688,3 +688,88 @@ def test_two_steps_at_once_on_two_streams():
     for (t, _), w in zip(steps, want):
         for p, q in zip([v for n in ("dx", "dw2", "dgamma") for v in t[n]], w):
             assert torch.equal(p, q)
+
+
+# ------------------------------------------------------------------ offsets past 32 bits
+def big_and_tail(rows, cols, dtype, tail, seed):
+    """A [rows, cols] tensor whose elements lie past 2^31, and a copy of its last `tail` rows."""
+    torch = torch_mod()
+    x = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(seed), device="cuda", dtype=dtype)
+    assert x.numel() > 2 ** 31
+    return x, x[-tail:].clone()
+
+
+def one(t, dtype, trans=0):
+    rows, cols = (t.shape[1], t.shape[0]) if trans else t.shape
+    return sbp.SbpTensor([t], rows, cols, dtype, trans)
+
+
+def test_elementwise_operators_past_32_bits():
+    """every element of an elementwise operator and every block's scale depend on a block alone: the last rows are what a small tensor gives, bit for bit"""
+    torch = torch_mod()
+    rows, cols, tail = 34000, 65536, 128 + 34000 % 128      # whole blocks where the blocks run along the rows
+    x, xt = big_and_tail(rows, cols, torch.bfloat16, tail, 1)
+    u8 = lambda *s: torch.zeros(*s, dtype=torch.uint8, device="cuda")  # noqa: E731
+    q, s, qt, st = u8(rows, cols), u8(rows, blocks(cols)), u8(tail, cols), u8(tail, blocks(cols))
+    sbp.sbp_quantize(one(x, sbp.BF16), sbp.B, one(q, sbp.F8E4M3), sbp.SbpScales([s]), 1)
+    sbp.sbp_quantize(one(xt, sbp.BF16), sbp.B, one(qt, sbp.F8E4M3), sbp.SbpScales([st]), 1)
+    assert torch.equal(q[-tail:], qt) and torch.equal(s[-tail:], st) and bool(qt.any())
+    y, yt = torch.zeros_like(x), torch.zeros_like(xt)
+    sbp.sbp_dequantize(one(q, sbp.F8E4M3), sbp.SbpScales([s]), sbp.B, one(y, sbp.BF16), 1)
+    sbp.sbp_dequantize(one(qt, sbp.F8E4M3), sbp.SbpScales([st]), sbp.B, one(yt, sbp.BF16), 1)
+    assert torch.equal(y[-tail:], yt) and bool(yt.any())
+    sbp.sbp_gelu_grad(one(q, sbp.F8E4M3), sbp.SbpScales([s]), sbp.B, one(x, sbp.BF16), one(y, sbp.BF16), 1)
+    sbp.sbp_gelu_grad(one(qt, sbp.F8E4M3), sbp.SbpScales([st]), sbp.B, one(xt, sbp.BF16), one(yt, sbp.BF16), 1)
+    assert torch.equal(y[-tail:], yt)
+    t, ts = u8(cols, rows), u8(cols, blocks(rows))
+    tt, tts = u8(cols, tail), u8(cols, blocks(tail))
+    sbp.sbp_quantize(one(x, sbp.BF16), sbp.B, one(t, sbp.F8E4M3, 1), sbp.SbpScales([ts]), 1)
+    sbp.sbp_quantize(one(xt, sbp.BF16), sbp.B, one(tt, sbp.F8E4M3, 1), sbp.SbpScales([tts]), 1)
+    assert torch.equal(t[:, -tail:], tt) and torch.equal(ts[:, -blocks(tail):], tts)
+    sbp.sbp_dequantize(one(t, sbp.F8E4M3, 1), sbp.SbpScales([ts]), sbp.B, one(y, sbp.BF16), 1)
+    sbp.sbp_dequantize(one(tt, sbp.F8E4M3, 1), sbp.SbpScales([tts]), sbp.B, one(yt, sbp.BF16), 1)
+    assert torch.equal(y[-tail:], yt)
+
+
+def test_layernorm_past_32_bits():
+    """a row of y, dx and the statistics depends on the row alone"""
+    torch = torch_mod()
+    rows, cols, tail = 140000, 16000, 5
+    x, xt = big_and_tail(rows, cols, torch.bfloat16, tail, 2)
+    out = []
+    for a in (x, xt):
+        n = a.shape[0]
+        y, mean, rstd = torch.zeros_like(a), torch.zeros(n, 1, device="cuda"), torch.zeros(n, 1, device="cuda")
+        q, s = torch.zeros(n, cols, dtype=torch.uint8, device="cuda"), torch.zeros(n, blocks(cols), dtype=torch.uint8, device="cuda")
+        sbp.sbp_layernorm(one(a, sbp.BF16), sbp.B, None, None, 1e-5, one(y, sbp.BF16), None, one(mean, sbp.F32), one(rstd, sbp.F32), 1)
+        sbp.sbp_layernorm(one(a, sbp.BF16), sbp.B, None, None, 1e-5, one(q, sbp.F8E5M2), sbp.SbpScales([s]), None, None, 1)
+        dx, dg, db = torch.zeros_like(a), torch.zeros(cols, 1, device="cuda"), torch.zeros(cols, 1, device="cuda")
+        need = sbp.sbp_layernorm_grad_workspace(n, cols, sbp.B, 1)
+        room = torch.empty(need, dtype=torch.uint8, device="cuda") if need else None
+        sbp.sbp_layernorm_grad(one(a, sbp.BF16), None, sbp.B, None, one(mean, sbp.F32), one(rstd, sbp.F32), one(y, sbp.BF16), one(dx, sbp.BF16),
+                               one(dg, sbp.F32), one(db, sbp.F32), room, 1)
+        out.append([v[-tail:].clone() for v in (y, mean, rstd, q, s, dx)])
+        if n == rows:   # the sum over rows of xhat^2 but for dy's rounding: n, to sqrt(2 / 140000) = 0.004, 12 of which are 0.05
+            assert bool((dg / rows - 1).abs().max() < 0.05)
+    for a, b in zip(*out):
+        assert torch.equal(a, b) and bool(a.any())
+
+
+@pytest.mark.parametrize("rows,K,N", [(140000, 16000, 32), (34000, 128, 65536)])
+def test_matmul_f8_past_32_bits(rows, K, N):
+    """operands, and results, past 2^31 elements: the last rows against the 64-bit product of what they stand for"""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randint(0, 120, (rows, K), generator=g, device="cuda", dtype=torch.uint8)     # finite e4m3
+    w = torch.randint(0, 120, (N, K), generator=g, device="cuda", dtype=torch.uint8) | 128 * torch.randint(0, 2, (N, K), generator=g, device="cuda", dtype=torch.uint8)
+    sx = torch.randint(117, 122, (rows, blocks(K)), generator=g, device="cuda", dtype=torch.uint8)
+    sw = torch.randint(117, 122, (N, blocks(K)), generator=g, device="cuda", dtype=torch.uint8)
+    y = torch.zeros(rows, N, device="cuda", dtype=torch.bfloat16)
+    assert max(x.numel(), y.numel()) > 2 ** 31
+    sbp.sbp_matmul_f8(one(x, sbp.F8E4M3), sbp.SbpScales([sx]), sbp.B, one(w, sbp.F8E4M3, 1), sbp.SbpScales([sw]), sbp.B, one(y, sbp.BF16), sbp.B, 1)
+    sync()
+    a = o8.dequantize(x[-7:].cpu().numpy(), sx[-7:].cpu().numpy(), "e4m3")
+    b = o8.dequantize(w.cpu().numpy(), sw.cpu().numpy(), "e4m3")
+    want, total = a @ b.T, np.abs(a) @ np.abs(b).T
+    tol = (K * U["f32"] + 2.0 ** -11) * total
+    close(y[-7:].float().cpu().numpy().astype(np.float64), want, tol + (np.abs(want) + tol) * U["bf16"])
