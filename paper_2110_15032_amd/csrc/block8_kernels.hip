@@ -41,7 +41,8 @@ __device__ inline float gelu_of(float x) {
     else return gelu_erf(x);
 }
 
-// IN: inputs past the caches
+// Bound by HBM: 8192 x 16384 on eight devices from bf16 (404 MB) 64 us, 6.3 TB/s; with GeLU 85 us, by its polynomial and exponential.  IN: inputs past
+// the caches.
 template <int XT, int QT, bool GELU, bool IN>
 __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
@@ -76,7 +77,8 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
 }
 
 // Transposed: the block runs along the rows.  A workgroup takes 128 rows by 64 columns; thread t holds rows 4 (t / 8) .. + 3 of the eight
-// columns 8 (t % 8), the column maxima meet over the lanes of a wave and over the waves in LDS, the bytes turn in LDS.
+// columns 8 (t % 8), the column maxima meet over the lanes of a wave and over the waves in LDS, the bytes turn in LDS.  8192 x 8192 from bf16 (202 MB)
+// 45 us, 4.4 TB/s: a tile's loads do not overlap its turn, other workgroups' do; with GeLU 16384 x 1024 (50 MB) 15.0 us.
 constexpr int TC = 64;
 // Bytes of one column in LDS.  Its 4-byte words are permuted by XOR with turn_key(column / 8), a multiple of four: the eight columns 8 co + e that a
 // wave's lanes write at once (eight consecutive words each) fall on different banks.
@@ -173,6 +175,7 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
     }
 }
 
+// Bound by HBM: 8192 x 8192 to bf16 (202 MB) 29.8 us, 6.8 TB/s; by GeLU with it, 7777 x 4081 on three devices (95 MB) 19.3 .. 20.2 us, 4.8 TB/s.
 template <int QT, int YT, bool GELU, bool IN>
 __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];
@@ -203,7 +206,8 @@ __global__ __launch_bounds__(NT) void dequantize_kernel(Block8Plan p) {
     }
 }
 
-// Restoring a tensor that was saved transposed: 128 saved bytes (128 rows of the result) of 64 saved rows (its columns) turn in LDS.
+// Restoring a tensor that was saved transposed: 128 saved bytes (128 rows of the result) of 64 saved rows (its columns) turn in LDS.  8192 x 8192
+// to bf16 31.6 us, 6.4 TB/s.
 template <int QT, int YT, bool GELU>
 __global__ __launch_bounds__(NT) void dequantize_transposed_kernel(Block8Plan p, int tiles_r, int tiles_c) {
     const Block8Shard& s = p.s[blockIdx.y];
@@ -264,7 +268,7 @@ __device__ inline float gelu_slope(float a) {
     return a == a ? fmaf(x * 0.39894228040143268f, e, cdf) : a;
 }
 
-// da = dh gelu'(a).  AT: the pre-activation's type, 8 bits or as it was.
+// da = dh gelu'(a).  AT: the pre-activation's type, 8 bits or as it was.  Bound by HBM: 8192 x 16384 on eight devices from 8 bits (672 MB) 110 us, 6.1 TB/s.
 template <int AT, int YT, bool IN>
 __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {
     const Block8Shard& s = p.s[blockIdx.y];

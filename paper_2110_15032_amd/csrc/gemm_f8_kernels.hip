@@ -154,8 +154,9 @@ __device__ inline void multiply_cut_block(const uint8_t* a, const uint32_t (&a_r
 
 // Tiles of MB 16 rows by NB 16 columns whose four waves take every fourth block of the reduction: for few rows, where the weights are the traffic,
 // and for few tiles.  The waves' sums meet in LDS, in order.
+// Bound by the weights' bytes: 1 x 4096 x 16384 on eight devices (68 MB) 11.9 us, 5.7 TB/s; for some 32 rows and more by the loads of a compute unit.
 // RING: every wave brings its blocks into LDS of its own, DEPTH of them on their way: a load takes whole cache lines of eight rows, where one into
-// registers takes halves of sixteen (see choose_tile), and what is on its way costs no registers.  Nobody else reads it, so there is no
+// registers takes halves of sixteen (choose_tile has both measured), and what is on its way costs no registers.  Nobody else reads it, so there is no
 // barrier before the sums.  Needs rows 16-byte and scales 4-byte aligned; else (any pitch) two sets of registers, U blocks each.
 template <int AT, int BT, bool F32, bool GELU, int MB, int NB, bool RING>
 __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm, int tn, int order) {
@@ -340,6 +341,10 @@ __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm,
 // first half of every wave's row blocks behind the first barrier, the other half behind the second.  Loads go straight into LDS and have a
 // step and a half to arrive (with one barrier and a step the loads alone took 467 us of the 515 of 8192 x 4096 x 16384).  The row blocks before a
 // barrier are multiplied behind it, underneath the reads of the next fragments.
+//
+// Bound by the matrix pipe: 8192 x 4096 x 16384 on eight devices, bf16 results, 452 us, 2.43 PFLOP/s (the
+// instruction alone, on random operands, 4.1); for fp32 results by the widening next to it, 128 conversions to 64 matrix instructions: 8192 x 16384 x 4096 1082 us, 1.02 PFLOP/s (of 2.06).
+// The larger tile brings half the operand bytes into LDS for a product, and reads three quarters from it.
 //
 // LDS image of an operand: rows of 128 bytes, 16-byte chunk c of a row at c ^ key(row), so that the 16 lanes of a read's pass fall on
 // different banks: row / 2 where a fragment is 16 consecutive rows, as A's are, and B's for fp32 results.  For bf16 results (PAIRS) B's fragments
