@@ -333,8 +333,8 @@ __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm,
     }
 }
 
-// Tiles of WM MI 16 rows by WN 64 columns, one persistent workgroup a compute unit (or two of the smaller tile) that walks over its share of
-// the (shard, tile) list; a wave has MI 16 rows by 64 columns.  A step is a block of 128 of the reduction: one instruction deep, one cache line
+// Tiles of WM MI 16 rows by WN NJ 16 columns, one persistent workgroup a compute unit (or two of the smaller tile) that walks over its share of
+// the (shard, tile) list; a wave has MI 16 rows by NJ 16 columns.  A step is a block of 128 of the reduction: one instruction deep, one cache line
 // of a row.
 //
 // Two stages in LDS, and two barriers a step, so that parts of a stage are free for the stage after next as soon as they have been read: B and the
@@ -343,8 +343,10 @@ __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm,
 // barrier are multiplied behind it, underneath the reads of the next fragments.
 //
 // Bound by the matrix pipe: 8192 x 4096 x 16384 on eight devices, bf16 results, 452 us, 2.43 PFLOP/s (the
-// instruction alone, on random operands, 4.1); for fp32 results by the widening next to it, 128 conversions to 64 matrix instructions: 8192 x 16384 x 4096 1082 us, 1.02 PFLOP/s (of 2.06).
-// The larger tile brings half the operand bytes into LDS for a product, and reads three quarters from it.
+// instruction alone, on random operands, 4.1), and by LDS, which is busy for as many cycles (192 KB read and 64 KB written a step at 128 bytes, against
+// 64 instructions of 32 on every SIMD).  fp32 results by the widening next to the products, once for every wave that reads a fragment:
+// the larger tile has four waves of 128 x 128, one a SIMD with all its 512 registers, and half the conversions of the smaller one (8192 x 4096 x 16384
+// 1109 -> 895 us, 4096 cubed 140 -> 114); bf16 results are better off with eight of 128 x 64 (505 -> 479), two a SIMD.
 //
 // LDS image of an operand: rows of 128 bytes, 16-byte chunk c of a row at c ^ key(row), so that the 16 lanes of a read's pass fall on
 // different banks: row / 2 where a fragment is 16 consecutive rows, as A's are, and B's for fp32 results.  For bf16 results (PAIRS) B's fragments
@@ -365,17 +367,18 @@ struct StageF8 {
 };
 
 // SCALES4: rows of scales at pitches of 4 bytes, which go straight into LDS too; else through registers, byte by byte at their end.
-template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, bool DIRECT, bool SCALES4>
-__global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Plan p, int tm, int tn, int order, int tiles) {
+template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, int NJ, bool DIRECT, bool SCALES4>
+__global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_kernel(GemmF8Plan p, int tm, int tn, int order, int tiles) {
     constexpr bool EXACT = F32;
-    constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * 64, NJ = 4;
+    constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * NJ * 16;
     using StA = StageF8<BM, NT, false>;
     using StB = StageF8<BN, NT, !F32>;
     constexpr int STAGE = StA::BYTES + StB::BYTES;
     constexpr int SCALE_ROWS = (BM + BN) / NT;   // of a thread
     static_assert((BM + BN) % NT == 0, "rows of scales divide over the workgroup");
-    // chunk i of a thread lies in rows NT / 8 i + 0..: half a wave's rows, so that even chunks of A are first halves
-    static_assert(NT / 8 == MI * 8 && StA::PER == 2 * WM, "an operand's chunks fall into halves of the waves' rows");
+    // chunk i of a thread lies in rows NT / 8 i + 0..; C of them are half a wave's rows, so that every other C chunks of A are first halves
+    constexpr int C = MI * 64 / NT;
+        static_assert(C * NT == MI * 64 && StA::PER == 2 * WM * C, "an operand's chunks fall into halves of the waves' rows");
     // scales of 16 blocks of the reduction, twice: four planes of [row] dwords, four blocks each
     constexpr int SCALE_PLANE = (BM + BN) * 4, SCALE_BYTES = 4 * SCALE_PLANE;
     __shared__ __attribute__((aligned(16))) char lds[2 * STAGE + 2 * SCALE_BYTES];
@@ -466,12 +469,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
         }
     };
     // B and the first halves of A, then the second halves
-    constexpr int FIRST = StB::PER + WM, SECOND = WM;
+    constexpr int FIRST = StB::PER + WM * C, SECOND = WM * C;
     auto bring_first = [&](uint32_t at, auto n) {
         if constexpr (n() < StB::PER) bring_b(at, n);
-        else bring_a(at, std::integral_constant<int, 2 * (n() - StB::PER)>{});
+        else bring_a(at, std::integral_constant<int, (n() - StB::PER) / C * 2 * C + (n() - StB::PER) % C>{});
     };
-    auto bring_second = [&](uint32_t at, auto n) { bring_a(at, std::integral_constant<int, 2 * n() + 1>{}); };
+    auto bring_second = [&](uint32_t at, auto n) { bring_a(at, std::integral_constant<int, n() / C * 2 * C + C + n() % C>{}); };
     auto put_held = [&](char* stage) {
         if constexpr (!DIRECT) {
 #pragma unroll
@@ -495,12 +498,14 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
 #pragma unroll
         for (int i = 0; i < StB::PER; ++i) cut(stage + StA::BYTES + (i * NT + threadIdx.x) * 16, left - StB::chunk_of(i * NT + (int)threadIdx.x) * 16);
 #pragma unroll
-        for (int i = 0; i < StA::PER; i += 2) cut(stage + (i * NT + threadIdx.x) * 16, left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+        for (int i = 0; i < StA::PER; ++i)
+            if (i / C % 2 == 0) cut(stage + (i * NT + threadIdx.x) * 16, left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
     };
     auto cut_second = [&](char* stage, int left) {
         if (!DIRECT || left >= F8_BLOCK) return;
 #pragma unroll
-        for (int i = 1; i < StA::PER; i += 2) cut(stage + (i * NT + threadIdx.x) * 16, left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
+        for (int i = 0; i < StA::PER; ++i)
+            if (i / C % 2 == 1) cut(stage + (i * NT + threadIdx.x) * 16, left - StA::chunk_of(i * NT + (int)threadIdx.x) * 16);
     };
 
     // ---- scales, 16 blocks of a row at a time
@@ -534,7 +539,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     char* const scale_lds = lds + 2 * STAGE;
 
     // ---- fragments
-    const int a_row = wm * MI * 16 + r, b_row = wn * 64 + StB::fragment_row(r);
+    const int a_row = wm * MI * 16 + r, b_row = wn * NJ * 16 + StB::fragment_row(r);
     const int a_lo = a_row * F8_BLOCK + ((g ^ StA::key(a_row)) << 4), b_lo = StA::BYTES + b_row * F8_BLOCK + ((g ^ StB::key(b_row)) << 4);
     auto frag_a = [&](const char* stage, int i) {
         return Frag{*reinterpret_cast<const u32x4*>(stage + a_lo + i * 16 * F8_BLOCK), *reinterpret_cast<const u32x4*>(stage + (a_lo ^ 64) + i * 16 * F8_BLOCK)};
@@ -557,12 +562,12 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
     // was brought since the second halves of this stage; at the second: since the first part of the next one.  `stores`: waits that a whole
     // tile's stores may be younger than what is waited for.
     constexpr int BEFORE_SECOND_BARRIER = (ROWS_FIRST - 2) * FIRST / ROWS_FIRST;   // first loads that go with rows before it
-    constexpr int NSTORE = MI * (F32 ? 4 : 2);
+    constexpr int NSTORE = MI * (F32 ? NJ : NJ / 2);
     int stores = 0;
     auto wait = [&](auto youngest, bool scales_too, bool scales_now) {
         if constexpr (!DIRECT) return;   // registers wait for themselves
         if (scales_now) __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
-        else if (stores > 0) __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest() + NSTORE));
+        else if (stores > 0) __builtin_amdgcn_s_waitcnt(vmcnt_only(std::min(63, youngest() + NSTORE)));
         else if (scales_too) __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest() + LOADS_SCALES));
         else __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest()));
         if (stores > 0) --stores;
@@ -630,7 +635,9 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
             auto product = [&](const Operand<AT, EXACT>& oa, int i, int j) {
                 acc[i][j] = multiply<BT, AT>(ob[j], oa, acc[i][j]);
                 // in its place: products put off to behind a barrier, or reads brought forward, keep more fragments than there are registers
-                asm volatile("" : "+v"(acc[i][j]));
+                // (256 of them fill the accumulation registers)
+                if constexpr (NJ == 8) asm volatile("" : "+a"(acc[i][j]));
+                else asm volatile("" : "+v"(acc[i][j]));
             };
             const uint32_t at_other = __builtin_amdgcn_readfirstlane(lds_wave + (uint32_t)(cur ^ 1) * STAGE);
             auto loads = [&](auto i) {
@@ -704,7 +711,7 @@ __global__ __launch_bounds__(WM * WN * 64, 2) void gemm_f8_tile_kernel(GemmF8Pla
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             const int64_t m = (int64_t)now.m0 + wm * MI * 16 + i * 16 + r;
-            const int n = now.n0 + wn * 64;
+            const int n = now.n0 + wn * NJ * 16;
             if constexpr (F32) {
 #pragma unroll
                 for (int j = 0; j < NJ; ++j) store_row<F32, GELU, 4>(s, m, n + j * 16 + g * 4, inside, {acc[i][j]});
@@ -738,7 +745,7 @@ struct Choice {
 //   100 x 16384 x 1000:     (2,1) 12.7  (2,2) 16.0  (4,4) 34.9 | 92.0 | 173        2048 cubed:  (2,2) 33.2  (4,4) 29.9 | 17.3 | 29.9
 //   500 x 8192 x 1000 (2):  (2,4) 13.8  (2,2) 16.2  (4,4) 20.1 | 48.9 | 91.0       4096 cubed:  (4,4) 173              | 72.8 | 58.7
 //   256 x 4096 x 4096:      (2,4) 15.7  (2,2) 16.4  (4,4) 13.0 | 27.0 | 49.9       64 x 2048 x 65536:  (4,4) 43.9      | 32.2 | 39.3
-//   fp32 results, 1024 cubed: (2,2) 8.6  (4,4) 7.5 | 16.2; 2048 cubed: (2,2) 37.7  (4,4) 34.9 | 28.2
+//   fp32 results, 1024 cubed: (2,2) 8.6  (4,4) 7.5 | 16.2; 2048 cubed: (2,2) 37.7  (4,4) 34.9 | 28.2 | 60.8; 4096 cubed 140 | 114
 // and with rows at odd pitches, through registers:
 //   300 x 8191 x 513: (2,2) 66.1  (4,4) 129 | 105; 1001 cubed: (2,2) 22.0  (4,4) 13.0 | 20.9; 1111 x 1531 x 1777: (2,4) 57.2  (4,4) 39.3 | 28.8
 Choice choose_tile(const GemmF8Plan& plan, int max_m, int max_n, bool aligned) {
@@ -765,7 +772,7 @@ Choice choose_tile(const GemmF8Plan& plan, int max_m, int max_n, bool aligned) {
     const int64_t n128 = tiles(128, 128);   // two share a compute unit where there are more than units
     if (n128 <= cu) offer(8, 8, blocks * (!aligned ? 1.9 : f32 ? 1.4 : 0.72) + 3.0);
     else offer(8, 8, rounds(n128, 2 * cu) * blocks * (!aligned ? 2.2 : f32 ? 1.95 : 1.1) + 3.0);
-    if (aligned && !f32) offer(16, 16, rounds(tiles(256, 256), cu) * blocks * 1.75 + 3.0);
+    if (aligned) offer(16, 16, rounds(tiles(256, 256), cu) * blocks * (f32 ? 3.3 : 1.75) + 3.0);
     return best;
 }
 
@@ -817,21 +824,22 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
                 if (direct && scales4) go(std::true_type{});
                 else go(std::false_type{});
             };
-            auto tile = [&](auto wm, auto wn, auto mi, auto direct, auto scales4) {
-                constexpr int BM = wm() * mi() * 16, BN = wn() * 64;
+            auto tile = [&](auto wm, auto wn, auto mi, auto nj, auto direct, auto scales4) {
+                constexpr int BM = wm() * mi() * 16, BN = wn() * nj() * 16;
                 const int tm = tiles_along(max_m, BM), tn = tiles_along(max_n, BN);
                 const int64_t tiles = (int64_t)tm * tn * plan.groups;
                 if (tiles > INT32_MAX - 65536) {
                     st = SBP_ERR_UNSUPPORTED;
                     return;
                 }
-                const int64_t at_once = (int64_t)compute_units() * (wm() * wn() > 4 ? 1 : 2), all = (tiles + 7) & ~7;
-                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), direct(), scales4()>), dim3((uint32_t)std::min(all, at_once)),
+                const int64_t at_once = (int64_t)compute_units() * (BM > 128 ? 1 : 2), all = (tiles + 7) & ~7;
+                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), nj(), direct(), scales4()>), dim3((uint32_t)std::min(all, at_once)),
                                    dim3(wm() * wn() * 64), 0, stream, plan, tm, tn, tn > 8 ? 6 : 2, (int)all);
             };
             using std::integral_constant;
             const auto i2 = integral_constant<int, 2>{};
             const auto i4 = integral_constant<int, 4>{};
+            const auto i8 = integral_constant<int, 8>{};
             const auto yes = std::true_type{};
             const auto no = std::false_type{};
             const auto i1 = integral_constant<int, 1>{};
@@ -844,9 +852,10 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
             if (c.mb == 1) columns(i1);
             else if (c.mb == 2) columns(i2);
             else if (c.mb == 4) columns(i4);
-            else if (!direct || !scales4) tile(i2, i2, i4, no, no);
-            else if (c.mb == 8) tile(i2, i2, i4, yes, yes);
-            else if constexpr (!f32()) tile(i2, i4, integral_constant<int, 8>{}, yes, yes);
+            else if (!direct || !scales4) tile(i2, i2, i4, i4, no, no);
+            else if (c.mb == 8) tile(i2, i2, i4, i4, yes, yes);
+            else if constexpr (f32()) tile(i2, i2, i8, i8, yes, yes);
+            else tile(i2, i4, i8, i4, yes, yes);
         });
     });
     return st != SBP_OK ? st : launch_status(__func__);

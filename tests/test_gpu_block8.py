@@ -506,6 +506,13 @@ def test_matmul_f8_gelu(M, K, N, yk):
     matmul_case(np.random.default_rng(13), M, K, N, 2, "S0", "e4m3", "e4m3", yk, gelu=True, dense=True)
 
 
+@pytest.mark.parametrize("xk,wk", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2"), ("e4m3", "e4m3")])
+@pytest.mark.parametrize("yk", ["bf16", "f32"])
+def test_matmul_f8_largest_tile_types_and_gelu(yk, xk, wk):
+    matmul_case(np.random.default_rng(14), 4000, 260, 4000, 1, "B", xk, wk, yk, gelu=True, aligned=True)
+    matmul_case(np.random.default_rng(15), 4096, 390, 1100, 4, "S1", xk, wk, yk, aligned=True)
+
+
 @pytest.mark.parametrize("yk", ["bf16", "f32"])
 @pytest.mark.parametrize("M,K,N", [(3, 200, 20), (300, 400, 270), (64, 2300, 512)])
 def test_matmul_f8_blocks_of_very_different_scale(M, K, N, yk):
