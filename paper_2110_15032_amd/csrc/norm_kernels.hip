@@ -5,14 +5,14 @@
 //
 // Both are bound by HBM: a row is read once and stays in registers, TPR threads a row with V vectors of eight elements each.  A workgroup
 // walks over rows, so that gamma and beta are read once, and reads the next row before it works on this one.  Measured: 8192 x 4096 on eight devices
-// from bf16 to 8 bits (101 MB) 22.4 us, 4.5 TB/s; the gradient of 16384 x 4096 on eight devices, x in 8 bits (336 MB), 75.5 us, 4.5 TB/s.
+// from bf16 to 8 bits (101 MB) 22.7 us, 4.5 TB/s; the gradient of 16384 x 4096 on eight devices, x in 8 bits (336 MB), 75.5 us, 4.5 TB/s.
 #include "block8_device.h"
 
 namespace sbp {
 namespace {
 
-// Workgroups of 256 threads of a launch, so that every compute unit has several (8192 x 4096 in bf16 into 8 bits, us: 512 24.9, 1024 20.5, 2048 22.7;
-// 2048 x 16384 38.6, 24.0, 27.5).
+// Workgroups of 256 threads of a launch, so that every compute unit has several (8192 x 4096 in bf16 into 8 bits on one device, without statistics,
+// us: 512 24.9, 1024 20.5, 2048 22.7; 2048 x 16384 38.6, 24.0, 27.5).
 constexpr int NORM_BLOCKS = 1024;
 constexpr int GRAD_NT = 512;
 
@@ -42,8 +42,26 @@ __device__ inline float inverse_root(float v) {
     return __builtin_amdgcn_rsqf(v);
 }
 
+// a / n, over = 1 / n: the product put right by its remainder, which gives the nearest number, so that the mean of equal values is their value
+__device__ inline float quotient(float a, float n, float over) {
+    const float q = a * over, r = fmaf(fmaf(-q, n, a), over, q);
+    return fabsf(q) < INFINITY ? r : q;
+}
+
+// the sum of N neighbouring lanes' numbers (4, 8 or 16) on each of them
+template <int N>
+__device__ inline float sum_lanes(float v) {
+    v += dpp<0xB1>(v);
+    v += dpp<0x4E>(v);
+    if constexpr (N > 4) v += dpp<0x141>(v);
+    if constexpr (N > 8) v += dpp<0x140>(v);
+    return v;
+}
+
 // The statistics are exact to fp32 sums whatever the row's offset: every wave sums its elements, then the squares of their distances from
-// its own mean, and the waves' pairs are joined with the distances of their means (one exchange for both).
+// its own mean, and the waves' pairs are joined with the distances of their means (one exchange for both, and a pair a lane, as sixteen pairs in every
+// lane's registers spilled).  y goes by the distance to the mean, as the gradient does: mean * rstd has a rounding that x * rstd does not take
+// back, up to 2^-24 |mean| rstd.
 template <int XT, int YT, int WT, int TPR, int V>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p) {
     constexpr int NT = TPR < 256 ? 256 : TPR, G = NT / TPR, NW = TPR / 64;
@@ -58,6 +76,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
     for (int v = 0; v < V; ++v) have += min(max(cols - (v * TPR + t) * 8, 0), 8);
     const bool whole = cols == TPR * V * 8;   // no lane is without elements
     const float of_wave = sum_wave((float)have), over_wave = of_wave > 0.0f ? 1.0f / of_wave : 0.0f, over = 1.0f / (float)cols;
+    float elements = 0.0f;   // of wave t % NW
+#pragma unroll
+    for (int v = 0; v < V; ++v) elements += (float)min(max(cols - (v * TPR + (t & (NW - 1)) * 64) * 8, 0), 512);
 
     // AHEAD rows on their way
     constexpr int AHEAD = XT == T_F32 ? 1 : 2;
@@ -87,7 +108,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
 #pragma unroll
         for (int i = 0; i < V * 8; ++i) sum += x[i];
         sum = sum_wave(sum);
-        const float centre = sum * over_wave;
+        const float centre = quotient(sum, of_wave, over_wave);
         float sq = 0.0f;
         if (whole) {
 #pragma unroll
@@ -112,25 +133,12 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
         if constexpr (NW > 1) {
             if ((threadIdx.x & 63) == 0) part[turn][wave] = float2{centre, sq};
             __syncthreads();   // one a row: the other half is written next, and this one again only behind the next barrier
-            float of[NW];   // elements of each wave
-            mean = 0.0f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                int n = 0;
-#pragma unroll
-                for (int v = 0; v < V; ++v) n += min(max(cols - (v * TPR + w * 64) * 8, 0), 512);
-                of[w] = (float)n;
-                mean = fmaf(of[w], part[turn][w].x, mean);
-            }
-            mean *= over;
-            m2 = 0.0f;
-#pragma unroll
-            for (int w = 0; w < NW; ++w) {
-                const float d = part[turn][w].x - mean;
-                m2 += fmaf(of[w] * d, d, part[turn][w].y);
-            }
+            const float2 of_one = part[turn][t & (NW - 1)];   // of a wave to each lane, and sums over NW lanes
+            mean = quotient(sum_lanes<NW>(of_one.x * elements), (float)cols, over);
+            const float d = of_one.x - mean;
+            m2 = sum_lanes<NW>(fmaf(elements * d, d, of_one.y));
         }
-        const float rstd = inverse_root(fmaf(m2, over, p.eps)), shift = -mean * rstd;
+        const float rstd = inverse_root(fmaf(m2, over, p.eps));
         if (row >= s.rows) return;
         if (t == 0 && s.mean) {
             s.mean[row] = mean;
@@ -140,7 +148,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[v][e] = fmaf(fmaf(x[v * 8 + e], rstd, shift), gamma[v * 8 + e], beta[v * 8 + e]);
+            for (int e = 0; e < 8; ++e) y[v][e] = fmaf((x[v * 8 + e] - mean) * rstd, gamma[v * 8 + e], beta[v * 8 + e]);
         char* const to = static_cast<char*>(s.y) + row * s.ldy * bytes_of<YT>;
         if constexpr (bytes_of<YT> == 1) {
             Raw8<YT> q[V];
@@ -375,7 +383,7 @@ int32_t launch_norm(const NormPlan& given, hipStream_t stream) {
                 using std::integral_constant;
                 // one wave a row needs no barrier; else two vectors a thread.  us, bf16 into 8 bits: 65536 x 512 one wave with one vector 20.7, two
                 // (half of them without elements) 29.2, two waves 38.3; 32768 x 1024 one wave 20.3, two 21.4; 8192 x 4096 two waves 28.2, four 20.5, eight 23.0;
-                // 2048 x 16384 eight 27.2, sixteen 24.0
+                // 2048 x 16384 eight 27.2, sixteen 24.0 (21.1 since their pairs are joined over lanes, and not by every lane)
                 if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
                 else if (plan.cols <= 1024) go(integral_constant<int, 64>{}, integral_constant<int, 2>{});
                 else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});

@@ -780,3 +780,40 @@ def test_matmul_f8_past_32_bits(rows, K, N):
     want, total = a @ b.T, np.abs(a) @ np.abs(b).T
     tol = (K * U["f32"] + 2.0 ** -11) * total
     close(y[-7:].float().cpu().numpy().astype(np.float64), want, tol + (np.abs(want) + tol) * U["bf16"])
+
+
+# ------------------------------------------------------------------ rows far from zero
+@pytest.mark.parametrize("xk", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", [1, 5, 64, 384, 512, 1000, 1024, 1001, 2048, 4095, 4096, 8192, 8200, 16384])
+def test_layernorm_rows_of_equal_values(cols, xk):
+    """A row of one value of bf16 (8 bits, so that sums of up to 2^16 of them are exact) has that value as its mean and no distance to it: y is beta, exactly."""
+    rng = np.random.default_rng(cols)
+    each = np.array([1000.0, 3008.0, -0.1015625, 1.0, 2.0 ** -20, -57344.0, 123.5])
+    w = store(np.repeat(each[:, None], cols, 1), xk)
+    assert (value(w) == each[:, None]).all()
+    rows = len(each)
+    gw, bw = (1 + 0.2 * rng.normal(size=(cols, 1))).astype(np.float32), (0.3 * rng.normal(size=(cols, 1))).astype(np.float32)
+    y, mean, rstd = Buf(rows, cols, np.float32), Buf(rows, 1, np.float32), Buf(rows, 1, np.float32)
+    sbp.sbp_layernorm(desc(up([w], xk), rows, cols, xk), sbp.B, desc(up([gw], "f32"), cols, 1, "f32"), desc(up([bw], "f32"), cols, 1, "f32"), 1e-5,
+                      desc([y], rows, cols, "f32"), None, desc([mean], rows, 1, "f32"), desc([rstd], rows, 1, "f32"), 1)
+    sync()
+    np.testing.assert_array_equal(mean.host()[:, 0], each)
+    np.testing.assert_array_equal(y.host(), np.repeat(bw.T, rows, 0))
+    np.testing.assert_allclose(rstd.host()[:, 0], 1e-5 ** -0.5, rtol=2 * 2.0 ** -23)   # eps's rounding halved, the root's last place
+
+
+@pytest.mark.parametrize("cols", [64, 1001, 4096, 16384])
+@pytest.mark.parametrize("far,deviation", [(1000.0, 0.1), (-3000.0, 1.0), (10.0, 1.0)])
+def test_layernorm_is_the_distance_to_its_mean(cols, far, deviation):
+    """y = (x - mean) rstd gamma + beta of the mean and rstd that the call returns: a rounding of the distance, of its product with rstd and of the rest
+    each, all relative to the distance, however far the row is from zero."""
+    rng = np.random.default_rng(cols)
+    x = (far + deviation * rng.normal(size=(9, cols))).astype(np.float32)
+    gw, bw = (1 + 0.2 * rng.normal(size=(cols, 1))).astype(np.float32), (0.3 * rng.normal(size=(cols, 1))).astype(np.float32)
+    y, mean, rstd = Buf(9, cols, np.float32), Buf(9, 1, np.float32), Buf(9, 1, np.float32)
+    sbp.sbp_layernorm(desc(up([x], "f32"), 9, cols, "f32"), sbp.B, desc(up([gw], "f32"), cols, 1, "f32"), desc(up([bw], "f32"), cols, 1, "f32"), 1e-5,
+                      desc([y], 9, cols, "f32"), None, desc([mean], 9, 1, "f32"), desc([rstd], 9, 1, "f32"), 1)
+    sync()
+    part = (x.astype(np.float64) - mean.host().astype(np.float64)) * rstd.host().astype(np.float64) * gw[:, 0].astype(np.float64)
+    want = part + bw[:, 0]
+    close(y.host().astype(np.float64), want, 2.001 * U["f32"] * np.abs(part) + 1.001 * U["f32"] * np.abs(want), "y")
