@@ -67,7 +67,7 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
         }
         Raw8<QT> q[2];
         uint32_t byte[2];
-        narrow_blocks<QT>(v, q, byte);
+        narrow_blocks<GELU, QT>(v, q, byte);
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             store8<QT>(to + u * F8_BLOCK, q[u], s.cols - c - u * F8_BLOCK, p.streams & STREAM_OUT);
@@ -116,20 +116,13 @@ __global__ __launch_bounds__(NT) void quantize_transposed_kernel(Block8Plan p, i
         bool finite = true;
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            m[e] = __float_as_uint(max3_abs(max3_abs(v[0][e], v[1][e], v[2][e]), v[3][e], v[3][e]));
+            m[e] = most_of<GELU>(v[0][e], v[1][e], v[2][e], v[3][e]);
             finite = finite && m[e] < 0x7F800000u;
         }
-        if (!finite) {   // infinities, or NaN alone
+        if (!finite) {
             asm volatile("");   // or it would be worked out always, and chosen from
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                m[e] = 0;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const uint32_t u = __float_as_uint(v[i][e]) & 0x7FFFFFFFu;
-                    m[e] = max(m[e], u < 0x7F800000u ? u : 0u);
-                }
-            }
+            for (int e = 0; e < 8; ++e) m[e] = max(max(finite_magnitude(v[0][e]), finite_magnitude(v[1][e])), max(finite_magnitude(v[2][e]), finite_magnitude(v[3][e])));
         }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {

@@ -153,7 +153,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void norm_kernel(NormPlan p)
         if constexpr (bytes_of<YT> == 1) {
             Raw8<YT> q[V];
             uint32_t byte[V];
-            narrow_blocks<YT>(y, q, byte);
+            narrow_blocks<true, YT>(y, q, byte);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const int c = (v * TPR + t) * 8;

@@ -817,3 +817,38 @@ def test_layernorm_is_the_distance_to_its_mean(cols, far, deviation):
     part = (x.astype(np.float64) - mean.host().astype(np.float64)) * rstd.host().astype(np.float64) * gw[:, 0].astype(np.float64)
     want = part + bw[:, 0]
     close(y.host().astype(np.float64), want, 2.001 * U["f32"] * np.abs(part) + 1.001 * U["f32"] * np.abs(want), "y")
+
+
+# ------------------------------------------------------------------ NaN whose quiet bit is not set
+@pytest.mark.parametrize("kind", ["e4m3", "e5m2"])
+@pytest.mark.parametrize("xk,word", [("bf16", 0x7F81), ("bf16", 0xFFA0), ("bf16", 0x7FC0), ("f32", 0x7F800001), ("f32", 0xFFBFFFFF), ("f32", 0x7FC00000)])
+@pytest.mark.parametrize("trans", [0, 1])
+@pytest.mark.parametrize("gelu", [False, True])
+def test_quantize_any_nan_leaves_its_block_alone(gelu, trans, xk, word, kind):
+    """One NaN, quiet or signalling, and the block's largest number at every pair of places of eight neighbours: scale and values are those of the other
+    127 (GeLU of the largest is that number itself).  Eight blocks of a kind side by side, so that none is gone through again for the sake of another's."""
+    rng = np.random.default_rng(9)
+    rows = 8 * 256
+    v = rng.uniform(-1, 1, (rows, 128))
+    case = np.arange(rows) // 8
+    place, largest = case % 128, case // 16 % 8 + case % 128 // 8 * 8
+    assert len(set(zip(place % 8, largest % 8))) == 64
+    v[np.arange(rows), largest] = 300.0 + case
+    w = store(v, xk).copy()
+    clear = place != largest
+    bits = w.view(np.uint32 if xk == "f32" else np.uint16)
+    bits[np.arange(rows)[clear], place[clear]] = word
+    with np.errstate(invalid="ignore"):
+        v = value(w.view(NP[xk]))
+    assert np.isnan(v).sum() == clear.sum()
+    stored = np.ascontiguousarray(w.T) if trans else w
+    x = up([stored], xk)
+    q, sc = Buf(rows, 128, np.uint8), Buf(rows, 1, np.uint8)
+    sbp.sbp_quantize(desc(x, *stored.shape, xk), sbp.B, desc([q], *stored.shape, kind, trans), sbp.SbpScales([sc]), 1, None, EPI[gelu])
+    sync()
+    want, wants = o8.quantize(v, kind)
+    np.testing.assert_array_equal(sc.host(), wants)
+    got, nan = q.host(), np.isnan(v)
+    assert np.isnan(o8.decode_table(kind)[got[nan]]).all() and not np.isnan(o8.decode_table(kind)[got[~nan]]).any()
+    same = v > 2 if gelu else ~nan
+    np.testing.assert_array_equal(got[same], want[same])
