@@ -198,6 +198,7 @@ int32_t sbp_layernorm(const sbp_tensor_t* x, sbp_t sx, const sbp_tensor_t* gamma
     if (beta && (st = check_column(beta, x->cols, SBP_B, k, true)) != SBP_OK) return st;
     if (gamma && beta && gamma->dtype != beta->dtype) return SBP_ERR_DTYPE;
     if (!mean != !rstd) return SBP_ERR_NULL;
+    if (mean && x->rows != 0 && x->cols == 0) return SBP_ERR_SHAPE;   // a row of nothing has none
     if (mean && (st = check_column(mean, x->rows, sx, k, false)) != SBP_OK) return st;
     if (rstd && (st = check_column(rstd, x->rows, sx, k, false)) != SBP_OK) return st;
     Buffers b;

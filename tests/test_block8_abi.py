@@ -145,3 +145,13 @@ def test_empty_tensors_are_fine():
     sbp.sbp_gelu_grad(none8, s, sbp.S(0), none, none, 2, STREAM)
     sbp.sbp_layernorm(none, sbp.S(0), None, None, 1e-5, none, None, None, None, 2, STREAM)
     sbp.sbp_matmul_f8(none8, s, sbp.S(0), T(2, 256, 96, sbp.F8E4M3, 2, trans=1), SC(2, 3), sbp.B, sbp.SbpTensor([None] * 2, 0, 96, sbp.BF16), sbp.AUTO, 2, STREAM)
+
+
+def test_rows_without_elements_have_no_statistics():
+    """the mean of nothing is not a number that a caller could go on with, and left unwritten it would be what the buffer held before"""
+    x, y = T(2, 64, 0), T(2, 64, 0, at=1)
+    m, r = T(2, 64, 1, sbp.F32, 5), T(2, 64, 1, sbp.F32, 6)
+    assert status(sbp.sbp_layernorm, x, sbp.S(0), None, None, 1e-5, y, None, m, r, 2, STREAM) == SHAPE
+    sbp.sbp_layernorm(x, sbp.S(0), None, None, 1e-5, y, None, None, None, 2, STREAM)
+    none = sbp.SbpTensor([None] * 2, 0, 1, sbp.F32)
+    sbp.sbp_layernorm(T(2, 0, 0), sbp.S(0), None, None, 1e-5, T(2, 0, 0, at=1), None, none, none, 2, STREAM)
