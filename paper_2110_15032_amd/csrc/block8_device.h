@@ -195,19 +195,6 @@ __device__ inline uint32_t narrow4(float a, float b, float c, float d, float sca
     }
     return __builtin_bit_cast(uint32_t, r);
 }
-// four bf16 values
-template <int T>
-__device__ inline uint32_t narrow4(uint32_t lo, uint32_t hi, float scale) {
-    s16x2 r = {0, 0};
-    if constexpr (T == T_E4M3) {
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, lo), scale, false);
-        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, hi), scale, true);
-    } else {
-        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, __builtin_bit_cast(bf16x2, lo), scale, false);
-        r = __builtin_amdgcn_cvt_scalef32_pk_bf8_bf16(r, __builtin_bit_cast(bf16x2, hi), scale, true);
-    }
-    return __builtin_bit_cast(uint32_t, r);
-}
 
 // The scale byte of a block whose largest finite magnitude is `most`: the smallest e >= -127 with most / 2^e within the type, whose
 // largest value is 1.75 * 2^8 (e4m3) or 1.75 * 2^15 (e5m2), so nothing saturates.  On the bits: the exponent, one more where the

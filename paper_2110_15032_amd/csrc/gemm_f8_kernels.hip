@@ -366,8 +366,8 @@ struct StageF8 {
     __device__ static uint32_t offset(int p, int rows_left, int pitch) { return (uint32_t)min(row_of(p), rows_left - 1) * (uint32_t)pitch + (uint32_t)chunk_of(p) * 16u; }
 };
 
-// SCALES4: rows of scales at pitches of 4 bytes, which go straight into LDS too; else through registers, byte by byte at their end.
-template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, int NJ, bool DIRECT, bool SCALES4>
+// DIRECT: rows at pitches of 16 bytes, and of scales at pitches of 4, go straight into LDS; else through registers, what lies at their end byte by byte.
+template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, int NJ, bool DIRECT>
 __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_kernel(GemmF8Plan p, int tm, int tn, int order, int tiles) {
     constexpr bool EXACT = F32;
     constexpr int NT = WM * WN * 64, BM = WM * MI * 16, BN = WN * NJ * 16;
@@ -378,7 +378,7 @@ __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_ke
     static_assert((BM + BN) % NT == 0, "rows of scales divide over the workgroup");
     // chunk i of a thread lies in rows NT / 8 i + 0..; C of them are half a wave's rows, so that every other C chunks of A are first halves
     constexpr int C = MI * 64 / NT;
-        static_assert(C * NT == MI * 64 && StA::PER == 2 * WM * C, "an operand's chunks fall into halves of the waves' rows");
+    static_assert(C * NT == MI * 64 && StA::PER == 2 * WM * C, "an operand's chunks fall into halves of the waves' rows");
     // scales of 16 blocks of the reduction, twice: four planes of [row] dwords, four blocks each
     constexpr int SCALE_PLANE = (BM + BN) * 4, SCALE_BYTES = 4 * SCALE_PLANE;
     __shared__ __attribute__((aligned(16))) char lds[2 * STAGE + 2 * SCALE_BYTES];
@@ -521,7 +521,7 @@ __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_ke
 #pragma unroll
             for (int d = 0; d < 4; ++d) {
                 char* const plane = to + d * SCALE_PLANE + (i * NT + wave * 64) * 4;
-                if constexpr (SCALES4) {
+                if constexpr (DIRECT) {
                     // four blocks from the row's last four on are those again (a row ends with them, its pitch being whole dwords)
                     const int b = min(step + 4 * d, (t.steps - 1) & ~3);
                     const uint32_t lds_at = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(lds_void*)plane);
@@ -785,11 +785,10 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
         max_n = std::max(max_n, plan.s[g].n);
     }
     if (max_m == 0 || max_n == 0) return SBP_OK;
-    bool direct = true, scales4 = true;   // rows of both operands 16-byte aligned, of their scales 4-byte
+    bool aligned = true;   // rows of both operands by 16 bytes, of their scales by 4
     for (int g = 0; g < plan.groups; ++g) {
         const GemmF8Shard& s = plan.s[g];
-        if (s.lda % 16 || s.ldb % 16) direct = false;
-        if (s.ldas % 4 || s.ldbs % 4) scales4 = false;
+        if (s.lda % 16 || s.ldb % 16 || s.ldas % 4 || s.ldbs % 4) aligned = false;
         if (s.lda > GEMM_F8_MAX_PITCH || s.ldb > GEMM_F8_MAX_PITCH || s.ldas > GEMM_F8_MAX_PITCH || s.ldbs > GEMM_F8_MAX_PITCH) return SBP_ERR_UNSUPPORTED;
     }
     auto types = [&](auto f) {
@@ -821,10 +820,10 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
                 auto go = [&](auto ring) {
                     hipLaunchKernelGGL((gemm_f8_wave_kernel<a(), b(), f32(), gelu(), mb(), nb(), ring()>), dim3((uint32_t)all), dim3(256), 0, stream, plan, tm, tn, 4);
                 };
-                if (direct && scales4) go(std::true_type{});
+                if (aligned) go(std::true_type{});
                 else go(std::false_type{});
             };
-            auto tile = [&](auto wm, auto wn, auto mi, auto nj, auto direct, auto scales4) {
+            auto tile = [&](auto wm, auto wn, auto mi, auto nj, auto direct) {
                 constexpr int BM = wm() * mi() * 16, BN = wn() * nj() * 16;
                 const int tm = tiles_along(max_m, BM), tn = tiles_along(max_n, BN);
                 const int64_t tiles = (int64_t)tm * tn * plan.groups;
@@ -833,7 +832,7 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
                     return;
                 }
                 const int64_t at_once = (int64_t)compute_units() * (BM > 128 ? 1 : 2), all = (tiles + 7) & ~7;
-                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), nj(), direct(), scales4()>), dim3((uint32_t)std::min(all, at_once)),
+                hipLaunchKernelGGL((gemm_f8_tile_kernel<a(), b(), f32(), gelu(), wm(), wn(), mi(), nj(), direct()>), dim3((uint32_t)std::min(all, at_once)),
                                    dim3(wm() * wn() * 64), 0, stream, plan, tm, tn, tn > 8 ? 6 : 2, (int)all);
             };
             using std::integral_constant;
@@ -843,7 +842,7 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
             const auto yes = std::true_type{};
             const auto no = std::false_type{};
             const auto i1 = integral_constant<int, 1>{};
-            const Choice c = choose_tile(plan, max_m, max_n, direct && scales4);
+            const Choice c = choose_tile(plan, max_m, max_n, aligned);
             auto columns = [&](auto mb) {
                 if (c.nb == 1) by_waves(mb, i1);
                 else if (c.nb == 2) by_waves(mb, i2);
@@ -852,10 +851,10 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream) {
             if (c.mb == 1) columns(i1);
             else if (c.mb == 2) columns(i2);
             else if (c.mb == 4) columns(i4);
-            else if (!direct || !scales4) tile(i2, i2, i4, i4, no, no);
-            else if (c.mb == 8) tile(i2, i2, i4, i4, yes, yes);
-            else if constexpr (f32()) tile(i2, i2, i8, i8, yes, yes);
-            else tile(i2, i4, i8, i4, yes, yes);
+            else if (!aligned) tile(i2, i2, i4, i4, no);
+            else if (c.mb == 8) tile(i2, i2, i4, i4, yes);
+            else if constexpr (f32()) tile(i2, i2, i8, i8, yes);
+            else tile(i2, i4, i8, i4, yes);
         });
     });
     return st != SBP_OK ? st : launch_status(__func__);
