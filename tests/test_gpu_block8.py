@@ -852,3 +852,26 @@ def test_quantize_any_nan_leaves_its_block_alone(gelu, trans, xk, word, kind):
     assert np.isnan(o8.decode_table(kind)[got[nan]]).all() and not np.isnan(o8.decode_table(kind)[got[~nan]]).any()
     same = v > 2 if gelu else ~nan
     np.testing.assert_array_equal(got[same], want[same])
+
+
+@pytest.mark.parametrize("M,K,N", [(1, 260, 16), (300, 900, 272), (2000, 2200, 2000), (4096, 2200, 8192)])
+def test_matmul_f8_the_most_that_an_eight_of_products_loses(M, K, N):
+    """In every eight of the reduction 2^7 and -2^7 times the smallest subnormal number, 2^-9, whose exponent counts as -6, and six products below 2^(7 - 6 - 13):
+    bf16 results may lose the six, which are 2^-8.6 of the products' magnitudes and all of the result, but less than 2^-10 2^(7 - 6).  fp32 results
+    have them."""
+    torch = torch_mod()
+    kp, nb = -(-K // 16) * 16, -(-blocks(K) // 4) * 4
+    place = torch.arange(kp, device="cuda")
+    row = lambda first, second, rest: torch.where(place >= K, 0, torch.where(place % 8 == 0, first, torch.where(place % 8 == 1, second, rest))).to(torch.uint8)  # noqa: E731
+    rx, rw = row(0x70, 0xF0, 0x07), row(0x01, 0x01, 0x08)
+    x, w = rx.repeat(M, 1), rw.repeat(N, 1)
+    one = lambda n: torch.full((n, nb), 127, dtype=torch.uint8, device="cuda")  # noqa: E731
+    sx, sw = one(M), one(N)
+    table = torch.from_numpy(o8.decode_table("e4m3")).cuda()
+    p = table[rx.long()] * table[rw.long()]
+    want, total = float(p.sum()), float(p.abs().sum())
+    for yk, dt, tol in (("f32", torch.float32, K * U["f32"] * total), ("bf16", torch.bfloat16, -(-K // 8) * 2.0 ** -9 + K * U["f32"] * total + 2 * U["bf16"] * want)):
+        y = torch.zeros(M, N, dtype=dt, device="cuda")
+        sbp.sbp_matmul_f8(desc([x], M, K, "e4m3", 0, kp), sbp.SbpScales([sx], nb), sbp.B, desc([w], K, N, "e4m3", 1, kp), sbp.SbpScales([sw], nb), sbp.B,
+                          desc([y], M, N, yk), sbp.B, 1)
+        assert float((y.double() - want).abs().max()) <= tol, yk
