@@ -854,6 +854,98 @@ def test_quantize_any_nan_leaves_its_block_alone(gelu, trans, xk, word, kind):
     np.testing.assert_array_equal(got[same], want[same])
 
 
+# ------------------------------------------------------------------ every kind of tile, every element, on the GPU in 64 bits
+#: M, K, N, devices, signature, result, aligned rows; 16s of rows of the tile that the sizes lead to on 256 compute units (asked of the choice itself on the
+#: CPU); what the sizes are for
+F8_TILES = [
+    (4096, 2200, 8192, 1, "B", "bf16", True, 16),      # two tiles a workgroup, scales read in two parts, a cut block
+    (4096, 2200, 8192, 1, "B", "f32", True, 16),
+    (2048, 2100, 16384, 8, "S1", "bf16", True, 16),    # tiles of several devices one after another
+    (4096, 513, 4096, 2, "P", "f32", True, 16),        # reductions of three and of two blocks
+    (8000, 260, 4000, 2, "S0", "bf16", True, 16),      # a cut block of four elements
+    (2000, 2200, 2000, 1, "B", "bf16", True, 8),
+    (2000, 2200, 1990, 1, "B", "f32", True, 8),
+    (777, 3001, 1501, 3, "P", "f32", True, 8),
+    (2500, 383, 2500, 3, "P", "f32", True, 8),         # several tiles a workgroup, of devices with one block, the last one cut
+    (2500, 385, 2500, 3, "P", "f32", True, 8),         # with one whole block and one element, and with one block
+    (1111, 1531, 1777, 1, "B", "bf16", False, 8),      # through registers
+    (1111, 1531, 1777, 1, "B", "f32", False, 8),
+    (3000, 2201, 3000, 1, "B", "bf16", False, 8),      # several tiles a workgroup
+    (2500, 385, 2500, 3, "P", "f32", False, 8),
+]
+
+
+def f8_pitches(k, aligned):
+    """pitches of rows of k values and of their scales"""
+    return (-(-k // 16) * 16 + 16, -(-blocks(k) // 4) * 4 + 4) if aligned else (k | 1, blocks(k))
+
+
+def f8_on_the_gpu(M, K, N, k, sig, xk, wk, yk, aligned, gelu, seed):
+    """Random codes of every finite value; scales from 2^-40 to 2^40 and three NaN an operand (moderate scales and no NaN with GeLU); what lies between and behind
+    the rows is NaN, and no scale.  Every element against the 64-bit product on the same card.
+
+    bf16 results: the instruction for 8 bits cuts the products of eight consecutive values at 2^-13 of the power of two that is the largest of their exponents'
+    sums (subnormal numbers' being the smallest normal one's), so eight of them lose less than 2^-10 of it."""
+    torch = torch_mod()
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    rand = lambda lo, hi, *s: torch.randint(lo, hi, s, generator=g, device="cuda", dtype=torch.int32).to(torch.uint8)  # noqa: E731
+    table = {t: torch.from_numpy(o8.decode_table(t)).cuda() for t in (xk, wk)}
+
+    parts_ = lambda n: [e - b for b, e in parts(n, k)]  # noqa: E731
+    ld, lds = f8_pitches(max(parts_(K)) if sig == "P" else K, aligned)   # one pitch for all devices
+
+    def operand(rows, cols, kind):
+        v, s = (torch.full((rows * p,), 255, dtype=torch.uint8, device="cuda").view(rows, p) for p in (ld, lds))
+        v[:, :cols] = rand(0, 120, rows, cols) | 128 * rand(0, 2, rows, cols)
+        s[:, :blocks(cols)] = rand(118, 123, rows, blocks(cols)) if gelu else rand(87, 168, rows, blocks(cols))
+        if not gelu:
+            for r, c in ((rows // 3, 0), (rows - 1, cols - 1), (rows // 2, cols // 2)):
+                v[r, c] = 255
+        power = torch.exp2(s[:, :blocks(cols)].double() - 127).repeat_interleave(128, 1)[:, :cols]
+        value_ = table[kind][v[:, :cols].long()]
+        most = torch.nn.functional.pad(value_.abs().nan_to_num(0.0), (0, -cols % 8)).unflatten(1, (-1, 8)).amax(2).clamp(min=2.0 ** (-6 if kind == "e4m3" else -14))
+        return v, s, value_ * power, torch.exp2(torch.floor(torch.log2(most))) * power[:, ::8]
+
+    if sig == "P":
+        x, w = [operand(M, n, xk) for n in parts_(K)], [operand(N, n, wk) for n in parts_(K)]
+    else:
+        x = [operand(n, K, xk) for n in parts_(M)] if sig == "S0" else [operand(M, K, xk)] * k
+        w = [operand(n, K, wk) for n in parts_(N)] if sig == "S1" else [operand(N, K, wk)] * k
+    ldy = max(o[0].shape[0] for o in w) + 3
+    y = [torch.full((a[0].shape[0], ldy), -7.0, dtype=torch.float32 if yk == "f32" else torch.bfloat16, device="cuda") for a in x]
+    a_sig, b_sig, y_sig = {"S0": (sbp.S(0), sbp.B, sbp.S(0)), "S1": (sbp.B, sbp.S(1), sbp.S(1)), "P": (sbp.S(1), sbp.S(0), sbp.P_SUM), "B": (sbp.B,) * 3}[sig]
+    sbp.sbp_matmul_f8(desc([o[0] for o in x], M, K, xk, 0, ld), sbp.SbpScales([o[1] for o in x], lds), a_sig,
+                      desc([o[0] for o in w], K, N, wk, 1, ld), sbp.SbpScales([o[1] for o in w], lds), b_sig, desc(y, M, N, yk, 0, ldy), y_sig, k, None, EPI[gelu])
+    for i in range(k):
+        xv, wv, n = x[i][2], w[i][2], w[i][2].shape[0]
+        assert bool((y[i][:, n:] == -7).all())
+        got, want, total = y[i][:, :n].double(), xv @ wv.T.contiguous(), xv.abs() @ wv.abs().T.contiguous()
+        tol = xv.shape[1] * U["f32"] * total + (2.0 ** -10 * (x[i][3] @ w[i][3].T.contiguous()) if yk == "bf16" else 0.0)
+        if gelu:
+            want = 0.5 * want * torch.special.erfc(-want * 0.5 ** 0.5)
+            tol = 1.13 * tol + 2.3e-5 * want.abs()
+        nan = want.isnan()
+        assert bool((got.isnan() == nan).all()) and int(nan.sum()) == (0 if gelu else 3 * n + 3 * got.shape[0] - 9)
+        bad = ~nan & ~((got - want).abs() <= tol + (want.abs() + tol) * U[yk] + 1e-37)
+        assert not bool(bad.any()), f"shard {i}: {int(bad.sum())} of {bad.numel()} off, first at {bad.nonzero()[0].tolist()}"
+
+
+@pytest.mark.parametrize("M,K,N,k,sig,yk,aligned,tile", F8_TILES)
+def test_matmul_f8_tiles_with_scales_far_apart(M, K, N, k, sig, yk, aligned, tile):
+    f8_on_the_gpu(M, K, N, k, sig, "e4m3", "e4m3", yk, aligned, False, 21)
+
+
+@pytest.mark.parametrize("xk,wk", [("e4m3", "e5m2"), ("e5m2", "e4m3"), ("e5m2", "e5m2")])
+@pytest.mark.parametrize("M,K,N,k,sig,yk,aligned,tile", [c for c in F8_TILES if not c[6]] + F8_TILES[:2] + F8_TILES[5:8])
+def test_matmul_f8_tiles_of_either_type(M, K, N, k, sig, yk, aligned, tile, xk, wk):
+    f8_on_the_gpu(M, K, N, k, sig, xk, wk, yk, aligned, False, 22)
+
+
+@pytest.mark.parametrize("M,K,N,k,sig,yk,aligned,tile", [c for c in F8_TILES if c[4] != "P"])
+def test_matmul_f8_tiles_with_gelu(M, K, N, k, sig, yk, aligned, tile):
+    f8_on_the_gpu(M, K, N, k, sig, "e4m3", "e5m2", yk, aligned, True, 23)
+
+
 @pytest.mark.parametrize("M,K,N", [(1, 260, 16), (300, 900, 272), (2000, 2200, 2000), (4096, 2200, 8192)])
 def test_matmul_f8_the_most_that_an_eight_of_products_loses(M, K, N):
     """In every eight of the reduction 2^7 and -2^7 times the smallest subnormal number, 2^-9, whose exponent counts as -6, and six products below 2^(7 - 6 - 13):
