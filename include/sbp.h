@@ -101,7 +101,9 @@ typedef struct sbp_tensor {
  * consecutive values of a stored row: the value stands for itself times that power.  Shard i's scales
  * are bytes [stored rows][ceil(stored row length / 128)] of the LOCAL tensor as it is stored (trans
  * included), counted from the row's start; byte b stands for 2^(b - 127).  255 is no scale.  A kernel may
- * read the bytes behind a row of scales up to the next multiple of 4; their values never reach a result.
+ * read the bytes behind a row of scales up to the next multiple of 4, and sbp_matmul_f8, where rows of values
+ * are a multiple of 16 apart, those behind a row of values up to the next multiple of 16: behind the last row
+ * too, where they share 16 aligned bytes with the tensor's last value.  What they hold never reaches a result.
  * Every operator on 8-bit tensors and layer normalisation takes at most 2^31 - 257 rows and columns
  * (SBP_ERR_UNSUPPORTED). */
 #define SBP_F8_BLOCK 128

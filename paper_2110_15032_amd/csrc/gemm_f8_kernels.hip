@@ -10,6 +10,7 @@
 // The instruction's first operand is B (weights), so that a lane holds one row m and four consecutive columns n of the result.
 #include "block8_device.h"
 #include "gemm_f8_choice.h"
+#include "gemm_f8_stage.h"
 
 namespace sbp {
 namespace {
@@ -351,24 +352,6 @@ __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm,
 // the larger tile has four waves of 128 x 128, one a SIMD with all its 512 registers, and half the conversions of the smaller one (8192 x 4096 x 16384
 // 1109 -> 895 us, 4096 cubed 140 -> 114); bf16 results are better off with eight of 128 x 64 (505 -> 479), two a SIMD.
 //
-// LDS image of an operand: rows of 128 bytes, 16-byte chunk c of a row at c ^ key(row), so that the 16 lanes of a read's pass fall on
-// different banks: row / 2 where a fragment is 16 consecutive rows, as A's are, and B's for fp32 results.  For bf16 results (PAIRS) B's fragments
-// are taken in pairs, rows 8 i + 0..3 of 32 and rows 8 i + 4..7, so that a lane ends with eight consecutive columns of a row, and four lanes
-// store 64 consecutive bytes either way; the key is the place in the fragment over 2.
-template <int ROWS, int NT, bool PAIRS>
-struct StageF8 {
-    static constexpr int PER = ROWS * 8 / NT;   // chunks of a thread
-    static constexpr int BYTES = ROWS * F8_BLOCK;
-    __device__ static int key(int row) { return PAIRS ? ((row >> 3) & 3) << 1 | ((row >> 1) & 1) : (row >> 1) & 7; }
-    // row of place r in fragment j, and the byte offset of fragment j from fragment 0
-    __device__ static int fragment_row(int r) { return PAIRS ? (r >> 2) * 8 + (r & 3) : r; }
-    static constexpr int fragment(int j) { return (PAIRS ? (j >> 1) * 32 + (j & 1) * 4 : j * 16) * F8_BLOCK; }
-    __device__ static int row_of(int p) { return p >> 3; }
-    __device__ static int chunk_of(int p) { return (p & 7) ^ key(p >> 3); }
-    // byte offset of chunk position p from the tile's first row; rows past the operand's end are its last one
-    __device__ static uint32_t offset(int p, int rows_left, int pitch) { return (uint32_t)min(row_of(p), rows_left - 1) * (uint32_t)pitch + (uint32_t)chunk_of(p) * 16u; }
-};
-
 // DIRECT: rows at pitches of 16 bytes, and of scales at pitches of 4, go straight into LDS; else through registers, what lies at their end byte by byte.
 template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, int NJ, bool DIRECT>
 __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_kernel(GemmF8Plan p, int tm, int tn, int order, int tiles) {
@@ -418,13 +401,12 @@ __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_ke
     int ahead_left;   // reduction elements from the cursor's stage to the end
     uint32_t off_a[StA::PER], off_b[StB::PER];
     gbl_char *src_a, *src_b;
-    // A stage that the reduction ends in: a chunk that starts behind the end is read from the last one that does not (cut_* clears both).  A
-    // thread's chunks of an operand lie at one place in their rows.
+    // A stage that the reduction ends in: StageF8::less() (cut_* clears what lies behind the end).  A thread's chunks of an operand lie at one place in
+    // their rows.
     uint32_t less_a, less_b;
     auto shorten = [&]() {
-        const int last = min(ahead_left - 1, F8_BLOCK - 1) >> 4;
-        less_a = DIRECT ? (uint32_t)max(StA::chunk_of((int)threadIdx.x) - last, 0) * 16u : 0u;
-        less_b = DIRECT ? (uint32_t)max(StB::chunk_of((int)threadIdx.x) - last, 0) * 16u : 0u;
+        less_a = DIRECT ? StA::less((int)threadIdx.x, ahead_left) : 0u;
+        less_b = DIRECT ? StB::less((int)threadIdx.x, ahead_left) : 0u;
     };
     auto enter = [&]() {
         const GemmF8Shard& s = p.s[ahead.g];
