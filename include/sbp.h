@@ -323,7 +323,8 @@ int32_t sbp_dequantize(const sbp_tensor_t* q, const sbp_scales_t* q_scales, sbp_
                        void* stream, int32_t epilogue);
 
 /* The gradient of GeLU (exact erf form): da = dh * (Phi(a) + a phi(a)), Phi and phi the normal
- * distribution and its density, evaluated in fp32 to 5e-7 before the single rounding.  a: the pre-activation, SBP_F32,
+ * distribution and its density, evaluated in fp32 to 5e-7 before the single rounding (fp32 results: to the
+ * roundings of fp32, 4e-8 root mean square).  a: the pre-activation, SBP_F32,
  * SBP_BF16 or in 8 bits (with a_scales; NULL else); dh and da SBP_F32 or SBP_BF16, one type; all
  * S or B under one signature (a nonlinear function of a partial is SBP_ERR_SIGNATURE). */
 int32_t sbp_gelu_grad(const sbp_tensor_t* a, const sbp_scales_t* a_scales, sbp_t sbp_a, const sbp_tensor_t* dh,

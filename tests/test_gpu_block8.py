@@ -967,3 +967,18 @@ def test_matmul_f8_the_most_that_an_eight_of_products_loses(M, K, N):
         sbp.sbp_matmul_f8(desc([x], M, K, "e4m3", 0, kp), sbp.SbpScales([sx], nb), sbp.B, desc([w], K, N, "e4m3", 1, kp), sbp.SbpScales([sw], nb), sbp.B,
                           desc([y], M, N, yk), sbp.B, 1)
         assert float((y.double() - want).abs().max()) <= tol, yk
+
+
+def test_gelu_grad_of_fp32_is_as_good_as_its_roundings():
+    """gelu' lies in -0.13 .. 1.13: four roundings (the tail's two products, the distance to 1, the sum) of numbers up to 1 are 2^-25 / sqrt 3 each, root mean
+    square, 3.5e-8 together; half as much again for the exponential, the reciprocal and the fit would be 5.2e-8."""
+    x = np.linspace(-4, 4, 1 << 20).astype(np.float32)[None]
+    out = Buf(*x.shape, np.float32)
+    sbp.sbp_gelu_grad(desc(up([x], "f32"), *x.shape, "f32"), None, sbp.B, desc(up([np.ones_like(x)], "f32"), *x.shape, "f32"), desc([out], *x.shape, "f32"), 1)
+    sync()
+    off = out.host().astype(np.float64) - o8.gelu_slope(x.astype(np.float64))
+    assert np.sqrt((off ** 2).mean()) < 5.2e-8 and np.abs(off).max() < 5e-7
+    # far out on the left what is left is a phi(a) and the tail, which a bf16 result still has to 2^-8 of itself
+    far = out.host()[0] < 0
+    far &= x[0] < -3
+    assert (np.abs(off[0][far]) < 1e-4 * np.abs(o8.gelu_slope(x[0][far].astype(np.float64)))).all()
