@@ -316,7 +316,8 @@ int32_t sbp_layernorm_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_x, in
  *   operand of a weight's gradient.
  * sbp_dequantize: x (SBP_F32 or SBP_BF16) = the values q stands for, or gelu of them.  Without GeLU exact
  *   in fp32, and in bf16 down to 2^-126 (2^128, to which the largest fp32 numbers round, is infinity).  q.trans as above, x.trans = 0.
- * epilogue: SBP_EPI_NONE or SBP_EPI_GELU (to 2.2e-5 of its value before rounding; 1e-7 for fp32 results). */
+ * epilogue: SBP_EPI_NONE or SBP_EPI_GELU (to 2.2e-5 of its value before rounding; 1e-7 for fp32 results; 0 of
+ * minus infinity). */
 int32_t sbp_quantize(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_tensor_t* q, const sbp_scales_t* q_scales, int32_t k,
                      void* stream, int32_t epilogue);
 int32_t sbp_dequantize(const sbp_tensor_t* q, const sbp_scales_t* q_scales, sbp_t sbp_q, const sbp_tensor_t* x, int32_t k,

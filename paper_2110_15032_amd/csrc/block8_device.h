@@ -130,6 +130,9 @@ inline int32_t streams_of(int64_t read, int64_t wrote, bool on_lines, int32_t ou
     return (wrote >= (int64_t)32 << 20 && on_lines && out_dtype != SBP_F32 ? STREAM_OUT : 0) | (read + wrote > (int64_t)256 << 20 ? STREAM_IN : 0);
 }
 
+// gelu of results in fp32: gelu_erf, but 0 of minus infinity, as gelu_fast has it (as a factor it is the lowest number, next to an erfc of 0)
+__device__ inline float gelu_whole(float x) { return 0.5f * __builtin_amdgcn_fmed3f(x, -3.4028235e38f, INFINITY) * erfcf(x * -0.70710678118654752f); }
+
 // A scale byte b stands for 2^(b - 127).  The conversions below take a power of two as the exponent field of an fp32 number, 0 there
 // standing for 2^-127.
 __device__ inline float scale_of(uint32_t byte) { return __uint_as_float(byte << 23); }

@@ -38,7 +38,7 @@ struct UnitWalk {
 template <bool FAST>
 __device__ inline float gelu_of(float x) {
     if constexpr (FAST) return gelu_fast(x);
-    else return gelu_erf(x);
+    else return gelu_whole(x);
 }
 
 // Bound by HBM: 8192 x 16384 on eight devices from bf16 (404 MB) 64 us, 6.3 TB/s; with GeLU 85 us, by its polynomial and exponential.  IN: inputs past

@@ -103,7 +103,7 @@ __device__ inline f32x4 multiply(const Operand<BT, true>& b, const Operand<AT, t
 template <bool F32, bool GELU>
 __device__ inline float finish(float v) {
     if constexpr (!GELU) return v;
-    else if constexpr (F32) return gelu_erf(v);
+    else if constexpr (F32) return gelu_whole(v);
     else return gelu_fast(v);
 }
 

@@ -982,3 +982,29 @@ def test_gelu_grad_of_fp32_is_as_good_as_its_roundings():
     far = out.host()[0] < 0
     far &= x[0] < -3
     assert (np.abs(off[0][far]) < 1e-4 * np.abs(o8.gelu_slope(x[0][far].astype(np.float64)))).all()
+
+
+@pytest.mark.parametrize("yk", ["bf16", "f32"])
+def test_gelu_of_infinities(yk):
+    """0 on the left and infinity on the right, in every form: of values restored from 8 bits (e5m2 has infinities), and of a product's results"""
+    x = np.zeros((3, 130), np.float32)
+    x[0, [0, 64, 129]], x[1, 5], x[2, 7] = [np.inf, -np.inf, 3.0], -np.inf, np.nan
+    q, sc, y = Buf(3, 130, np.uint8), Buf(3, 2, np.uint8), Buf(3, 130, NP[yk])
+    dq, ds = desc([q], 3, 130, "e5m2"), sbp.SbpScales([sc])
+    sbp.sbp_quantize(desc(up([x], "f32"), 3, 130, "f32"), sbp.B, dq, ds, 1)
+    sbp.sbp_dequantize(dq, ds, sbp.B, desc([y], 3, 130, yk), 1, None, sbp.EPI_GELU)
+    w = Buf(20, 130, np.uint8, 0, np.full((20, 130), 0x38, np.uint8))             # ones
+    ws, p = Buf(20, 2, np.uint8, 0, np.full((20, 2), 127, np.uint8)), Buf(3, 20, NP[yk])
+    x2 = x.copy()
+    x2[0, 64] = 0.0
+    q2, sc2 = Buf(3, 130, np.uint8), Buf(3, 2, np.uint8)
+    dq2, ds2 = desc([q2], 3, 130, "e5m2"), sbp.SbpScales([sc2])
+    sbp.sbp_quantize(desc(up([x2], "f32"), 3, 130, "f32"), sbp.B, dq2, ds2, 1)
+    sbp.sbp_matmul_f8(dq2, ds2, sbp.B, desc([w], 130, 20, "e4m3", 1), sbp.SbpScales([ws]), sbp.B, desc([p], 3, 20, yk), sbp.B, 1, None, sbp.EPI_GELU)
+    sync()
+    got, want = value(y.host()), x.astype(np.float64)
+    want[want == -np.inf] = 0.0
+    keep = ~((want == 3.0))
+    np.testing.assert_array_equal(got[keep], want[keep])
+    got = value(p.host())
+    assert (got[0] == np.inf).all() and (got[1] == 0).all() and np.isnan(got[2]).all()
