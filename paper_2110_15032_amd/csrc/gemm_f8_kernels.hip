@@ -556,6 +556,7 @@ __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_ke
         else if (scales_too) __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest() + LOADS_SCALES));
         else __builtin_amdgcn_s_waitcnt(vmcnt_only(youngest()));
         if (stores > 0) --stores;
+        asm volatile("" ::: "memory");   // nothing that loads wrote into LDS is read ahead of this
     };
     auto barrier = [&]() {
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // what this wave read and wrote in LDS
@@ -577,6 +578,7 @@ __global__ __launch_bounds__(WM * WN * 64, NJ == 8 ? 1 : 2) void gemm_f8_tile_ke
         hold();
     }
     __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    asm volatile("" ::: "memory");
     cut_first(lds, left0);
     barrier();
 
