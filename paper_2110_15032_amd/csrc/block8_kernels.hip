@@ -78,10 +78,11 @@ __global__ __launch_bounds__(NT) void quantize_kernel(Block8Plan p) {
 
 // Transposed: the block runs along the rows.  A workgroup takes 128 rows by 64 columns; thread t holds rows 4 (t / 8) .. + 3 of the eight
 // columns 8 (t % 8), the column maxima meet over the lanes of a wave and over the waves in LDS, the bytes turn in LDS.  8192 x 8192 from bf16 (202 MB)
-// 45 us, 4.4 TB/s: a tile's loads do not overlap its turn, other workgroups' do; with GeLU 16384 x 1024 (50 MB) 15.0 us.
+// 43 .. 46 us, 4.5 TB/s: a tile's loads do not overlap its turn, other workgroups' do; with GeLU 16384 x 1024 (50 MB) 14.9 us.
 constexpr int TC = 64;
 // Bytes of one column in LDS.  Its 4-byte words are permuted by XOR with turn_key(column / 8), a multiple of four: the eight columns 8 co + e that a
-// wave's lanes write at once (eight consecutive words each) fall on different banks.
+// wave's lanes write at once (eight consecutive words each) fall on different banks.  The reads of 16 bytes on the way out take twice as long as they could: a
+// pass has pieces of columns 36 words apart, two of which share banks (34 % of the LDS cycles are conflicts).
 constexpr int QPITCH = F8_BLOCK + 16;
 __device__ inline int turn_key(int co) { return (co >> 1 & 3) * 8; }
 template <int XT, int QT, bool GELU>

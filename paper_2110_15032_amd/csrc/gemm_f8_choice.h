@@ -20,7 +20,7 @@ struct F8Choice {
 //   100 x 16384 x 1000:     (2,1) 12.7  (2,2) 16.0  (4,4) 34.9 | 92.0 | 173        2048 cubed:  (2,2) 33.2  (4,4) 29.9 | 17.3 | 29.9
 //   500 x 8192 x 1000 (2):  (2,4) 13.8  (2,2) 16.2  (4,4) 20.1 | 48.9 | 91.0       4096 cubed:  (4,4) 173              | 72.8 | 58.7
 //   256 x 4096 x 4096:      (2,4) 15.7  (2,2) 16.4  (4,4) 13.0 | 27.0 | 49.9       64 x 2048 x 65536:  (4,4) 43.9      | 32.2 | 39.3
-//   fp32 results, 1024 cubed: (2,2) 8.6  (4,4) 7.5 | 16.2; 2048 cubed: (2,2) 37.7  (4,4) 34.9 | 28.2 | 60.8; 4096 cubed 140 | 114
+//   fp32 results, 1024 cubed: (2,2) 8.6  (4,4) 7.5 | 16.2; 2048 cubed: (2,2) 37.7  (4,4) 34.9 | 28.2 | 60.8; 4096 cubed 140 | 112
 // and with rows at odd pitches, through registers:
 //   300 x 8191 x 513: (2,2) 66.1  (4,4) 129 | 105; 1001 cubed: (2,2) 22.0  (4,4) 13.0 | 20.9; 1111 x 1531 x 1777: (2,4) 57.2  (4,4) 39.3 | 28.8
 // cu: compute units

@@ -346,11 +346,12 @@ __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm,
 // step and a half to arrive (with one barrier and a step the loads alone took 467 us of the 515 of 8192 x 4096 x 16384).  The row blocks before a
 // barrier are multiplied behind it, underneath the reads of the next fragments.
 //
-// Bound by the matrix pipe: 8192 x 4096 x 16384 on eight devices, bf16 results, 452 us, 2.43 PFLOP/s (the
+// Bound by the matrix pipe: 8192 x 4096 x 16384 on eight devices, bf16 results, 456 .. 464 us, 2.4 PFLOP/s (the
 // instruction alone, on random operands, 4.1), and by LDS, which is busy for as many cycles (192 KB read and 64 KB written a step at 128 bytes, against
 // 64 instructions of 32 on every SIMD).  fp32 results by the widening next to the products, once for every wave that reads a fragment:
 // the larger tile has four waves of 128 x 128, one a SIMD with all its 512 registers, and half the conversions of the smaller one (8192 x 4096 x 16384
-// 1109 -> 895 us, 4096 cubed 140 -> 114); bf16 results are better off with eight of 128 x 64 (505 -> 479), two a SIMD.
+// 1005 -> 848 us, 4096 cubed 140 -> 112); bf16 results are better off with eight of 128 x 64, two a SIMD (505 with four, 479 with eight, both at an
+// earlier stage of the rest).
 //
 // DIRECT: rows at pitches of 16 bytes, and of scales at pitches of 4, go straight into LDS; else through registers, what lies at their end byte by byte.
 template <int AT, int BT, bool F32, bool GELU, int WM, int WN, int MI, int NJ, bool DIRECT>
