@@ -1008,3 +1008,77 @@ def test_gelu_of_infinities(yk):
     np.testing.assert_array_equal(got[keep], want[keep])
     got = value(p.host())
     assert (got[0] == np.inf).all() and (got[1] == 0).all() and np.isnan(got[2]).all()
+
+
+# ------------------------------------------------------------------ the ends of what the calls allow
+@pytest.mark.parametrize("which", ["gamma", "beta"])
+@pytest.mark.parametrize("wk", ["f32", "bf16"])
+def test_layernorm_with_one_weight(wk, which):
+    rng = np.random.default_rng(31)
+    x, v = (rng.normal(size=(5, 700))).astype(np.float32), store(rng.normal(size=(700, 1)), wk)
+    d = desc(up([v], wk), 700, 1, wk)
+    y = Buf(5, 700, np.float32)
+    sbp.sbp_layernorm(desc(up([x], "f32"), 5, 700, "f32"), sbp.B, d if which == "gamma" else None, d if which == "beta" else None, 1e-5, desc([y], 5, 700, "f32"),
+                      None, None, None, 1)
+    sync()
+    g, b = (value(v)[:, 0], 0.0) if which == "gamma" else (1.0, value(v)[:, 0])
+    want, m, r = o8.layernorm(x.astype(np.float64), g, b, 1e-5)
+    close(y.host().astype(np.float64), want, norm_tolerance(x.astype(np.float64), np.broadcast_to(g, 700), np.broadcast_to(b, 700), m, r) + np.abs(want) * U["f32"])
+
+
+def test_layernorm_grad_of_no_rows_is_zero():
+    og, ob = [Buf(300, 1, np.float32) for _ in range(2)], [Buf(300, 1, np.float32) for _ in range(2)]
+    none = lambda cols, kind: sbp.SbpTensor([None, None], 0, cols, CODE[kind])  # noqa: E731
+    assert sbp.sbp_layernorm_grad_workspace(0, 300, sbp.S(0), 2) == 0
+    sbp.sbp_layernorm_grad(none(300, "bf16"), None, sbp.S(0), None, none(1, "f32"), none(1, "f32"), none(300, "bf16"), none(300, "bf16"), desc(og, 300, 1, "f32"),
+                           desc(ob, 300, 1, "f32"), None, 2)
+    sync()
+    assert all((b.host() == 0).all() for b in og + ob)
+
+
+@pytest.mark.parametrize("gelu", [False, True])
+@pytest.mark.parametrize("yk", ["bf16", "f32"])
+def test_matmul_f8_of_no_reduction_is_zero(yk, gelu):
+    none, s = sbp.SbpTensor([None], 70, 0, sbp.F8E4M3), sbp.SbpScales([None])
+    y = Buf(70, 33, NP[yk], 40)
+    sbp.sbp_matmul_f8(none, s, sbp.B, sbp.SbpTensor([None], 0, 33, sbp.F8E5M2, 1), s, sbp.B, desc([y], 70, 33, yk, 0, 40), sbp.B, 1, None, EPI[gelu])
+    sync()
+    assert (y.host() == 0).all()
+
+
+@pytest.mark.parametrize("sig", ["S0", "S1", "B"])
+def test_as_many_devices_as_there_may_be(sig):
+    """64 for the elementwise operators, 32 for the others; more devices than rows or columns among them"""
+    rng = np.random.default_rng(33)
+    for rows, cols in ((50, 300), (130, 40), (200, 260)):
+        w = store(rng.normal(size=(rows, cols)), "bf16")
+        shards, k = split(w, sig, 64), 64
+        x, dh = up(shards, "bf16"), up(shards, "bf16")
+        q, sc = [Buf(*s.shape, np.uint8) for s in shards], [Buf(s.shape[0], blocks(s.shape[1]) if s.size else 0, np.uint8) for s in shards]
+        y, da = [Buf(*s.shape, np.float32) for s in shards], [Buf(*s.shape, np.uint16) for s in shards]
+        dq, ds = desc(q, rows, cols, "e4m3"), sbp.SbpScales(sc)
+        sbp.sbp_quantize(desc(x, rows, cols, "bf16"), SIG[sig], dq, ds, k)
+        sbp.sbp_dequantize(dq, ds, SIG[sig], desc(y, rows, cols, "f32"), k)
+        sbp.sbp_gelu_grad(dq, ds, SIG[sig], desc(dh, rows, cols, "bf16"), desc(da, rows, cols, "bf16"), k)
+        sync()
+        for i, s in enumerate(shards):
+            if not s.size:
+                continue
+            want, wants = o8.quantize(value(np.ascontiguousarray(s)), "e4m3")
+            stands = o8.dequantize(want, wants, "e4m3")
+            np.testing.assert_array_equal(q[i].host(), want)
+            np.testing.assert_array_equal(y[i].host(), stands)
+            grad = value(s) * o8.gelu_slope(stands)
+            close(value(da[i].host()), grad, np.abs(value(s)) * 5e-7 + np.abs(grad) * 1.001 * U["bf16"] + 1e-38)
+
+
+@pytest.mark.parametrize("sig,yk", [("S0", "bf16"), ("S1", "f32"), ("P", "f32"), ("B", "bf16")])
+@pytest.mark.parametrize("M,K,N", [(20, 300, 20), (70, 40, 90), (300, 33 * 128, 260)])
+def test_matmul_f8_on_32_devices(M, K, N, sig, yk):
+    matmul_case(np.random.default_rng(34), M, K, N, 32, sig, "e4m3", "e5m2", yk)
+
+
+@pytest.mark.parametrize("rows,cols", [(20, 600), (2000, 130)])
+def test_layernorm_on_32_devices(rows, cols):
+    test_layernorm(rows, cols, 32, "S0", "bf16", "e4m3", "f32")
+    test_layernorm_grad(rows, cols, 32, "S0", "e4m3", "bf16", "bf16")
