@@ -235,6 +235,13 @@ __global__ __launch_bounds__(GRAD_NT, TPR == 512 ? 2 : 4) void norm_grad_kernel(
                 dy[v * 8 + e] = w[e];
             }
         }
+        if (!whole) {   // where no element is, mean * rstd may be infinite, and times 0 NaN
+            asm volatile("");   // or it would be chosen from always
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) xhat[v * 8 + e] = (v * TPR + t) * 8 + e < cols ? xhat[v * 8 + e] : 0.0f;
+        }
         fetch(row + step);
         float s1 = 0.0f, s2 = 0.0f;
 #pragma unroll

@@ -1082,3 +1082,24 @@ def test_matmul_f8_on_32_devices(M, K, N, sig, yk):
 def test_layernorm_on_32_devices(rows, cols):
     test_layernorm(rows, cols, 32, "S0", "bf16", "e4m3", "f32")
     test_layernorm_grad(rows, cols, 32, "S0", "e4m3", "bf16", "bf16")
+
+
+@pytest.mark.parametrize("xk,yk", [("f32", "f32"), ("bf16", "bf16")])
+@pytest.mark.parametrize("cols", [5, 100, 129])
+def test_layernorm_grad_of_rows_whose_mean_times_rstd_overflows(cols, xk, yk):
+    """rows of one large value: their elements are at no distance, and what is behind their end counts for nothing"""
+    rng = np.random.default_rng(35)
+    w = store(np.full((4, cols), 2.0 ** 120), xk)
+    dy = store(rng.normal(size=(4, cols)), yk)
+    mean, rstd = Buf(4, 1, np.float32), Buf(4, 1, np.float32)
+    y, dx = Buf(4, cols, np.float32), Buf(4, cols, NP[yk])
+    og, ob = Buf(cols, 1, np.float32), Buf(cols, 1, np.float32)
+    x, room = desc(up([w], xk), 4, cols, xk), torch_mod().zeros(1 << 20, dtype=torch_mod().uint8, device="cuda")
+    sbp.sbp_layernorm(x, sbp.B, None, None, 1e-5, desc([y], 4, cols, "f32"), None, desc([mean], 4, 1, "f32"), desc([rstd], 4, 1, "f32"), 1)
+    sbp.sbp_layernorm_grad(x, None, sbp.B, None, desc([mean], 4, 1, "f32"), desc([rstd], 4, 1, "f32"), desc(up([dy], yk), 4, cols, yk), desc([dx], 4, cols, yk),
+                           desc([og], cols, 1, "f32"), desc([ob], cols, 1, "f32"), room, 1)
+    sync()
+    assert (y.host() == 0).all() and (og.host() == 0).all()
+    d, r = value(dy), float(rstd.host()[0, 0])
+    want = r * (d - d.mean(1, keepdims=True))
+    close(value(dx.host()), want, r * 16 * U["f32"] * (np.abs(d) + np.abs(d).mean(1, keepdims=True)) + np.abs(want) * 1.001 * U[yk], "dx")
