@@ -286,7 +286,8 @@ int32_t sbp_xent_grad(const sbp_tensor_t* logits, sbp_t sbp_l, const sbp_tensor_
  * (the variance over C, computed from the distances to the mean).  x SBP_F32 or SBP_BF16; y under x's
  * signature, in any of the two or in 8 bits (with y_scales, NULL else); gamma, beta [C,1] of one type,
  * SBP_F32 or SBP_BF16, B, or NULL (ones, zeros); mean, rstd [R,1] SBP_F32 under x's signature, or both
- * NULL.  Everything is computed in fp32; y is rounded once.  At most 32 devices and rows of 16384
+ * NULL.  Everything is computed in fp32 (the sum of a row, and of the squares of its distances to the mean,
+ * have to be below 2^128); y is rounded once.  At most 32 devices and rows of 16384
  * elements, and no S(1) (SBP_ERR_UNSUPPORTED); a P tensor is SBP_ERR_SIGNATURE; rows of no elements have no
  * statistics (SBP_ERR_SHAPE where mean and rstd are asked for). */
 int32_t sbp_layernorm(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_tensor_t* gamma, const sbp_tensor_t* beta, float eps,
