@@ -343,8 +343,8 @@ int32_t sbp_gelu_grad(const sbp_tensor_t* a, const sbp_scales_t* a_scales, sbp_t
  *   of the largest one's power of two: an error, for every eight, of less than 2^-10 of the largest |x|
  *   times the largest |w| among them (a subnormal 8-bit number counting as the smallest normal one), next
  *   to the rounding to bf16 of up to 2^-8 of the result.  On random operands it is 2^-17 to 2^-14 of a
- *   result's root mean square; a result far smaller than its products can lose all its bits, as a
- *   sum of products rounded to 12 bits would.  For exact products ask for fp32 results.
+ *   result's root mean square; a result far smaller than its products can lose all its bits.  For exact
+ *   products ask for fp32 results.
  * At most 32 devices, and rows at most 2^23 bytes apart (SBP_ERR_UNSUPPORTED). */
 int32_t sbp_matmul_f8(const sbp_tensor_t* x, const sbp_scales_t* x_scales, sbp_t sbp_x, const sbp_tensor_t* w,
                       const sbp_scales_t* w_scales, sbp_t sbp_w, const sbp_tensor_t* y, sbp_t sbp_y, int32_t k, void* stream,

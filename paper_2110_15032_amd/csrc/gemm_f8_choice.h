@@ -12,7 +12,7 @@ struct F8Choice {
     bool aligned;   // rows of both operands by 16 bytes, of their scales by 4
 };
 
-// The variant whose time the sizes give as the least.  Every one is its rounds over the compute units times a workgroup's time, which goes with the
+// The variant whose time the sizes give as the least.  Every one is its rounds over the compute units (`cu`) times a workgroup's time, which goes with the
 // blocks of 128 of the reduction and, for tiles of waves, with the operand rows that they bring: 16 (MB + NB) of 128 bytes a block.  The coefficients are
 // fits, us, to what the variants measured; where memory or the launch is the bound they are too low for all of them alike.
 // us, M x K x N (devices), bf16 results, (MB, NB) of waves | tiles of 128 | of 256:
@@ -23,7 +23,6 @@ struct F8Choice {
 //   fp32 results, 1024 cubed: (2,2) 8.6  (4,4) 7.5 | 16.2; 2048 cubed: (2,2) 37.7  (4,4) 34.9 | 28.2 | 60.8; 4096 cubed 140 | 112
 // and with rows at odd pitches, through registers:
 //   300 x 8191 x 513: (2,2) 66.1  (4,4) 129 | 105; 1001 cubed: (2,2) 22.0  (4,4) 13.0 | 20.9; 1111 x 1531 x 1777: (2,4) 57.2  (4,4) 39.3 | 28.8
-// cu: compute units
 inline F8Choice choose_f8_tile(const GemmF8Plan& plan, int64_t cu) {
     const bool f32 = plan.out_dtype == SBP_F32;
     int max_m = 0, max_n = 0, max_k = 0;

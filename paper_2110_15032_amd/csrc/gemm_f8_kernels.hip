@@ -160,7 +160,7 @@ __device__ inline void multiply_cut_block(const uint8_t* a, const uint32_t (&a_r
 // and for few tiles.  The waves' sums meet in LDS, in order.
 // Bound by the weights' bytes: 1 x 4096 x 16384 on eight devices (68 MB) 11.9 us, 5.7 TB/s; for some 32 rows and more by the loads of a compute unit.
 // RING: every wave brings its blocks into LDS of its own, DEPTH of them on their way: a load takes whole cache lines of eight rows, where one into
-// registers takes halves of sixteen (choose_tile has both measured), and what is on its way costs no registers.  Nobody else reads it, so there is no
+// registers takes halves of sixteen (choose_f8_tile has both measured), and what is on its way costs no registers.  Nobody else reads it, so there is no
 // barrier before the sums.  Needs rows 16-byte and scales 4-byte aligned; else (any pitch) two sets of registers, U blocks each.
 template <int AT, int BT, bool F32, bool GELU, int MB, int NB, bool RING>
 __global__ __launch_bounds__(256) void gemm_f8_wave_kernel(GemmF8Plan p, int tm, int tn, int order) {
