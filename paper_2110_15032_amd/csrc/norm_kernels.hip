@@ -5,7 +5,7 @@
 //
 // Both are bound by HBM: a row is read once and stays in registers, TPR threads a row with V vectors of eight elements each.  A workgroup
 // walks over rows, so that gamma and beta are read once, and reads the next row before it works on this one.  Measured: 8192 x 4096 on eight devices
-// from bf16 to 8 bits (101 MB) 22.7 us, 4.5 TB/s; the gradient of 16384 x 4096 on eight devices, x in 8 bits (336 MB), 75.5 us, 4.5 TB/s.
+// from bf16 to 8 bits (101 MB) 22.7 us, 4.5 TB/s; the gradient of 16384 x 4096 on eight devices, x in 8 bits (336 MB), 74 us, 4.5 TB/s.
 #include "block8_device.h"
 
 namespace sbp {
