@@ -350,6 +350,26 @@ int32_t sbp_matmul_f8(const sbp_tensor_t* x, const sbp_scales_t* x_scales, sbp_t
                       const sbp_scales_t* w_scales, sbp_t sbp_w, const sbp_tensor_t* y, sbp_t sbp_y, int32_t k, void* stream,
                       int32_t epilogue);
 
+/* The norm of all gradients, and clipping by it.  tensors: n descriptors (a host array, read during the call), sbp their
+ * signatures, each S or B; SBP_F32 or SBP_BF16, any pitch, stored either way (trans).
+ * sbp_square_sum: out [1,1] SBP_F32, P(sum): out_i = the sum of the squares of the elements that device i counts: its slice of
+ *   an S tensor; of a B tensor, which every device has whole, its balanced share of the stored rows.  Squares are added in 64 bits
+ *   in an order that depends on the sizes alone, and the sum is rounded once (a sum of 2^128 or more is infinity).  workspace: device
+ *   memory of sbp_square_sum_workspace() bytes for the same list, 16-byte aligned, whose contents do not matter before or after the call;
+ *   calls that may overlap in time need one each.
+ * sbp_clip: with norm = sqrt(squares), out = in * min(1, max_norm / norm) on every device (each writes its own copy of a B
+ *   tensor), one rounding to out's type, SBP_F32 or SBP_BF16, of fp32 products.  squares [1,1] SBP_F32: sbp_square_sum's P(sum), whose parts
+ *   every device then adds itself in the order of the devices, or B, boxed.  norm [1,1] SBP_F32, B, receives the norm
+ *   (NULL: not wanted).  A norm that is NaN makes all results NaN, an infinite one makes finite values 0.  max_norm >= 0, not NaN.  out's
+ *   shapes, signatures and trans are in's.  A local tensor of out may be that of in itself (the same address, type and pitch): in
+ *   place; any other overlap is SBP_ERR_ALIAS.
+ * An empty list has norm 0.  At most 2^31 - 1 rows and columns of a tensor, and 2^43 elements of a local one (SBP_ERR_UNSUPPORTED). */
+int32_t sbp_square_sum(const sbp_tensor_t* tensors, const sbp_t* sbp, int32_t n, const sbp_tensor_t* out, void* workspace,
+                       int64_t workspace_bytes, int32_t k, void* stream);
+int32_t sbp_square_sum_workspace(const sbp_tensor_t* tensors, const sbp_t* sbp, int32_t n, int32_t k, int64_t* bytes);
+int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* sbp, int32_t n, const sbp_tensor_t* squares, sbp_t sbp_squares, float max_norm,
+                 const sbp_tensor_t* out, const sbp_tensor_t* norm, int32_t k, void* stream);
+
 /* Tuning knobs; they never change what is computed beyond the order of fp32 sums inside a GEMM tile
  * and, for fp32 operands, whether a product is formed by the fp32 instruction or from bf16 terms
  * (45-47 and 49, 50 below): results stay within the error of an fp32 sum.  Unknown knob or value:

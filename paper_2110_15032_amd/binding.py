@@ -34,7 +34,8 @@ KNOB_BOX_REDUCE = 2
 EXPORTS = ("sbp_infer_matmul", "sbp_local_shape", "sbp_matmul", "sbp_matmul_ex", "sbp_matmul_rowmax", "sbp_boxing", "sbp_boxing_across", "sbp_boxing_cast",
            "sbp_infer_matmul_2d", "sbp_local_shape_2d", "sbp_matmul_2d", "sbp_boxing_2d",
            "sbp_row_max", "sbp_row_sumexp", "sbp_xent_loss", "sbp_xent_grad",
-           "sbp_layernorm", "sbp_layernorm_grad", "sbp_layernorm_grad_workspace", "sbp_quantize", "sbp_dequantize", "sbp_gelu_grad", "sbp_matmul_f8", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
+           "sbp_layernorm", "sbp_layernorm_grad", "sbp_layernorm_grad_workspace", "sbp_quantize", "sbp_dequantize", "sbp_gelu_grad", "sbp_matmul_f8",
+           "sbp_square_sum", "sbp_square_sum_workspace", "sbp_clip", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
 
 
 class _CTensor(ctypes.Structure):
@@ -102,6 +103,9 @@ def lib() -> ctypes.CDLL:
         L.sbp_dequantize.argtypes = [T, C, i32, T, i32, vp, i32]
         L.sbp_gelu_grad.argtypes = [T, C, i32, T, T, i32, vp]
         L.sbp_matmul_f8.argtypes = [T, C, i32, T, C, i32, T, i32, i32, vp, i32]
+        L.sbp_square_sum.argtypes = [T, P2, i32, T, vp, i64, i32, vp]
+        L.sbp_square_sum_workspace.argtypes = [T, P2, i32, i32, ctypes.POINTER(i64)]
+        L.sbp_clip.argtypes = [T, P2, i32, T, i32, f32, T, T, i32, vp]
         L.sbp_set_knob.argtypes = [i32, i32]
         L.sbp_probe_mfma.argtypes = [i32, i32, i32, vp, vp]
         L.sbp_probe_mfma_static.argtypes = [i32, i32, i32, vp, vp]
@@ -146,6 +150,19 @@ class SbpScales:
 
     def ref(self):
         return self._ref
+
+
+class SbpList:
+    """Global tensors with their signatures, as sbp_square_sum and sbp_clip take them; keeps them alive."""
+
+    def __init__(self, tensors: Sequence[SbpTensor], sbp: Sequence[int]):
+        self.keep = list(tensors)
+        self.n = len(self.keep)
+        if len(sbp) != self.n:
+            raise ValueError(f"{self.n} tensors and {len(sbp)} signatures")
+        self.k = min((t.k for t in self.keep), default=64)
+        self.c = (_CTensor * max(1, self.n))(*(t.c for t in self.keep))
+        self.sbp = (ctypes.c_int32 * max(1, self.n))(*sbp)
 
 
 def _ref(t):
@@ -339,6 +356,32 @@ def sbp_matmul_f8(x: SbpTensor, x_scales: SbpScales, sbp_x: int, w: SbpTensor, w
     _need(k, x, x_scales, w, w_scales, y)
     _check(lib().sbp_matmul_f8(x.ref(), _ref(x_scales), sbp_x, w.ref(), _ref(w_scales), sbp_w, y.ref(), sbp_y, k, _stream_ptr(stream), epilogue),
            "sbp_matmul_f8")
+
+
+def _room(workspace) -> tuple[ctypes.c_void_p, int]:
+    """Address and bytes of a workspace, a torch tensor or None."""
+    room = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    return ctypes.c_void_p(workspace.data_ptr() if room else 0), room
+
+
+def sbp_square_sum_workspace(tensors: SbpList, k: int) -> int:
+    _need(k, tensors)
+    out = ctypes.c_int64()
+    _check(lib().sbp_square_sum_workspace(tensors.c, tensors.sbp, tensors.n, k, ctypes.byref(out)), "sbp_square_sum_workspace")
+    return out.value
+
+
+def sbp_square_sum(tensors: SbpList, out: SbpTensor, workspace, k: int, stream=None) -> None:
+    """workspace: a device buffer of sbp_square_sum_workspace() bytes (a torch tensor)."""
+    _need(k, tensors, out)
+    _check(lib().sbp_square_sum(tensors.c, tensors.sbp, tensors.n, out.ref(), *_room(workspace), k, _stream_ptr(stream)), "sbp_square_sum")
+
+
+def sbp_clip(inp: SbpList, squares: SbpTensor, sbp_squares: int, max_norm: float, out: SbpList, norm: SbpTensor | None, k: int, stream=None) -> None:
+    _need(k, inp, squares, out, norm)
+    if inp.n != out.n or list(inp.sbp)[:inp.n] != list(out.sbp)[:out.n]:
+        raise ValueError("the lists differ in length or signatures")
+    _check(lib().sbp_clip(inp.c, inp.sbp, inp.n, squares.ref(), sbp_squares, max_norm, out.c, _ref(norm), k, _stream_ptr(stream)), "sbp_clip")
 
 
 def sbp_probe_mfma(mode: int, iters: int, zero_operands: int, scratch, stream=None) -> None:

@@ -257,4 +257,41 @@ struct GemmF8Plan {
 };
 int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream);
 
+// ---------------------------------------------------------------------------------------------
+// Lists of tensors: the sum of their squares, and all of them times a factor.
+// ---------------------------------------------------------------------------------------------
+constexpr int LIST_PARTS = 64;      // local tensors of a launch: the argument blocks stay below 4 KB
+constexpr int LIST_CHUNK = 1024;    // vectors of eight elements that a workgroup takes at a time, of one local tensor
+constexpr int LIST_BLOCKS = 2048;   // workgroups of a launch: eight a compute unit, as many as it holds
+struct ListPart {
+    const void* in;
+    void* out;            // clipping only
+    int64_t cols;         // of a row as it is stored; a dense tensor is one row
+    int32_t rows, ldi, ldo;
+    int32_t types;        // bit 0: in is bf16, bit 1: out is; from bit 2 on: the device
+};
+struct ListPlan {
+    ListPart s[LIST_PARTS];
+    int32_t first[LIST_PARTS];       // a part's first chunk
+    int32_t chunk0[SBP_MAX_K + 1];   // sums of squares: chunks of the devices of this launch, one after the other; clipping: [1] the number of chunks
+    int32_t slot[SBP_MAX_K];         // where such a device's partial sums go, in units of the workgroups it has
+    double* partial;
+    int32_t parts;
+};
+struct SquareJoin {
+    const double* partial;
+    int64_t per_device;
+    int32_t count[SBP_MAX_K];
+    float* out[SBP_MAX_K];
+};
+struct ClipSum {
+    const float* sum[SBP_MAX_K];
+    float* norm[SBP_MAX_K];   // null: not wanted
+    float most;
+    int32_t k, partial;       // partial: the sums are P(sum)
+};
+int32_t launch_square_sum(const ListPlan& plan, int devices, int blocks, hipStream_t stream);
+int32_t launch_square_join(const SquareJoin& join, int32_t k, hipStream_t stream);
+int32_t launch_clip(const ListPlan& plan, const ClipSum& sums, hipStream_t stream);
+
 }  // namespace sbp
