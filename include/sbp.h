@@ -350,6 +350,50 @@ int32_t sbp_matmul_f8(const sbp_tensor_t* x, const sbp_scales_t* x_scales, sbp_t
                       const sbp_scales_t* w_scales, sbp_t sbp_w, const sbp_tensor_t* y, sbp_t sbp_y, int32_t k, void* stream,
                       int32_t epilogue);
 
+/* What stands between two blocks, over the rows of x [R,C], S(0) or B, on the devices that hold them: the norm behind a block, its
+ * gate, the residual, and the norm in front of the next block:
+ *   t = post(x) (post NULL: x),  h = alpha * r + gate * t,  y = pre(h) (pre NULL: none, and y NULL)
+ * A norm is (v - mean) * rstd * gamma + beta with the row's mean (SBP_NORM_RMS: 0, no beta, no mean) and rstd = 1 / sqrt(sum((v - mean)^2)
+ * / C + eps).  x and the residual stream (r, h, one type) SBP_F32 or SBP_BF16; y in any of the two or in 8 bits (with
+ * y_scales, NULL else); all under x's signature.  gate [C,1], B, or NULL (ones); gate and the norms' gamma and beta are of
+ * one type, SBP_F32 or SBP_BF16.  Everything is computed in fp32 (the sums of a row's elements and of their squares have to be below 2^128),
+ * y and the second norm's statistics from h before its rounding; h and y are rounded once.  At most 32 devices and rows of 16384
+ * elements, and no S(1) (SBP_ERR_UNSUPPORTED); a P tensor is SBP_ERR_SIGNATURE; rows of no elements have no statistics
+ * (SBP_ERR_SHAPE where they are asked for). */
+enum {
+    SBP_NORM_LAYER = 0,
+    SBP_NORM_RMS = 1
+};
+typedef struct sbp_norm {
+    int32_t kind;                /* SBP_NORM_*                                                                   */
+    float eps;                   /* >= 0                                                                         */
+    const sbp_tensor_t* gamma;   /* [C,1], B, or NULL: ones                                                      */
+    const sbp_tensor_t* beta;    /* [C,1], B, or NULL: zeros; layer only                                         */
+    const sbp_tensor_t* mean;    /* [R,1] SBP_F32 under x's signature, layer only: written by the forward call   */
+    const sbp_tensor_t* rstd;    /* (layer: both or neither), read by the gradient                               */
+    const sbp_tensor_t* dgamma;  /* gradient only: [C,1] SBP_F32 or NULL                                         */
+    const sbp_tensor_t* dbeta;   /* gradient only, layer only: the same                                          */
+} sbp_norm_t;
+int32_t sbp_residual_norm(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_norm_t* post, const sbp_tensor_t* gate,
+                          const sbp_tensor_t* r, float alpha, const sbp_tensor_t* h, const sbp_norm_t* pre,
+                          const sbp_tensor_t* y, const sbp_scales_t* y_scales, int32_t k, void* stream);
+
+/* Its gradient, from x, the h that was stored, and the statistics that were: with dh the gradient of h by the residual stream (NULL: none, where
+ * there is pre), dy that of y (with pre, and only then, as h), hhat = (h - mean2) * rstd2, g = dy * gamma2,
+ *   d = dh + rstd2 * (g - sum(g) / C - hhat * sum(g * hhat) / C)      (RMS: without sum(g) / C)
+ *   dr = alpha * d                                         the residual stream's type, which h and dh have
+ *   dx = post's gradient of gate * d, likewise             x's type
+ *   dgate = sum over the device's rows of d * t, dgamma and dbeta of both norms those of their outputs' gradients   [C,1] SBP_F32
+ * The sums hold a whole vector on every device: P(sum) for x S(0), B for x B; any of them may be NULL.  They are made in fp32 in an order
+ * that depends on the sizes alone.  workspace: device memory of sbp_residual_norm_grad_workspace() bytes, 16-byte aligned, whose contents do
+ * not matter before or after the call (NULL where none of the sums is wanted or that is 0; SBP_ERR_SHAPE if workspace_bytes is too little).
+ * Calls that may overlap in time need one each.  Of both norms eps is not looked at beyond its range. */
+int32_t sbp_residual_norm_grad(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_norm_t* post, const sbp_tensor_t* gate,
+                               float alpha, const sbp_tensor_t* h, const sbp_norm_t* pre, const sbp_tensor_t* dh,
+                               const sbp_tensor_t* dy, const sbp_tensor_t* dx, const sbp_tensor_t* dr,
+                               const sbp_tensor_t* dgate, void* workspace, int64_t workspace_bytes, int32_t k, void* stream);
+int32_t sbp_residual_norm_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_x, int32_t k, int64_t* bytes);
+
 /* The norm of all gradients, and clipping by it.  tensors: n descriptors (a host array, read during the call), sbp their
  * signatures, each S or B; SBP_F32 or SBP_BF16, any pitch, stored either way (trans).
  * sbp_square_sum: out [1,1] SBP_F32, P(sum): out_i = the sum of the squares of the elements that device i counts: its slice of

@@ -25,6 +25,9 @@ F8E5M2 = 4
 # epilogues
 EPI_NONE = 0
 EPI_GELU = 1
+# norms
+NORM_LAYER = 0
+NORM_RMS = 1
 # knobs
 KNOB_GEMM_VARIANT = 0
 KNOB_TILE_ORDER = 1
@@ -35,7 +38,7 @@ EXPORTS = ("sbp_infer_matmul", "sbp_local_shape", "sbp_matmul", "sbp_matmul_ex",
            "sbp_infer_matmul_2d", "sbp_local_shape_2d", "sbp_matmul_2d", "sbp_boxing_2d",
            "sbp_row_max", "sbp_row_sumexp", "sbp_xent_loss", "sbp_xent_grad",
            "sbp_layernorm", "sbp_layernorm_grad", "sbp_layernorm_grad_workspace", "sbp_quantize", "sbp_dequantize", "sbp_gelu_grad", "sbp_matmul_f8",
-           "sbp_square_sum", "sbp_square_sum_workspace", "sbp_clip", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
+           "sbp_residual_norm", "sbp_residual_norm_grad", "sbp_residual_norm_grad_workspace", "sbp_square_sum", "sbp_square_sum_workspace", "sbp_clip", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
 
 
 class _CTensor(ctypes.Structure):
@@ -46,6 +49,10 @@ class _CTensor(ctypes.Structure):
 
 class _CScales(ctypes.Structure):
     _fields_ = [("shard", ctypes.POINTER(ctypes.c_void_p)), ("ld", ctypes.c_int64)]
+
+
+class _CNorm(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int32), ("eps", ctypes.c_float)] + [(n, ctypes.POINTER(_CTensor)) for n in ("gamma", "beta", "mean", "rstd", "dgamma", "dbeta")]
 
 
 class SbpError(RuntimeError):
@@ -103,6 +110,10 @@ def lib() -> ctypes.CDLL:
         L.sbp_dequantize.argtypes = [T, C, i32, T, i32, vp, i32]
         L.sbp_gelu_grad.argtypes = [T, C, i32, T, T, i32, vp]
         L.sbp_matmul_f8.argtypes = [T, C, i32, T, C, i32, T, i32, i32, vp, i32]
+        N = ctypes.POINTER(_CNorm)
+        L.sbp_residual_norm.argtypes = [T, i32, N, T, T, f32, T, N, T, C, i32, vp]
+        L.sbp_residual_norm_grad.argtypes = [T, i32, N, T, f32, T, N, T, T, T, T, T, vp, i64, i32, vp]
+        L.sbp_residual_norm_grad_workspace.argtypes = [i64, i64, i32, i32, ctypes.POINTER(i64)]
         L.sbp_square_sum.argtypes = [T, P2, i32, T, vp, i64, i32, vp]
         L.sbp_square_sum_workspace.argtypes = [T, P2, i32, i32, ctypes.POINTER(i64)]
         L.sbp_clip.argtypes = [T, P2, i32, T, i32, f32, T, T, i32, vp]
@@ -146,6 +157,20 @@ class SbpScales:
         self.k = len(ptrs)
         self._arr = (ctypes.c_void_p * max(1, self.k))(*ptrs)
         self.c = _CScales(ctypes.cast(self._arr, ctypes.POINTER(ctypes.c_void_p)), ld)
+        self._ref = ctypes.byref(self.c)
+
+    def ref(self):
+        return self._ref
+
+
+class SbpNorm:
+    """A norm over rows: NORM_LAYER or NORM_RMS, its weights, statistics and, for the gradient, its weights' gradients; keeps them alive."""
+
+    def __init__(self, kind: int, eps: float, gamma: SbpTensor | None = None, beta: SbpTensor | None = None, mean: SbpTensor | None = None, rstd: SbpTensor | None = None,
+                 dgamma: SbpTensor | None = None, dbeta: SbpTensor | None = None):
+        self.keep = [gamma, beta, mean, rstd, dgamma, dbeta]
+        self.k = min((t.k for t in self.keep if t is not None), default=64)
+        self.c = _CNorm(kind, eps, *(None if t is None else ctypes.pointer(t.c) for t in self.keep))
         self._ref = ctypes.byref(self.c)
 
     def ref(self):
@@ -362,6 +387,27 @@ def _room(workspace) -> tuple[ctypes.c_void_p, int]:
     """Address and bytes of a workspace, a torch tensor or None."""
     room = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return ctypes.c_void_p(workspace.data_ptr() if room else 0), room
+
+
+def sbp_residual_norm(x: SbpTensor, sbp_x: int, post: SbpNorm | None, gate: SbpTensor | None, r: SbpTensor, alpha: float, h: SbpTensor, pre: SbpNorm | None,
+                      y: SbpTensor | None, y_scales: SbpScales | None, k: int, stream=None) -> None:
+    _need(k, x, post, gate, r, h, pre, y, y_scales)
+    _check(lib().sbp_residual_norm(x.ref(), sbp_x, _ref(post), _ref(gate), r.ref(), alpha, h.ref(), _ref(pre), _ref(y), _ref(y_scales), k, _stream_ptr(stream)),
+           "sbp_residual_norm")
+
+
+def sbp_residual_norm_grad_workspace(rows: int, cols: int, sbp_x: int, k: int) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sbp_residual_norm_grad_workspace(rows, cols, sbp_x, k, ctypes.byref(out)), "sbp_residual_norm_grad_workspace")
+    return out.value
+
+
+def sbp_residual_norm_grad(x: SbpTensor, sbp_x: int, post: SbpNorm | None, gate: SbpTensor | None, alpha: float, h: SbpTensor | None, pre: SbpNorm | None,
+                           dh: SbpTensor | None, dy: SbpTensor | None, dx: SbpTensor, dr: SbpTensor, dgate: SbpTensor | None, workspace, k: int, stream=None) -> None:
+    """workspace: a device buffer of sbp_residual_norm_grad_workspace() bytes (a torch tensor), or None where no weight's gradient is wanted."""
+    _need(k, x, post, gate, h, pre, dh, dy, dx, dr, dgate)
+    _check(lib().sbp_residual_norm_grad(x.ref(), sbp_x, _ref(post), _ref(gate), alpha, _ref(h), _ref(pre), _ref(dh), _ref(dy), dx.ref(), dr.ref(), _ref(dgate), *_room(workspace), k,
+                                        _stream_ptr(stream)), "sbp_residual_norm_grad")
 
 
 def sbp_square_sum_workspace(tensors: SbpList, k: int) -> int:

@@ -1,0 +1,337 @@
+// The gradient of what stands between two blocks (residual_norm_kernels.hip).  With hhat = (h - mean2) rstd2, xhat = (x - mean1) rstd1,
+//
+//   d = dh + rstd2 (g - sum g / n - hhat sum (g hhat) / n),  g = dy gamma2          (RMS: without sum g)
+//   dr = alpha d,  e = gate gamma1 d,  dx = rstd1 (e - sum e / n - xhat sum (e xhat) / n)
+//   A = sum over rows d xhat,  B = sum d,  C = sum dy hhat,  D = sum dy:
+//   dgate = gamma1 A + beta1 B,  dgamma1 = gate A,  dbeta1 = gate B,  dgamma2 = C,  dbeta2 = D
+//
+// so that five weights' gradients need four sums a column.  Without the first norm xhat is x, gamma1 1 and beta1 0.  Bound by HBM: the four inputs
+// of a row are read once.  Sums over rows stay in a workgroup's registers (rows of more than 8192: half of them in LDS), its partial sums go to the caller's workspace
+// and are joined in order.
+#include "row_device.h"
+
+namespace sbp {
+namespace {
+
+template <int XT, int RT, int YT, int TPR, int V, int S>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kernel(ResNormGradPlan<S> p) {
+    constexpr int NT = TPR < 256 ? 256 : TPR, G = NT / TPR, NW = TPR / 64, N = V * 8, CAP = TPR * V * 8;
+    constexpr bool KEEP = V == 1;   // weights and two of the sums stay in registers
+    const ResNormGradShard& s = p.s[S > 1 ? blockIdx.y : 0];
+    if ((int)blockIdx.x >= s.blocks) return;
+    const int t = threadIdx.x % TPR, group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0, cols = p.cols;   // whole waves
+    const bool post = p.flags & RN_POST, pre = p.flags & RN_PRE, with_dh = p.flags & RN_DH, narrow_weights = p.flags & RN_BF16_WEIGHTS;
+    __shared__ float2 part[2][2][G][NW];
+    __shared__ float sums[KEEP ? (G > 1 ? G * 4 * CAP : 4) : 2 * CAP];   // KEEP: the groups' sums at the end; else C and D
+    const RowPart<TPR, V> part_of_row(t, cols);
+    float gamma2[N], through[N];   // through: gate gamma1
+    auto load1 = [&]() {
+        load_column<V, TPR>(s.gate, narrow_weights, t, cols, 1.0f, through);
+        if (post) {
+            float w[N];
+            load_column<V, TPR>(s.gamma1, narrow_weights, t, cols, 1.0f, w);
+#pragma unroll
+            for (int i = 0; i < N; ++i) through[i] *= w[i];
+        }
+    };
+    auto load2 = [&]() {
+        if (pre) load_column<V, TPR>(s.gamma2, narrow_weights, t, cols, 1.0f, gamma2);
+    };
+    if constexpr (KEEP) {
+        load1();
+        load2();
+    }
+    float sum_a[N], sum_b[N], sum_c[KEEP ? N : 1], sum_d[KEEP ? N : 1];
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum_a[i] = sum_b[i] = 0.0f;
+    if constexpr (KEEP) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sum_c[i] = sum_d[i] = 0.0f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < N; ++i) sums[i * TPR + t] = sums[CAP + i * TPR + t] = 0.0f;   // a thread's own places
+    }
+
+    const int step = s.blocks * G;
+    Raw8<XT> next_x[V];
+    Raw8<RT> next_h[V], next_dh[V];
+    Raw8<YT> next_dy[V];
+    float next_mean1 = 0.0f, next_rstd1 = 1.0f, next_mean2 = 0.0f, next_rstd2 = 0.0f;
+    auto fetch = [&](int64_t row) {
+        const bool there = row < s.rows;
+        const int upto = there ? cols : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int c = (v * TPR + t) * 8;
+            next_x[v] = load8<XT>(static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>, c, upto);
+            next_h[v] = load8<RT>(static_cast<const char*>(s.h) + row * s.ldh * bytes_of<RT>, c, pre ? upto : 0);
+            next_dy[v] = load8<YT>(static_cast<const char*>(s.dy) + row * s.lddy * bytes_of<YT>, c, pre ? upto : 0);
+            next_dh[v] = load8<RT>(static_cast<const char*>(s.dh) + row * s.lddh * bytes_of<RT>, c, with_dh ? upto : 0);
+        }
+        if (there && post) {
+            next_mean1 = s.mean1 ? s.mean1[row] : 0.0f;
+            next_rstd1 = s.rstd1[row];
+        }
+        if (there && pre) {
+            next_mean2 = s.mean2 ? s.mean2[row] : 0.0f;
+            next_rstd2 = s.rstd2[row];
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * G + group;
+    if constexpr (KEEP) fetch(row);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * G; first < s.rows; first += step, row += step, turn ^= 1) {
+        if constexpr (!KEEP) fetch(row);
+        const int there = row < s.rows ? cols : 0;
+        const float mean1 = next_mean1, rstd1 = next_rstd1, mean2 = next_mean2, rstd2 = next_rstd2;
+        float xhat[N], d[N], hhat[N], dy[N];
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float u[8], w[8], z[8], q[8];
+            const int c = (v * TPR + t) * 8;
+            const bool whole = part_of_row.whole;
+            widen<XT>(whole ? next_x[v] : settle8<XT>(next_x[v], c, there), 1.0f, u);
+            widen<RT>(whole ? next_dh[v] : settle8<RT>(next_dh[v], c, with_dh ? there : 0), 1.0f, w);
+            widen<RT>(whole ? next_h[v] : settle8<RT>(next_h[v], c, pre ? there : 0), 1.0f, z);
+            widen<YT>(whole ? next_dy[v] : settle8<YT>(next_dy[v], c, pre ? there : 0), 1.0f, q);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                xhat[v * 8 + e] = post ? (u[e] - mean1) * rstd1 : u[e];
+                d[v * 8 + e] = w[e];
+                hhat[v * 8 + e] = (z[e] - mean2) * rstd2;
+                dy[v * 8 + e] = q[e];
+            }
+        }
+        if (!part_of_row.whole || row >= s.rows) {   // where no element is, mean * rstd may be infinite, and times 0 NaN
+            asm volatile("");   // or it would be chosen from always
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const bool is = (v * TPR + t) * 8 + e < there;
+                    xhat[v * 8 + e] = is ? xhat[v * 8 + e] : 0.0f;
+                    hhat[v * 8 + e] = is ? hhat[v * 8 + e] : 0.0f;
+                }
+        }
+        if constexpr (KEEP) fetch(row + step);
+        if (pre) {
+            if constexpr (!KEEP) load2();
+            float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float g = dy[i] * gamma2[i];
+                s1 += g;
+                s2 = fmaf(g, hhat[i], s2);
+                if constexpr (KEEP) {
+                    sum_c[i] = fmaf(dy[i], hhat[i], sum_c[i]);
+                    sum_d[i] += dy[i];
+                } else {
+                    sums[i * TPR + t] = fmaf(dy[i], hhat[i], sums[i * TPR + t]);
+                    sums[CAP + i * TPR + t] += dy[i];
+                }
+            }
+            part_of_row.sums(s1, s2, part[turn][0][group]);
+            s1 = p.flags & RN_PRE_LAYER ? s1 * part_of_row.over : 0.0f;
+            s2 *= part_of_row.over;
+#pragma unroll
+            for (int i = 0; i < N; ++i) d[i] = fmaf(rstd2, fmaf(dy[i], gamma2[i], -s1) - hhat[i] * s2, d[i]);
+            if (!part_of_row.whole || row >= s.rows) {   // s1 is behind the row's end too
+                asm volatile("");
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) d[v * 8 + e] = (v * TPR + t) * 8 + e < there ? d[v * 8 + e] : 0.0f;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            sum_a[i] = fmaf(d[i], xhat[i], sum_a[i]);
+            sum_b[i] += d[i];
+        }
+        if (row < s.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = p.alpha * d[v * 8 + e];
+                store8<RT>(static_cast<char*>(s.dr) + (row * s.lddr + c) * bytes_of<RT>, narrow<RT>(u), cols - c, p.flags & RN_STREAM_H);
+            }
+        }
+        if constexpr (!KEEP) load1();
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] *= through[i];
+        if (post) {
+            float s1 = 0.0f, s2 = 0.0f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                s1 += d[i];
+                s2 = fmaf(d[i], xhat[i], s2);
+            }
+            part_of_row.sums(s1, s2, part[turn][1][group]);
+            s1 = p.flags & RN_POST_LAYER ? s1 * part_of_row.over : 0.0f;
+            s2 *= part_of_row.over;
+#pragma unroll
+            for (int i = 0; i < N; ++i) d[i] = rstd1 * ((d[i] - s1) - xhat[i] * s2);
+        }
+        if (row < s.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = d[v * 8 + e];
+                store8<XT>(static_cast<char*>(s.dx) + (row * s.lddx + c) * bytes_of<XT>, narrow<XT>(u), cols - c, p.flags & RN_STREAM_Y);
+            }
+        }
+    }
+    if (!s.part) return;
+    float* const to = s.part + (int64_t)blockIdx.x * 4 * cols;
+    auto put = [&](int which, const float (&v)[N]) {
+#pragma unroll
+        for (int i = 0; i < V; ++i) {
+            const int c = (i * TPR + t) * 8;
+            Raw8<T_F32> a;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                a.a[e] = v[i * 8 + e];
+                a.b[e] = v[i * 8 + 4 + e];
+            }
+            store8<T_F32>(to + (int64_t)which * cols + c, a, cols - c);
+        }
+    };
+    if constexpr (G > 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {   // V is 1
+            float* const at = sums + group * 4 * CAP + t * 8 + i;
+            at[0] = sum_a[i];
+            at[CAP] = sum_b[i];
+            at[2 * CAP] = sum_c[i];
+            at[3 * CAP] = sum_d[i];
+        }
+        __syncthreads();
+        for (int c = threadIdx.x; c < cols; c += NT)
+#pragma unroll
+            for (int which = 0; which < 4; ++which) {
+                float a = 0.0f;
+#pragma unroll
+                for (int g = 0; g < G; ++g) a += sums[(g * 4 + which) * CAP + c];
+                to[(int64_t)which * cols + c] = a;
+            }
+    } else {
+        put(0, sum_a);
+        put(1, sum_b);
+        if constexpr (KEEP) {
+            put(2, sum_c);
+            put(3, sum_d);
+        } else {
+#pragma unroll
+            for (int which = 0; which < 2; ++which) {
+                float v[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) v[i] = sums[which * CAP + i * TPR + t];
+                put(2 + which, v);
+            }
+        }
+    }
+}
+
+// The workgroups' partial sums in order, and the weights' gradients from them: 32 columns a workgroup, eight runs of partial sums side by side.
+template <int S>
+__global__ __launch_bounds__(256) void residual_norm_join_kernel(ResNormJoin<S> p) {
+    const ResNormJoinShard& s = p.s[S > 1 ? blockIdx.y : 0];
+    __shared__ float sums[4][8][33];
+    const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
+    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (c < p.cols) {
+        for (int b = run; b < s.blocks; b += 16) {   // two on their way, past the end the last one again, which does not count
+            float v[2][4];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int which = 0; which < 4; ++which) v[u][which] = s.part[((int64_t)min(b + 8 * u, s.blocks - 1) * 4 + which) * p.cols + c];
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int which = 0; which < 4; ++which) a[which] += b + 8 * u < s.blocks ? v[u][which] : 0.0f;
+        }
+    }
+#pragma unroll
+    for (int which = 0; which < 4; ++which) sums[which][run][lane] = a[which];
+    __syncthreads();
+    if (run != 0 || c >= p.cols) return;
+#pragma unroll
+    for (int which = 0; which < 4; ++which) {
+        a[which] = 0.0f;
+#pragma unroll
+        for (int r = 0; r < 8; ++r) a[which] += sums[which][r][lane];
+    }
+    auto weight = [&](const void* w, float otherwise) {
+        return !w ? otherwise : p.flags & RN_BF16_WEIGHTS ? bf16_to_f32(static_cast<const uint16_t*>(w)[c]) : static_cast<const float*>(w)[c];
+    };
+    const float gate = weight(s.gate, 1.0f);
+    if (s.dgate) s.dgate[c] = p.flags & RN_POST ? fmaf(weight(s.gamma1, 1.0f), a[0], weight(s.beta1, 0.0f) * a[1]) : a[0];
+    if (s.dgamma1) s.dgamma1[c] = gate * a[0];
+    if (s.dbeta1) s.dbeta1[c] = gate * a[1];
+    if (s.dgamma2) s.dgamma2[c] = a[2];
+    if (s.dbeta2) s.dbeta2[c] = a[3];
+}
+
+// threads of a row
+int threads_of(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : cols <= 2048 ? 256 : cols <= 4096 ? 512 : 1024; }
+
+}  // namespace
+
+int32_t residual_norm_grad_blocks(int64_t rows, int64_t cols, int32_t k) {
+    const int64_t g = std::max(1, 256 / threads_of(cols)), most = 256;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + g - 1) / g, most / k));
+}
+
+template <int S>
+int32_t launch_residual_norm_grad(const ResNormGradPlan<S>& given, int n, int32_t x_type, int32_t r_type, int32_t y_type, hipStream_t stream) {
+    ResNormGradPlan<S> plan = given;
+    int blocks = 1;
+    int64_t all = 0;
+    bool r_lines = true, x_lines = true;
+    for (int i = 0; i < n; ++i) {
+        blocks = std::max(blocks, plan.s[i].blocks);
+        all += plan.s[i].rows;
+        if ((int64_t)plan.s[i].lddr * bytes_of_type(r_type) % 128 || reinterpret_cast<uintptr_t>(plan.s[i].dr) % 128) r_lines = false;
+        if ((int64_t)plan.s[i].lddx * bytes_of_type(x_type) % 128 || reinterpret_cast<uintptr_t>(plan.s[i].dx) % 128) x_lines = false;
+    }
+    const int64_t elements = all * plan.cols;
+    if (streams_of(0, elements * bytes_of_type(r_type), r_lines, r_type) & STREAM_OUT) plan.flags |= RN_STREAM_H;
+    if (streams_of(0, elements * bytes_of_type(x_type), x_lines, x_type) & STREAM_OUT) plan.flags |= RN_STREAM_Y;
+    with_wide_type(x_type, [&](auto x) {
+        with_wide_type(r_type, [&](auto r) {
+            with_wide_type(y_type, [&](auto y) {
+                auto go = [&](auto tpr, auto v) {
+                    hipLaunchKernelGGL((residual_norm_grad_kernel<x(), r(), y(), tpr(), v(), S>), dim3((uint32_t)blocks, (uint32_t)n), dim3(tpr() < 256 ? 256 : tpr()), 0, stream, plan);
+                };
+                using std::integral_constant;
+                switch (threads_of(plan.cols)) {
+                    case 64: go(integral_constant<int, 64>{}, integral_constant<int, 1>{}); break;
+                    case 128: go(integral_constant<int, 128>{}, integral_constant<int, 1>{}); break;
+                    case 256: go(integral_constant<int, 256>{}, integral_constant<int, 1>{}); break;
+                    case 512: go(integral_constant<int, 512>{}, integral_constant<int, 1>{}); break;
+                    default:
+                        if (plan.cols <= 8192) go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+                        else go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+                }
+            });
+        });
+    });
+    return launch_status(__func__);
+}
+
+template <int S>
+int32_t launch_residual_norm_join(const ResNormJoin<S>& join, int n, hipStream_t stream) {
+    hipLaunchKernelGGL(residual_norm_join_kernel<S>, dim3((uint32_t)((join.cols + 31) / 32), (uint32_t)n), dim3(256), 0, stream, join);
+    return launch_status(__func__);
+}
+template int32_t launch_residual_norm_grad<1>(const ResNormGradPlan<1>&, int, int32_t, int32_t, int32_t, hipStream_t);
+template int32_t launch_residual_norm_grad<RESNORM_SHARDS>(const ResNormGradPlan<RESNORM_SHARDS>&, int, int32_t, int32_t, int32_t, hipStream_t);
+template int32_t launch_residual_norm_join<1>(const ResNormJoin<1>&, int, hipStream_t);
+template int32_t launch_residual_norm_join<RESNORM_SHARDS>(const ResNormJoin<RESNORM_SHARDS>&, int, hipStream_t);
+
+}  // namespace sbp

@@ -1,0 +1,188 @@
+// What stands between two blocks: the norm behind a block, its gate, the residual, and the norm in front of the next block.
+//
+//   t = norm1(x),  h = alpha r + gate t,  y = norm2(h)
+//   norm(v) = (v - mean) rstd gamma + beta,  mean = sum v / n (RMS: 0),  rstd = 1 / sqrt(sum (v - mean)^2 / n + eps)
+//
+// Bound by HBM: a row of x and r is read once and stays in registers until h and y are written, TPR threads a row with V vectors of eight
+// elements each.  y is computed from h before its rounding.
+#include "row_device.h"
+
+namespace sbp {
+namespace {
+
+// Workgroups of 256 threads of a launch
+constexpr int NORM_BLOCKS = 1024;
+
+template <int XT, int RT, int YT, int TPR, int V, int S>
+__global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(ResNormPlan<S> p) {
+    constexpr int NT = TPR < 256 ? 256 : TPR, G = NT / TPR, NW = TPR / 64, N = V * 8;
+    constexpr bool KEEP = V == 1;   // weights stay in registers; else they are read again for every row, from the caches
+    const ResNormShard& s = p.s[S > 1 ? blockIdx.y : 0];
+    const int t = threadIdx.x % TPR, group = G > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / TPR) : 0, cols = p.cols;   // whole waves
+    const bool post = p.flags & RN_POST, pre = p.flags & RN_PRE, narrow_weights = p.flags & RN_BF16_WEIGHTS;
+    __shared__ float2 part[2][2][G][NW];
+    const RowPart<TPR, V> part_of_row(t, cols);
+    float gate[N], gamma1[N], beta1[N], gamma2[N], beta2[N];
+    auto load1 = [&]() {
+        load_column<V, TPR>(s.gate, narrow_weights, t, cols, 1.0f, gate);
+        if (post) {
+            load_column<V, TPR>(s.gamma1, narrow_weights, t, cols, 1.0f, gamma1);
+            load_column<V, TPR>(s.beta1, narrow_weights, t, cols, 0.0f, beta1);
+        }
+    };
+    auto load2 = [&]() {
+        if (pre) {
+            load_column<V, TPR>(s.gamma2, narrow_weights, t, cols, 1.0f, gamma2);
+            load_column<V, TPR>(s.beta2, narrow_weights, t, cols, 0.0f, beta2);
+        }
+    };
+    if constexpr (KEEP) {
+        load1();
+        load2();
+    }
+
+    const int step = gridDim.x * G;
+    Raw8<XT> next_x[V];
+    Raw8<RT> next_r[V];
+    auto fetch = [&](int64_t row) {
+        const char* const from_x = static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>;
+        const char* const from_r = static_cast<const char*>(s.r) + row * s.ldr * bytes_of<RT>;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            next_x[v] = load8<XT>(from_x, (v * TPR + t) * 8, row < s.rows ? cols : 0);
+            next_r[v] = load8<RT>(from_r, (v * TPR + t) * 8, row < s.rows ? cols : 0);
+        }
+    };
+    int64_t row = (int64_t)blockIdx.x * G + group;
+    fetch(row);
+    int turn = 0;
+    for (int64_t first = (int64_t)blockIdx.x * G; first < s.rows; first += step, row += step, turn ^= 1) {
+        float x[N], h[N];
+        const int there = row < s.rows ? cols : 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            float u[8], w[8];
+            const int c = (v * TPR + t) * 8;
+            widen<XT>(part_of_row.whole ? next_x[v] : settle8<XT>(next_x[v], c, there), 1.0f, u);
+            widen<RT>(part_of_row.whole ? next_r[v] : settle8<RT>(next_r[v], c, there), 1.0f, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                x[v * 8 + e] = u[e];
+                h[v * 8 + e] = p.alpha * w[e];
+            }
+        }
+        fetch(row + step);
+        if constexpr (!KEEP) load1();
+        if (post) {
+            float mean, m2;
+            part_of_row.spread(x, p.flags & RN_POST_LAYER, part[turn][0][group], mean, m2);
+            const float rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps1));
+            if (t == 0 && row < s.rows) {
+                if (s.mean1) s.mean1[row] = mean;
+                if (s.rstd1) s.rstd1[row] = rstd;
+            }
+#pragma unroll
+            for (int i = 0; i < N; ++i) x[i] = fmaf((x[i] - mean) * rstd, gamma1[i], beta1[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) h[i] = fmaf(gate[i], x[i], h[i]);
+        if (row < s.rows) {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                float u[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] = h[v * 8 + e];
+                store8<RT>(static_cast<char*>(s.h) + (row * s.ldh + c) * bytes_of<RT>, narrow<RT>(u), cols - c, p.flags & RN_STREAM_H);
+            }
+        }
+        if (!pre) continue;
+        if constexpr (!KEEP) load2();
+        if (!part_of_row.whole) {   // behind the row's end gate is 0, but x need not be finite there times it
+            asm volatile("");
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) h[v * 8 + e] = (v * TPR + t) * 8 + e < cols ? h[v * 8 + e] : 0.0f;
+        }
+        float mean, m2;
+        part_of_row.spread(h, p.flags & RN_PRE_LAYER, part[turn][1][group], mean, m2);
+        const float rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps2));
+        if (row >= s.rows) continue;
+        if (t == 0) {
+            if (s.mean2) s.mean2[row] = mean;
+            if (s.rstd2) s.rstd2[row] = rstd;
+        }
+        float y[V][8];
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) y[v][e] = fmaf((h[v * 8 + e] - mean) * rstd, gamma2[v * 8 + e], beta2[v * 8 + e]);
+        char* const to = static_cast<char*>(s.y) + row * s.ldy * bytes_of<YT>;
+        if constexpr (bytes_of<YT> == 1) {
+            if (!part_of_row.whole) {   // a block's largest magnitude is of elements alone
+                asm volatile("");
+#pragma unroll
+                for (int v = 0; v < V; ++v)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) y[v][e] = (v * TPR + t) * 8 + e < cols ? y[v][e] : 0.0f;
+            }
+            Raw8<YT> q[V];
+            uint32_t byte[V];
+            narrow_blocks<true, YT>(y, q, byte);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                store8<YT>(to + c, q[v], cols - c, p.flags & RN_STREAM_Y);
+                if ((t & 15) == 0 && c < cols) static_cast<uint8_t*>(s.y_scales)[row * s.lds + c / F8_BLOCK] = (uint8_t)byte[v];
+            }
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int c = (v * TPR + t) * 8;
+                store8<YT>(to + c * bytes_of<YT>, narrow<YT>(y[v]), cols - c, p.flags & RN_STREAM_Y);
+            }
+        }
+    }
+}
+
+}  // namespace
+
+template <int S>
+int32_t launch_residual_norm(const ResNormPlan<S>& given, int n, int32_t x_type, int32_t r_type, int32_t y_type, hipStream_t stream) {
+    ResNormPlan<S> plan = given;
+    int64_t rows = 0, all = 0;
+    bool h_lines = true, y_lines = true;
+    for (int i = 0; i < n; ++i) {
+        rows = std::max<int64_t>(rows, plan.s[i].rows);
+        all += plan.s[i].rows;
+        if ((int64_t)plan.s[i].ldh * bytes_of_type(r_type) % 128 || reinterpret_cast<uintptr_t>(plan.s[i].h) % 128) h_lines = false;
+        if ((int64_t)plan.s[i].ldy * bytes_of_type(y_type) % 128 || reinterpret_cast<uintptr_t>(plan.s[i].y) % 128) y_lines = false;
+    }
+    const int64_t elements = all * plan.cols;
+    if (streams_of(0, elements * bytes_of_type(r_type), h_lines, r_type) & STREAM_OUT) plan.flags |= RN_STREAM_H;
+    if (streams_of(0, elements * bytes_of_type(y_type), y_lines, y_type) & STREAM_OUT) plan.flags |= RN_STREAM_Y;
+    with_wide_type(x_type, [&](auto x) {
+        with_wide_type(r_type, [&](auto r) {
+            with_any_type(y_type, [&](auto y) {
+                auto go = [&](auto tpr, auto v) {
+                    constexpr int NT = tpr() < 256 ? 256 : tpr(), G = NT / tpr();
+                    const int64_t bx = std::max<int64_t>(1, std::min<int64_t>((rows + G - 1) / G, NORM_BLOCKS * 256 / NT / n));
+                    hipLaunchKernelGGL((residual_norm_kernel<x(), r(), y(), tpr(), v(), S>), dim3((uint32_t)bx, (uint32_t)n), dim3(NT), 0, stream, plan);
+                };
+                using std::integral_constant;
+                if (plan.cols <= 512) go(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 1024) go(integral_constant<int, 128>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 2048) go(integral_constant<int, 256>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 4096) go(integral_constant<int, 512>{}, integral_constant<int, 1>{});
+                else if (plan.cols <= 8192) go(integral_constant<int, 1024>{}, integral_constant<int, 1>{});
+                else go(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+            });
+        });
+    });
+    return launch_status(__func__);
+}
+template int32_t launch_residual_norm<1>(const ResNormPlan<1>&, int, int32_t, int32_t, int32_t, hipStream_t);
+template int32_t launch_residual_norm<RESNORM_SHARDS>(const ResNormPlan<RESNORM_SHARDS>&, int, int32_t, int32_t, int32_t, hipStream_t);
+
+}  // namespace sbp

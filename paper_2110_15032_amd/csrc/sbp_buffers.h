@@ -6,7 +6,7 @@ namespace sbp {
 
 // The buffers of a call, in place (a C entry must not throw, and a vector may).
 struct Buffers {
-    static constexpr int MOST = 6 * SBP_MAX_K;
+    static constexpr int MOST = 7 * SBP_MAX_K;   // inputs or outputs: up to 13 tensors of 32 devices, 6 of 64
     Span outs[MOST], ins[MOST];
     int n_out = 0, n_in = 0;
 
