@@ -350,6 +350,33 @@ int32_t sbp_matmul_f8(const sbp_tensor_t* x, const sbp_scales_t* x_scales, sbp_t
                       const sbp_scales_t* w_scales, sbp_t sbp_w, const sbp_tensor_t* y, sbp_t sbp_y, int32_t k, void* stream,
                       int32_t epilogue);
 
+/* A layer: Y = act(XW + bias) + residual under SBP, and pre = XW + bias for its gradient.  sbp_matmul_ex with an epilogue in the
+ * product's kernel:
+ *   x [M,K], w [K,N], both SBP_F32 or both SBP_BF16, stored either way, at any pitch; signatures as in Table 1 where the result is S or
+ *   B (what follows the product is not linear, or would count k times: a P result is SBP_ERR_SIGNATURE).
+ *   bias [N,1], SBP_F32 or SBP_BF16, along y's columns: S(0) for y S(1), else B; NULL: none.
+ *   residual and pre: y's shape and signature, SBP_F32 or SBP_BF16 each; NULL: none, not wanted.
+ *   act: epilogue, SBP_EPI_NONE or SBP_EPI_GELU (to 2.2e-5 of its value for SBP_BF16 y, to 1e-7 for SBP_F32; 0 of minus infinity).
+ *   y SBP_F32 or SBP_BF16; y, residual and pre with trans = 0.
+ * Products are summed in fp32 as sbp_matmul's are, everything behind them is in fp32, and pre and y are rounded once each, to nearest
+ * even; y is not made from the rounded pre.  At most 2^31 - 257 rows and columns of any tensor (SBP_ERR_UNSUPPORTED). */
+int32_t sbp_linear(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_tensor_t* w, sbp_t sbp_w, const sbp_tensor_t* bias,
+                   const sbp_tensor_t* residual, const sbp_tensor_t* pre, const sbp_tensor_t* y, sbp_t sbp_y, int32_t k,
+                   void* stream, int32_t epilogue);
+
+/* The gradient of that epilogue (that of the residual is dy itself, those of x and w are products with da):
+ *   SBP_EPI_GELU: da = dy * gelu'(pre), as sbp_gelu_grad gives it, pre SBP_F32, SBP_BF16 or in 8 bits (with pre_scales; NULL else);
+ *                 dbias = the sum of da, before its rounding, over the rows
+ *   SBP_EPI_NONE: dbias = the sum of dy over the rows; pre, pre_scales and da are NULL (SBP_ERR_UNSUPPORTED)
+ * dy, da SBP_F32 or SBP_BF16, one type; all S or B under one signature.  dbias [N,1] SBP_F32: for dy S(0) a whole vector on every
+ * device, P(sum); for S(1) S(0); for B B.  Sums are made in fp32 in an order that depends on the sizes alone.  workspace: device memory of
+ * sbp_linear_grad_workspace() bytes, 16-byte aligned, whose contents do not matter before or after the call (NULL where that is 0;
+ * SBP_ERR_SHAPE if workspace_bytes is too little).  Calls that may overlap in time need one each. */
+int32_t sbp_linear_grad(const sbp_tensor_t* dy, sbp_t sbp_dy, const sbp_tensor_t* pre, const sbp_scales_t* pre_scales,
+                        const sbp_tensor_t* da, const sbp_tensor_t* dbias, void* workspace, int64_t workspace_bytes, int32_t k,
+                        void* stream, int32_t epilogue);
+int32_t sbp_linear_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_dy, int32_t k, int64_t* bytes);
+
 /* What stands between two blocks, over the rows of x [R,C], S(0) or B, on the devices that hold them: the norm behind a block, its
  * gate, the residual, and the norm in front of the next block:
  *   t = post(x) (post NULL: x),  h = alpha * r + gate * t,  y = pre(h) (pre NULL: none, and y NULL)

@@ -12,6 +12,6 @@ from .binding import (  # noqa: F401
     sbp_infer_matmul_2d, sbp_local_shape_2d, sbp_matmul_2d, sbp_boxing_2d,
     sbp_row_max, sbp_row_sumexp, sbp_xent_loss, sbp_xent_grad,
     sbp_layernorm, sbp_layernorm_grad, sbp_layernorm_grad_workspace, sbp_quantize, sbp_dequantize, sbp_gelu_grad, sbp_matmul_f8,
-    sbp_residual_norm, sbp_residual_norm_grad, sbp_residual_norm_grad_workspace, sbp_square_sum, sbp_square_sum_workspace, sbp_clip,
+    sbp_linear, sbp_linear_grad, sbp_linear_grad_workspace, sbp_residual_norm, sbp_residual_norm_grad, sbp_residual_norm_grad_workspace, sbp_square_sum, sbp_square_sum_workspace, sbp_clip,
     sbp_set_knob, sbp_probe_mfma, sbp_probe_mfma_static, sbp_strerror, EXPORTS,
 )

@@ -38,7 +38,7 @@ EXPORTS = ("sbp_infer_matmul", "sbp_local_shape", "sbp_matmul", "sbp_matmul_ex",
            "sbp_infer_matmul_2d", "sbp_local_shape_2d", "sbp_matmul_2d", "sbp_boxing_2d",
            "sbp_row_max", "sbp_row_sumexp", "sbp_xent_loss", "sbp_xent_grad",
            "sbp_layernorm", "sbp_layernorm_grad", "sbp_layernorm_grad_workspace", "sbp_quantize", "sbp_dequantize", "sbp_gelu_grad", "sbp_matmul_f8",
-           "sbp_residual_norm", "sbp_residual_norm_grad", "sbp_residual_norm_grad_workspace", "sbp_square_sum", "sbp_square_sum_workspace", "sbp_clip", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
+           "sbp_linear", "sbp_linear_grad", "sbp_linear_grad_workspace", "sbp_residual_norm", "sbp_residual_norm_grad", "sbp_residual_norm_grad_workspace", "sbp_square_sum", "sbp_square_sum_workspace", "sbp_clip", "sbp_set_knob", "sbp_probe_mfma", "sbp_probe_mfma_static", "sbp_strerror")
 
 
 class _CTensor(ctypes.Structure):
@@ -110,6 +110,9 @@ def lib() -> ctypes.CDLL:
         L.sbp_dequantize.argtypes = [T, C, i32, T, i32, vp, i32]
         L.sbp_gelu_grad.argtypes = [T, C, i32, T, T, i32, vp]
         L.sbp_matmul_f8.argtypes = [T, C, i32, T, C, i32, T, i32, i32, vp, i32]
+        L.sbp_linear.argtypes = [T, i32, T, i32, T, T, T, T, i32, i32, vp, i32]
+        L.sbp_linear_grad.argtypes = [T, i32, T, C, T, T, vp, i64, i32, vp, i32]
+        L.sbp_linear_grad_workspace.argtypes = [i64, i64, i32, i32, ctypes.POINTER(i64)]
         N = ctypes.POINTER(_CNorm)
         L.sbp_residual_norm.argtypes = [T, i32, N, T, T, f32, T, N, T, C, i32, vp]
         L.sbp_residual_norm_grad.argtypes = [T, i32, N, T, f32, T, N, T, T, T, T, T, vp, i64, i32, vp]
@@ -387,6 +390,25 @@ def _room(workspace) -> tuple[ctypes.c_void_p, int]:
     """Address and bytes of a workspace, a torch tensor or None."""
     room = 0 if workspace is None else workspace.numel() * workspace.element_size()
     return ctypes.c_void_p(workspace.data_ptr() if room else 0), room
+
+
+def sbp_linear(x: SbpTensor, sbp_x: int, w: SbpTensor, sbp_w: int, bias: SbpTensor | None, residual: SbpTensor | None, pre: SbpTensor | None, y: SbpTensor, sbp_y: int, k: int,
+               stream=None, epilogue: int = EPI_NONE) -> None:
+    _need(k, x, w, bias, residual, pre, y)
+    _check(lib().sbp_linear(x.ref(), sbp_x, w.ref(), sbp_w, _ref(bias), _ref(residual), _ref(pre), y.ref(), sbp_y, k, _stream_ptr(stream), epilogue), "sbp_linear")
+
+
+def sbp_linear_grad_workspace(rows: int, cols: int, sbp_dy: int, k: int) -> int:
+    out = ctypes.c_int64()
+    _check(lib().sbp_linear_grad_workspace(rows, cols, sbp_dy, k, ctypes.byref(out)), "sbp_linear_grad_workspace")
+    return out.value
+
+
+def sbp_linear_grad(dy: SbpTensor, sbp_dy: int, pre: SbpTensor | None, pre_scales: SbpScales | None, da: SbpTensor | None, dbias: SbpTensor, workspace, k: int, stream=None,
+                    epilogue: int = EPI_NONE) -> None:
+    """workspace: a device buffer of sbp_linear_grad_workspace() bytes (a torch tensor), or None where none is needed."""
+    _need(k, dy, pre, pre_scales, da, dbias)
+    _check(lib().sbp_linear_grad(dy.ref(), sbp_dy, _ref(pre), _ref(pre_scales), _ref(da), dbias.ref(), *_room(workspace), k, _stream_ptr(stream), epilogue), "sbp_linear_grad")
 
 
 def sbp_residual_norm(x: SbpTensor, sbp_x: int, post: SbpNorm | None, gate: SbpTensor | None, r: SbpTensor, alpha: float, h: SbpTensor, pre: SbpNorm | None,

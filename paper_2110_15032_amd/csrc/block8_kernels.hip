@@ -244,38 +244,6 @@ __global__ __launch_bounds__(NT) void dequantize_transposed_kernel(Block8Plan p,
     }
 }
 
-// gelu'(a) = Phi(a) + a phi(a), with the upper tail of Phi as phi(|a|)'s exponential times t Q(t), t = 1 / (1 + p |a| / sqrt 2).  One exponential serves
-// both terms.  FAST, for results rounded to bf16: Abramowitz and Stegun 7.1.26, the tail to 7.5e-8 (gelu' is off by 6e-8, root mean square).  Else a minimax fit of
-// erfc(z) e^(z^2) / (2 t) made for this kernel, the tail to 2e-8 absolute and 2e-4 of itself, which leaves the roundings (3.3e-8, at most 2e-7, as
-// with erf itself).  Its two steps more are not seen in fp32 (8192 x 4096 73.3 us either way) and are in bf16 (4096 x 4096 from 8 bits 15.5, 16.0).
-// Past |a| = 14 both tails are below fp32's range (the clamp keeps infinity times zero out); NaN stays NaN.
-template <bool FAST>
-__device__ inline float gelu_slope(float a) {
-    const float x = __builtin_amdgcn_fmed3f(a, -14.0f, 14.0f);
-    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(x), (FAST ? 0.3275911f : 0.65f) * 0.70710678118654752f, 1.0f));
-    const float w = x * 0.84932180028801905f;   // sqrt(log2(e) / 2)
-    const float e = __builtin_amdgcn_exp2f(-w * w);
-    float q;
-    if constexpr (FAST) {
-        q = 0.5f * 1.061405429f;
-        q = fmaf(q, t, 0.5f * -1.453152027f);
-        q = fmaf(q, t, 0.5f * 1.421413741f);
-        q = fmaf(q, t, 0.5f * -0.284496736f);
-        q = fmaf(q, t, 0.5f * 0.254829592f);
-    } else {
-        q = -0.036686562f;
-        q = fmaf(q, t, 0.20678362f);
-        q = fmaf(q, t, -0.43400198f);
-        q = fmaf(q, t, 0.325305f);
-        q = fmaf(q, t, 0.058065444f);
-        q = fmaf(q, t, 0.1981496f);
-        q = fmaf(q, t, 0.18238488f);
-    }
-    const float tail = q * t * e;   // 1 - Phi(|x|)
-    const float cdf = x < 0.0f ? tail : 1.0f - tail;
-    return a == a ? fmaf(x * 0.39894228040143268f, e, cdf) : a;
-}
-
 // da = dh gelu'(a).  AT: the pre-activation's type, 8 bits or as it was.  Bound by HBM: 8192 x 16384 on eight devices from 8 bits (672 MB) 110 us, 6.1 TB/s.
 template <int AT, int YT, bool IN>
 __global__ __launch_bounds__(NT) void gelu_grad_kernel(Block8Plan p) {

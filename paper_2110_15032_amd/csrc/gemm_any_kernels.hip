@@ -49,7 +49,7 @@ constexpr int partial_blocks() { return FM * FN * NW <= 128 ? FM * FN : 128 / NW
 template <int NW, int FM, int FN>
 constexpr int partial_bytes() { return partial_blocks<NW, FM, FN>() * NW * 1024; }
 template <int NW, int FM, int FN, int EPI, typename OutT>
-__device__ __attribute__((always_inline)) inline void add_partial_tiles(const f32x4 (&acc)[FM][FN], char* smem, const GemmShard& s, int m0, int n0, int wave, int lane) {
+__device__ __attribute__((always_inline)) inline void add_partial_tiles(const f32x4 (&acc)[FM][FN], char* smem, const GemmShard& s, const Ending<EPI>& end, int m0, int n0, int wave, int lane) {
     constexpr int NB = partial_blocks<NW, FM, FN>(), ROUNDS = FM * FN / NB, SIDE = sizeof(OutT) == 4 ? 2 : 4;
     static_assert(FM * FN % NB == 0 && NB % SIDE == 0 && FN % SIDE == 0, "whole units of blocks side by side");
     // A block is kept as it lies in the registers:
@@ -82,13 +82,13 @@ __device__ __attribute__((always_inline)) inline void add_partial_tiles(const f3
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * h + e] = mfma_epilogue<EPI>(sum[e]);
             }
-            store_columns<OutT>(s, m, n, v);
+            finish_columns<EPI, OutT>(end, s, m, n, v);
         }
     });
 }
 
 template <int BM, int BN, int NW, bool A_KC, bool B_KC, bool DIRECT, int EPI, typename OutT>
-__global__ __launch_bounds__(NW * 64) void gemm_wavek_kernel(GemmPlan p, int tm, int tn, int order) {
+__global__ __launch_bounds__(NW * 64) void gemm_wavek_kernel(PlanOf<EPI> p, int tm, int tn, int order) {
     constexpr int BKT = 32, FM = BM / 16, FN = BN / 16;
     using TA = Tile<BM, A_KC, 64, BKT, true>;
     using TB = Tile<BN, B_KC, 64, BKT, true>;
@@ -252,7 +252,7 @@ __global__ __launch_bounds__(NW * 64) void gemm_wavek_kernel(GemmPlan p, int tm,
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     }
 
-    add_partial_tiles<NW, FM, FN, EPI, OutT>(acc, smem, s, m0, n0, wave, lane);
+    add_partial_tiles<NW, FM, FN, EPI, OutT>(acc, smem, s, Ending<EPI>(p, tc.g), m0, n0, wave, lane);
 }
 
 // gemm_rows_kernel: both operands reduction-contiguous, rows at any pitch, fp32 results, few output tiles: as gemm_wavek_kernel, every
@@ -381,14 +381,14 @@ __global__ __launch_bounds__(512) void gemm_rows_kernel(GemmPlan p, int tm, int 
         __syncthreads();
         multiply(smem);
     }
-    add_partial_tiles<NW, FM, FN, SBP_EPI_NONE, float>(acc, smem, s, m0, n0, wave, lane);
+    add_partial_tiles<NW, FM, FN, SBP_EPI_NONE, float>(acc, smem, s, Ending<SBP_EPI_NONE>(p, tc.g), m0, n0, wave, lane);
 }
 
 // 4 waves of BM/2 x BN/2, two 32-deep LDS stages filled from registers that run two stages ahead, one barrier a
 // stage.  Two or three workgroups share a compute unit and cover each other's waits; a register ring of four stages was
 // no faster (odd sizes 1500 x 1501 x 2501, 2 devices: 42.0 us with two stages, 43.2 with four).
 template <int BM, int BN, bool A_KC, bool B_KC, int EPI, typename OutT>
-__global__ __launch_bounds__(256, 2) void gemm_reg_kernel(GemmPlan p, int tm, int tn, int order) {
+__global__ __launch_bounds__(256, 2) void gemm_reg_kernel(PlanOf<EPI> p, int tm, int tn, int order) {
     constexpr int BKT = 32, NT = 256, TM = BM / 2, TN = BN / 2, FM = TM / 16, FN = TN / 16, BLOCKS = FM * FN;
     using TA = Tile<BM, A_KC, NT, BKT, true>;
     using TB = Tile<BN, B_KC, NT, BKT, true>;
@@ -488,6 +488,7 @@ __global__ __launch_bounds__(256, 2) void gemm_reg_kernel(GemmPlan p, int tm, in
     static_assert(BLOCKS % NB == 0 && NB % FN == 0 && FN % UNIT == 0, "whole rows of blocks");
     char* const win = smem + wave * (NB * 1024);
     const int q = lane >> 4, r = lane & 15;
+    const Ending<EPI> end(p, tc.g);
     static_for<BLOCKS / NB>([&](auto rix) {
         constexpr int B0 = decltype(rix)::value * NB;
         static_for<NB>([&](auto bix) {
@@ -495,7 +496,7 @@ __global__ __launch_bounds__(256, 2) void gemm_reg_kernel(GemmPlan p, int tm, in
             *reinterpret_cast<f32x4*>(win + decltype(bix)::value * 1024 + (16 * q + (r ^ (4 * q))) * 16) = acc[b / FN][b % FN];
         });
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll EPI == EPI_GELU_ERF ? 1 : 64   // erfcf is long
+#pragma unroll EPI == EPI_GELU_ERF || EPI == EPI_BLOCK ? 1 : 64   // erfcf is long
         for (int u = 0; u < NB / UNIT * (16 / ROWS); ++u) {
             const int blk = u / (16 / ROWS) * UNIT, row = u % (16 / ROWS) * ROWS + lane / LPR;
             float v[EPV];
@@ -506,7 +507,7 @@ __global__ __launch_bounds__(256, 2) void gemm_reg_kernel(GemmPlan p, int tm, in
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[4 * h + e] = mfma_epilogue<EPI>(x[e]);
             }
-            store_columns<OutT>(s, m0 + wm * TM + (B0 + blk) / FN * 16 + row, n0 + wn * TN + (B0 + blk) % FN * 16 + (lane % LPR) * EPV, v);
+            finish_columns<EPI, OutT>(end, s, m0 + wm * TM + (B0 + blk) / FN * 16 + row, n0 + wn * TN + (B0 + blk) % FN * 16 + (lane % LPR) * EPV, v);
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     });
@@ -532,7 +533,7 @@ __global__ __launch_bounds__(256, 2) void gemm_reg_kernel(GemmPlan p, int tm, in
 // and its LDS reads take 0.36.
 // LINES: some row of a reduction-contiguous operand starts inside a cache line.  TOUCH: see touches_pay.
 template <bool A_KC, bool B_KC, bool LINES, bool TOUCH, int EPI, typename OutT>
-__global__ __launch_bounds__(512) void gemm_deep_kernel(GemmPlan p, int tm, int tn, int order) {
+__global__ __launch_bounds__(512) void gemm_deep_kernel(PlanOf<EPI> p, int tm, int tn, int order) {
     constexpr int BM = 128, BN = 128, BKT = 64, NT = 512, NST = 4, FM = 4, FN = 4;
     using TA = Tile<BM, A_KC, NT, BKT, true>;
     using TB = Tile<BN, B_KC, NT, BKT, true>;
@@ -712,7 +713,8 @@ __global__ __launch_bounds__(512) void gemm_deep_kernel(GemmPlan p, int tm, int 
         *reinterpret_cast<f32x4*>(smem + wave * PART + b * 1024 + (16 * q + (r ^ (4 * q))) * 16) = acc[b / FN][b % FN];
     });
     __syncthreads();
-#pragma unroll EPI == EPI_GELU_ERF ? 1 : 64
+    const Ending<EPI> end(p, tc.g);
+#pragma unroll EPI == EPI_GELU_ERF || EPI == EPI_BLOCK ? 1 : 64
     for (int u = 0; u < FM * FN / UNIT; ++u) {   // this wave: eight of every 16 rows
         const int blk = u * UNIT, row = 8 * half + (lane >> 3);
         float v[EPV];
@@ -724,7 +726,7 @@ __global__ __launch_bounds__(512) void gemm_deep_kernel(GemmPlan p, int tm, int 
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[4 * h + e] = mfma_epilogue<EPI>(sum[e]);
         }
-        store_columns<OutT>(s, m0 + wm * 64 + blk / FN * 16 + row, n0 + wn * 64 + blk % FN * 16 + (lane & 7) * EPV, v);
+        finish_columns<EPI, OutT>(end, s, m0 + wm * 64 + blk / FN * 16 + row, n0 + wn * 64 + blk % FN * 16 + (lane & 7) * EPV, v);
     }
 }
 
@@ -735,11 +737,11 @@ constexpr auto pick_kernel() {   // NW = 0: gemm_reg_kernel
 }
 
 template <int BM, int BN, int NW, bool DIRECT, int EPI, typename OutT>
-int32_t launch_layout(const GemmPlan& plan, int max_m, int max_n, int order, hipStream_t st) {
+int32_t launch_layout(const PlanOf<EPI>& plan, int max_m, int max_n, int order, hipStream_t st) {
     const int tm = tiles_along(max_m, BM), tn = tiles_along(max_n, BN);
     const int64_t nblk = ((int64_t)tm * tn * plan.groups + 7) / 8 * 8;
     if (!grid_fits(nblk, NW > 0 ? NW * 64 : 256)) return SBP_ERR_UNSUPPORTED;
-    void (*kern)(GemmPlan, int, int, int) = nullptr;
+    void (*kern)(PlanOf<EPI>, int, int, int) = nullptr;
     if (plan.a_kc) {
         if (plan.b_kc) kern = pick_kernel<BM, BN, NW, DIRECT, true, true, EPI, OutT>();
         else kern = pick_kernel<BM, BN, NW, DIRECT, true, false, EPI, OutT>();
@@ -777,7 +779,7 @@ int32_t launch_rows(const GemmPlan& plan, int max_m, int max_n, int order, hipSt
 }
 
 template <int EPI, typename OutT>
-int32_t launch_deep_layout(const GemmPlan& plan, int max_m, int max_n, int order, bool touch, hipStream_t st) {
+int32_t launch_deep_layout(const PlanOf<EPI>& plan, int max_m, int max_n, int order, bool touch, hipStream_t st) {
     const int tm = tiles_along(max_m, 128), tn = tiles_along(max_n, 128);
     const int64_t nblk = ((int64_t)tm * tn * plan.groups + 7) / 8 * 8;
     if (!grid_fits(nblk, 512)) return SBP_ERR_UNSUPPORTED;
@@ -816,6 +818,21 @@ int32_t launch_gemm_any(const GemmPlan& plan, int max_m, int max_n, int tile, bo
         case ROWS_64: return launch_rows<64, 64>(plan, max_m, max_n, order, stream);
         case REG_128: return launch_out<128, 128, 0, false>(plan, max_m, max_n, order, stream);
         case REG_64: return launch_out<64, 64, 0, false>(plan, max_m, max_n, order, stream);
+        default: return SBP_ERR_UNSUPPORTED;
+    }
+}
+
+int32_t launch_gemm_deep(const GemmBlockPlan& plan, int max_m, int max_n, int order, bool touch, hipStream_t stream) {
+    return launch_deep_layout<EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, touch, stream);
+}
+
+int32_t launch_gemm_any(const GemmBlockPlan& plan, int max_m, int max_n, int tile, bool direct, int order, hipStream_t stream) {
+    switch (tile) {
+        case WAVEK_128: return direct ? launch_layout<128, 64, 4, true, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream) : SBP_ERR_UNSUPPORTED;
+        case WAVEK_64: return direct ? launch_layout<64, 64, 8, true, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream) : launch_layout<64, 64, 8, false, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream);
+        case WAVEK_32: return direct ? launch_layout<32, 64, 8, true, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream) : launch_layout<32, 64, 8, false, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream);
+        case REG_128: return launch_layout<128, 128, 0, false, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream);
+        case REG_64: return launch_layout<64, 64, 0, false, EPI_BLOCK, uint16_t>(plan, max_m, max_n, order, stream);
         default: return SBP_ERR_UNSUPPORTED;
     }
 }

@@ -4,6 +4,7 @@
 // the compiler's bookkeeping.  Everything is internal (anonymous namespace, one copy per unit).
 #pragma once
 #include <cstdlib>
+#include <type_traits>
 #include <utility>
 
 #include "sbp_internal.h"
@@ -343,7 +344,8 @@ __host__ inline int deep_band(int tm, int tn, int64_t tiles) { return tm <= 255 
 constexpr int DEEP_TOUCH_STEPS = 48, DEEP_TOUCH_MAX_KC = 224, DEEP_TOUCH_MAX = 320;
 
 // Does every row along the reduction start on a cache line?
-__host__ inline bool rows_on_lines(const GemmPlan& plan) {
+template <typename Plan>
+__host__ inline bool rows_on_lines(const Plan& plan) {
     for (int g = 0; g < plan.groups; ++g) {
         const GemmShard& s = plan.s[g];
         if (!s.m || !s.n || !s.kk) continue;
@@ -417,6 +419,9 @@ __device__ inline float gelu_fast(float x) {
 
 // 0.5 x (1 + erf(x / sqrt 2)) written with erfc so that the negative tail keeps its relative accuracy; NaN stays NaN
 __device__ inline float gelu_erf(float x) { return 0.5f * x * erfcf(x * -0.70710678118654752f); }
+
+// gelu of results in fp32: gelu_erf, but 0 of minus infinity, as gelu_fast has it (as a factor it is the lowest number, next to an erfc of 0)
+__device__ inline float gelu_whole(float x) { return 0.5f * __builtin_amdgcn_fmed3f(x, -3.4028235e38f, INFINITY) * erfcf(x * -0.70710678118654752f); }
 
 template <int EPI>
 __device__ inline float mfma_epilogue(float v) {
@@ -525,6 +530,127 @@ __device__ inline void store_rest_untracked(uint16_t* c, const u32x4 v, int n) {
     if (n & 4) asm volatile("global_store_dwordx2 %0, %1, off" : : "v"(c), "v"(four) : "memory");
     if (n & 2) asm volatile("global_store_dword %0, %1, off" : : "v"(c + (n & 4)), "v"(a) : "memory");
     if (n & 1) asm volatile("global_store_short %0, %1, off" : : "v"(c + (n & 6)), "v"(n & 2 ? b : a) : "memory");
+}
+
+// ---- bias, activation and residual in front of the store (EPI_BLOCK) ----------------------------
+template <int EPI>
+using PlanOf = std::conditional_t<EPI == EPI_BLOCK, GemmBlockPlan, GemmPlan>;
+
+typedef u32x2 __attribute__((aligned(2))) u32x2_half;
+
+// EPV (1, 4 or 8) consecutive elements of a row from element `at` on, at any alignment; `valid` of them exist, and those behind are 0.
+template <int EPV>
+__device__ inline void read_columns(const void* from, bool bf16, int64_t at, int valid, float (&v)[EPV]) {
+    const uint16_t* const h = static_cast<const uint16_t*>(from) + at;
+    const float* const f = static_cast<const float*>(from) + at;
+    if (EPV > 1 && valid >= EPV) {
+        if (bf16) {
+            uint32_t w[EPV > 1 ? EPV / 2 : 1];
+            if constexpr (EPV == 8) {
+                const u32x4 q = *reinterpret_cast<const u32x4_any*>(h);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = q[e];
+            } else if constexpr (EPV == 4) {
+                const u32x2 q = *reinterpret_cast<const u32x2_half*>(h);
+                w[0] = q[0];
+                w[1] = q[1];
+            }
+            if constexpr (EPV > 1) {
+#pragma unroll
+                for (int e = 0; e < EPV / 2; ++e) {
+                    v[2 * e] = __uint_as_float(w[e] << 16);
+                    v[2 * e + 1] = __uint_as_float(w[e] & 0xFFFF0000u);
+                }
+            }
+        } else {
+#pragma unroll
+            for (int q = 0; q < EPV / 4; ++q) {
+                const f32x4 u = *reinterpret_cast<const f32x4_any*>(f + 4 * q);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[4 * q + e] = u[e];
+            }
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) v[e] = e < valid ? bf16 ? bf16_to_f32(h[e]) : f[e] : 0.0f;
+    }
+}
+template <int EPV>
+__device__ inline void write_columns(void* to, bool bf16, int64_t at, int valid, const float (&v)[EPV]) {
+    uint16_t* const h = static_cast<uint16_t*>(to) + at;
+    float* const f = static_cast<float*>(to) + at;
+    if (EPV > 1 && valid >= EPV) {
+        if (bf16) {
+            if constexpr (EPV == 8) *reinterpret_cast<u32x4_any*>(h) = u32x4{f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3]), f32_to_bf16x2(v[4], v[5]), f32_to_bf16x2(v[6], v[7])};
+            else if constexpr (EPV == 4) *reinterpret_cast<u32x2_half*>(h) = u32x2{f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3])};
+        } else {
+#pragma unroll
+            for (int q = 0; q < EPV / 4; ++q) *reinterpret_cast<f32x4_any*>(f + 4 * q) = f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < EPV; ++e)
+            if (e < valid) {
+                if (bf16) h[e] = f32_to_bf16(v[e]);
+                else f[e] = v[e];
+            }
+    }
+}
+
+// What stands at the end of a kernel for shard g of its plan: nothing but a store, or the block's epilogue.
+template <int EPI>
+struct Ending {
+    __device__ Ending(const GemmPlan&, int) {}
+};
+template <>
+struct Ending<EPI_BLOCK> {
+    GemmExtra x;
+    int flags;
+    __device__ Ending(const GemmBlockPlan& p, int g) : x(p.x[g]), flags(p.flags) {}
+    // v = A B + bias, r the residual (0: none): pre and the result of EPV columns of row m from column n on.  GeLU as sbp_matmul_ex has it: to
+    // 2.2e-5 in front of a rounding to bf16, by erfc where the result is in fp32 (0 of minus infinity).
+    template <int EPV>
+    __device__ inline void put(const GemmShard& s, int m, int n, int valid, float (&v)[EPV], const float (&r)[EPV]) const {
+        if (x.pre) write_columns<EPV>(x.pre, flags & GB_PRE_BF16, (int64_t)m * x.ldp + n, valid, v);
+        if (flags & GB_GELU) {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) v[e] = gelu_fast(v[e]);
+        } else if (flags & GB_GELU_ERF) {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) v[e] = gelu_whole(v[e]);
+        }
+#pragma unroll
+        for (int e = 0; e < EPV; ++e) v[e] += r[e];
+        write_columns<EPV>(s.c, flags & GB_OUT_BF16, (int64_t)m * s.ldc + n, valid, v);
+    }
+    template <int EPV>
+    __device__ inline void residual(int m, int n, int valid, float (&r)[EPV]) const {
+        if (x.residual) read_columns<EPV>(x.residual, flags & GB_RESIDUAL_BF16, (int64_t)m * x.ldr + n, valid, r);
+        else {
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) r[e] = 0.0f;
+        }
+    }
+    template <int EPV>
+    __device__ inline void finish(const GemmShard& s, int m, int n, float (&v)[EPV]) const {
+        if (m >= s.m || n >= s.n) return;
+        const int valid = s.n - n;
+        float b[EPV], r[EPV];
+        residual<EPV>(m, n, valid, r);
+        if (x.bias) {
+            read_columns<EPV>(x.bias, flags & GB_BIAS_BF16, n, valid, b);
+#pragma unroll
+            for (int e = 0; e < EPV; ++e) v[e] += b[e];
+        }
+        put<EPV>(s, m, n, valid, v, r);
+    }
+};
+
+// EPV consecutive columns of row m from column n on: stored, or through the block's epilogue
+template <int EPI, typename OutT, int EPV>
+__device__ inline void finish_columns(const Ending<EPI>& end, const GemmShard& s, int m, int n, float (&v)[EPV]) {
+    if constexpr (EPI == EPI_BLOCK) end.template finish<EPV>(s, m, n, v);
+    else store_columns<OutT>(s, m, n, v);
 }
 
 }  // namespace

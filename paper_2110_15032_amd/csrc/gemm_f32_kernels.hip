@@ -124,7 +124,7 @@ constexpr int f32_tile_floats() {
 }
 // The tile at (m0, n0) of s; smem: f32_tile_floats of them.  All threads of the workgroup.
 template <int BM, int BN, int BK, int WM, int WN, int WK, typename TA, typename TB, bool A_KC, bool B_KC, int EPI>
-__device__ inline void f32_tile(const GemmShard& s, int m0, int n0, float* smem) {
+__device__ inline void f32_tile(const GemmShard& s, const Ending<EPI>& end, int m0, int n0, float* smem) {
     constexpr int NT = WM * WN * WK * 64, TM = BM / WM, TN = BN / WN, FM = TM / 32, FN = TN / 32;
     constexpr int GROUPS = BK / 8 / WK;   // 8-deep groups of a stage per wave
     using OA = Operand<TA, BM, A_KC, BK, NT>;
@@ -210,11 +210,11 @@ __device__ inline void f32_tile(const GemmShard& s, int m0, int n0, float* smem)
         }
     }
 
-    auto finish = [](float v) {
+    [[maybe_unused]] auto finish = [](float v) {
         if constexpr (EPI == SBP_EPI_GELU) return gelu_erf(v);
         else return v;
     };
-    float* const C = static_cast<float*>(s.c);
+    [[maybe_unused]] float* const C = static_cast<float*>(s.c);
     // acc[i][j][r] is row 8 (r / 4) + 4 (lane / 32) + r % 4, column lane % 32 of its block: 128 bytes of a row per half-wave
     if constexpr (WK == 1) {
         const int n = n0 + wn * TN + (lane & 31), mb = m0 + wm * TM + 4 * (lane >> 5);
@@ -225,7 +225,12 @@ __device__ inline void f32_tile(const GemmShard& s, int m0, int n0, float* smem)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) {
                     const int m = mb + i * 32 + 8 * (r >> 2) + (r & 3);
-                    if (m < s.m && n + j * 32 < s.n) C[(int64_t)m * s.ldc + n + j * 32] = finish(acc[i][j][r]);
+                    if constexpr (EPI == EPI_BLOCK) {
+                        float v[1] = {acc[i][j][r]};
+                        end.template finish<1>(s, m, n + j * 32, v);
+                    } else {
+                        if (m < s.m && n + j * 32 < s.n) C[(int64_t)m * s.ldc + n + j * 32] = finish(acc[i][j][r]);
+                    }
                 }
     } else {
         // every stage ends with a barrier: the stages are free.  [wk][row of the tile][column]
@@ -244,20 +249,25 @@ __device__ inline void f32_tile(const GemmShard& s, int m0, int n0, float* smem)
             float v = smem[e];
 #pragma unroll
             for (int w = 1; w < WK; ++w) v += smem[w * TILE + e];
-            if (m < s.m && n < s.n) C[(int64_t)m * s.ldc + n] = finish(v);
+            if constexpr (EPI == EPI_BLOCK) {
+                float of_one[1] = {v};
+                end.template finish<1>(s, m, n, of_one);
+            } else {
+                if (m < s.m && n < s.n) C[(int64_t)m * s.ldc + n] = finish(v);
+            }
         }
     }
 }
 
 template <int BM, int BN, int BK, int WM, int WN, int WK, typename TA, typename TB, bool A_KC, bool B_KC, int EPI>
-__global__ __launch_bounds__(WM * WN * WK * 64) void gemm_f32_kernel(GemmPlan p, int tm, int tn, int order) {
+__global__ __launch_bounds__(WM * WN * WK * 64) void gemm_f32_kernel(PlanOf<EPI> p, int tm, int tn, int order) {
     __shared__ __attribute__((aligned(16))) float smem[f32_tile_floats<BM, BN, BK, WM, WN, WK, TA, TB, A_KC, B_KC>()];
     const TileCoord tc = map_tile(blockIdx.x, gridDim.x, tm, tn, p.groups, order);
     if (!tc.valid) return;
     const GemmShard s = p.s[tc.g];
     const int m0 = tc.tile_m * BM, n0 = tc.tile_n * BN;
     if (m0 >= s.m || n0 >= s.n) return;
-    f32_tile<BM, BN, BK, WM, WN, WK, TA, TB, A_KC, B_KC, EPI>(s, m0, n0, smem);
+    f32_tile<BM, BN, BK, WM, WN, WK, TA, TB, A_KC, B_KC, EPI>(s, Ending<EPI>(p, tc.g), m0, n0, smem);
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
@@ -405,7 +415,7 @@ struct TermOperand {
 };
 
 template <int BM, int BN, int WPS, typename T1, typename T2, bool A_KC, bool B_KC, int EPI>
-__global__ __launch_bounds__(256, WPS) void gemm_terms_kernel(GemmPlan p, int tm, int tn, int order) {
+__global__ __launch_bounds__(256, WPS) void gemm_terms_kernel(PlanOf<EPI> p, int tm, int tn, int order) {
     constexpr int NT = 256, TM = BM / 2, TN = BN / 2, FM = TM / 16, FN = TN / 16, BLOCKS = FM * FN;
     constexpr bool ONE_F32 = sizeof(T1) != sizeof(T2);
     using OA = TermOperand<T1, BM, A_KC, NT, ONE_F32>;
@@ -522,6 +532,7 @@ __global__ __launch_bounds__(256, WPS) void gemm_terms_kernel(GemmPlan p, int tm
     constexpr float BACK = 1.0f / (float)((int64_t)1 << CUT_EXP * ((OA::F32 ? 1 : 0) + (OB::F32 ? 1 : 0)));
     static_assert(NB * 4096 <= (int)sizeof(smem) && BLOCKS % NB == 0 && NB % FN == 0 && FN % 2 == 0, "whole rows of blocks");
     char* const win = smem + wave * (NB * 1024);
+    const Ending<EPI> end(p, tc.g);
     if (!again) {
         static_for<BLOCKS / NB>([&](auto rix) {
             constexpr int B0 = decltype(rix)::value * NB;
@@ -530,20 +541,20 @@ __global__ __launch_bounds__(256, WPS) void gemm_terms_kernel(GemmPlan p, int tm
                 *reinterpret_cast<f32x4*>(win + decltype(bix)::value * 1024 + (16 * q + (r ^ (4 * q))) * 16) = acc[b / FN][b % FN];
             });
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll EPI == SBP_EPI_GELU ? 1 : 64
+#pragma unroll EPI == SBP_EPI_GELU || EPI == EPI_BLOCK ? 1 : 64
             for (int u = 0; u < NB; ++u) {
                 const int blk = u / 2 * 2, row = u % 2 * 8 + lane / 8, cg = lane % 8;
                 const f32x4 x = *reinterpret_cast<const f32x4*>(win + (blk + cg / 4) * 1024 + (16 * (cg & 3) + (row ^ (4 * (cg & 3)))) * 16);
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) v[e] = EPI == SBP_EPI_GELU ? gelu_erf(x[e] * BACK) : x[e] * BACK;
-                store_columns<float>(s, m0 + wm * TM + (B0 + blk) / FN * 16 + row, n0 + wn * TN + (B0 + blk) % FN * 16 + cg * 4, v);
+                finish_columns<EPI, float>(end, s, m0 + wm * TM + (B0 + blk) / FN * 16 + row, n0 + wn * TN + (B0 + blk) % FN * 16 + cg * 4, v);
             }
             __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         });
     }
     asm volatile("" : "+s"(again));   // a branch of its own: as one, both ways would be laid out so that the accumulators outlive the second one's
-    if (again) f32_tile<BM, BN, BM == 128 ? 16 : 32, 2, 2, 1, T1, T2, A_KC, B_KC, EPI>(s, m0, n0, reinterpret_cast<float*>(smem));
+    if (again) f32_tile<BM, BN, BM == 128 ? 16 : 32, 2, 2, 1, T1, T2, A_KC, B_KC, EPI>(s, end, m0, n0, reinterpret_cast<float*>(smem));
 }
 
 // Tiles of gemm_f32_kernel, or (TERMS: waves per SIMD) of gemm_terms_kernel.
@@ -553,11 +564,11 @@ constexpr auto pick_kernel() {
     else return gemm_f32_kernel<BM, BN, BK, WM, WN, WK, TA, TB, A_KC, B_KC, EPI>;
 }
 template <int TERMS, int BM, int BN, int BK, int WM, int WN, int WK, typename TA, typename TB, int EPI>
-int32_t launch_layout(const GemmPlan& plan, int max_m, int max_n, int order, hipStream_t st) {
+int32_t launch_layout(const PlanOf<EPI>& plan, int max_m, int max_n, int order, hipStream_t st) {
     const int tm = tiles_along(max_m, BM), tn = tiles_along(max_n, BN);
     const int64_t nblk = ((int64_t)tm * tn * plan.groups + 7) / 8 * 8;
     if (!grid_fits(nblk, WM * WN * WK * 64)) return SBP_ERR_UNSUPPORTED;
-    void (*kern)(GemmPlan, int, int, int);
+    void (*kern)(PlanOf<EPI>, int, int, int);
     if (plan.a_kc) kern = plan.b_kc ? pick_kernel<TERMS, BM, BN, BK, WM, WN, WK, TA, TB, true, true, EPI>() : pick_kernel<TERMS, BM, BN, BK, WM, WN, WK, TA, TB, true, false, EPI>();
     else kern = plan.b_kc ? pick_kernel<TERMS, BM, BN, BK, WM, WN, WK, TA, TB, false, true, EPI>() : pick_kernel<TERMS, BM, BN, BK, WM, WN, WK, TA, TB, false, false, EPI>();
     hipLaunchKernelGGL(kern, dim3((uint32_t)nblk), dim3(WM * WN * WK * 64), 0, st, plan, tm, tn, order);
@@ -582,6 +593,17 @@ int32_t launch_gemm_f32(const GemmPlan& plan, int max_m, int max_n, int tile, in
         case TERMS_128: return launch_types<3, 128, 128, 16, 2, 2, 1>(plan, max_m, max_n, order, stream);
         case TERMS_64: return launch_types<4, 64, 64, 32, 2, 2, 1>(plan, max_m, max_n, order, stream);
         case F32_32: return launch_types<0, 32, 32, 64, 1, 1, 8>(plan, max_m, max_n, order, stream);
+        default: return SBP_ERR_UNSUPPORTED;
+    }
+}
+
+int32_t launch_gemm_f32(const GemmBlockPlan& plan, int max_m, int max_n, int tile, int order, hipStream_t stream) {
+    switch (tile) {
+        case F32_128: return launch_layout<0, 128, 128, 16, 2, 2, 1, float, float, EPI_BLOCK>(plan, max_m, max_n, order, stream);
+        case F32_64: return launch_layout<0, 64, 64, 32, 2, 2, 1, float, float, EPI_BLOCK>(plan, max_m, max_n, order, stream);
+        case TERMS_128: return launch_layout<3, 128, 128, 16, 2, 2, 1, float, float, EPI_BLOCK>(plan, max_m, max_n, order, stream);
+        case TERMS_64: return launch_layout<4, 64, 64, 32, 2, 2, 1, float, float, EPI_BLOCK>(plan, max_m, max_n, order, stream);
+        case F32_32: return launch_layout<0, 32, 32, 64, 1, 1, 8, float, float, EPI_BLOCK>(plan, max_m, max_n, order, stream);
         default: return SBP_ERR_UNSUPPORTED;
     }
 }

@@ -52,7 +52,7 @@ __device__ inline void store_out(uint16_t* c, int64_t pos, float v) {
 // ------------------------------------------------------------------------------------------------
 // A_BF16 / B_BF16: element type of each operand (a P(sum) operand is fp32 next to a bf16 one)
 template <bool A_BF16, bool B_BF16, typename OutT, int EPI>
-__global__ __launch_bounds__(256) void gemm_generic_kernel(GemmPlan p) {
+__global__ __launch_bounds__(256) void gemm_generic_kernel(PlanOf<EPI> p) {
     const GemmShard s = p.s[blockIdx.z];
     const int m = blockIdx.y * 16 + threadIdx.y;
     const int n = blockIdx.x * 16 + threadIdx.x;
@@ -68,7 +68,12 @@ __global__ __launch_bounds__(256) void gemm_generic_kernel(GemmPlan p) {
         else b = static_cast<const float*>(s.b)[ib];
         acc = fmaf(a, b, acc);
     }
-    store_out(static_cast<OutT*>(s.c), (int64_t)m * s.ldc + n, epilogue<EPI>(acc));
+    if constexpr (EPI == EPI_BLOCK) {
+        float v[1] = {acc};
+        Ending<EPI>(p, blockIdx.z).template finish<1>(s, m, n, v);
+    } else {
+        store_out(static_cast<OutT*>(s.c), (int64_t)m * s.ldc + n, epilogue<EPI>(acc));
+    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -621,6 +626,100 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_kernel(GemmPlan p, int
     store_tile<BM, BN, TM, TN, FM, FN, EPI, OutT>(acc, s, m0, n0, wm, wn, lane, sOut);
 }
 
+// The block's epilogue (bias, activation, residual) for accumulators of v_mfma_f32_16x16x32_bf16, as store_tile16 has them.  Strips of 32 rows x 64
+// columns pass through a window of LDS in fp32, row pitch 256 bytes, the 64-byte groups of a row permuted by XOR with row / 4 % 4, which
+// puts the four rows of a write on four groups of banks; a lane then owns eight consecutive columns of a row, whose bias stays in registers.
+// Tiles inside the matrix: the residual of a strip is on its way before the strip is staged.  Tiles cut by the edge, and GeLU by erfc, whose code is
+// long, take a loop.
+constexpr int BLOCK_WINDOW = 32 * 64 * 4;
+template <int BM, int BN, int TM, int TN>
+__device__ __attribute__((always_inline)) inline void store_block16(const f32x4 (&acc)[TM / 16][TN / 16], const GemmShard& s, const Ending<EPI_BLOCK>& end, int m0, int n0, int wm, int wn,
+                                                                    int lane, char* win) {
+    static_assert(TN == 64, "a strip is 64 columns wide");
+    const int g = lane >> 4, c = lane & 15, h = lane >> 5;
+    const int m = m0 + wm * TM + (lane >> 3), n = n0 + wn * TN + (lane & 7) * 8;   // of this lane's first row and columns
+    int w[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) w[j] = 4 * g * 256 + (j ^ g) * 64 + c * 4;
+    auto stage = [&](auto ix) __attribute__((always_inline)) {
+        constexpr int i = decltype(ix)::value;
+        static_for<2>([&](auto ibx) {
+            static_for<4>([&](auto jx) {
+                static_for<4>([&](auto rx) {
+                    constexpr int ib = decltype(ibx)::value, j = decltype(jx)::value, r = decltype(rx)::value;
+                    *reinterpret_cast<float*>(win + (w[j] + (16 * ib + r) * 256)) = acc[2 * i + ib][j][r];
+                });
+            });
+        });
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    auto take = [&](int q, float (&v)[8]) {   // row lane / 8 + 8 q of the strip
+        const char* const at = win + ((lane >> 3) + 8 * q) * 256 + (((lane & 7) >> 1) ^ (2 * (q & 1) + h)) * 64 + (lane & 1) * 32;
+        const f32x4 a = *reinterpret_cast<const f32x4*>(at), b = *reinterpret_cast<const f32x4*>(at + 16);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            v[e] = a[e];
+            v[4 + e] = b[e];
+        }
+    };
+    if (m0 + BM <= s.m && n0 + BN <= s.n && !(end.flags & GB_GELU_ERF)) {
+        float bias[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+        if (end.x.bias) read_columns<8>(end.x.bias, end.flags & GB_BIAS_BF16, n, 8, bias);
+        static_for<TM / 32>([&](auto ix) {
+            constexpr int i = decltype(ix)::value;
+            u32x4 raw[4][2];   // bf16: the first half
+            if (end.x.residual) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const int64_t at = (int64_t)(m + i * 32 + 8 * q) * end.x.ldr + n;
+                    if (end.flags & GB_RESIDUAL_BF16) {
+                        raw[q][0] = *reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(end.x.residual) + at);
+                    } else {
+                        const float* const f = static_cast<const float*>(end.x.residual) + at;
+                        raw[q][0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(f));
+                        raw[q][1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(f + 4));
+                    }
+                }
+            }
+            stage(ix);
+            static_for<4>([&](auto qx) {
+                constexpr int q = decltype(qx)::value;
+                float v[8], r[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+                take(q, v);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += bias[e];
+                if (end.x.residual) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if (end.flags & GB_RESIDUAL_BF16) {
+                            r[2 * e] = __uint_as_float(raw[q][0][e] << 16);
+                            r[2 * e + 1] = __uint_as_float(raw[q][0][e] & 0xFFFF0000u);
+                        } else {
+                            r[e] = __uint_as_float(raw[q][0][e]);
+                            r[4 + e] = __uint_as_float(raw[q][1][e]);
+                        }
+                    }
+                }
+                end.put<8>(s, m + i * 32 + 8 * q, n, 8, v, r);
+            });
+            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        });
+        return;
+    }
+    static_for<TM / 32>([&](auto ix) {
+        constexpr int i = decltype(ix)::value;
+        if (m0 + wm * TM + i * 32 >= s.m || n0 + wn * TN >= s.n) return;   // uniform: nothing of the strip exists
+        stage(ix);
+#pragma unroll 1
+        for (int q = 0; q < 4; ++q) {
+            float v[8];
+            take(q, v);
+            end.finish<8>(s, m + i * 32 + 8 * q, n, v);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    });
+}
+
 // ------------------------------------------------------------------------------------------------
 // Deeper pipeline: NST LDS stages of 32 reduction elements each (same 128 KB as 2 x 64 when
 // NST = 4), so that NST - 1 tiles are in flight while one is being multiplied.  One step t:
@@ -766,7 +865,7 @@ __global__ __launch_bounds__(WM * WN * 64, (BM * BN <= 256 * 128 && WM * WN == 4
 // [1024, 125000] x [125000, 512] per device, 8 devices: 661 ms with the generic kernel, 2.0 ms with the 128 x 128 tile
 // here; [777, 1000] x [1000, 1000], 3 devices: 1170 us against 15.
 template <int BM, int BN, int WM, int WN, bool A_KC, bool B_KC, int NST, int EPI, typename OutT>
-__global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_pipe16_kernel(GemmPlan p, int tm, int tn, int order) {
+__global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_pipe16_kernel(PlanOf<EPI> p, int tm, int tn, int order) {
     constexpr int BKT = 32;
     constexpr int NT = WM * WN * 64;
     constexpr int TM = BM / WM, TN = BN / WN;
@@ -790,7 +889,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_pipe16_kernel(GemmPlan
     __shared__ __attribute__((aligned(1024))) char sB2[TB::BYTES];
     __shared__ __attribute__((aligned(1024))) char sB3[NST > 3 ? TB::BYTES : 16];
     __shared__ __attribute__((aligned(1024))) char sB4[NST > 4 ? TB::BYTES : 16];
-    __shared__ __attribute__((aligned(1024))) char sOut[WM * WN * STAGE_BYTES];   // epilogue windows, one per wave
+    __shared__ __attribute__((aligned(1024))) char sOut[EPI == EPI_BLOCK ? 16 : WM * WN * STAGE_BYTES];   // epilogue windows, one per wave
     auto stA = [&](auto i) -> char* {
         constexpr int I = decltype(i)::value;
         if constexpr (I == 0) return sA0; else if constexpr (I == 1) return sA1; else if constexpr (I == 2) return sA2;
@@ -913,7 +1012,16 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_pipe16_kernel(GemmPlan
         mfmas(1, 0);
     }
 
-    store_tile16<BM, BN, TM, TN, EPI, OutT>(acc, s, m0, n0, wm, wn, lane, sOut);
+    if constexpr (EPI == EPI_BLOCK) {
+        // a stage of either operand is a wave's window: nobody reads them any more
+        static_assert(TA::BYTES >= BLOCK_WINDOW && TB::BYTES >= BLOCK_WINDOW && WM * WN <= 8, "a window for every wave");
+        __syncthreads();
+        char* const low = wave & 2 ? (wave & 1 ? sA3 : sA2) : (wave & 1 ? sA1 : sA0);
+        char* const high = wave & 2 ? (wave & 1 ? sB3 : sB2) : (wave & 1 ? sB1 : sB0);
+        store_block16<BM, BN, TM, TN>(acc, s, Ending<EPI>(p, tc.g), m0, n0, wm, wn, lane, wave & 4 ? high : low);
+    } else {
+        store_tile16<BM, BN, TM, TN, EPI, OutT>(acc, s, m0, n0, wm, wn, lane, sOut);
+    }
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1960,6 +2068,72 @@ int32_t launch_gemm(const GemmPlan& plan, int32_t variant, hipStream_t stream) {
     // tiles and up; the one-element-per-lane kernel spreads its grid over three dimensions.
     if (st == SBP_ERR_UNSUPPORTED && variant == 0 && plan.epilogue != EPI_ROWMAX) return launch_generic(plan, max_m, max_n, stream);
     return st;
+}
+
+namespace {
+
+template <int B>   // 256: eight waves, 128: four
+int32_t launch_block_pipe16(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t st) {
+    constexpr int WM = 2, WN = B == 256 ? 4 : 2;
+    const int tm = tiles_along(max_m, B), tn = tiles_along(max_n, B);
+    const int64_t nblk = ((int64_t)tm * tn * plan.groups + 7) / 8 * 8;
+    if (!grid_fits(nblk, WM * WN * 64)) return SBP_ERR_UNSUPPORTED;
+    void (*kern)(GemmBlockPlan, int, int, int);
+    if (plan.a_kc) kern = plan.b_kc ? gemm_mfma_pipe16_kernel<B, B, WM, WN, true, true, 4, EPI_BLOCK, uint16_t> : gemm_mfma_pipe16_kernel<B, B, WM, WN, true, false, 4, EPI_BLOCK, uint16_t>;
+    else kern = plan.b_kc ? gemm_mfma_pipe16_kernel<B, B, WM, WN, false, true, 4, EPI_BLOCK, uint16_t> : gemm_mfma_pipe16_kernel<B, B, WM, WN, false, false, 4, EPI_BLOCK, uint16_t>;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)nblk), dim3(WM * WN * 64), 0, st, plan, tm, tn, tile_order_for(tm, tn));
+    return launch_status(__func__);
+}
+int32_t launch_block_generic(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream) {
+    const dim3 grid((uint32_t)tiles_along(max_n, 16), (uint32_t)tiles_along(max_m, 16), (uint32_t)plan.groups);
+    if (grid.y > 65535) return SBP_ERR_UNSUPPORTED;
+    if (plan.in_dtype == SBP_BF16) hipLaunchKernelGGL((gemm_generic_kernel<true, true, uint16_t, EPI_BLOCK>), grid, dim3(16, 16), 0, stream, plan);
+    else hipLaunchKernelGGL((gemm_generic_kernel<false, false, float, EPI_BLOCK>), grid, dim3(16, 16), 0, stream, plan);
+    return launch_status(__func__);
+}
+
+// The kernel for a product with a block's epilogue: launch_chosen's rules, over the kernels that have one.
+int32_t launch_block_chosen(const GemmBlockPlan& plan, const GemmPlan& like, int max_m, int max_n, hipStream_t stream) {
+    const bool bf16 = plan.in_dtype == SBP_BF16, direct = rows_aligned(like);
+    if (one_element_pays(like, max_m, max_n, bf16 && direct) || (bf16 && !mfma_ok(like))) return launch_block_generic(plan, max_m, max_n, stream);
+    auto order = [&](int bm, int bn) { return tile_order_for(tiles_along(max_m, bm), tiles_along(max_n, bn)); };
+    if (!bf16) {
+        const int tile = f32_tile(like, max_m, max_n), b = tile == F32_128 || tile == TERMS_128 ? 128 : tile == F32_64 || tile == TERMS_64 ? 64 : 32;
+        return launch_gemm_f32(plan, max_m, max_n, tile, order(b, b), stream);
+    }
+    auto any = [&](int tile) {
+        const int bm = tile == WAVEK_32 ? 32 : tile == WAVEK_64 || tile == REG_64 ? 64 : 128, bn = tile == REG_128 ? 128 : 64;
+        return launch_gemm_any(plan, max_m, max_n, tile, direct, order(bm, bn), stream);
+    };
+    if (!direct) return any(any_tile(like, max_m, max_n));
+    if (deep_pays(like, max_m, max_n)) {
+        const int tm = tiles_along(max_m, 128), tn = tiles_along(max_n, 128), band = deep_band(tm, tn, tiles_of(like, max_m, max_n, 128, 128));
+        const bool touch = !g_tile_order.load(std::memory_order_relaxed) && touches_pay(like, tm, tn, band);
+        return launch_gemm_deep(plan, max_m, max_n, touch ? band : tile_order_for(tm, tn), touch, stream);
+    }
+    if (wavek_pays(like, max_m, max_n)) return any(wavek_tile(like, max_m, max_n));
+    return large_tiles_pay(like, max_m, max_n) ? launch_block_pipe16<256>(plan, max_m, max_n, stream) : launch_block_pipe16<128>(plan, max_m, max_n, stream);
+}
+
+}  // namespace
+
+int32_t launch_linear(const GemmBlockPlan& plan, hipStream_t stream) {
+    GemmPlan like{};   // what the rules look at
+    like.groups = plan.groups;
+    like.in_dtype = plan.in_dtype;
+    like.out_dtype = plan.flags & GB_OUT_BF16 ? SBP_BF16 : SBP_F32;
+    like.a_kc = plan.a_kc;
+    like.b_kc = plan.b_kc;
+    int max_m = 0, max_n = 0;
+    for (int g = 0; g < plan.groups; ++g) {
+        like.s[g] = plan.s[g];
+        if (plan.s[g].m == 0 || plan.s[g].n == 0) continue;
+        max_m = std::max(max_m, plan.s[g].m);
+        max_n = std::max(max_n, plan.s[g].n);
+    }
+    if (max_m == 0) return SBP_OK;
+    const int32_t st = launch_block_chosen(plan, like, max_m, max_n, stream);
+    return st == SBP_ERR_UNSUPPORTED ? launch_block_generic(plan, max_m, max_n, stream) : st;   // as launch_gemm
 }
 
 }  // namespace sbp

@@ -65,17 +65,6 @@ void add_if(Buffers& b, bool out, const sbp_tensor_t* t, sbp_t s, int32_t k) {
     if (t) b.add(out, t, s, k);
 }
 
-// F(integral constant S, first shard, number): one device has a launch of its own size, others go eight at a time
-template <typename F>
-int32_t each_group(int32_t k, F&& f) {
-    if (k == 1) return f(std::integral_constant<int, 1>{}, 0, 1);
-    for (int32_t i = 0; i < k; i += RESNORM_SHARDS) {
-        const int32_t st = f(std::integral_constant<int, RESNORM_SHARDS>{}, i, std::min(k - i, RESNORM_SHARDS));
-        if (st != SBP_OK) return st;
-    }
-    return SBP_OK;
-}
-
 }  // namespace
 
 extern "C" {
@@ -114,7 +103,7 @@ int32_t sbp_residual_norm(const sbp_tensor_t* x, sbp_t sx, const sbp_norm_t* pos
     }
     if ((st = b.check()) != SBP_OK) return st;
     if (x->rows == 0 || x->cols == 0) return SBP_OK;
-    return each_group(k, [&](auto shards, int32_t first, int32_t n) {
+    return each_group<RESNORM_SHARDS>(k, [&](auto shards, int32_t first, int32_t n) {
         ResNormPlan<shards()> plan{};
         plan.cols = (int32_t)x->cols;
         plan.flags = flags_of(post, pre, weights);
@@ -206,7 +195,7 @@ int32_t sbp_residual_norm_grad(const sbp_tensor_t* x, sbp_t sx, const sbp_norm_t
         used += (int64_t)blocks[i] * 4 * x->cols;
     }
     const int32_t flags = flags_of(post, pre, weights) | (dh ? RN_DH : 0);
-    st = each_group(k, [&](auto shards, int32_t first, int32_t n) {
+    st = each_group<RESNORM_SHARDS>(k, [&](auto shards, int32_t first, int32_t n) {
         ResNormGradPlan<shards()> plan{};
         plan.cols = (int32_t)x->cols;
         plan.flags = flags;
@@ -223,7 +212,7 @@ int32_t sbp_residual_norm_grad(const sbp_tensor_t* x, sbp_t sx, const sbp_norm_t
         return launch_residual_norm_grad(plan, n, x->dtype, dr->dtype, dy ? dy->dtype : SBP_BF16, static_cast<hipStream_t>(stream));
     });
     if (st != SBP_OK || !sums) return st;
-    return each_group(k, [&](auto shards, int32_t first, int32_t n) {
+    return each_group<RESNORM_SHARDS>(k, [&](auto shards, int32_t first, int32_t n) {
         ResNormJoin<shards()> join{};
         join.cols = (int32_t)x->cols;
         join.flags = flags;

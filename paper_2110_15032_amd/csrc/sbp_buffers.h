@@ -1,5 +1,7 @@
 // Host side of the operators whose calls name many buffers: the buffers of a call, 8-bit tensors, activations and vectors.
 #pragma once
+#include <type_traits>
+
 #include "sbp_check.h"
 
 namespace sbp {
@@ -81,6 +83,18 @@ inline int32_t check_column(const sbp_tensor_t* t, int64_t n, sbp_t s, int32_t k
     if (t->dtype != SBP_F32 && !(bf16 && t->dtype == SBP_BF16)) return SBP_ERR_DTYPE;
     if (t->trans) return SBP_ERR_UNSUPPORTED;
     return check_tensor(t, s, k);
+}
+
+// Devices dealt out over launches: one has a launch of its own size, more go MOST at a time, as an argument block costs about a microsecond a KB
+// (a kernel that does nothing, us: 256 bytes 3.4, 1024 4.4, 4000 6.9).  F(integral constant: shards of the block, first shard, number of shards).
+template <int MOST, typename F>
+int32_t each_group(int32_t k, F&& f) {
+    if (k == 1) return f(std::integral_constant<int, 1>{}, 0, 1);
+    for (int32_t i = 0; i < k; i += MOST) {
+        const int32_t st = f(std::integral_constant<int, MOST>{}, i, std::min(k - i, MOST));
+        if (st != SBP_OK) return st;
+    }
+    return SBP_OK;
 }
 
 }  // namespace sbp

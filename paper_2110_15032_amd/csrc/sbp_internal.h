@@ -77,6 +77,8 @@ struct GemmShard {
 constexpr int32_t EPI_ROWMAX = 2;
 // GeLU through erfcf (about 1e-7) where SBP_EPI_GELU is the fit of gelu_fast (2.2e-5): see launch_chosen
 constexpr int32_t EPI_GELU_ERF = 3;
+// Bias, activation, residual (sbp_linear): GemmBlockPlan in GemmPlan's place
+constexpr int32_t EPI_BLOCK = 4;
 struct GemmPlan {
     GemmShard s[SBP_MAX_K];
     int32_t groups;
@@ -86,6 +88,22 @@ struct GemmPlan {
     int32_t a_kc, b_kc;
     int32_t epilogue;   // SBP_EPI_*
 };
+
+// C = act(A B + bias) + residual, pre = A B + bias.  A launch takes eight shards, as its argument block costs about a microsecond a KB.
+struct GemmExtra {
+    const void* bias;       // [n], null: none
+    const void* residual;   // [m][n], null: none
+    void* pre;              // [m][n], null: not wanted
+    int32_t ldr, ldp;
+};
+constexpr int GEMM_BLOCK_SHARDS = 8;
+enum GemmBlockFlags : int32_t { GB_BIAS_BF16 = 1, GB_RESIDUAL_BF16 = 2, GB_PRE_BF16 = 4, GB_OUT_BF16 = 8, GB_GELU = 16, GB_GELU_ERF = 32 };
+struct GemmBlockPlan {
+    GemmShard s[GEMM_BLOCK_SHARDS];
+    GemmExtra x[GEMM_BLOCK_SHARDS];
+    int32_t groups, in_dtype, a_kc, b_kc, flags;
+};
+int32_t launch_linear(const GemmBlockPlan& plan, hipStream_t stream);
 
 // variant: SBP_KNOB_GEMM_VARIANT.  The launch_gemm_* functions below return SBP_ERR_UNSUPPORTED, with nothing enqueued, for a
 // grid that cannot be launched (grid_fits).
@@ -106,8 +124,10 @@ enum AnyTile : int32_t {
     ROWS_64         // 64 x 64, the same
 };
 int32_t launch_gemm_any(const GemmPlan& plan, int max_m, int max_n, int tile, bool direct, int order, hipStream_t stream);
+int32_t launch_gemm_any(const GemmBlockPlan& plan, int max_m, int max_n, int tile, bool direct, int order, hipStream_t stream);   // not ROWS_*
 // gemm_any_kernels.hip, 128 x 128 tile, any operand layout, rows 16-byte aligned, any reduction length
 int32_t launch_gemm_deep(const GemmPlan& plan, int max_m, int max_n, int order, bool touch, hipStream_t stream);
+int32_t launch_gemm_deep(const GemmBlockPlan& plan, int max_m, int max_n, int order, bool touch, hipStream_t stream);
 // gemm_f32_kernels.hip: fp32 x fp32 (fp32 results, GeLU or no epilogue) and fp32 next to bf16 (f32_operand), any pitch and extent.
 enum F32Tile : int32_t {
     F32_128 = 0,   // 128 x 128
@@ -117,6 +137,7 @@ enum F32Tile : int32_t {
     TERMS_64
 };
 int32_t launch_gemm_f32(const GemmPlan& plan, int max_m, int max_n, int tile, int order, hipStream_t stream);
+int32_t launch_gemm_f32(const GemmBlockPlan& plan, int max_m, int max_n, int tile, int order, hipStream_t stream);
 // Compute units of the current device, asked of the runtime once per device and kept.
 int compute_units();
 // Diagnostic matrix-pipe loop (probe_kernels.hip); scratch: 1 MiB of device memory.
@@ -293,6 +314,29 @@ struct ClipSum {
 int32_t launch_square_sum(const ListPlan& plan, int devices, int blocks, hipStream_t stream);
 int32_t launch_square_join(const SquareJoin& join, int32_t k, hipStream_t stream);
 int32_t launch_clip(const ListPlan& plan, const ClipSum& sums, hipStream_t stream);
+
+// ---------------------------------------------------------------------------------------------
+// The gradient of a block's epilogue: da = dy gelu'(pre), and the sum of da (or of dy) over the rows.
+// ---------------------------------------------------------------------------------------------
+constexpr int LINEAR_GRAD_SHARDS = 8;
+struct LinearGradShard {
+    const void* dy;
+    const void* pre;      // null: no activation
+    const void* scales;   // of pre, 8 bits only
+    void* da;             // null: no activation
+    float* dbias;
+    float* part;          // [blocks][cols], where blocks > 1
+    int32_t rows, cols, lddy, ldp, lds, ldda, blocks;
+};
+template <int S>
+struct LinearGradPlan {
+    LinearGradShard s[S];
+    int32_t streams;      // of block8_device.h, chosen at the launch
+};
+template <int S>
+int32_t launch_linear_grad(const LinearGradPlan<S>& plan, int n, int32_t dy, int32_t pre, bool gelu, hipStream_t stream);
+// workgroups along the rows of a shard, each of which leaves a partial sum
+int32_t linear_grad_blocks(int64_t rows, int64_t cols, int32_t k);
 
 // ---------------------------------------------------------------------------------------------
 // The norms behind and in front of a block, with its gate and the residual.  A launch takes S shards: the argument block costs about a

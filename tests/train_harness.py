@@ -112,9 +112,19 @@ def normal(*shape, seed=0, scale=1.0):
     return scale * torch.randn(*shape, generator=g, dtype=torch.float64)
 
 
+def same(a, b):
+    """Equal bit for bit (tensors in 64 bits)."""
+    return torch.equal(a.contiguous().view(torch.int64), b.contiguous().view(torch.int64))
+
+
 def close(got, want, bound, what=""):
-    """|got - want| <= bound everywhere (tensors in 64 bits)."""
+    """|got - want| <= bound everywhere (tensors in 64 bits), and NaN where want is, there alone."""
     assert got.shape == want.shape, (what, got.shape, want.shape)
+    if got.numel() == 0:
+        return
+    none = want.isnan()
+    assert torch.equal(none, got.isnan()), f"{what}: NaN in other places"
+    got, want, bound = got[~none], want[~none], bound.expand(none.shape)[~none]
     if got.numel() == 0:
         return
     excess = (got - want).abs() - bound
