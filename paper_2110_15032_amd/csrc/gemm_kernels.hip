@@ -626,97 +626,140 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_kernel(GemmPlan p, int
     store_tile<BM, BN, TM, TN, FM, FN, EPI, OutT>(acc, s, m0, n0, wm, wn, lane, sOut);
 }
 
-// The block's epilogue (bias, activation, residual) for accumulators of v_mfma_f32_16x16x32_bf16, as store_tile16 has them.  Strips of 32 rows x 64
-// columns pass through a window of LDS in fp32, row pitch 256 bytes, the 64-byte groups of a row permuted by XOR with row / 4 % 4, which
-// puts the four rows of a write on four groups of banks; a lane then owns eight consecutive columns of a row, whose bias stays in registers.
-// Tiles inside the matrix: the residual of a strip is on its way before the strip is staged.  Tiles cut by the edge, and GeLU by erfc, whose code is
-// long, take a loop.
-constexpr int BLOCK_WINDOW = 32 * 64 * 4;
-template <int BM, int BN, int TM, int TN>
-__device__ __attribute__((always_inline)) inline void store_block16(const f32x4 (&acc)[TM / 16][TN / 16], const GemmShard& s, const Ending<EPI_BLOCK>& end, int m0, int n0, int wm, int wn,
-                                                                    int lane, char* win) {
-    static_assert(TN == 64, "a strip is 64 columns wide");
-    const int g = lane >> 4, c = lane & 15, h = lane >> 5;
-    const int m = m0 + wm * TM + (lane >> 3), n = n0 + wn * TN + (lane & 7) * 8;   // of this lane's first row and columns
+// The block's epilogue (bias, activation, residual) for accumulators of v_mfma_f32_16x16x32_bf16, as store_tile16 has them.  Strips of 16 rows x 64
+// columns pass through a wave's window of LDS in fp32, row pitch 256 bytes, the 64-byte groups of a row permuted by XOR with row / 4, which
+// puts the four rows of a write on four groups of banks; a lane then owns eight consecutive columns of a row, whose bias stays in registers.  The residual of
+// the next strip is on its way while one is worked on.  What the edge leaves of a row's last eight columns is done element by element behind
+// each strip, and so is GeLU by erfc, whose code is long.  Loads of the persistent kernel's next tile are waited for here, all of them, so that its first steps
+// need not; stores are outside the compiler's bookkeeping, as in store_tile16.
+template <int TM, int TN>
+__device__ __attribute__((always_inline)) inline void store_block16(const f32x4 (&acc)[TM / 16][TN / 16], const GemmShard& s, const Ending<EPI_BLOCK>& end, int m_first, int n_first, int lane,
+                                                                    char* win) {
+    static_assert(TN == 64 && STAGE_BYTES == 16 * 64 * 4, "a strip is 64 columns wide and fills a window");
+    asm volatile("" : "+v"(lane));   // as in store_tile16
+    const int g = lane >> 4, c = lane & 15;
+    const int m = m_first + (lane >> 3), n = n_first + (lane & 7) * 8;   // this lane's first row and columns
+    const int rows = s.m - m, rest = s.n - n_first < 64 ? (s.n - n_first) & 7 : 0;   // rest: columns behind the last whole eight (not positive: none of the wave's exist)
+    const bool full = n + 8 <= s.n;
     int w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) w[j] = 4 * g * 256 + (j ^ g) * 64 + c * 4;
     auto stage = [&](auto ix) __attribute__((always_inline)) {
         constexpr int i = decltype(ix)::value;
-        static_for<2>([&](auto ibx) {
-            static_for<4>([&](auto jx) {
-                static_for<4>([&](auto rx) {
-                    constexpr int ib = decltype(ibx)::value, j = decltype(jx)::value, r = decltype(rx)::value;
-                    *reinterpret_cast<float*>(win + (w[j] + (16 * ib + r) * 256)) = acc[2 * i + ib][j][r];
-                });
+        static_for<4>([&](auto jx) {
+            static_for<4>([&](auto rx) {
+                constexpr int j = decltype(jx)::value, r = decltype(rx)::value;
+                *reinterpret_cast<float*>(win + (w[j] + r * 256)) = acc[i][j][r];
             });
         });
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     };
-    auto take = [&](int q, float (&v)[8]) {   // row lane / 8 + 8 q of the strip
-        const char* const at = win + ((lane >> 3) + 8 * q) * 256 + (((lane & 7) >> 1) ^ (2 * (q & 1) + h)) * 64 + (lane & 1) * 32;
-        const f32x4 a = *reinterpret_cast<const f32x4*>(at), b = *reinterpret_cast<const f32x4*>(at + 16);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            v[e] = a[e];
-            v[4 + e] = b[e];
-        }
+    // element (row, column) of the staged strip through the epilogue
+    auto one = [&](int i, int row, int col) {
+        float v[1] = {*reinterpret_cast<const float*>(win + row * 256 + ((col >> 4) ^ (row >> 2)) * 64 + (col & 15) * 4)};
+        end.finish<1>(s, m_first + i * 16 + row, n_first + col, v);
     };
-    if (m0 + BM <= s.m && n0 + BN <= s.n && !(end.flags & GB_GELU_ERF)) {
-        float bias[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-        if (end.x.bias) read_columns<8>(end.x.bias, end.flags & GB_BIAS_BF16, n, 8, bias);
-        static_for<TM / 32>([&](auto ix) {
+    __builtin_amdgcn_s_waitcnt(vmcnt_only(0));
+    if (end.flags & GB_GELU_ERF) {
+        static_for<TM / 16>([&](auto ix) {
             constexpr int i = decltype(ix)::value;
-            u32x4 raw[4][2];   // bf16: the first half
-            if (end.x.residual) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const int64_t at = (int64_t)(m + i * 32 + 8 * q) * end.x.ldr + n;
-                    if (end.flags & GB_RESIDUAL_BF16) {
-                        raw[q][0] = *reinterpret_cast<const u32x4_any*>(static_cast<const uint16_t*>(end.x.residual) + at);
-                    } else {
-                        const float* const f = static_cast<const float*>(end.x.residual) + at;
-                        raw[q][0] = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(f));
-                        raw[q][1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(f + 4));
-                    }
-                }
-            }
+            if (m_first + i * 16 >= s.m || n_first >= s.n) return;   // uniform: nothing of the strip exists
             stage(ix);
-            static_for<4>([&](auto qx) {
-                constexpr int q = decltype(qx)::value;
-                float v[8], r[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
-                take(q, v);
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += bias[e];
-                if (end.x.residual) {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        if (end.flags & GB_RESIDUAL_BF16) {
-                            r[2 * e] = __uint_as_float(raw[q][0][e] << 16);
-                            r[2 * e + 1] = __uint_as_float(raw[q][0][e] & 0xFFFF0000u);
-                        } else {
-                            r[e] = __uint_as_float(raw[q][0][e]);
-                            r[4 + e] = __uint_as_float(raw[q][1][e]);
-                        }
-                    }
-                }
-                end.put<8>(s, m + i * 32 + 8 * q, n, 8, v, r);
-            });
-            __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll 1
+            for (int row = 0; row < 16; ++row) one(i, row, lane);
+            __builtin_amdgcn_wave_barrier();
         });
         return;
     }
-    static_for<TM / 32>([&](auto ix) {
-        constexpr int i = decltype(ix)::value;
-        if (m0 + wm * TM + i * 32 >= s.m || n0 + wn * TN >= s.n) return;   // uniform: nothing of the strip exists
-        stage(ix);
-#pragma unroll 1
-        for (int q = 0; q < 4; ++q) {
-            float v[8];
-            take(q, v);
-            end.finish<8>(s, m + i * 32 + 8 * q, n, v);
+    const bool out_bf16 = end.flags & GB_OUT_BF16, pre_bf16 = end.flags & GB_PRE_BF16, res_bf16 = end.flags & GB_RESIDUAL_BF16;
+    const bool out_nt = out_bf16 && s.ldc % 64 == 0, pre_nt = pre_bf16 && end.x.ldp % 64 == 0;   // whole cache lines past the caches
+    float bias[8] = {0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f, 0.0f};
+    if (end.x.bias && full) read_columns<8>(end.x.bias, end.flags & GB_BIAS_BF16, n, 8, bias);
+    // This lane's places, eight rows further with every turn t (rows lane / 8 + 8 t); opaque, or an address for every turn would be held in registers.
+    constexpr int TURNS = TM / 8;
+    const char* res = static_cast<const char*>(end.x.residual) + ((int64_t)m * end.x.ldr + n) * (res_bf16 ? 2 : 4);
+    char* pre = static_cast<char*>(end.x.pre) + ((int64_t)m * end.x.ldp + n) * (pre_bf16 ? 2 : 4);
+    char* out = static_cast<char*>(s.c) + ((int64_t)m * s.ldc + n) * (out_bf16 ? 2 : 4);
+    const int64_t res_step = (int64_t)end.x.ldr * (res_bf16 ? 16 : 32), pre_step = (int64_t)end.x.ldp * (pre_bf16 ? 16 : 32), out_step = (int64_t)s.ldc * (out_bf16 ? 16 : 32);
+    u32x4 ring[4];   // the residual of the turns to come: three in bf16, two in fp32
+    auto fetch = [&](auto tx) __attribute__((always_inline)) {
+        constexpr int t = decltype(tx)::value;
+        if constexpr (t < TURNS) {
+            if (full && 8 * t < rows) {
+                if (res_bf16) {
+                    ring[t & 3] = *reinterpret_cast<const u32x4_any*>(res);
+                } else {
+                    ring[2 * (t & 1)] = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(res));
+                    ring[2 * (t & 1) + 1] = __builtin_bit_cast(u32x4, *reinterpret_cast<const f32x4_any*>(res + 16));
+                }
+            }
+            res += res_step;
+            asm volatile("" : "+v"(res));
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    };
+    auto put = [&](char* to, bool bf16, bool nt, const float (&v)[8]) __attribute__((always_inline)) {
+        if (bf16) {
+            const u32x4 q = {f32_to_bf16x2(v[0], v[1]), f32_to_bf16x2(v[2], v[3]), f32_to_bf16x2(v[4], v[5]), f32_to_bf16x2(v[6], v[7])};
+            store16_untracked(reinterpret_cast<u32x4*>(to), q, nt);
+        } else {
+            store16_untracked(reinterpret_cast<f32x4*>(to), f32x4{v[0], v[1], v[2], v[3]}, false);
+            store16_untracked(reinterpret_cast<f32x4*>(to) + 1, f32x4{v[4], v[5], v[6], v[7]}, false);
+        }
+    };
+    if (end.x.residual) {
+        fetch(std::integral_constant<int, 0>{});
+        fetch(std::integral_constant<int, 1>{});
+        if (res_bf16) fetch(std::integral_constant<int, 2>{});
+    }
+    static_for<TM / 16>([&](auto ix) {
+        constexpr int i = decltype(ix)::value;
+        if (m_first + i * 16 >= s.m || n_first >= s.n) return;
+        stage(ix);
+        static_for<2>([&](auto qx) {
+            constexpr int q = decltype(qx)::value, t = 2 * i + q;
+            __builtin_amdgcn_sched_barrier(0);   // one turn at a time, for its registers
+            if (full && 8 * t < rows) {
+                const int row = (lane >> 3) + 8 * q;
+                const char* const from = win + row * 256 + (((lane & 7) >> 1) ^ (row >> 2)) * 64 + (lane & 1) * 32;
+                const f32x4 a = *reinterpret_cast<const f32x4*>(from), b = *reinterpret_cast<const f32x4*>(from + 16);
+                float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += bias[e];
+                if (end.x.pre) put(pre, pre_bf16, pre_nt, v);
+                if (end.flags & GB_GELU) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] = gelu_fast(v[e]);
+                }
+                if (end.x.residual) {
+                    if (res_bf16) {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            v[2 * e] += __uint_as_float(ring[t & 3][e] << 16);
+                            v[2 * e + 1] += __uint_as_float(ring[t & 3][e] & 0xFFFF0000u);
+                        }
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) {
+                            v[e] += __uint_as_float(ring[2 * (t & 1)][e]);
+                            v[4 + e] += __uint_as_float(ring[2 * (t & 1) + 1][e]);
+                        }
+                    }
+                }
+                put(out, out_bf16, out_nt, v);
+            }
+            pre += pre_step;
+            out += out_step;
+            asm volatile("" : "+v"(pre), "+v"(out));
+            if (end.x.residual) {
+                if (res_bf16) fetch(std::integral_constant<int, t + 3>{});
+                else fetch(std::integral_constant<int, t + 2>{});
+            }
+        });
+        if (rest) {   // row lane % 16, two rounds of four columns
+#pragma unroll 1
+            for (int e = lane >> 4; e < rest; e += 4) one(i, lane & 15, ((s.n - n_first) & ~7) + e);
+        }
+        __builtin_amdgcn_wave_barrier();
     });
 }
 
@@ -889,7 +932,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_pipe16_kernel(PlanOf<E
     __shared__ __attribute__((aligned(1024))) char sB2[TB::BYTES];
     __shared__ __attribute__((aligned(1024))) char sB3[NST > 3 ? TB::BYTES : 16];
     __shared__ __attribute__((aligned(1024))) char sB4[NST > 4 ? TB::BYTES : 16];
-    __shared__ __attribute__((aligned(1024))) char sOut[EPI == EPI_BLOCK ? 16 : WM * WN * STAGE_BYTES];   // epilogue windows, one per wave
+    __shared__ __attribute__((aligned(1024))) char sOut[WM * WN * STAGE_BYTES];   // epilogue windows, one per wave
     auto stA = [&](auto i) -> char* {
         constexpr int I = decltype(i)::value;
         if constexpr (I == 0) return sA0; else if constexpr (I == 1) return sA1; else if constexpr (I == 2) return sA2;
@@ -1012,16 +1055,8 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_pipe16_kernel(PlanOf<E
         mfmas(1, 0);
     }
 
-    if constexpr (EPI == EPI_BLOCK) {
-        // a stage of either operand is a wave's window: nobody reads them any more
-        static_assert(TA::BYTES >= BLOCK_WINDOW && TB::BYTES >= BLOCK_WINDOW && WM * WN <= 8, "a window for every wave");
-        __syncthreads();
-        char* const low = wave & 2 ? (wave & 1 ? sA3 : sA2) : (wave & 1 ? sA1 : sA0);
-        char* const high = wave & 2 ? (wave & 1 ? sB3 : sB2) : (wave & 1 ? sB1 : sB0);
-        store_block16<BM, BN, TM, TN>(acc, s, Ending<EPI>(p, tc.g), m0, n0, wm, wn, lane, wave & 4 ? high : low);
-    } else {
-        store_tile16<BM, BN, TM, TN, EPI, OutT>(acc, s, m0, n0, wm, wn, lane, sOut);
-    }
+    if constexpr (EPI == EPI_BLOCK) store_block16<TM, TN>(acc, s, Ending<EPI>(p, tc.g), m0 + wm * TM, n0 + wn * TN, lane, sOut + wave * STAGE_BYTES);
+    else store_tile16<BM, BN, TM, TN, EPI, OutT>(acc, s, m0, n0, wm, wn, lane, sOut);
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -1230,7 +1265,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_persist_kernel(GemmPla
 // elements 107 / 107 and 229 / 229.
 // ------------------------------------------------------------------------------------------------
 template <int BM, int BN, int WM, int WN, bool A_KC, bool B_KC, int NST, int EPI, typename OutT>
-__global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_persist16_kernel(GemmPlan p, int tm, int tn, int order, int nblk) {
+__global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_persist16_kernel(PlanOf<EPI> p, int tm, int tn, int order, int nblk) {
     constexpr int BKT = 32;
     constexpr int NT = WM * WN * 64;
     constexpr int TM = BM / WM, TN = BN / WN;
@@ -1357,7 +1392,7 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_persist16_kernel(GemmP
         mfmas(0, CUR & 1);
         pace<HM * FN, NDS_A, NS>();
         if constexpr (CUR % 2 == 1 || NS > 0) {
-            if constexpr (FRESH && (CUR == 0 || NP == 0)) __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0)
+            if constexpr (FRESH && (CUR == 0 || NP == 0 || EPI == EPI_BLOCK)) __builtin_amdgcn_s_waitcnt(0xC07F);   // lgkmcnt(0); a block's epilogue waits for the second pair too
             else if constexpr (FRESH) {
                 if (young) __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * NS + NSTORE) & ~0x0F00);
                 else __builtin_amdgcn_s_waitcnt(vmcnt_only(2 * NS) & ~0x0F00);
@@ -1420,7 +1455,13 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_persist16_kernel(GemmP
             step(I2{}, Old{}, false);
             step(I3{}, Old{}, false);
         }
-        store_tile16<BM, BN, TM, TN, EPI, OutT, true, NP>(acc, s, m0, n0, wm, wn, lane, sOut);
+        if constexpr (EPI == EPI_BLOCK) {   // what it needs is read here: held over the reduction loop, it took registers that the loop lacks
+            int g = tc.g;
+            asm volatile("" : "+s"(g));
+            store_block16<TM, TN>(acc, p.s[g], Ending<EPI>(p, g), m0 + wm * TM, n0 + wn * TN, lane, sOut + wave * STAGE_BYTES);
+        } else {
+            store_tile16<BM, BN, TM, TN, EPI, OutT, true, NP>(acc, s, m0, n0, wm, wn, lane, sOut);
+        }
         young = EPI != EPI_ROWMAX && !ends_inside<BN, OutT>(s, n0);
         cv = nv;
     }
@@ -2084,6 +2125,17 @@ int32_t launch_block_pipe16(const GemmBlockPlan& plan, int max_m, int max_n, hip
     hipLaunchKernelGGL(kern, dim3((uint32_t)nblk), dim3(WM * WN * 64), 0, st, plan, tm, tn, tile_order_for(tm, tn));
     return launch_status(__func__);
 }
+int32_t launch_block_persist16(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t st) {
+    const int tm = tiles_along(max_m, 256), tn = tiles_along(max_n, 256);
+    const int64_t nblk = ((int64_t)tm * tn * plan.groups + 7) / 8 * 8;
+    if (nblk > 0x7FFFFFFF) return SBP_ERR_UNSUPPORTED;
+    const int grid = (int)std::min<int64_t>(compute_units() / 8 * 8, nblk);
+    void (*kern)(GemmBlockPlan, int, int, int, int);
+    if (plan.a_kc) kern = plan.b_kc ? gemm_mfma_persist16_kernel<256, 256, 2, 4, true, true, 4, EPI_BLOCK, uint16_t> : gemm_mfma_persist16_kernel<256, 256, 2, 4, true, false, 4, EPI_BLOCK, uint16_t>;
+    else kern = plan.b_kc ? gemm_mfma_persist16_kernel<256, 256, 2, 4, false, true, 4, EPI_BLOCK, uint16_t> : gemm_mfma_persist16_kernel<256, 256, 2, 4, false, false, 4, EPI_BLOCK, uint16_t>;
+    hipLaunchKernelGGL(kern, dim3((uint32_t)grid), dim3(512), 0, st, plan, tm, tn, tile_order_for(tm, tn) & 0xFFFF, (int)nblk);
+    return launch_status(__func__);
+}
 int32_t launch_block_generic(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream) {
     const dim3 grid((uint32_t)tiles_along(max_n, 16), (uint32_t)tiles_along(max_m, 16), (uint32_t)plan.groups);
     if (grid.y > 65535) return SBP_ERR_UNSUPPORTED;
@@ -2112,7 +2164,10 @@ int32_t launch_block_chosen(const GemmBlockPlan& plan, const GemmPlan& like, int
         return launch_gemm_deep(plan, max_m, max_n, touch ? band : tile_order_for(tm, tn), touch, stream);
     }
     if (wavek_pays(like, max_m, max_n)) return any(wavek_tile(like, max_m, max_n));
-    return large_tiles_pay(like, max_m, max_n) ? launch_block_pipe16<256>(plan, max_m, max_n, stream) : launch_block_pipe16<128>(plan, max_m, max_n, stream);
+    if (!large_tiles_pay(like, max_m, max_n)) return launch_block_pipe16<128>(plan, max_m, max_n, stream);
+    for (int g = 0; g < like.groups; ++g)
+        if (like.s[g].m && like.s[g].n && (like.s[g].kk == 0 || like.s[g].kk % 128)) return launch_block_pipe16<256>(plan, max_m, max_n, stream);
+    return launch_block_persist16(plan, max_m, max_n, stream);
 }
 
 }  // namespace
