@@ -34,83 +34,158 @@ int32_t check_list(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k) 
 }
 int32_t check_scalar(const sbp_tensor_t* t, int32_t k) { return check_column(t, 1, SBP_B, k, false); }
 
-// What device i counts of tensor t.
-struct Counted {
-    const char* at;
-    Stored s;
+// A local tensor of a list: what device i counts of it, or (clipping) holds of it.
+struct Item {
+    const char* in;
+    char* out;
+    Stored s;              // as_rows()
+    int64_t ldo;
+    int32_t what;          // without the device
+    int64_t chunks;
 };
-Counted counted(const sbp_tensor_t* t, sbp_t s, int32_t k, int32_t i) {
+bool counted(const sbp_tensor_t* t, sbp_t s, int32_t k, int32_t i, Item& to) {
     Stored l = stored_of(t, s, k, i);
+    if (l.rows * l.cols == 0) return false;
     const bool dense = l.pitch == l.cols;
     const char* at = static_cast<const char*>(t->shard[i]);
-    if (s == SBP_B && l.rows * l.cols) {
+    if (s == SBP_B) {   // its share of the stored rows
         at += split_begin(l.rows, k, i) * l.pitch * elem_bytes(t->dtype);
         l.rows = split_len(l.rows, k, i);
+        if (l.rows == 0) return false;
     }
-    return {at, as_rows(l, dense)};
+    const Stored r = as_rows(l, dense);
+    to = {at, nullptr, r, 0, of_list(t->dtype == SBP_BF16, false, 0), chunks_of(r)};
+    return true;
+}
+bool clipped(const sbp_tensor_t* in, const sbp_tensor_t* out, sbp_t s, int32_t k, int32_t i, Item& to) {
+    const Stored a = stored_of(in, s, k, i), o = stored_of(out, s, k, i);
+    if (a.rows * a.cols == 0) return false;
+    const Stored r = as_rows(a, a.pitch == a.cols && o.pitch == o.cols);
+    to = {static_cast<const char*>(in->shard[i]), static_cast<char*>(out->shard[i]), r, o.pitch, of_list(in->dtype == SBP_BF16, out->dtype == SBP_BF16, 0), chunks_of(r)};
+    return true;
 }
 
-// The launches of a sum of squares: devices in turn, parts of each in order, as many as a launch takes.  `blocks` workgroups for every
-// device in every launch, each of which leaves a partial sum; device d's lie from d * turns * blocks on, launch by launch.
-struct SquarePlan {
-    int blocks;
-    int32_t turns;
-    int32_t used[SBP_MAX_K];   // launches that a device has parts in
+// Local tensors of one launch, in the order of their devices.
+struct Batch {
+    Item item[LIST_DENSE];
+    int32_t device[LIST_DENSE];
+    int32_t n, first_device, devices;
+    int32_t turn;          // launches that the first device has parts in already
+    int64_t chunks, most;  // all, and the most of a device
 };
-template <typename F>   // F(plan, devices of the launch): a full launch
-int32_t each_launch(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, SquarePlan& sq, ListPlan& plan, F&& launch) {
-    for (int32_t d = 0; d < k; ++d) sq.used[d] = 0;
-    int devices = 0;
-    int64_t chunk = 0;
-    plan.parts = 0;
-    plan.chunk0[0] = 0;
-    auto flush = [&]() {
-        const int32_t st = devices ? launch(plan, devices) : SBP_OK;
-        devices = 0;
-        chunk = 0;
-        plan.parts = 0;
-        return st;
-    };
+// F(batch) for the local tensors that lie in one row, or for those with rows at a pitch; ITEM(tensor, device, item): false where there is nothing.
+// used: batches that a device has parts in.
+template <typename ITEM, typename F>
+int32_t each_batch(int32_t n, int32_t k, bool dense, Batch& b, int16_t* used, ITEM&& make, F&& f) {
+    const int32_t cap = dense ? LIST_DENSE : LIST_PITCHED;
+    b.n = 0;
     for (int32_t d = 0; d < k; ++d) {
-        bool open = false;   // this device has its place in the launch being filled
+        used[d] = 0;
+        int64_t mine = 0;   // chunks of this device in the batch
         for (int32_t j = 0; j < n; ++j) {
-            const Local l = local_of(t[j].rows, t[j].cols, s[j], k, d);
-            if (l.rows * l.cols == 0) continue;
-            const Counted c = counted(t + j, s[j], k, d);
-            const int64_t chunks = chunks_of(c.s);
-            if (chunks == 0) continue;
-            if (chunks > INT32_MAX / 2) return SBP_ERR_UNSUPPORTED;
-            if (plan.parts == LIST_PARTS || chunk + chunks > INT32_MAX / 2) {
-                const int32_t st = flush();
+            Item it;
+            if (!make(j, d, it) || (it.s.rows == 1) != dense) continue;
+            if (it.chunks > INT32_MAX / 2) return SBP_ERR_UNSUPPORTED;
+            if (b.n && (b.n == cap || b.chunks + it.chunks > INT32_MAX / 2)) {
+                const int32_t st = f(b);
                 if (st != SBP_OK) return st;
-                open = false;
+                b.n = 0;
             }
-            if (!open) {
-                plan.slot[devices] = d * sq.turns + sq.used[d]++;
-                ++devices;
-                open = true;
+            if (b.n == 0) {
+                b.first_device = d;
+                b.turn = used[d];
+                b.chunks = b.most = mine = 0;
             }
-            plan.first[plan.parts] = (int32_t)chunk;
-            plan.s[plan.parts++] = {c.at, nullptr, c.s.cols, (int32_t)c.s.rows, (int32_t)c.s.pitch, 0, t[j].dtype == SBP_BF16 ? 1 : 0};
-            chunk += chunks;
-            plan.chunk0[devices] = (int32_t)chunk;
+            if (mine == 0) ++used[d];
+            b.item[b.n] = it;
+            b.device[b.n++] = d - b.first_device;
+            b.devices = d - b.first_device + 1;
+            b.chunks += it.chunks;
+            mine += it.chunks;
+            b.most = std::max(b.most, mine);
         }
     }
-    return flush();
+    return b.n ? f(b) : SBP_OK;
 }
-int32_t plan_squares(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, SquarePlan& sq, ListPlan& plan) {
-    sq.turns = 0;
+template <bool OUT>
+DensePart<OUT> dense_part(const Item& it, int32_t device) {
+    const uint64_t info = (uint64_t)it.s.cols | (uint64_t)(it.what | device << 2) << 48;
+    if constexpr (OUT) return {it.in, it.out, info};
+    else return {it.in, info};
+}
+template <bool OUT>
+PitchedPart<OUT> pitched_part(const Item& it, int32_t device) {
+    return {it.in, it.out, (int32_t)it.s.rows, (int32_t)it.s.cols, (int32_t)it.s.pitch, (int32_t)it.ldo, it.what | device << 2};
+}
+
+// How a sum of squares is dealt out.
+struct SquareShape {
+    int32_t blocks;                                    // workgroups of every device in every launch
+    int32_t dense_turns, turns;                        // places of a device's partial sums, in units of them
+    int16_t dense[SBP_MAX_K], pitched[SBP_MAX_K];      // launches that a device has parts in
+    int64_t bytes(int32_t k) const { return (int64_t)k * turns * blocks * 8; }
+};
+int32_t square_shape(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, SquareShape& sq, Batch& b) {
     int64_t most = 1;
-    int devices_most = 1;
-    const int32_t st = each_launch(t, s, n, k, sq, plan, [&](const ListPlan& p, int devices) {
-        devices_most = std::max(devices_most, devices);
-        for (int d = 0; d < devices; ++d) most = std::max<int64_t>(most, p.chunk0[d + 1] - p.chunk0[d]);
+    int32_t devices = 1, st;
+    auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], k, d, it); };
+    auto look = [&](const Batch& b) {
+        most = std::max(most, b.most);
+        devices = std::max(devices, b.devices);
         return (int32_t)SBP_OK;
-    });
-    if (st != SBP_OK) return st;
-    sq.blocks = (int)std::min<int64_t>(most, std::max(1, LIST_BLOCKS / devices_most));
-    for (int32_t d = 0; d < k; ++d) sq.turns = std::max(sq.turns, sq.used[d]);
+    };
+    if ((st = each_batch(n, k, true, b, sq.dense, make, look)) != SBP_OK) return st;
+    if ((st = each_batch(n, k, false, b, sq.pitched, make, look)) != SBP_OK) return st;
+    sq.blocks = (int32_t)std::min<int64_t>(most, std::max(1, LIST_BLOCKS / devices));
+    sq.dense_turns = *std::max_element(sq.dense, sq.dense + k);
+    sq.turns = sq.dense_turns + *std::max_element(sq.pitched, sq.pitched + k);
     return SBP_OK;
+}
+template <template <bool> class PART, int CAP, typename MAKE>
+int32_t square_batch(const Batch& b, const SquareShape& sq, int32_t base, double* partial, MAKE&& make, hipStream_t stream) {
+    SquarePlan<PART, CAP> plan;
+    for (int32_t i = 0; i < CAP; ++i) plan.s[i] = i < b.n ? make(b.item[i], b.device[i]) : PART<false>{};
+    plan.partial = partial;
+    plan.parts = b.n;
+    plan.first_device = b.first_device;
+    plan.turns = sq.turns;
+    plan.first_turn = base + b.turn;
+    plan.other_turn = base;
+    return launch_square_sum(plan, b.devices, sq.blocks, stream);
+}
+template <int S>
+int32_t square_join(const SquareShape& sq, const double* partial, const sbp_tensor_t* out, int32_t k, hipStream_t stream) {
+    SquareJoin<S> join{};
+    join.partial = partial;
+    join.blocks = sq.blocks;
+    join.turns = sq.turns;
+    join.dense_turns = sq.dense_turns;
+    for (int32_t d = 0; d < k; ++d) {
+        join.dense[d] = sq.dense[d];
+        join.pitched[d] = sq.pitched[d];
+        join.out[d] = static_cast<float*>(out->shard[d]);
+    }
+    return launch_square_join(join, k, stream);
+}
+template <template <bool> class PART, int CAP, int S, typename MAKE>
+int32_t clip_batch(const Batch& b, const sbp_tensor_t* squares, bool partial, float most, const sbp_tensor_t* norm, int32_t k, MAKE&& make, hipStream_t stream) {
+    ClipPlan<PART, CAP, S> plan{};
+    for (int32_t i = 0; i < b.n; ++i) plan.s[i] = make(b.item[i], b.device[i]);
+    for (int32_t i = 0; i < k; ++i) {
+        plan.sum[i] = static_cast<const float*>(squares->shard[i]);
+        plan.norm[i] = norm ? static_cast<float*>(norm->shard[i]) : nullptr;
+    }
+    plan.most = most;
+    plan.parts = b.n;
+    plan.chunks = (int32_t)b.chunks;
+    plan.k = k;
+    plan.partial = partial;
+    plan.first_device = b.first_device;
+    return launch_clip(plan, stream);
+}
+template <template <bool> class PART, int CAP, typename MAKE>
+int32_t clip_devices(const Batch& b, const sbp_tensor_t* squares, bool partial, float most, const sbp_tensor_t* norm, int32_t k, MAKE&& make, hipStream_t stream) {
+    return k <= 8 ? clip_batch<PART, CAP, 8>(b, squares, partial, most, norm, k, make, stream) : clip_batch<PART, CAP, SBP_MAX_K>(b, squares, partial, most, norm, k, make, stream);
 }
 
 }  // namespace
@@ -121,10 +196,10 @@ int32_t sbp_square_sum_workspace(const sbp_tensor_t* t, const sbp_t* s, int32_t 
     if (!bytes) return SBP_ERR_NULL;
     int32_t st;
     if ((st = check_list(t, s, n, k)) != SBP_OK) return st;
-    SquarePlan sq;
-    ListPlan plan;
-    if ((st = plan_squares(t, s, n, k, sq, plan)) != SBP_OK) return st;
-    *bytes = (int64_t)k * sq.turns * sq.blocks * 8;
+    SquareShape sq;
+    Batch batch;
+    if ((st = square_shape(t, s, n, k, sq, batch)) != SBP_OK) return st;
+    *bytes = sq.bytes(k);
     return SBP_OK;
 }
 
@@ -132,10 +207,10 @@ int32_t sbp_square_sum(const sbp_tensor_t* t, const sbp_t* s, int32_t n, const s
     int32_t st;
     if ((st = check_list(t, s, n, k)) != SBP_OK) return st;
     if ((st = check_scalar(out, k)) != SBP_OK) return st;
-    SquarePlan sq;
-    ListPlan plan;
-    if ((st = plan_squares(t, s, n, k, sq, plan)) != SBP_OK) return st;
-    const int64_t room = (int64_t)k * sq.turns * sq.blocks * 8;
+    SquareShape sq;
+    Batch batch;
+    if ((st = square_shape(t, s, n, k, sq, batch)) != SBP_OK) return st;
+    const int64_t room = sq.bytes(k);
     if (room) {
         if (!workspace) return SBP_ERR_NULL;
         if (reinterpret_cast<uintptr_t>(workspace) & 15u) return SBP_ERR_ALIGN;
@@ -150,17 +225,20 @@ int32_t sbp_square_sum(const sbp_tensor_t* t, const sbp_t* s, int32_t n, const s
         b.add(false, t + j, s[j], k);
         if ((st = b.check()) != SBP_OK) return st;
     }
-    plan.partial = static_cast<double*>(workspace);
-    st = each_launch(t, s, n, k, sq, plan, [&](const ListPlan& p, int devices) { return launch_square_sum(p, devices, sq.blocks, static_cast<hipStream_t>(stream)); });
+    double* const partial = static_cast<double*>(workspace);
+    const hipStream_t on = static_cast<hipStream_t>(stream);
+    auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], k, d, it); };
+    int16_t used[SBP_MAX_K];
+    st = each_batch(n, k, true, batch, used, make, [&](const Batch& b) {
+        return b.n <= LIST_FEW ? square_batch<DensePart, LIST_FEW>(b, sq, 0, partial, dense_part<false>, on) : square_batch<DensePart, LIST_DENSE>(b, sq, 0, partial, dense_part<false>, on);
+    });
     if (st != SBP_OK) return st;
-    SquareJoin join{};
-    join.partial = plan.partial;
-    join.per_device = (int64_t)sq.turns * sq.blocks;
-    for (int32_t d = 0; d < k; ++d) {
-        join.count[d] = sq.used[d] * sq.blocks;
-        join.out[d] = static_cast<float*>(out->shard[d]);
-    }
-    return launch_square_join(join, k, static_cast<hipStream_t>(stream));
+    st = each_batch(n, k, false, batch, used, make, [&](const Batch& b) {
+        return b.n <= LIST_FEW ? square_batch<PitchedPart, LIST_FEW>(b, sq, sq.dense_turns, partial, pitched_part<false>, on)
+                               : square_batch<PitchedPart, LIST_PITCHED>(b, sq, sq.dense_turns, partial, pitched_part<false>, on);
+    });
+    if (st != SBP_OK) return st;
+    return k <= 8 ? square_join<8>(sq, partial, out, k, on) : square_join<SBP_MAX_K>(sq, partial, out, k, on);
 }
 
 int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_tensor_t* squares, sbp_t sbp_squares, float max_norm, const sbp_tensor_t* out,
@@ -220,41 +298,29 @@ int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_te
     std::free(outs);
     if (!good) return SBP_ERR_ALIAS;
 
-    ClipSum sums{};
-    sums.most = max_norm;
-    sums.k = k;
-    sums.partial = sbp_squares == SBP_P_SUM;
-    for (int32_t i = 0; i < k; ++i) {
-        sums.sum[i] = static_cast<const float*>(squares->shard[i]);
-        sums.norm[i] = norm ? static_cast<float*>(norm->shard[i]) : nullptr;
-    }
-    ListPlan plan{};
-    int64_t chunk = 0;
-    bool launched = false;
-    auto flush = [&]() {
-        plan.chunk0[1] = (int32_t)chunk;
-        const int32_t status = launch_clip(plan, sums, static_cast<hipStream_t>(stream));
-        for (int32_t i = 0; i < k; ++i) sums.norm[i] = nullptr;   // the first launch writes it
-        plan.parts = 0;
-        chunk = 0;
-        launched = true;
+    const hipStream_t on = static_cast<hipStream_t>(stream);
+    const bool partial = sbp_squares == SBP_P_SUM;
+    auto make = [&](int32_t j, int32_t d, Item& it) { return clipped(in + j, out + j, s[j], k, d, it); };
+    int16_t used[SBP_MAX_K];
+    Batch batch;
+    const sbp_tensor_t* to = norm;   // the first launch writes it
+    st = each_batch(n, k, true, batch, used, make, [&](const Batch& b) {
+        const int32_t status = b.n <= LIST_FEW ? clip_devices<DensePart, LIST_FEW>(b, squares, partial, max_norm, to, k, dense_part<true>, on)
+                                               : clip_devices<DensePart, LIST_DENSE>(b, squares, partial, max_norm, to, k, dense_part<true>, on);
+        to = nullptr;
         return status;
-    };
-    for (int32_t i = 0; i < k; ++i)
-        for (int32_t j = 0; j < n; ++j) {
-            const Stored a = stored_of(in + j, s[j], k, i), o = stored_of(out + j, s[j], k, i);
-            if (a.rows * a.cols == 0) continue;
-            const bool dense = a.pitch == a.cols && o.pitch == o.cols;
-            const Stored l = as_rows(a, dense);
-            const int64_t chunks = chunks_of(l);
-            if (plan.parts == LIST_PARTS || chunk + chunks > INT32_MAX / 2)
-                if ((st = flush()) != SBP_OK) return st;
-            plan.first[plan.parts] = (int32_t)chunk;
-            plan.s[plan.parts++] = {in[j].shard[i], out[j].shard[i], l.cols, (int32_t)l.rows, (int32_t)a.pitch, (int32_t)o.pitch,
-                                    (in[j].dtype == SBP_BF16 ? 1 : 0) | (out[j].dtype == SBP_BF16 ? 2 : 0) | i << 2};
-            chunk += chunks;
-        }
-    return plan.parts || (norm && !launched) ? flush() : SBP_OK;
+    });
+    if (st != SBP_OK) return st;
+    st = each_batch(n, k, false, batch, used, make, [&](const Batch& b) {
+        const int32_t status = b.n <= LIST_FEW ? clip_devices<PitchedPart, LIST_FEW>(b, squares, partial, max_norm, to, k, pitched_part<true>, on)
+                                               : clip_devices<PitchedPart, LIST_PITCHED>(b, squares, partial, max_norm, to, k, pitched_part<true>, on);
+        to = nullptr;
+        return status;
+    });
+    if (st != SBP_OK || !to) return st;
+    batch.n = 0;   // nothing but the norm
+    batch.chunks = batch.first_device = 0;
+    return clip_devices<DensePart, LIST_FEW>(batch, squares, partial, max_norm, to, k, dense_part<true>, on);
 }
 
 }  // extern "C"

@@ -2,72 +2,132 @@
 //
 //   s_i = sum over the tensors of x^2 over what device i counts,  norm = sqrt(sum of s_i),  out = x min(1, max_norm / norm)
 //
-// Both are bound by HBM.  A launch takes PARTS local tensors, which its argument block names; their vectors of eight elements are numbered
-// through, a workgroup takes 1024 of them at a time (a chunk, of one tensor) and finds the tensor among the parts with one comparison a lane.
+// Both are bound by HBM.  The argument block of a launch names local tensors (parts); their vectors of eight elements are numbered
+// through, a workgroup takes 1024 of them at a time (a chunk, of one part).  Where a part's chunks start is summed up over the lanes of every wave, so that the
+// argument block need not hold it.
 #include "block8_device.h"
 
 namespace sbp {
 namespace {
 
 constexpr int NT = 256, PER = LIST_CHUNK / NT;
+constexpr uint64_t ELEMENTS = ((uint64_t)1 << 48) - 1;
 
-// A chunk's part: the last whose first chunk is not behind it.  Every lane looks at two of the first chunks (LIST_PARTS <= 128).
-struct PartOf {
-    int32_t a, b;
-    __device__ PartOf(const ListPlan& p) {
+// A part as the kernels see it: `count` elements in one row (rows 1), or rows of `cols` at a pitch.
+struct Shape {
+    int64_t cols;
+    int32_t rows, ldi, ldo, what;
+};
+template <bool OUT>
+__device__ inline Shape shape_of(const DensePart<OUT>& s) { return {(int64_t)(s.info & ELEMENTS), 1, 0, 0, (int32_t)(s.info >> 48)}; }
+template <bool OUT>
+__device__ inline Shape shape_of(const PitchedPart<OUT>& s) { return {s.cols, s.rows, s.ldi, s.ldo, s.what}; }
+__device__ inline int chunks_of(const Shape& s) {
+    const int64_t vectors = s.rows == 1 ? (s.cols + 7) / 8 : s.rows * ((s.cols + 7) / 8);
+    return (int)((vectors + LIST_CHUNK - 1) / LIST_CHUNK);
+}
+
+// First chunk of every part: lane l holds those of parts l, l + 64, l + 128.
+template <int CAP>
+struct Starts {
+    static constexpr int N = (CAP + 63) / 64;
+    int32_t start[N], total;
+    int32_t device[N];   // of a part, behind the last one a number that is none
+    template <typename PART>
+    __device__ Starts(const PART (&s)[CAP], int parts) {
         const int lane = threadIdx.x & 63;
-        a = lane < p.parts ? p.first[lane] : INT32_MAX;
-        b = lane + 64 < p.parts ? p.first[lane + 64] : INT32_MAX;
+        total = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int at = i * 64 + lane;
+            int mine = 0;
+            device[i] = INT32_MAX;
+            if (at < parts) {
+                const Shape h = shape_of(s[at]);
+                mine = chunks_of(h);
+                device[i] = h.what >> 2;
+            }
+            int sum = mine;
+#pragma unroll
+            for (int off = 1; off < 64; off <<= 1) {
+                const int other = __shfl_up(sum, off, 64);
+                sum += lane >= off ? other : 0;
+            }
+            start[i] = at < parts ? total + sum - mine : INT32_MAX;
+            total += __shfl(sum, 63, 64);
+        }
     }
-    __device__ int operator()(int chunk) const {
-        return __popcll(__builtin_amdgcn_ballot_w64(a <= chunk)) + __popcll(__builtin_amdgcn_ballot_w64(b <= chunk)) - 1;
+    // parts of devices before the d-th
+    __device__ int parts_before(int d) const {
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(device[i] < d));
+        return n;
+    }
+    __device__ int start_of(int part) const {   // part is uniform; behind the last one the number of chunks
+        int v = total;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (part >> 6 == i) v = __builtin_amdgcn_readlane(start[i], part & 63);
+        return v == INT32_MAX ? total : v;
+    }
+    __device__ int part_of(int chunk) const {
+        int n = -1;
+#pragma unroll
+        for (int i = 0; i < N; ++i) n += __popcll(__builtin_amdgcn_ballot_w64(start[i] <= chunk));
+        return n;
     }
 };
 
-// Vector `off` of a chunk: row and first column, from the chunk's first vector on.
-struct Place {
-    int64_t row;     // of the chunk's first vector
-    int64_t vector;  // in that row
-    int32_t per_row;
-    bool single;
-    __device__ Place(const ListPart& s, int chunk) {
-        const int64_t first = (int64_t)chunk * LIST_CHUNK;
-        single = s.rows == 1;
-        per_row = single ? 0 : (int32_t)((s.cols + 7) / 8);
-        row = single ? 0 : first / per_row;
-        vector = single ? first : first - row * per_row;
-    }
-};
-
-// F(row, column, length of the row from the column that the pointer stands for on): of every vector of the chunk that exists.
+// F(turn, row, first column that the pointer stands for, column from there on, length of the row from there on) of the chunk's vectors.  The first
+// column counts from the row's start in 64 bits, as a dense tensor may be longer than 2^31.
 template <typename F>
-__device__ inline void each_vector(const ListPart& s, int chunk, F&& f) {
-    const Place at(s, chunk);
+__device__ inline void each_vector(const Shape& s, int chunk, F&& f) {
+    const int64_t first = (int64_t)chunk * LIST_CHUNK;
+    if (s.rows == 1) {
+        const int64_t left = s.cols - first * 8;
+#pragma unroll
+        for (int u = 0; u < PER; ++u) f(u, (int64_t)0, first * 8, (u * NT + (int)threadIdx.x) * 8, (int)(left < LIST_CHUNK * 8 + 8 ? left : LIST_CHUNK * 8 + 8));
+        return;
+    }
+    const int32_t per_row = (int32_t)((s.cols + 7) / 8);
+    const int64_t row0 = first / per_row;
+    const uint32_t vector0 = (uint32_t)(first - row0 * per_row);
 #pragma unroll
     for (int u = 0; u < PER; ++u) {
-        const int off = u * NT + (int)threadIdx.x;
-        if (at.single) {   // columns counted from the chunk's start, as a row may be longer than 2^31
-            const int64_t left = s.cols - at.vector * 8;
-            f(u, (int64_t)0, at.vector * 8, off * 8, (int)(left < LIST_CHUNK * 8 + 8 ? left : LIST_CHUNK * 8 + 8));
-        } else {
-            uint32_t v = (uint32_t)at.vector + (uint32_t)off, r = 0;
-            if (at.per_row > LIST_CHUNK) {
-                if (v >= (uint32_t)at.per_row) {
-                    v -= (uint32_t)at.per_row;
-                    r = 1;
-                }
-            } else {
-                r = v / (uint32_t)at.per_row;
-                v -= r * (uint32_t)at.per_row;
+        uint32_t v = vector0 + (uint32_t)(u * NT) + threadIdx.x, r = 0;
+        if (per_row > LIST_CHUNK) {
+            if (v >= (uint32_t)per_row) {
+                v -= (uint32_t)per_row;
+                r = 1;
             }
-            const int64_t row = at.row + r;
-            f(u, row, (int64_t)0, (int)v * 8, row < s.rows ? (int)s.cols : 0);
+        } else {
+            r = v / (uint32_t)per_row;
+            v -= r * (uint32_t)per_row;
+        }
+        const int64_t row = row0 + r;
+        f(u, row, (int64_t)0, (int)v * 8, row < s.rows ? (int)s.cols : 0);
+    }
+}
+// all of the chunk's vectors are whole ones of one row
+__device__ inline bool whole_chunk(const Shape& s, int chunk) { return s.rows == 1 && ((int64_t)chunk + 1) * (LIST_CHUNK * 8) <= s.cols; }
+template <int T>
+__device__ inline void load_whole(const void* in, int chunk, Raw8<T> (&raw)[PER]) {
+    const char* const from = static_cast<const char*>(in) + ((int64_t)chunk * LIST_CHUNK + threadIdx.x) * (8 * bytes_of<T>);
+#pragma unroll
+    for (int u = 0; u < PER; ++u) {
+        const char* const at = from + u * (NT * 8 * bytes_of<T>);
+        if constexpr (T == T_F32) {
+            raw[u].a = *reinterpret_cast<const f32x4*>(at);
+            raw[u].b = *reinterpret_cast<const f32x4*>(at + 16);
+        } else {
+            raw[u].w = *reinterpret_cast<const u32x4*>(at);
         }
     }
 }
 
-// Squares are summed in 64 bits: neither the number of elements nor their size loses anything before the sum is rounded to fp32, and
-// the conversion and the fused product of eight elements cost less than loading them.  Lane, wave and workgroup sums in an order of the sizes alone.
+// Squares are summed in 64 bits: neither the number of elements nor their size loses anything before the sum is rounded to fp32.  Lane, wave and workgroup
+// sums in an order of the sizes alone.
 __device__ inline double sum_block(double v, double* waves) {
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
@@ -78,106 +138,151 @@ __device__ inline double sum_block(double v, double* waves) {
     for (int w = 1; w < NT / 64; ++w) v += waves[w];
     return v;
 }
+__device__ inline void add_squares(const float (&v)[8], double (&acc)[2]) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e & 1] = fma((double)v[e], (double)v[e], acc[e & 1]);
+}
 
 template <int T>
-__device__ inline void square_chunk(const ListPart& s, int chunk, double (&acc)[2]) {
+__device__ inline void square_chunk(const void* in, const Shape& s, int chunk, double (&acc)[2]) {
     Raw8<T> raw[PER];
-    each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) {
-        raw[u] = load8<T>(static_cast<const char*>(s.in) + (row * s.ldi + from) * bytes_of<T>, c, cols);
-    });
-    each_vector(s, chunk, [&](int u, int64_t, int64_t, int c, int cols) {
-        float v[8];
-        widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
+    float v[8];
+    if (whole_chunk(s, chunk)) {
+        load_whole<T>(in, chunk, raw);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) acc[e & 1] = fma((double)v[e], (double)v[e], acc[e & 1]);
+        for (int u = 0; u < PER; ++u) {
+            widen<T>(raw[u], 1.0f, v);
+            add_squares(v, acc);
+        }
+        return;
+    }
+    each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) { raw[u] = load8<T>(static_cast<const char*>(in) + (row * s.ldi + from) * bytes_of<T>, c, cols); });
+    each_vector(s, chunk, [&](int u, int64_t, int64_t, int c, int cols) {
+        widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
+        add_squares(v, acc);
     });
 }
 
-__global__ __launch_bounds__(NT) void square_sum_kernel(ListPlan p) {
+template <template <bool> class PART, int CAP>
+__global__ __launch_bounds__(NT) void square_sum_kernel(SquarePlan<PART, CAP> p) {
     __shared__ double waves[NT / 64];
-    const PartOf part_of(p);
-    const int d = blockIdx.y;
+    const Starts<CAP> starts(p.s, p.parts);
+    const int d = blockIdx.y, end = starts.start_of(starts.parts_before(d + 1));
     double acc[2] = {0.0, 0.0};
-    for (int c = p.chunk0[d] + blockIdx.x; c < p.chunk0[d + 1]; c += gridDim.x) {
-        const int part = __builtin_amdgcn_readfirstlane(part_of(c));
-        const ListPart& s = p.s[part];
-        const int chunk = c - p.first[part];
-        if (s.types & 1) square_chunk<T_BF16>(s, chunk, acc);
-        else square_chunk<T_F32>(s, chunk, acc);
+    for (int c = starts.start_of(starts.parts_before(d)) + blockIdx.x; c < end; c += gridDim.x) {
+        const int part = __builtin_amdgcn_readfirstlane(starts.part_of(c));
+        const Shape s = shape_of(p.s[part]);
+        const int chunk = c - starts.start_of(part);
+        if (s.what & 1) square_chunk<T_BF16>(p.s[part].in, s, chunk, acc);
+        else square_chunk<T_F32>(p.s[part].in, s, chunk, acc);
     }
     const double sum = sum_block(acc[0] + acc[1], waves);
-    if (threadIdx.x == 0) p.partial[(int64_t)p.slot[d] * gridDim.x + blockIdx.x] = sum;
+    if (threadIdx.x == 0) p.partial[((int64_t)(p.first_device + d) * p.turns + (d ? p.other_turn : p.first_turn)) * gridDim.x + blockIdx.x] = sum;
 }
 
 // The partial sums of every device, joined in order and rounded once.
-__global__ __launch_bounds__(NT) void square_join_kernel(SquareJoin p) {
+template <int S>
+__global__ __launch_bounds__(NT) void square_join_kernel(SquareJoin<S> p) {
     __shared__ double waves[NT / 64];
     const int d = blockIdx.x;
-    const double* const part = p.partial + (int64_t)d * p.per_device;
+    const double* const part = p.partial + (int64_t)d * p.turns * p.blocks;
     double v = 0.0;
-    for (int i = threadIdx.x; i < p.count[d]; i += NT) v += part[i];
+    for (int i = threadIdx.x; i < p.dense[d] * p.blocks; i += NT) v += part[i];
+    for (int i = threadIdx.x; i < p.pitched[d] * p.blocks; i += NT) v += part[p.dense_turns * p.blocks + i];
     v = sum_block(v, waves);
     if (threadIdx.x == 0) *p.out[d] = (float)v;
 }
 
-// The factor of a device's gradients.  A norm that is no number makes it NaN, an infinite one 0.
-__device__ inline float sum_of(const ClipSum& p, int d) {
+template <typename PLAN>
+__device__ inline float sum_of(const PLAN& p, int d) {
     if (!p.partial) return *p.sum[d];
     float v = *p.sum[0];
     for (int i = 1; i < p.k; ++i) v += *p.sum[i];   // in the order of the devices, as boxing adds
     return v;
 }
+// A norm that is no number makes the factor NaN, an infinite one 0.
 __device__ inline float factor_of(float sum, float most) {
     const float norm = sqrtf(sum);
     return norm <= most ? 1.0f : most / norm;
 }
 
 template <int T, int U>
-__device__ inline void clip_chunk(const ListPart& s, int chunk, float factor) {
+__device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int chunk, float factor) {
     Raw8<T> raw[PER];
+    float v[8];
+    if (whole_chunk(s, chunk)) {
+        load_whole<T>(in, chunk, raw);
+        char* const to = static_cast<char*>(out) + ((int64_t)chunk * LIST_CHUNK + threadIdx.x) * (8 * bytes_of<U>);
+#pragma unroll
+        for (int u = 0; u < PER; ++u) {
+            widen<T>(raw[u], 1.0f, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] *= factor;
+            store8<U>(to + u * (NT * 8 * bytes_of<U>), narrow<U>(v), 8);
+        }
+        return;
+    }
+    each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) { raw[u] = load8<T>(static_cast<const char*>(in) + (row * s.ldi + from) * bytes_of<T>, c, cols); });
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) {
-        raw[u] = load8<T>(static_cast<const char*>(s.in) + (row * s.ldi + from) * bytes_of<T>, c, cols);
-    });
-    each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) {
-        float v[8];
         widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= factor;
-        if (c < cols) store8<U>(static_cast<char*>(s.out) + (row * s.ldo + from + c) * bytes_of<U>, narrow<U>(v), cols - c);
+        store8<U>(static_cast<char*>(out) + (row * s.ldo + from + c) * bytes_of<U>, narrow<U>(v), cols - c);   // none of them where cols - c is not positive
     });
 }
 
-__global__ __launch_bounds__(NT) void clip_kernel(ListPlan p, ClipSum sums) {
-    const PartOf part_of(p);
-    for (int c = blockIdx.x; c < p.chunk0[1]; c += gridDim.x) {
-        const int part = __builtin_amdgcn_readfirstlane(part_of(c));
-        const ListPart& s = p.s[part];
-        const int chunk = c - p.first[part];
-        const float factor = factor_of(sum_of(sums, s.types >> 2), sums.most);
-        switch (s.types & 3) {
-            case 0: clip_chunk<T_F32, T_F32>(s, chunk, factor); break;
-            case 1: clip_chunk<T_BF16, T_F32>(s, chunk, factor); break;
-            case 2: clip_chunk<T_F32, T_BF16>(s, chunk, factor); break;
-            default: clip_chunk<T_BF16, T_BF16>(s, chunk, factor);
+template <template <bool> class PART, int CAP, int S>
+__global__ __launch_bounds__(NT) void clip_kernel(ClipPlan<PART, CAP, S> p) {
+    const Starts<CAP> starts(p.s, p.parts);
+    for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
+        const int part = __builtin_amdgcn_readfirstlane(starts.part_of(c));
+        const Shape s = shape_of(p.s[part]);
+        const int chunk = c - starts.start_of(part);
+        const float factor = factor_of(sum_of(p, p.first_device + (s.what >> 2)), p.most);
+        const void* const in = p.s[part].in;
+        void* const out = p.s[part].out;
+        switch (s.what & 3) {
+            case 0: clip_chunk<T_F32, T_F32>(in, out, s, chunk, factor); break;
+            case 1: clip_chunk<T_BF16, T_F32>(in, out, s, chunk, factor); break;
+            case 2: clip_chunk<T_F32, T_BF16>(in, out, s, chunk, factor); break;
+            default: clip_chunk<T_BF16, T_BF16>(in, out, s, chunk, factor);
         }
     }
-    if (sums.norm[0] && blockIdx.x == 0 && (int)threadIdx.x < sums.k) *sums.norm[threadIdx.x] = sqrtf(sum_of(sums, threadIdx.x));
+    if (p.norm[0] && blockIdx.x == 0 && (int)threadIdx.x < p.k) *p.norm[threadIdx.x] = sqrtf(sum_of(p, threadIdx.x));
 }
 
 }  // namespace
 
-int32_t launch_square_sum(const ListPlan& plan, int devices, int blocks, hipStream_t stream) {
-    hipLaunchKernelGGL(square_sum_kernel, dim3((uint32_t)blocks, (uint32_t)devices), dim3(NT), 0, stream, plan);
+template <template <bool> class PART, int CAP>
+int32_t launch_square_sum(const SquarePlan<PART, CAP>& plan, int devices, int blocks, hipStream_t stream) {
+    hipLaunchKernelGGL((square_sum_kernel<PART, CAP>), dim3((uint32_t)blocks, (uint32_t)devices), dim3(NT), 0, stream, plan);
     return launch_status(__func__);
 }
-int32_t launch_square_join(const SquareJoin& join, int32_t k, hipStream_t stream) {
-    hipLaunchKernelGGL(square_join_kernel, dim3((uint32_t)k), dim3(NT), 0, stream, join);
+template <int S>
+int32_t launch_square_join(const SquareJoin<S>& join, int32_t k, hipStream_t stream) {
+    hipLaunchKernelGGL(square_join_kernel<S>, dim3((uint32_t)k), dim3(NT), 0, stream, join);
     return launch_status(__func__);
 }
-int32_t launch_clip(const ListPlan& plan, const ClipSum& sums, hipStream_t stream) {
-    const int blocks = std::max(1, std::min<int>(plan.chunk0[1], LIST_BLOCKS));
-    hipLaunchKernelGGL(clip_kernel, dim3((uint32_t)blocks), dim3(NT), 0, stream, plan, sums);
+template <template <bool> class PART, int CAP, int S>
+int32_t launch_clip(const ClipPlan<PART, CAP, S>& plan, hipStream_t stream) {
+    const int blocks = std::max(1, std::min<int>(plan.chunks, LIST_BLOCKS));
+    hipLaunchKernelGGL((clip_kernel<PART, CAP, S>), dim3((uint32_t)blocks), dim3(NT), 0, stream, plan);
     return launch_status(__func__);
 }
+
+template int32_t launch_square_sum(const SquarePlan<DensePart, LIST_FEW>&, int, int, hipStream_t);
+template int32_t launch_square_sum(const SquarePlan<DensePart, LIST_DENSE>&, int, int, hipStream_t);
+template int32_t launch_square_sum(const SquarePlan<PitchedPart, LIST_FEW>&, int, int, hipStream_t);
+template int32_t launch_square_sum(const SquarePlan<PitchedPart, LIST_PITCHED>&, int, int, hipStream_t);
+template int32_t launch_square_join(const SquareJoin<8>&, int32_t, hipStream_t);
+template int32_t launch_square_join(const SquareJoin<SBP_MAX_K>&, int32_t, hipStream_t);
+template int32_t launch_clip(const ClipPlan<DensePart, LIST_FEW, 8>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<DensePart, LIST_FEW, SBP_MAX_K>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<DensePart, LIST_DENSE, 8>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<DensePart, LIST_DENSE, SBP_MAX_K>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<PitchedPart, LIST_FEW, 8>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<PitchedPart, LIST_FEW, SBP_MAX_K>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<PitchedPart, LIST_PITCHED, 8>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<PitchedPart, LIST_PITCHED, SBP_MAX_K>&, hipStream_t);
 
 }  // namespace sbp

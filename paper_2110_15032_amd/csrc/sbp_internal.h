@@ -281,145 +281,61 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream);
 // ---------------------------------------------------------------------------------------------
 // Lists of tensors: the sum of their squares, and all of them times a factor.
 // ---------------------------------------------------------------------------------------------
-constexpr int LIST_PARTS = 64;      // local tensors of a launch: the argument blocks stay below 4 KB
+// An argument block costs about a microsecond a KB, so a launch has one of about its own size: places for CAP local tensors, S devices.
 constexpr int LIST_CHUNK = 1024;    // vectors of eight elements that a workgroup takes at a time, of one local tensor
 constexpr int LIST_BLOCKS = 2048;   // workgroups of a launch: eight a compute unit, as many as it holds
-struct ListPart {
+constexpr int LIST_DENSE = 160, LIST_PITCHED = 80, LIST_FEW = 16;   // CAP, at most 192
+// A dense local tensor.  info: elements, from bit 48 on what of_list() says.
+template <bool OUT>
+struct DensePart {
+    const void* in;
+    uint64_t info;
+};
+template <>
+struct DensePart<true> {
+    const void* in;
+    void* out;
+    uint64_t info;
+};
+// Rows at a pitch.
+template <bool OUT>
+struct PitchedPart {
     const void* in;
     void* out;            // clipping only
-    int64_t cols;         // of a row as it is stored; a dense tensor is one row
-    int32_t rows, ldi, ldo;
-    int32_t types;        // bit 0: in is bf16, bit 1: out is; from bit 2 on: the device
+    int32_t rows, cols, ldi, ldo, what;
 };
-struct ListPlan {
-    ListPart s[LIST_PARTS];
-    int32_t first[LIST_PARTS];       // a part's first chunk
-    int32_t chunk0[SBP_MAX_K + 1];   // sums of squares: chunks of the devices of this launch, one after the other; clipping: [1] the number of chunks
-    int32_t slot[SBP_MAX_K];         // where such a device's partial sums go, in units of the workgroups it has
+// bit 0: in is bf16, bit 1: out is; from bit 2 on: the device, counted from the launch's first
+constexpr int32_t of_list(bool in_bf16, bool out_bf16, int32_t device) { return (in_bf16 ? 1 : 0) | (out_bf16 ? 2 : 0) | device << 2; }
+// Parts in the order of their devices.  Sums of squares: workgroup (x, d) takes the chunks of the launch's d-th device and leaves its sum at
+// partial[(device * turns + turn) * gridDim.x + x], turn: first_turn for the launch's first device, other_turn else.
+template <template <bool> class PART, int CAP>
+struct SquarePlan {
+    PART<false> s[CAP];
     double* partial;
-    int32_t parts;
+    int32_t parts, first_device, turns, first_turn, other_turn;
 };
+// The partial sums of a device: `count` from its first place on, and those of tensors with a pitch, `pitched` from behind `dense_turns` turns on.
+template <int S>
 struct SquareJoin {
     const double* partial;
-    int64_t per_device;
-    int32_t count[SBP_MAX_K];
-    float* out[SBP_MAX_K];
+    int32_t blocks, turns, dense_turns;
+    int16_t dense[S], pitched[S];   // turns
+    float* out[S];
 };
-struct ClipSum {
-    const float* sum[SBP_MAX_K];
-    float* norm[SBP_MAX_K];   // null: not wanted
+template <template <bool> class PART, int CAP, int S>
+struct ClipPlan {
+    PART<true> s[CAP];
+    const float* sum[S];
+    float* norm[S];           // null: not wanted
     float most;
-    int32_t k, partial;       // partial: the sums are P(sum)
+    int32_t parts, chunks, k, partial;   // partial: the sums are P(sum)
+    int32_t first_device;
 };
-int32_t launch_square_sum(const ListPlan& plan, int devices, int blocks, hipStream_t stream);
-int32_t launch_square_join(const SquareJoin& join, int32_t k, hipStream_t stream);
-int32_t launch_clip(const ListPlan& plan, const ClipSum& sums, hipStream_t stream);
-
-// ---------------------------------------------------------------------------------------------
-// The gradient of a block's epilogue: da = dy gelu'(pre), and the sum of da (or of dy) over the rows.
-// ---------------------------------------------------------------------------------------------
-constexpr int LINEAR_GRAD_SHARDS = 8;
-struct LinearGradShard {
-    const void* dy;
-    const void* pre;      // null: no activation
-    const void* scales;   // of pre, 8 bits only
-    void* da;             // null: no activation
-    float* dbias;
-    float* part;          // [blocks][cols], where blocks > 1
-    int32_t rows, cols, lddy, ldp, lds, ldda, blocks;
-};
+template <template <bool> class PART, int CAP>
+int32_t launch_square_sum(const SquarePlan<PART, CAP>& plan, int devices, int blocks, hipStream_t stream);
 template <int S>
-struct LinearGradPlan {
-    LinearGradShard s[S];
-    int32_t streams;      // of block8_device.h, chosen at the launch
-};
-template <int S>
-int32_t launch_linear_grad(const LinearGradPlan<S>& plan, int n, int32_t dy, int32_t pre, bool gelu, hipStream_t stream);
-// workgroups along the rows of a shard, each of which leaves a partial sum
-int32_t linear_grad_blocks(int64_t rows, int64_t cols, int32_t k);
-
-// ---------------------------------------------------------------------------------------------
-// The norms behind and in front of a block, with its gate and the residual.  A launch takes S shards: the argument block costs about a
-// microsecond a KB, so that a single device has a launch of its own size.
-// ---------------------------------------------------------------------------------------------
-constexpr int RESNORM_SHARDS = 8;
-enum ResNormFlags : int32_t {
-    RN_POST = 1, RN_POST_LAYER = 2, RN_PRE = 4, RN_PRE_LAYER = 8,   // which norms, and whether they take the mean off
-    RN_DH = 16,                                                     // gradient: the residual stream's own
-    RN_BF16_WEIGHTS = 32,
-    RN_STREAM_H = 64, RN_STREAM_Y = 128                             // results past the caches (dr and dx in the gradient)
-};
-struct ResNormShard {
-    const void* x;
-    const void* r;
-    void* h;
-    void* y;             // pre only
-    void* y_scales;
-    float* mean1;        // null: not wanted
-    float* rstd1;
-    float* mean2;
-    float* rstd2;
-    const void* gate;    // null: ones
-    const void* gamma1;
-    const void* beta1;   // null: zeros
-    const void* gamma2;
-    const void* beta2;
-    int32_t rows, ldx, ldr, ldh, ldy, lds;
-};
-template <int S>
-struct ResNormPlan {
-    ResNormShard s[S];
-    int32_t cols, flags;
-    float alpha, eps1, eps2;
-};
-struct ResNormGradShard {
-    const void* x;
-    const void* h;       // pre only
-    const void* dh;      // RN_DH only
-    const void* dy;      // pre only
-    void* dx;
-    void* dr;
-    const float* mean1;
-    const float* rstd1;
-    const float* mean2;
-    const float* rstd2;
-    const void* gate;    // null: ones
-    const void* gamma1;
-    const void* gamma2;
-    float* part;         // [blocks][4][cols], null: no weight's gradient is wanted
-    int32_t rows, ldx, ldh, lddh, lddy, lddx, lddr, blocks;
-};
-template <int S>
-struct ResNormGradPlan {
-    ResNormGradShard s[S];
-    int32_t cols, flags;
-    float alpha;
-};
-struct ResNormJoinShard {
-    const float* part;
-    const void* gate;
-    const void* gamma1;
-    const void* beta1;
-    float* dgate;        // null: not wanted
-    float* dgamma1;
-    float* dbeta1;
-    float* dgamma2;
-    float* dbeta2;
-    int32_t blocks;
-};
-template <int S>
-struct ResNormJoin {
-    ResNormJoinShard s[S];
-    int32_t cols, flags;
-};
-// types of x, of the residual stream and of y (its gradient); n shards, 1 .. S
-template <int S>
-int32_t launch_residual_norm(const ResNormPlan<S>& plan, int n, int32_t x, int32_t r, int32_t y, hipStream_t stream);
-template <int S>
-int32_t launch_residual_norm_grad(const ResNormGradPlan<S>& plan, int n, int32_t x, int32_t r, int32_t y, hipStream_t stream);
-template <int S>
-int32_t launch_residual_norm_join(const ResNormJoin<S>& join, int n, hipStream_t stream);
-// workgroups that a shard of so many rows gets, each of which leaves one partial sum of the weights' gradients
-int32_t residual_norm_grad_blocks(int64_t rows, int64_t cols, int32_t k);
+int32_t launch_square_join(const SquareJoin<S>& join, int32_t k, hipStream_t stream);
+template <template <bool> class PART, int CAP, int S>
+int32_t launch_clip(const ClipPlan<PART, CAP, S>& plan, hipStream_t stream);
 
 }  // namespace sbp
