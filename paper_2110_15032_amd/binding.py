@@ -190,6 +190,7 @@ class SbpList:
             raise ValueError(f"{self.n} tensors and {len(sbp)} signatures")
         self.k = min((t.k for t in self.keep), default=64)
         self.c = (_CTensor * max(1, self.n))(*(t.c for t in self.keep))
+        self.signatures = tuple(sbp)
         self.sbp = (ctypes.c_int32 * max(1, self.n))(*sbp)
 
 
@@ -447,7 +448,7 @@ def sbp_square_sum(tensors: SbpList, out: SbpTensor, workspace, k: int, stream=N
 
 def sbp_clip(inp: SbpList, squares: SbpTensor, sbp_squares: int, max_norm: float, out: SbpList, norm: SbpTensor | None, k: int, stream=None) -> None:
     _need(k, inp, squares, out, norm)
-    if inp.n != out.n or list(inp.sbp)[:inp.n] != list(out.sbp)[:out.n]:
+    if inp.signatures != out.signatures:
         raise ValueError("the lists differ in length or signatures")
     _check(lib().sbp_clip(inp.c, inp.sbp, inp.n, squares.ref(), sbp_squares, max_norm, out.c, _ref(norm), k, _stream_ptr(stream)), "sbp_clip")
 

@@ -10,29 +10,61 @@ namespace {
 // A local tensor as it is stored.
 struct Stored {
     int64_t rows, cols, pitch;
+    bool empty() const { return rows == 0 || cols == 0; }
+    bool dense() const { return pitch == cols || rows == 1; }
 };
-Stored stored_of(const sbp_tensor_t* t, sbp_t s, int32_t k, int32_t i) {
-    const Local l = local_of(t->rows, t->cols, s, k, i);
-    return {stored_rows(t, l), stored_cols(t, l), pitch_of(t, l)};
-}
+// Those of a list, tensor j's on device i at [j * k + i], worked out once: a call goes through them several times, and 64-bit divisions are slow.
+struct Locals {
+    Stored* of = nullptr;
+    ~Locals() { std::free(of); }
+    bool room(int32_t n, int32_t k) {
+        of = static_cast<Stored*>(std::malloc(((size_t)n * k + 1) * sizeof(Stored)));
+        return of != nullptr;
+    }
+};
 // one row where rows lie back to back
-Stored as_rows(Stored s, bool dense) { return dense || s.rows == 1 ? Stored{1, s.rows * s.cols, 0} : s; }
+Stored as_rows(const Stored& s, bool dense) { return dense ? Stored{1, s.rows * s.cols, 0} : s; }
 int64_t chunks_of(const Stored& s) { return (s.rows * ((s.cols + 7) / 8) + LIST_CHUNK - 1) / LIST_CHUNK; }
+constexpr int64_t MOST_CHUNKS = INT32_MAX / 2;
 
-int32_t check_list(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k) {
+// check_tensor's rules, with the local tensors noted
+int32_t check_one(const sbp_tensor_t* t, sbp_t s, int32_t k, Stored* of) {
+    const int32_t st = check_whole(s);
+    if (st != SBP_OK) return st;
+    if (!t->shard) return SBP_ERR_NULL;
+    if (t->rows > INT32_MAX || t->cols > INT32_MAX) return SBP_ERR_UNSUPPORTED;   // before anything is multiplied
+    if (t->rows < 0 || t->cols < 0 || t->ld < 0) return SBP_ERR_SHAPE;
+    if (t->dtype != SBP_F32 && t->dtype != SBP_BF16) return SBP_ERR_DTYPE;
+    if (t->trans != 0 && t->trans != 1) return SBP_ERR_SHAPE;
+    if (t->ld > INT32_MAX) return SBP_ERR_UNSUPPORTED;
+    const int64_t along = s == SBP_S(0) ? t->rows : t->cols, least = s == SBP_B ? 0 : along / k, more = s == SBP_B ? 0 : along % k;
+    for (int32_t i = 0; i < k; ++i) {
+        const int64_t part = least + (i < more ? 1 : 0), rows = s == SBP_S(0) ? part : t->rows, cols = s == SBP_S(1) ? part : t->cols;
+        of[i] = t->trans ? Stored{cols, rows, t->ld ? t->ld : rows} : Stored{rows, cols, t->ld ? t->ld : cols};
+        if (of[i].empty()) continue;
+        if (of[i].cols > of[i].pitch) return SBP_ERR_SHAPE;
+        if (!t->shard[i]) return SBP_ERR_NULL;
+        if (reinterpret_cast<uintptr_t>(t->shard[i]) & 15u) return SBP_ERR_ALIGN;
+        if (chunks_of(of[i]) > MOST_CHUNKS) return SBP_ERR_UNSUPPORTED;
+    }
+    return SBP_OK;
+}
+int32_t check_list(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, Locals& locals) {
     if (k < 1 || k > SBP_MAX_K) return SBP_ERR_K;
     if (n < 0) return SBP_ERR_SHAPE;
     if (n && (!t || !s)) return SBP_ERR_NULL;
-    constexpr int64_t MOST = INT32_MAX;
+    if (!locals.room(n, k)) return SBP_ERR_UNSUPPORTED;
     for (int32_t j = 0; j < n; ++j) {
-        int32_t st;
-        if ((st = check_whole(s[j])) != SBP_OK) return st;
-        if (t[j].rows > MOST || t[j].cols > MOST) return SBP_ERR_UNSUPPORTED;   // before anything is multiplied
-        if ((st = check_tensor(t + j, s[j], k, true)) != SBP_OK) return st;
+        const int32_t st = check_one(t + j, s[j], k, locals.of + (int64_t)j * k);
+        if (st != SBP_OK) return st;
     }
     return SBP_OK;
 }
 int32_t check_scalar(const sbp_tensor_t* t, int32_t k) { return check_column(t, 1, SBP_B, k, false); }
+Span span_of(const sbp_tensor_t* t, const Stored& l, int32_t i) {
+    const uintptr_t lo = reinterpret_cast<uintptr_t>(t->shard[i]);
+    return l.empty() ? Span{0, 0} : Span{lo, lo + (uintptr_t)((l.rows - 1) * l.pitch + l.cols) * elem_bytes(t->dtype)};
+}
 
 // A local tensor of a list: what device i counts of it, or (clipping) holds of it.
 struct Item {
@@ -43,9 +75,8 @@ struct Item {
     int32_t what;          // without the device
     int64_t chunks;
 };
-bool counted(const sbp_tensor_t* t, sbp_t s, int32_t k, int32_t i, Item& to) {
-    Stored l = stored_of(t, s, k, i);
-    if (l.rows * l.cols == 0) return false;
+bool counted(const sbp_tensor_t* t, sbp_t s, Stored l, int32_t k, int32_t i, Item& to) {
+    if (l.empty()) return false;
     const bool dense = l.pitch == l.cols;
     const char* at = static_cast<const char*>(t->shard[i]);
     if (s == SBP_B) {   // its share of the stored rows
@@ -53,16 +84,19 @@ bool counted(const sbp_tensor_t* t, sbp_t s, int32_t k, int32_t i, Item& to) {
         l.rows = split_len(l.rows, k, i);
         if (l.rows == 0) return false;
     }
-    const Stored r = as_rows(l, dense);
+    const Stored r = as_rows(l, dense || l.rows == 1);
     to = {at, nullptr, r, 0, of_list(t->dtype == SBP_BF16, false, 0), chunks_of(r)};
     return true;
 }
-bool clipped(const sbp_tensor_t* in, const sbp_tensor_t* out, sbp_t s, int32_t k, int32_t i, Item& to) {
-    const Stored a = stored_of(in, s, k, i), o = stored_of(out, s, k, i);
-    if (a.rows * a.cols == 0) return false;
-    const Stored r = as_rows(a, a.pitch == a.cols && o.pitch == o.cols);
+bool clipped(const sbp_tensor_t* in, const Stored& a, const sbp_tensor_t* out, const Stored& o, int32_t i, Item& to) {
+    if (a.empty()) return false;
+    const Stored r = as_rows(a, a.dense() && o.dense());
     to = {static_cast<const char*>(in->shard[i]), static_cast<char*>(out->shard[i]), r, o.pitch, of_list(in->dtype == SBP_BF16, out->dtype == SBP_BF16, 0), chunks_of(r)};
     return true;
+}
+// Two local tensors that lie back to back, results as well, are one.
+bool joins(const Item& a, const Item& b) {
+    return a.what == b.what && a.in + a.s.cols * (a.what & 1 ? 2 : 4) == b.in && (!a.out || a.out + a.s.cols * (a.what & 2 ? 2 : 4) == b.out);
 }
 
 // Local tensors of one launch, in the order of their devices.
@@ -85,16 +119,27 @@ int32_t each_batch(int32_t n, int32_t k, bool dense, Batch& b, int16_t* used, IT
         for (int32_t j = 0; j < n; ++j) {
             Item it;
             if (!make(j, d, it) || (it.s.rows == 1) != dense) continue;
-            if (it.chunks > INT32_MAX / 2) return SBP_ERR_UNSUPPORTED;
-            if (b.n && (b.n == cap || b.chunks + it.chunks > INT32_MAX / 2)) {
+            if (it.chunks > MOST_CHUNKS) return SBP_ERR_UNSUPPORTED;
+            if (dense && mine && b.chunks + it.chunks <= MOST_CHUNKS && joins(b.item[b.n - 1], it)) {
+                Item& last = b.item[b.n - 1];
+                last.s.cols += it.s.cols;
+                const int64_t more = chunks_of(last.s) - last.chunks;
+                last.chunks += more;
+                b.chunks += more;
+                mine += more;
+                b.most = std::max(b.most, mine);
+                continue;
+            }
+            if (b.n && (b.n == cap || b.chunks + it.chunks > MOST_CHUNKS)) {
                 const int32_t st = f(b);
                 if (st != SBP_OK) return st;
                 b.n = 0;
+                mine = 0;
             }
             if (b.n == 0) {
                 b.first_device = d;
                 b.turn = used[d];
-                b.chunks = b.most = mine = 0;
+                b.chunks = b.most = 0;
             }
             if (mine == 0) ++used[d];
             b.item[b.n] = it;
@@ -123,12 +168,19 @@ struct SquareShape {
     int32_t blocks;                                    // workgroups of every device in every launch
     int32_t dense_turns, turns;                        // places of a device's partial sums, in units of them
     int16_t dense[SBP_MAX_K], pitched[SBP_MAX_K];      // launches that a device has parts in
-    int64_t bytes(int32_t k) const { return (int64_t)k * turns * blocks * 8; }
+    int64_t bytes;                                     // for the workspace
 };
-int32_t square_shape(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, SquareShape& sq, Batch& b) {
-    int64_t most = 1;
+// The workspace goes by the sizes alone, and not by which tensors lie back to back: a device has parts in at most so many launches, and at most so many
+// workgroups there.
+int32_t square_shape(const sbp_tensor_t* t, const sbp_t* s, const Locals& locals, int32_t n, int32_t k, SquareShape& sq, Batch& b) {
+    int64_t most = 1, all = 0;
     int32_t devices = 1, st;
-    auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], k, d, it); };
+    for (int32_t d = 0; d < k; ++d) {
+        int64_t mine = 0;
+        for (int32_t j = 0; j < n; ++j) mine += locals.of[(int64_t)j * k + d].empty() ? 0 : chunks_of(locals.of[(int64_t)j * k + d]);
+        all = std::max(all, mine);
+    }
+    auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], locals.of[(int64_t)j * k + d], k, d, it); };
     auto look = [&](const Batch& b) {
         most = std::max(most, b.most);
         devices = std::max(devices, b.devices);
@@ -139,6 +191,9 @@ int32_t square_shape(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k
     sq.blocks = (int32_t)std::min<int64_t>(most, std::max(1, LIST_BLOCKS / devices));
     sq.dense_turns = *std::max_element(sq.dense, sq.dense + k);
     sq.turns = sq.dense_turns + *std::max_element(sq.pitched, sq.pitched + k);
+    const int64_t turns = (n + LIST_DENSE - 1) / LIST_DENSE + (n + LIST_PITCHED - 1) / LIST_PITCHED + 2;
+    if (sq.turns > turns) return SBP_ERR_UNSUPPORTED;   // tensors that no memory holds
+    sq.bytes = (all ? k * turns * std::min<int64_t>(all, LIST_BLOCKS) : 0) * 8;
     return SBP_OK;
 }
 template <template <bool> class PART, int CAP, typename MAKE>
@@ -151,6 +206,7 @@ int32_t square_batch(const Batch& b, const SquareShape& sq, int32_t base, double
     plan.turns = sq.turns;
     plan.first_turn = base + b.turn;
     plan.other_turn = base;
+    plan.stream = 1;
     return launch_square_sum(plan, b.devices, sq.blocks, stream);
 }
 template <int S>
@@ -181,6 +237,7 @@ int32_t clip_batch(const Batch& b, const sbp_tensor_t* squares, bool partial, fl
     plan.k = k;
     plan.partial = partial;
     plan.first_device = b.first_device;
+    plan.stream = 1;
     return launch_clip(plan, stream);
 }
 template <template <bool> class PART, int CAP, typename MAKE>
@@ -195,42 +252,43 @@ extern "C" {
 int32_t sbp_square_sum_workspace(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, int64_t* bytes) {
     if (!bytes) return SBP_ERR_NULL;
     int32_t st;
-    if ((st = check_list(t, s, n, k)) != SBP_OK) return st;
+    Locals locals;
+    if ((st = check_list(t, s, n, k, locals)) != SBP_OK) return st;
     SquareShape sq;
     Batch batch;
-    if ((st = square_shape(t, s, n, k, sq, batch)) != SBP_OK) return st;
-    *bytes = sq.bytes(k);
+    if ((st = square_shape(t, s, locals, n, k, sq, batch)) != SBP_OK) return st;
+    *bytes = sq.bytes;
     return SBP_OK;
 }
 
 int32_t sbp_square_sum(const sbp_tensor_t* t, const sbp_t* s, int32_t n, const sbp_tensor_t* out, void* workspace, int64_t workspace_bytes, int32_t k, void* stream) {
     int32_t st;
-    if ((st = check_list(t, s, n, k)) != SBP_OK) return st;
+    Locals locals;
+    if ((st = check_list(t, s, n, k, locals)) != SBP_OK) return st;
     if ((st = check_scalar(out, k)) != SBP_OK) return st;
     SquareShape sq;
     Batch batch;
-    if ((st = square_shape(t, s, n, k, sq, batch)) != SBP_OK) return st;
-    const int64_t room = sq.bytes(k);
-    if (room) {
+    if ((st = square_shape(t, s, locals, n, k, sq, batch)) != SBP_OK) return st;
+    if (sq.bytes) {
         if (!workspace) return SBP_ERR_NULL;
         if (reinterpret_cast<uintptr_t>(workspace) & 15u) return SBP_ERR_ALIGN;
-        if (workspace_bytes < room) return SBP_ERR_SHAPE;
+        if (workspace_bytes < sq.bytes) return SBP_ERR_SHAPE;
     }
     Buffers b;
     b.add(true, out, SBP_B, k);
-    b.add(true, workspace, 1, room, room, 1);
+    b.add(true, workspace, 1, sq.bytes, sq.bytes, 1);
     if ((st = b.check()) != SBP_OK) return st;
-    for (int32_t j = 0; j < n; ++j) {   // the outputs are in order now: the inputs against them, a few at a time
-        b.n_in = 0;
-        b.add(false, t + j, s[j], k);
-        if ((st = b.check()) != SBP_OK) return st;
-    }
+    for (int32_t j = 0; j < n; ++j)   // the outputs are in order now
+        for (int32_t i = 0; i < k; ++i)
+            if (b.meets(span_of(t + j, locals.of[(int64_t)j * k + i], i))) return SBP_ERR_ALIAS;
     double* const partial = static_cast<double*>(workspace);
     const hipStream_t on = static_cast<hipStream_t>(stream);
-    auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], k, d, it); };
+    auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], locals.of[(int64_t)j * k + d], k, d, it); };
     int16_t used[SBP_MAX_K];
     st = each_batch(n, k, true, batch, used, make, [&](const Batch& b) {
-        return b.n <= LIST_FEW ? square_batch<DensePart, LIST_FEW>(b, sq, 0, partial, dense_part<false>, on) : square_batch<DensePart, LIST_DENSE>(b, sq, 0, partial, dense_part<false>, on);
+        if (b.n <= LIST_FEW) return square_batch<DensePart, LIST_FEW>(b, sq, 0, partial, dense_part<false>, on);
+        if (b.n <= LIST_SOME) return square_batch<DensePart, LIST_SOME>(b, sq, 0, partial, dense_part<false>, on);
+        return square_batch<DensePart, LIST_DENSE>(b, sq, 0, partial, dense_part<false>, on);
     });
     if (st != SBP_OK) return st;
     st = each_batch(n, k, false, batch, used, make, [&](const Batch& b) {
@@ -244,13 +302,12 @@ int32_t sbp_square_sum(const sbp_tensor_t* t, const sbp_t* s, int32_t n, const s
 int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_tensor_t* squares, sbp_t sbp_squares, float max_norm, const sbp_tensor_t* out,
                  const sbp_tensor_t* norm, int32_t k, void* stream) {
     int32_t st;
-    if ((st = check_list(in, s, n, k)) != SBP_OK) return st;
-    if ((st = check_list(out, s, n, k)) != SBP_OK) return st;
+    Locals from, to;
+    if ((st = check_list(in, s, n, k, from)) != SBP_OK) return st;
+    if ((st = check_list(out, s, n, k, to)) != SBP_OK) return st;
     for (int32_t j = 0; j < n; ++j) {
         if (in[j].rows != out[j].rows || in[j].cols != out[j].cols) return SBP_ERR_SHAPE;
         if (in[j].trans != out[j].trans) return SBP_ERR_UNSUPPORTED;
-        for (int32_t i = 0; i < k; ++i)
-            if (chunks_of(stored_of(in + j, s[j], k, i)) > INT32_MAX / 2) return SBP_ERR_UNSUPPORTED;
     }
     if (!is_sbp(sbp_squares)) return SBP_ERR_AXIS;
     if (sbp_squares != SBP_P_SUM && sbp_squares != SBP_B) return SBP_ERR_SIGNATURE;
@@ -267,11 +324,6 @@ int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_te
     Out* const outs = static_cast<Out*>(std::malloc((size_t)most * sizeof(Out)));
     if (!outs) return SBP_ERR_UNSUPPORTED;
     int64_t n_out = 0;
-    auto span = [&](const sbp_tensor_t* t, sbp_t sig, int32_t i) {
-        const Stored l = stored_of(t, sig, k, i);
-        const uintptr_t lo = reinterpret_cast<uintptr_t>(t->shard[i]);
-        return l.rows * l.cols ? Span{lo, lo + (uintptr_t)((l.rows - 1) * l.pitch + l.cols) * elem_bytes(t->dtype)} : Span{0, 0};
-    };
     auto clear = [&](const Span& v, int64_t id, bool in_place) {   // no output but its own, in place
         if (v.hi == 0) return true;
         const Out* o = std::upper_bound(outs, outs + n_out, v.lo, [](uintptr_t lo, const Out& b) { return lo < b.span.hi; });
@@ -280,10 +332,11 @@ int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_te
         return true;
     };
     bool good = true;
-    for (int32_t j = 0; j <= n; ++j)
-        for (int32_t i = 0; i < k; ++i) {
+    constexpr Stored SCALAR = {1, 1, 1};
+    for (int32_t i = 0; i < k; ++i)
+        for (int32_t j = 0; j <= n; ++j) {
             if (j == n && !norm) continue;
-            const Span v = j < n ? span(out + j, s[j], i) : span(norm, SBP_B, i);
+            const Span v = j < n ? span_of(out + j, to.of[(int64_t)j * k + i], i) : span_of(norm, SCALAR, i);
             if (v.hi) outs[n_out++] = {v, (int64_t)j * k + i};
         }
     auto before = [](const Out& a, const Out& b) { return a.span.lo < b.span.lo; };
@@ -291,36 +344,38 @@ int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_te
     for (int64_t i = 1; i < n_out; ++i) good = good && outs[i].span.lo >= outs[i - 1].span.hi;
     for (int32_t j = 0; good && j < n; ++j)
         for (int32_t i = 0; good && i < k; ++i) {
-            const bool same = in[j].shard[i] == out[j].shard[i] && in[j].dtype == out[j].dtype && stored_of(in + j, s[j], k, i).pitch == stored_of(out + j, s[j], k, i).pitch;
-            good = clear(span(in + j, s[j], i), (int64_t)j * k + i, same);
+            const int64_t id = (int64_t)j * k + i;
+            const bool same = in[j].shard[i] == out[j].shard[i] && in[j].dtype == out[j].dtype && from.of[id].pitch == to.of[id].pitch;
+            good = clear(span_of(in + j, from.of[id], i), id, same);
         }
-    for (int32_t i = 0; good && i < k; ++i) good = clear(span(squares, SBP_B, i), -1, false);
+    for (int32_t i = 0; good && i < k; ++i) good = clear(span_of(squares, SCALAR, i), -1, false);
     std::free(outs);
     if (!good) return SBP_ERR_ALIAS;
 
     const hipStream_t on = static_cast<hipStream_t>(stream);
     const bool partial = sbp_squares == SBP_P_SUM;
-    auto make = [&](int32_t j, int32_t d, Item& it) { return clipped(in + j, out + j, s[j], k, d, it); };
+    auto make = [&](int32_t j, int32_t d, Item& it) { return clipped(in + j, from.of[(int64_t)j * k + d], out + j, to.of[(int64_t)j * k + d], d, it); };
     int16_t used[SBP_MAX_K];
     Batch batch;
-    const sbp_tensor_t* to = norm;   // the first launch writes it
+    const sbp_tensor_t* write = norm;   // the first launch does
     st = each_batch(n, k, true, batch, used, make, [&](const Batch& b) {
-        const int32_t status = b.n <= LIST_FEW ? clip_devices<DensePart, LIST_FEW>(b, squares, partial, max_norm, to, k, dense_part<true>, on)
-                                               : clip_devices<DensePart, LIST_DENSE>(b, squares, partial, max_norm, to, k, dense_part<true>, on);
-        to = nullptr;
+        const int32_t status = b.n <= LIST_FEW ? clip_devices<DensePart, LIST_FEW>(b, squares, partial, max_norm, write, k, dense_part<true>, on)
+                             : b.n <= LIST_SOME ? clip_devices<DensePart, LIST_SOME>(b, squares, partial, max_norm, write, k, dense_part<true>, on)
+                                               : clip_devices<DensePart, LIST_DENSE>(b, squares, partial, max_norm, write, k, dense_part<true>, on);
+        write = nullptr;
         return status;
     });
     if (st != SBP_OK) return st;
     st = each_batch(n, k, false, batch, used, make, [&](const Batch& b) {
-        const int32_t status = b.n <= LIST_FEW ? clip_devices<PitchedPart, LIST_FEW>(b, squares, partial, max_norm, to, k, pitched_part<true>, on)
-                                               : clip_devices<PitchedPart, LIST_PITCHED>(b, squares, partial, max_norm, to, k, pitched_part<true>, on);
-        to = nullptr;
+        const int32_t status = b.n <= LIST_FEW ? clip_devices<PitchedPart, LIST_FEW>(b, squares, partial, max_norm, write, k, pitched_part<true>, on)
+                                               : clip_devices<PitchedPart, LIST_PITCHED>(b, squares, partial, max_norm, write, k, pitched_part<true>, on);
+        write = nullptr;
         return status;
     });
-    if (st != SBP_OK || !to) return st;
+    if (st != SBP_OK || !write) return st;
     batch.n = 0;   // nothing but the norm
     batch.chunks = batch.first_device = 0;
-    return clip_devices<DensePart, LIST_FEW>(batch, squares, partial, max_norm, to, k, dense_part<true>, on);
+    return clip_devices<DensePart, LIST_FEW>(batch, squares, partial, max_norm, write, k, dense_part<true>, on);
 }
 
 }  // extern "C"

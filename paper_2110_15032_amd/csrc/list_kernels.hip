@@ -13,6 +13,11 @@ namespace {
 constexpr int NT = 256, PER = LIST_CHUNK / NT;
 constexpr uint64_t ELEMENTS = ((uint64_t)1 << 48) - 1;
 
+// Waves a SIMD: eight, for all of a launch's workgroups at once (seven, with the rest in a second turn, took 117 us where eight take 109, 2^28 bf16
+// elements); rows at a pitch need more registers.
+template <template <bool> class PART>
+constexpr int waves_with(int pitched) { return std::is_same_v<PART<false>, DensePart<false>> ? 8 : pitched; }
+
 // A part as the kernels see it: `count` elements in one row (rows 1), or rows of `cols` at a pitch.
 struct Shape {
     int64_t cols;
@@ -111,18 +116,52 @@ __device__ inline void each_vector(const Shape& s, int chunk, F&& f) {
 }
 // all of the chunk's vectors are whole ones of one row
 __device__ inline bool whole_chunk(const Shape& s, int chunk) { return s.rows == 1 && ((int64_t)chunk + 1) * (LIST_CHUNK * 8) <= s.cols; }
-template <int T>
-__device__ inline void load_whole(const void* in, int chunk, Raw8<T> (&raw)[PER]) {
-    const char* const from = static_cast<const char*>(in) + ((int64_t)chunk * LIST_CHUNK + threadIdx.x) * (8 * bytes_of<T>);
+// Whole chunks: G consecutive elements a lane and load, so that the loads and stores of a wave are of consecutive bytes where the wider side has 16 of a lane.
+template <int T, int G>
+struct Group;   // G elements as they are stored
+template <>
+struct Group<T_F32, 4> {
+    typedef f32x4 type;
+};
+template <>
+struct Group<T_BF16, 4> {
+    typedef u32x2 type;
+};
+template <>
+struct Group<T_BF16, 8> {
+    typedef u32x4 type;
+};
+template <int T, int G>
+__device__ inline void widen_group(const typename Group<T, G>::type r, float (&v)[G]) {
 #pragma unroll
-    for (int u = 0; u < PER; ++u) {
-        const char* const at = from + u * (NT * 8 * bytes_of<T>);
-        if constexpr (T == T_F32) {
-            raw[u].a = *reinterpret_cast<const f32x4*>(at);
-            raw[u].b = *reinterpret_cast<const f32x4*>(at + 16);
-        } else {
-            raw[u].w = *reinterpret_cast<const u32x4*>(at);
-        }
+    for (int e = 0; e < G; ++e) {
+        if constexpr (T == T_F32) v[e] = r[e];
+        else v[e] = __uint_as_float(e & 1 ? r[e >> 1] & 0xFFFF0000u : r[e >> 1] << 16);
+    }
+}
+template <int T, int G>
+__device__ inline typename Group<T, G>::type narrow_group(const float (&v)[G]) {
+    typename Group<T, G>::type r;
+#pragma unroll
+    for (int e = 0; e < G; ++e) {
+        if constexpr (T == T_F32) r[e] = v[e];
+        else if (e & 1) r[e >> 1] = f32_to_bf16x2(v[e - 1], v[e]);
+    }
+    return r;
+}
+template <int T, int G>
+__device__ inline const typename Group<T, G>::type* group_at(const void* p, int chunk) {
+    return reinterpret_cast<const typename Group<T, G>::type*>(static_cast<const char*>(p) + (int64_t)chunk * (LIST_CHUNK * 8 * bytes_of<T>)) + threadIdx.x;
+}
+template <int T, int G, int N>
+__device__ inline void load_whole(const void* in, int chunk, bool stream, typename Group<T, G>::type (&raw)[N]) {
+    const auto* const from = group_at<T, G>(in, chunk);
+    if (stream) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) raw[u] = __builtin_nontemporal_load(from + u * NT);
+    } else {
+#pragma unroll
+        for (int u = 0; u < N; ++u) raw[u] = from[u * NT];
     }
 }
 
@@ -138,24 +177,28 @@ __device__ inline double sum_block(double v, double* waves) {
     for (int w = 1; w < NT / 64; ++w) v += waves[w];
     return v;
 }
-__device__ inline void add_squares(const float (&v)[8], double (&acc)[2]) {
+template <int G>
+__device__ inline void add_squares(const float (&v)[G], double (&acc)[2]) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e & 1] = fma((double)v[e], (double)v[e], acc[e & 1]);
+    for (int e = 0; e < G; ++e) acc[e & 1] = fma((double)v[e], (double)v[e], acc[e & 1]);
 }
 
 template <int T>
-__device__ inline void square_chunk(const void* in, const Shape& s, int chunk, double (&acc)[2]) {
-    Raw8<T> raw[PER];
-    float v[8];
+__device__ inline void square_chunk(const void* in, const Shape& s, int chunk, bool stream, double (&acc)[2]) {
     if (whole_chunk(s, chunk)) {
-        load_whole<T>(in, chunk, raw);
+        constexpr int G = T == T_F32 ? 4 : 8, N = LIST_CHUNK * 8 / NT / G;
+        typename Group<T, G>::type raw[N];
+        load_whole<T, G>(in, chunk, stream, raw);
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            widen<T>(raw[u], 1.0f, v);
+        for (int u = 0; u < N; ++u) {
+            float v[G];
+            widen_group<T, G>(raw[u], v);
             add_squares(v, acc);
         }
         return;
     }
+    Raw8<T> raw[PER];
+    float v[8];
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) { raw[u] = load8<T>(static_cast<const char*>(in) + (row * s.ldi + from) * bytes_of<T>, c, cols); });
     each_vector(s, chunk, [&](int u, int64_t, int64_t, int c, int cols) {
         widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
@@ -164,7 +207,7 @@ __device__ inline void square_chunk(const void* in, const Shape& s, int chunk, d
 }
 
 template <template <bool> class PART, int CAP>
-__global__ __launch_bounds__(NT) void square_sum_kernel(SquarePlan<PART, CAP> p) {
+__global__ __launch_bounds__(NT, waves_with<PART>(5)) void square_sum_kernel(SquarePlan<PART, CAP> p) {
     __shared__ double waves[NT / 64];
     const Starts<CAP> starts(p.s, p.parts);
     const int d = blockIdx.y, end = starts.start_of(starts.parts_before(d + 1));
@@ -173,8 +216,8 @@ __global__ __launch_bounds__(NT) void square_sum_kernel(SquarePlan<PART, CAP> p)
         const int part = __builtin_amdgcn_readfirstlane(starts.part_of(c));
         const Shape s = shape_of(p.s[part]);
         const int chunk = c - starts.start_of(part);
-        if (s.what & 1) square_chunk<T_BF16>(p.s[part].in, s, chunk, acc);
-        else square_chunk<T_F32>(p.s[part].in, s, chunk, acc);
+        if (s.what & 1) square_chunk<T_BF16>(p.s[part].in, s, chunk, p.stream, acc);
+        else square_chunk<T_F32>(p.s[part].in, s, chunk, p.stream, acc);
     }
     const double sum = sum_block(acc[0] + acc[1], waves);
     if (threadIdx.x == 0) p.partial[((int64_t)(p.first_device + d) * p.turns + (d ? p.other_turn : p.first_turn)) * gridDim.x + blockIdx.x] = sum;
@@ -207,21 +250,25 @@ __device__ inline float factor_of(float sum, float most) {
 }
 
 template <int T, int U>
-__device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int chunk, float factor) {
-    Raw8<T> raw[PER];
-    float v[8];
+__device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int chunk, float factor, bool stream) {
     if (whole_chunk(s, chunk)) {
-        load_whole<T>(in, chunk, raw);
-        char* const to = static_cast<char*>(out) + ((int64_t)chunk * LIST_CHUNK + threadIdx.x) * (8 * bytes_of<U>);
+        constexpr int G = T == T_BF16 && U == T_BF16 ? 8 : 4, N = LIST_CHUNK * 8 / NT / G;
+        typename Group<T, G>::type raw[N];
+        load_whole<T, G>(in, chunk, stream, raw);
+        auto* const to = const_cast<typename Group<U, G>::type*>(group_at<U, G>(out, chunk));
 #pragma unroll
-        for (int u = 0; u < PER; ++u) {
-            widen<T>(raw[u], 1.0f, v);
+        for (int u = 0; u < N; ++u) {
+            float v[G];
+            widen_group<T, G>(raw[u], v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] *= factor;
-            store8<U>(to + u * (NT * 8 * bytes_of<U>), narrow<U>(v), 8);
+            for (int e = 0; e < G; ++e) v[e] *= factor;
+            if (stream) __builtin_nontemporal_store(narrow_group<U, G>(v), to + u * NT);
+            else to[u * NT] = narrow_group<U, G>(v);
         }
         return;
     }
+    Raw8<T> raw[PER];
+    float v[8];
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) { raw[u] = load8<T>(static_cast<const char*>(in) + (row * s.ldi + from) * bytes_of<T>, c, cols); });
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) {
         widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
@@ -232,7 +279,7 @@ __device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int
 }
 
 template <template <bool> class PART, int CAP, int S>
-__global__ __launch_bounds__(NT) void clip_kernel(ClipPlan<PART, CAP, S> p) {
+__global__ __launch_bounds__(NT, waves_with<PART>(6)) void clip_kernel(ClipPlan<PART, CAP, S> p) {
     const Starts<CAP> starts(p.s, p.parts);
     for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
         const int part = __builtin_amdgcn_readfirstlane(starts.part_of(c));
@@ -242,10 +289,10 @@ __global__ __launch_bounds__(NT) void clip_kernel(ClipPlan<PART, CAP, S> p) {
         const void* const in = p.s[part].in;
         void* const out = p.s[part].out;
         switch (s.what & 3) {
-            case 0: clip_chunk<T_F32, T_F32>(in, out, s, chunk, factor); break;
-            case 1: clip_chunk<T_BF16, T_F32>(in, out, s, chunk, factor); break;
-            case 2: clip_chunk<T_F32, T_BF16>(in, out, s, chunk, factor); break;
-            default: clip_chunk<T_BF16, T_BF16>(in, out, s, chunk, factor);
+            case 0: clip_chunk<T_F32, T_F32>(in, out, s, chunk, factor, p.stream); break;
+            case 1: clip_chunk<T_BF16, T_F32>(in, out, s, chunk, factor, p.stream); break;
+            case 2: clip_chunk<T_F32, T_BF16>(in, out, s, chunk, factor, p.stream); break;
+            default: clip_chunk<T_BF16, T_BF16>(in, out, s, chunk, factor, p.stream);
         }
     }
     if (p.norm[0] && blockIdx.x == 0 && (int)threadIdx.x < p.k) *p.norm[threadIdx.x] = sqrtf(sum_of(p, threadIdx.x));
@@ -271,6 +318,7 @@ int32_t launch_clip(const ClipPlan<PART, CAP, S>& plan, hipStream_t stream) {
 }
 
 template int32_t launch_square_sum(const SquarePlan<DensePart, LIST_FEW>&, int, int, hipStream_t);
+template int32_t launch_square_sum(const SquarePlan<DensePart, LIST_SOME>&, int, int, hipStream_t);
 template int32_t launch_square_sum(const SquarePlan<DensePart, LIST_DENSE>&, int, int, hipStream_t);
 template int32_t launch_square_sum(const SquarePlan<PitchedPart, LIST_FEW>&, int, int, hipStream_t);
 template int32_t launch_square_sum(const SquarePlan<PitchedPart, LIST_PITCHED>&, int, int, hipStream_t);
@@ -278,6 +326,8 @@ template int32_t launch_square_join(const SquareJoin<8>&, int32_t, hipStream_t);
 template int32_t launch_square_join(const SquareJoin<SBP_MAX_K>&, int32_t, hipStream_t);
 template int32_t launch_clip(const ClipPlan<DensePart, LIST_FEW, 8>&, hipStream_t);
 template int32_t launch_clip(const ClipPlan<DensePart, LIST_FEW, SBP_MAX_K>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<DensePart, LIST_SOME, 8>&, hipStream_t);
+template int32_t launch_clip(const ClipPlan<DensePart, LIST_SOME, SBP_MAX_K>&, hipStream_t);
 template int32_t launch_clip(const ClipPlan<DensePart, LIST_DENSE, 8>&, hipStream_t);
 template int32_t launch_clip(const ClipPlan<DensePart, LIST_DENSE, SBP_MAX_K>&, hipStream_t);
 template int32_t launch_clip(const ClipPlan<PitchedPart, LIST_FEW, 8>&, hipStream_t);

@@ -29,11 +29,14 @@ struct Buffers {
         std::sort(outs, outs + n_out, [](const Span& a, const Span& b) { return a.lo < b.lo; });
         for (int i = 1; i < n_out; ++i)
             if (outs[i].lo < outs[i - 1].hi) return SBP_ERR_ALIAS;
-        for (int i = 0; i < n_in; ++i) {   // the first output that ends behind the input's start
-            const Span* o = std::upper_bound(outs, outs + n_out, ins[i].lo, [](uintptr_t lo, const Span& b) { return lo < b.hi; });
-            if (o != outs + n_out && o->lo < ins[i].hi) return SBP_ERR_ALIAS;
-        }
+        for (int i = 0; i < n_in; ++i)
+            if (meets(ins[i])) return SBP_ERR_ALIAS;
         return SBP_OK;
+    }
+    // behind check(): does an output overlap it?
+    bool meets(const Span& v) const {   // the first output that ends behind its start
+        const Span* o = std::upper_bound(outs, outs + n_out, v.lo, [](uintptr_t lo, const Span& b) { return lo < b.hi; });
+        return o != outs + n_out && o->lo < v.hi;
     }
 };
 

@@ -284,7 +284,7 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream);
 // An argument block costs about a microsecond a KB, so a launch has one of about its own size: places for CAP local tensors, S devices.
 constexpr int LIST_CHUNK = 1024;    // vectors of eight elements that a workgroup takes at a time, of one local tensor
 constexpr int LIST_BLOCKS = 2048;   // workgroups of a launch: eight a compute unit, as many as it holds
-constexpr int LIST_DENSE = 160, LIST_PITCHED = 80, LIST_FEW = 16;   // CAP, at most 192
+constexpr int LIST_DENSE = 160, LIST_PITCHED = 80, LIST_SOME = 64, LIST_FEW = 16;   // CAP, at most 192
 // A dense local tensor.  info: elements, from bit 48 on what of_list() says.
 template <bool OUT>
 struct DensePart {
@@ -313,6 +313,7 @@ struct SquarePlan {
     PART<false> s[CAP];
     double* partial;
     int32_t parts, first_device, turns, first_turn, other_turn;
+    int32_t stream;   // past the caches
 };
 // The partial sums of a device: `count` from its first place on, and those of tensors with a pitch, `pitched` from behind `dense_turns` turns on.
 template <int S>
@@ -329,7 +330,7 @@ struct ClipPlan {
     float* norm[S];           // null: not wanted
     float most;
     int32_t parts, chunks, k, partial;   // partial: the sums are P(sum)
-    int32_t first_device;
+    int32_t first_device, stream;
 };
 template <template <bool> class PART, int CAP>
 int32_t launch_square_sum(const SquarePlan<PART, CAP>& plan, int devices, int blocks, hipStream_t stream);

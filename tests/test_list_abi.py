@@ -81,10 +81,11 @@ def test_square_sum_raw_entries():
 def test_workspace_counts_partial_sums():
     def room(tensors, sigs, k):
         return sbp.sbp_square_sum_workspace(sbp.SbpList(tensors, sigs), k)
-    assert room([T(1, 1, 1)], [sbp.B], 1) == 8 and room([T(1, 0, 8)], [sbp.B], 1) == 0
-    assert room([T(1, 8, 1024)], [sbp.B], 1) == 8 and room([T(1, 8, 1025)], [sbp.B], 1) == 16       # 8192 elements a workgroup at a time
-    assert room([T(8, 1 << 16, 1 << 14)], [sbp.S(0)], 8) == 8 * 2048                                 # at most 2048 workgroups
-    assert room([T(2, 1, 8)], [sbp.S(0)], 2) == 2 * 8                                               # as if the second device had something
+    # launches of 160 tensors, of 80 with rows at a pitch, one more of each; workgroups of 8192 elements, at most 2048
+    assert room([T(1, 1, 1)], [sbp.B], 1) == 4 * 8 and room([T(1, 0, 8)], [sbp.B], 1) == 0 and room([], [], 1) == 0
+    assert room([T(1, 8, 1024)], [sbp.B], 1) == 4 * 8 and room([T(1, 8, 1025)], [sbp.B], 1) == 4 * 2 * 8
+    assert room([T(8, 1 << 16, 1 << 14)], [sbp.S(0)], 8) == 8 * 4 * 2048 * 8
+    assert room([T(2, 1, 8)] * 161, [sbp.S(0)] * 161, 2) == 2 * (2 + 3 + 2) * 161 * 8
 
 
 def clip(inp=None, sigs=None, sq=None, ssq=sbp.P_SUM, most=1.0, out=None, norm=None, k=2):
