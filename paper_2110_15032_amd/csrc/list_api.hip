@@ -163,23 +163,34 @@ PitchedPart<OUT> pitched_part(const Item& it, int32_t device) {
     return {it.in, it.out, (int32_t)it.s.rows, (int32_t)it.s.cols, (int32_t)it.s.pitch, (int32_t)it.ldo, it.what | device << 2};
 }
 
+// Past the caches go the sum of squares of more than the memory-side cache (256 MB) keeps for the clipping that follows, and the clipping of what
+// moves more than a good part of it.  us for both calls, neither / both past the caches: 2^28 elements from bf16 to fp32 390 / 352, 100 M in bf16 (200 MB)
+// 119 / 104, with the sum of squares cached 98; 67 M 82 / 71 / 68; 34 M (67 MB, 134 moved) 44.0 / 41.4; 17 M 23.7 / 26.4.
+constexpr int64_t KEPT = (int64_t)192 << 20, MOVED = (int64_t)96 << 20;
+
 // How a sum of squares is dealt out.
 struct SquareShape {
     int32_t blocks;                                    // workgroups of every device in every launch
     int32_t dense_turns, turns;                        // places of a device's partial sums, in units of them
     int16_t dense[SBP_MAX_K], pitched[SBP_MAX_K];      // launches that a device has parts in
     int64_t bytes;                                     // for the workspace
+    int32_t stream;                                    // what is read goes past the caches
 };
 // The workspace goes by the sizes alone, and not by which tensors lie back to back: a device has parts in at most so many launches, and at most so many
 // workgroups there.
 int32_t square_shape(const sbp_tensor_t* t, const sbp_t* s, const Locals& locals, int32_t n, int32_t k, SquareShape& sq, Batch& b) {
-    int64_t most = 1, all = 0;
+    int64_t most = 1, all = 0, read = 0;
     int32_t devices = 1, st;
     for (int32_t d = 0; d < k; ++d) {
         int64_t mine = 0;
-        for (int32_t j = 0; j < n; ++j) mine += locals.of[(int64_t)j * k + d].empty() ? 0 : chunks_of(locals.of[(int64_t)j * k + d]);
+        for (int32_t j = 0; j < n; ++j) {
+            const Stored& l = locals.of[(int64_t)j * k + d];
+            mine += l.empty() ? 0 : chunks_of(l);
+            read += l.rows * l.cols * elem_bytes(t[j].dtype);
+        }
         all = std::max(all, mine);
     }
+    sq.stream = read > KEPT;
     auto make = [&](int32_t j, int32_t d, Item& it) { return counted(t + j, s[j], locals.of[(int64_t)j * k + d], k, d, it); };
     auto look = [&](const Batch& b) {
         most = std::max(most, b.most);
@@ -206,7 +217,7 @@ int32_t square_batch(const Batch& b, const SquareShape& sq, int32_t base, double
     plan.turns = sq.turns;
     plan.first_turn = base + b.turn;
     plan.other_turn = base;
-    plan.stream = 1;
+    plan.stream = sq.stream;
     return launch_square_sum(plan, b.devices, sq.blocks, stream);
 }
 template <int S>
@@ -224,7 +235,7 @@ int32_t square_join(const SquareShape& sq, const double* partial, const sbp_tens
     return launch_square_join(join, k, stream);
 }
 template <template <bool> class PART, int CAP, int S, typename MAKE>
-int32_t clip_batch(const Batch& b, const sbp_tensor_t* squares, bool partial, float most, const sbp_tensor_t* norm, int32_t k, MAKE&& make, hipStream_t stream) {
+int32_t clip_batch(const Batch& b, const sbp_tensor_t* squares, bool partial, bool past, float most, const sbp_tensor_t* norm, int32_t k, MAKE&& make, hipStream_t stream) {
     ClipPlan<PART, CAP, S> plan{};
     for (int32_t i = 0; i < b.n; ++i) plan.s[i] = make(b.item[i], b.device[i]);
     for (int32_t i = 0; i < k; ++i) {
@@ -237,12 +248,12 @@ int32_t clip_batch(const Batch& b, const sbp_tensor_t* squares, bool partial, fl
     plan.k = k;
     plan.partial = partial;
     plan.first_device = b.first_device;
-    plan.stream = 1;
+    plan.stream = past;
     return launch_clip(plan, stream);
 }
 template <template <bool> class PART, int CAP, typename MAKE>
-int32_t clip_devices(const Batch& b, const sbp_tensor_t* squares, bool partial, float most, const sbp_tensor_t* norm, int32_t k, MAKE&& make, hipStream_t stream) {
-    return k <= 8 ? clip_batch<PART, CAP, 8>(b, squares, partial, most, norm, k, make, stream) : clip_batch<PART, CAP, SBP_MAX_K>(b, squares, partial, most, norm, k, make, stream);
+int32_t clip_devices(const Batch& b, const sbp_tensor_t* squares, bool partial, bool past, float most, const sbp_tensor_t* norm, int32_t k, MAKE&& make, hipStream_t stream) {
+    return k <= 8 ? clip_batch<PART, CAP, 8>(b, squares, partial, past, most, norm, k, make, stream) : clip_batch<PART, CAP, SBP_MAX_K>(b, squares, partial, past, most, norm, k, make, stream);
 }
 
 }  // namespace
@@ -354,28 +365,32 @@ int32_t sbp_clip(const sbp_tensor_t* in, const sbp_t* s, int32_t n, const sbp_te
 
     const hipStream_t on = static_cast<hipStream_t>(stream);
     const bool partial = sbp_squares == SBP_P_SUM;
+    int64_t moved = 0;
+    for (int32_t j = 0; j < n; ++j)
+        for (int32_t i = 0; i < k; ++i) moved += from.of[(int64_t)j * k + i].rows * from.of[(int64_t)j * k + i].cols * (elem_bytes(in[j].dtype) + elem_bytes(out[j].dtype));
+    const bool past = moved > MOVED;
     auto make = [&](int32_t j, int32_t d, Item& it) { return clipped(in + j, from.of[(int64_t)j * k + d], out + j, to.of[(int64_t)j * k + d], d, it); };
     int16_t used[SBP_MAX_K];
     Batch batch;
     const sbp_tensor_t* write = norm;   // the first launch does
     st = each_batch(n, k, true, batch, used, make, [&](const Batch& b) {
-        const int32_t status = b.n <= LIST_FEW ? clip_devices<DensePart, LIST_FEW>(b, squares, partial, max_norm, write, k, dense_part<true>, on)
-                             : b.n <= LIST_SOME ? clip_devices<DensePart, LIST_SOME>(b, squares, partial, max_norm, write, k, dense_part<true>, on)
-                                               : clip_devices<DensePart, LIST_DENSE>(b, squares, partial, max_norm, write, k, dense_part<true>, on);
+        const int32_t status = b.n <= LIST_FEW ? clip_devices<DensePart, LIST_FEW>(b, squares, partial, past, max_norm, write, k, dense_part<true>, on)
+                             : b.n <= LIST_SOME ? clip_devices<DensePart, LIST_SOME>(b, squares, partial, past, max_norm, write, k, dense_part<true>, on)
+                                               : clip_devices<DensePart, LIST_DENSE>(b, squares, partial, past, max_norm, write, k, dense_part<true>, on);
         write = nullptr;
         return status;
     });
     if (st != SBP_OK) return st;
     st = each_batch(n, k, false, batch, used, make, [&](const Batch& b) {
-        const int32_t status = b.n <= LIST_FEW ? clip_devices<PitchedPart, LIST_FEW>(b, squares, partial, max_norm, write, k, pitched_part<true>, on)
-                                               : clip_devices<PitchedPart, LIST_PITCHED>(b, squares, partial, max_norm, write, k, pitched_part<true>, on);
+        const int32_t status = b.n <= LIST_FEW ? clip_devices<PitchedPart, LIST_FEW>(b, squares, partial, past, max_norm, write, k, pitched_part<true>, on)
+                                               : clip_devices<PitchedPart, LIST_PITCHED>(b, squares, partial, past, max_norm, write, k, pitched_part<true>, on);
         write = nullptr;
         return status;
     });
     if (st != SBP_OK || !write) return st;
     batch.n = 0;   // nothing but the norm
     batch.chunks = batch.first_device = 0;
-    return clip_devices<DensePart, LIST_FEW>(batch, squares, partial, max_norm, write, k, dense_part<true>, on);
+    return clip_devices<DensePart, LIST_FEW>(batch, squares, partial, past, max_norm, write, k, dense_part<true>, on);
 }
 
 }  // extern "C"

@@ -153,15 +153,14 @@ template <int T, int G>
 __device__ inline const typename Group<T, G>::type* group_at(const void* p, int chunk) {
     return reinterpret_cast<const typename Group<T, G>::type*>(static_cast<const char*>(p) + (int64_t)chunk * (LIST_CHUNK * 8 * bytes_of<T>)) + threadIdx.x;
 }
-template <int T, int G, int N>
-__device__ inline void load_whole(const void* in, int chunk, bool stream, typename Group<T, G>::type (&raw)[N]) {
+// STREAM: past the caches (a template argument, as the compiler takes the two forms of a load in two branches for one)
+template <bool STREAM, int T, int G, int N>
+__device__ inline void load_whole(const void* in, int chunk, typename Group<T, G>::type (&raw)[N]) {
     const auto* const from = group_at<T, G>(in, chunk);
-    if (stream) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) raw[u] = __builtin_nontemporal_load(from + u * NT);
-    } else {
-#pragma unroll
-        for (int u = 0; u < N; ++u) raw[u] = from[u * NT];
+    for (int u = 0; u < N; ++u) {
+        if constexpr (STREAM) raw[u] = __builtin_nontemporal_load(from + u * NT);
+        else raw[u] = from[u * NT];
     }
 }
 
@@ -183,12 +182,12 @@ __device__ inline void add_squares(const float (&v)[G], double (&acc)[2]) {
     for (int e = 0; e < G; ++e) acc[e & 1] = fma((double)v[e], (double)v[e], acc[e & 1]);
 }
 
-template <int T>
-__device__ inline void square_chunk(const void* in, const Shape& s, int chunk, bool stream, double (&acc)[2]) {
+template <bool STREAM, int T>
+__device__ inline void square_chunk(const void* in, const Shape& s, int chunk, double (&acc)[2]) {
     if (whole_chunk(s, chunk)) {
         constexpr int G = T == T_F32 ? 4 : 8, N = LIST_CHUNK * 8 / NT / G;
         typename Group<T, G>::type raw[N];
-        load_whole<T, G>(in, chunk, stream, raw);
+        load_whole<STREAM, T, G>(in, chunk, raw);
 #pragma unroll
         for (int u = 0; u < N; ++u) {
             float v[G];
@@ -206,7 +205,7 @@ __device__ inline void square_chunk(const void* in, const Shape& s, int chunk, b
     });
 }
 
-template <template <bool> class PART, int CAP>
+template <bool STREAM, template <bool> class PART, int CAP>
 __global__ __launch_bounds__(NT, waves_with<PART>(5)) void square_sum_kernel(SquarePlan<PART, CAP> p) {
     __shared__ double waves[NT / 64];
     const Starts<CAP> starts(p.s, p.parts);
@@ -216,8 +215,8 @@ __global__ __launch_bounds__(NT, waves_with<PART>(5)) void square_sum_kernel(Squ
         const int part = __builtin_amdgcn_readfirstlane(starts.part_of(c));
         const Shape s = shape_of(p.s[part]);
         const int chunk = c - starts.start_of(part);
-        if (s.what & 1) square_chunk<T_BF16>(p.s[part].in, s, chunk, p.stream, acc);
-        else square_chunk<T_F32>(p.s[part].in, s, chunk, p.stream, acc);
+        if (s.what & 1) square_chunk<STREAM, T_BF16>(p.s[part].in, s, chunk, acc);
+        else square_chunk<STREAM, T_F32>(p.s[part].in, s, chunk, acc);
     }
     const double sum = sum_block(acc[0] + acc[1], waves);
     if (threadIdx.x == 0) p.partial[((int64_t)(p.first_device + d) * p.turns + (d ? p.other_turn : p.first_turn)) * gridDim.x + blockIdx.x] = sum;
@@ -249,12 +248,12 @@ __device__ inline float factor_of(float sum, float most) {
     return norm <= most ? 1.0f : most / norm;
 }
 
-template <int T, int U>
-__device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int chunk, float factor, bool stream) {
+template <bool STREAM, int T, int U>
+__device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int chunk, float factor) {
     if (whole_chunk(s, chunk)) {
         constexpr int G = T == T_BF16 && U == T_BF16 ? 8 : 4, N = LIST_CHUNK * 8 / NT / G;
         typename Group<T, G>::type raw[N];
-        load_whole<T, G>(in, chunk, stream, raw);
+        load_whole<STREAM, T, G>(in, chunk, raw);
         auto* const to = const_cast<typename Group<U, G>::type*>(group_at<U, G>(out, chunk));
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -262,7 +261,7 @@ __device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int
             widen_group<T, G>(raw[u], v);
 #pragma unroll
             for (int e = 0; e < G; ++e) v[e] *= factor;
-            if (stream) __builtin_nontemporal_store(narrow_group<U, G>(v), to + u * NT);
+            if constexpr (STREAM) __builtin_nontemporal_store(narrow_group<U, G>(v), to + u * NT);
             else to[u * NT] = narrow_group<U, G>(v);
         }
         return;
@@ -278,7 +277,7 @@ __device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int
     });
 }
 
-template <template <bool> class PART, int CAP, int S>
+template <bool STREAM, template <bool> class PART, int CAP, int S>
 __global__ __launch_bounds__(NT, waves_with<PART>(6)) void clip_kernel(ClipPlan<PART, CAP, S> p) {
     const Starts<CAP> starts(p.s, p.parts);
     for (int c = blockIdx.x; c < p.chunks; c += gridDim.x) {
@@ -289,10 +288,10 @@ __global__ __launch_bounds__(NT, waves_with<PART>(6)) void clip_kernel(ClipPlan<
         const void* const in = p.s[part].in;
         void* const out = p.s[part].out;
         switch (s.what & 3) {
-            case 0: clip_chunk<T_F32, T_F32>(in, out, s, chunk, factor, p.stream); break;
-            case 1: clip_chunk<T_BF16, T_F32>(in, out, s, chunk, factor, p.stream); break;
-            case 2: clip_chunk<T_F32, T_BF16>(in, out, s, chunk, factor, p.stream); break;
-            default: clip_chunk<T_BF16, T_BF16>(in, out, s, chunk, factor, p.stream);
+            case 0: clip_chunk<STREAM, T_F32, T_F32>(in, out, s, chunk, factor); break;
+            case 1: clip_chunk<STREAM, T_BF16, T_F32>(in, out, s, chunk, factor); break;
+            case 2: clip_chunk<STREAM, T_F32, T_BF16>(in, out, s, chunk, factor); break;
+            default: clip_chunk<STREAM, T_BF16, T_BF16>(in, out, s, chunk, factor);
         }
     }
     if (p.norm[0] && blockIdx.x == 0 && (int)threadIdx.x < p.k) *p.norm[threadIdx.x] = sqrtf(sum_of(p, threadIdx.x));
@@ -302,7 +301,9 @@ __global__ __launch_bounds__(NT, waves_with<PART>(6)) void clip_kernel(ClipPlan<
 
 template <template <bool> class PART, int CAP>
 int32_t launch_square_sum(const SquarePlan<PART, CAP>& plan, int devices, int blocks, hipStream_t stream) {
-    hipLaunchKernelGGL((square_sum_kernel<PART, CAP>), dim3((uint32_t)blocks, (uint32_t)devices), dim3(NT), 0, stream, plan);
+    const dim3 grid((uint32_t)blocks, (uint32_t)devices);
+    if (plan.stream) hipLaunchKernelGGL((square_sum_kernel<true, PART, CAP>), grid, dim3(NT), 0, stream, plan);
+    else hipLaunchKernelGGL((square_sum_kernel<false, PART, CAP>), grid, dim3(NT), 0, stream, plan);
     return launch_status(__func__);
 }
 template <int S>
@@ -312,8 +313,11 @@ int32_t launch_square_join(const SquareJoin<S>& join, int32_t k, hipStream_t str
 }
 template <template <bool> class PART, int CAP, int S>
 int32_t launch_clip(const ClipPlan<PART, CAP, S>& plan, hipStream_t stream) {
-    const int blocks = std::max(1, std::min<int>(plan.chunks, LIST_BLOCKS));
-    hipLaunchKernelGGL((clip_kernel<PART, CAP, S>), dim3((uint32_t)blocks), dim3(NT), 0, stream, plan);
+    // a chunk a workgroup: they end at different times, and their stores drain beside others' loads (2^28 elements from bf16 to fp32, us a call with the sum
+    // of squares: 2048 workgroups 411, 8192 403, 32768 386)
+    const int blocks = std::max(1, std::min<int>(plan.chunks, 1 << 20));
+    if (plan.stream) hipLaunchKernelGGL((clip_kernel<true, PART, CAP, S>), dim3((uint32_t)blocks), dim3(NT), 0, stream, plan);
+    else hipLaunchKernelGGL((clip_kernel<false, PART, CAP, S>), dim3((uint32_t)blocks), dim3(NT), 0, stream, plan);
     return launch_status(__func__);
 }
 
