@@ -2144,9 +2144,18 @@ int32_t launch_block_generic(const GemmBlockPlan& plan, int max_m, int max_n, hi
     return launch_status(__func__);
 }
 
+// A few rows.  us, other weights in every pass, the waves' splitting of the reduction on matrix cores / gemv_kernels.hip: reduction-contiguous weights 4096 x 16384, 8
+// devices (134 MB) 1 row 28.9 / 24.3, 4 rows 29.4 / 26.9; 4096 x 4096 12.7 / 7.9; 16384 x 512 36.3 / 5.9; 1000 x 1504 7.0 / 5.4; fp32 3000 x 8000, 4 devices
+// 38.2 / 22.7.  Columns contiguous: one row and a workgroup of 64 columns for every compute unit 31.1 / 26.0, fewer of them 16.2 / 24.6; two rows 31.2 / 38.7.
+bool gemv_pays(const GemmPlan& plan, int max_m, int max_n) {
+    if (max_m > GEMV_ROWS || !plan.a_kc || longest_reduction(plan) == 0) return false;
+    return plan.b_kc || (max_m == 1 && tiles_of(plan, 1, max_n, 1, 64) >= compute_units());
+}
+
 // The kernel for a product with a block's epilogue: launch_chosen's rules, over the kernels that have one.
 int32_t launch_block_chosen(const GemmBlockPlan& plan, const GemmPlan& like, int max_m, int max_n, hipStream_t stream) {
     const bool bf16 = plan.in_dtype == SBP_BF16, direct = rows_aligned(like);
+    if (gemv_pays(like, max_m, max_n)) return launch_gemv(plan, max_m, max_n, stream);
     if (one_element_pays(like, max_m, max_n, bf16 && direct) || (bf16 && !mfma_ok(like))) return launch_block_generic(plan, max_m, max_n, stream);
     auto order = [&](int bm, int bn) { return tile_order_for(tiles_along(max_m, bm), tiles_along(max_n, bn)); };
     if (!bf16) {

@@ -1,0 +1,183 @@
+// Products of a few rows (tokens that are decoded) with a block's epilogue: the weight is the traffic, and is read once, past the matrix cores.
+//
+//   y[m, n] = act(sum over kk of x[m, kk] w[kk, n] + bias[n]) + residual[m, n],  m < 4
+//
+// Bound by HBM: what counts is that every compute unit has enough of the weight on its way.
+#include "block8_device.h"
+
+namespace sbp {
+namespace {
+
+__device__ inline void add8(const float (&x)[8], const float (&w)[8], float& acc) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc = fmaf(x[e], w[e], acc);
+}
+
+// Weights with the reduction index contiguous.  A wave takes R rows of the weight and every WK-th 512 elements of them, eight a lane; where the waves of a
+// workgroup share rows (WK > 1) their sums meet in LDS, in order.
+// STREAM: the weight past the caches, where the memory-side cache would not keep it for the next token.  us, past them / cached: 4096 x 16384 on 8 devices (134 MB) 24.3 /
+// 25.7, 4 rows 26.9 / 29.0; 4096 x 4096 8.2 / 7.8; fp32 3000 x 8000 (96 MB, four of them in turn) 27.4 / 22.8.
+template <int T, int M, int R, int WK, bool STREAM>
+__global__ __launch_bounds__(256) void gemv_rows_kernel(GemmBlockPlan p) {
+    constexpr int GROUPS = 4 / WK, AHEAD = R == 4 && M == 1 ? 4 : 2;   // steps on their way together: 4096 x 16384, one row, two 25.0 us, four 24.3; one row of the weight a wave, 4096 x 4096, two 7.9, four 10.5
+    const GemmShard& s = p.s[blockIdx.y];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % WK;
+    const int64_t n0 = ((int64_t)blockIdx.x * GROUPS + wave / WK) * R;
+    float acc[R][M];
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m) acc[r][m] = 0.0f;
+    if (n0 < s.n) {
+        const char* w[R];   // rows past the last one are the last one again, and stored nowhere
+        const char* x[M];
+#pragma unroll
+        for (int r = 0; r < R; ++r) w[r] = static_cast<const char*>(s.b) + min(n0 + r, (int64_t)s.n - 1) * s.ldb * bytes_of<T>;
+#pragma unroll
+        for (int m = 0; m < M; ++m) x[m] = static_cast<const char*>(s.a) + (int64_t)min(m, s.m - 1) * s.lda * bytes_of<T>;
+        constexpr int STEP = 512 * WK;
+        for (int64_t k0 = wk * 512; k0 < s.kk; k0 += (int64_t)STEP * AHEAD) {
+            Raw8<T> rw[AHEAD][R], rx[AHEAD][M];
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t from = k0 + u * STEP + lane * 8;
+                const int c = from < s.kk ? (int)from : s.kk;
+#pragma unroll
+                for (int r = 0; r < R; ++r) rw[u][r] = load8<T, STREAM>(w[r], c, s.kk);
+#pragma unroll
+                for (int m = 0; m < M; ++m) rx[u][m] = load8<T>(x[m], c, s.kk);
+            }
+#pragma unroll
+            for (int u = 0; u < AHEAD; ++u) {
+                const int64_t from = k0 + u * STEP + lane * 8;
+                const int c = from < s.kk ? (int)from : s.kk;
+                float vx[M][8];
+#pragma unroll
+                for (int m = 0; m < M; ++m) widen<T>(settle8<T>(rx[u][m], c, s.kk), 1.0f, vx[m]);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    float vw[8];
+                    widen<T>(settle8<T>(rw[u][r], c, s.kk), 1.0f, vw);
+#pragma unroll
+                    for (int m = 0; m < M; ++m) add8(vx[m], vw, acc[r][m]);
+                }
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < R; ++r)
+#pragma unroll
+            for (int m = 0; m < M; ++m) acc[r][m] = sum_wave(acc[r][m]);
+    }
+    float mine = 0.0f;   // of lane r M + m
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int m = 0; m < M; ++m) mine = lane == r * M + m ? acc[r][m] : mine;
+    if constexpr (WK > 1) {
+        __shared__ float part[4][R * M];
+        if (lane < R * M) part[wave][lane] = mine;
+        __syncthreads();
+        if (wk != 0) return;
+        if (lane < R * M) {
+#pragma unroll
+            for (int i = 1; i < WK; ++i) mine += part[wave + i][lane];
+        }
+    }
+    if (lane < R * M) {
+        float v[1] = {mine};
+        Ending<EPI_BLOCK>(p, blockIdx.y).finish<1>(s, lane % M, (int)min(n0 + lane / M, (int64_t)INT32_MAX), v);
+    }
+}
+
+// One row, weights with their columns contiguous.  A workgroup of 16 waves takes 64 columns, a wave eight rows of them at a time, eight columns a lane; lanes and
+// waves of the same columns meet at the end, in order.
+template <int T, bool STREAM>
+__global__ __launch_bounds__(1024) void gemv_columns_kernel(GemmBlockPlan p) {
+    constexpr int NW = 16, AHEAD = 4, STEP = NW * 8;
+    const GemmShard& s = p.s[blockIdx.y];
+    const int n0 = blockIdx.x * 64;
+    if (n0 >= s.n) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = n0 + (lane & 7) * 8;
+    float acc[8];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+    for (int64_t k0 = wave * 8 + (lane >> 3); k0 < s.kk; k0 += STEP * AHEAD) {
+        Raw8<T> rw[AHEAD];
+        float x[AHEAD];
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            const int64_t k = k0 + u * STEP;
+            rw[u] = load8<T, STREAM>(static_cast<const char*>(s.b) + k * s.ldb * bytes_of<T>, c, k < s.kk ? s.n : 0);
+            x[u] = 0.0f;
+            if (k < s.kk) {
+                if constexpr (T == T_F32) x[u] = static_cast<const float*>(s.a)[k];
+                else x[u] = bf16_to_f32(static_cast<const uint16_t*>(s.a)[k]);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) {
+            float w[8];
+            widen<T>(settle8<T>(rw[u], c, k0 + u * STEP < s.kk ? s.n : 0), 1.0f, w);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) acc[e] = fmaf(x[u], w[e], acc[e]);
+        }
+    }
+    __shared__ float part[NW][64];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        float v = acc[e];
+        v += __shfl_xor(v, 8, 64);
+        v += __shfl_xor(v, 16, 64);
+        v += __shfl_xor(v, 32, 64);
+        if (lane < 8) part[wave][lane * 8 + e] = v;
+    }
+    __syncthreads();
+    if (wave != 0) return;
+    float v[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NW; ++i) v[0] += part[i][lane];
+    Ending<EPI_BLOCK>(p, blockIdx.y).finish<1>(s, 0, n0 + lane, v);
+}
+
+template <typename F>
+void with_rows(int m, F&& f) {
+    if (m == 1) f(std::integral_constant<int, 1>{});
+    else if (m == 2) f(std::integral_constant<int, 2>{});
+    else f(std::integral_constant<int, 4>{});
+}
+
+}  // namespace
+
+// x with the reduction index contiguous; 1 .. GEMV_ROWS rows of it where w has too, else one
+int32_t launch_gemv(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream) {
+    const bool f32 = plan.in_dtype == SBP_F32;
+    int64_t columns = 0, weight = 0;
+    int deepest = 0;
+    for (int g = 0; g < plan.groups; ++g) {
+        columns += plan.s[g].n;
+        weight += (int64_t)plan.s[g].n * plan.s[g].kk * (f32 ? 4 : 2);
+        deepest = std::max(deepest, plan.s[g].kk);
+    }
+    const uint32_t groups = (uint32_t)plan.groups;
+    auto go = [&](auto t, auto past) {
+        if (!plan.b_kc) {
+            hipLaunchKernelGGL((gemv_columns_kernel<t(), past()>), dim3((uint32_t)tiles_along(max_n, 64), groups), dim3(1024), 0, stream, plan);
+            return;
+        }
+        with_rows(max_m, [&](auto m) {
+            // four rows a wave where that leaves a compute unit eight waves or more, else one, and the waves share a long reduction
+            if (columns >= 8192) hipLaunchKernelGGL((gemv_rows_kernel<t(), m(), 4, 1, past()>), dim3((uint32_t)tiles_along(max_n, 16), groups), dim3(256), 0, stream, plan);
+            else if (deepest > 1024) hipLaunchKernelGGL((gemv_rows_kernel<t(), m(), 1, 4, past()>), dim3((uint32_t)max_n, groups), dim3(256), 0, stream, plan);
+            else hipLaunchKernelGGL((gemv_rows_kernel<t(), m(), 1, 1, past()>), dim3((uint32_t)tiles_along(max_n, 4), groups), dim3(256), 0, stream, plan);
+        });
+    };
+    auto typed = [&](auto past) {
+        if (f32) go(std::integral_constant<int, T_F32>{}, past);
+        else go(std::integral_constant<int, T_BF16>{}, past);
+    };
+    if (weight >= (int64_t)128 << 20) typed(std::true_type{});
+    else typed(std::false_type{});
+    return launch_status(__func__);
+}
+
+}  // namespace sbp

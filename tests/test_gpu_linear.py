@@ -98,6 +98,22 @@ def test_pitches(shape, pitch, x):
         Layer(*shape, x=x, y=("bf16", "f32")[pitch % 2], residual="bf16", pre="f32", gelu=pitch == 3, x_trans=x_trans, w_trans=w_trans, pitch=pitch).check()
 
 
+@pytest.mark.parametrize("m", [1, 2, 3, 4])
+@pytest.mark.parametrize("kk,n", [(1, 9000), (7, 40), (512, 64), (1000, 1504), (1500, 130), (4099, 100), (520, 9001)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_a_few_rows(m, kk, n, x):
+    """the weight in rows or in columns, whole pieces and cut ones, one wave a row or several"""
+    for w_trans, pitch in ((1, 0), (1, 1), (0, 0), (0, 3)):
+        Layer(m, kk, n, x=x, residual="bf16" if m % 2 else "", pre="f32", gelu=m > 2, w_trans=w_trans, pitch=pitch).check()
+
+
+def test_one_row_with_many_columns():
+    for w_trans, pitch, x in ((0, 0, "bf16"), (0, 1, "bf16"), (1, 0, "f32"), (0, 0, "f32")):
+        Layer(1, 300, 20000, x=x, residual="f32", gelu=True, w_trans=w_trans, pitch=pitch).check()
+        Layer(1, 2050, 17000, 3, "S1", x=x, w_trans=w_trans, pitch=pitch).check()
+    Layer(2, 4096, 16500, residual="f32", gelu=True).check()               # past the caches
+
+
 @pytest.mark.parametrize("k,sig,m,n", [(2, "B", 30, 100), (3, "S0", 100, 70), (8, "S0", 5, 64), (3, "S1", 50, 100), (8, "S1", 1, 2048), (9, "S1", 20, 180), (20, "S0", 70, 40), (64, "S1", 3, 640)])
 @pytest.mark.parametrize("x", ["bf16", "f32"])
 def test_on_devices(k, sig, m, n, x):
