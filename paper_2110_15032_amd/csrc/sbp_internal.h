@@ -342,4 +342,111 @@ int32_t launch_square_join(const SquareJoin<S>& join, int32_t k, hipStream_t str
 template <template <bool> class PART, int CAP, int S>
 int32_t launch_clip(const ClipPlan<PART, CAP, S>& plan, hipStream_t stream);
 
+// ---------------------------------------------------------------------------------------------
+// The gradient of a block's epilogue: da = dy gelu'(pre), and the sum of da (or of dy) over the rows.
+// ---------------------------------------------------------------------------------------------
+constexpr int LINEAR_GRAD_SHARDS = 8;
+struct LinearGradShard {
+    const void* dy;
+    const void* pre;      // null: no activation
+    const void* scales;   // of pre, 8 bits only
+    void* da;             // null: no activation
+    float* dbias;
+    float* part;          // [blocks][cols], where blocks > 1
+    int32_t rows, cols, lddy, ldp, lds, ldda, blocks;
+};
+template <int S>
+struct LinearGradPlan {
+    LinearGradShard s[S];
+    int32_t streams;      // of block8_device.h, chosen at the launch
+};
+template <int S>
+int32_t launch_linear_grad(const LinearGradPlan<S>& plan, int n, int32_t dy, int32_t pre, bool gelu, hipStream_t stream);
+// workgroups along the rows of a shard, each of which leaves a partial sum
+int32_t linear_grad_blocks(int64_t rows, int64_t cols, int32_t k);
+
+// ---------------------------------------------------------------------------------------------
+// The norms behind and in front of a block, with its gate and the residual.  A launch takes S shards: the argument block costs about a
+// microsecond a KB, so that a single device has a launch of its own size.
+// ---------------------------------------------------------------------------------------------
+constexpr int RESNORM_SHARDS = 8;
+enum ResNormFlags : int32_t {
+    RN_POST = 1, RN_POST_LAYER = 2, RN_PRE = 4, RN_PRE_LAYER = 8,   // which norms, and whether they take the mean off
+    RN_DH = 16,                                                     // gradient: the residual stream's own
+    RN_BF16_WEIGHTS = 32,
+    RN_STREAM_H = 64, RN_STREAM_Y = 128                             // results past the caches (dr and dx in the gradient)
+};
+struct ResNormShard {
+    const void* x;
+    const void* r;
+    void* h;
+    void* y;             // pre only
+    void* y_scales;
+    float* mean1;        // null: not wanted
+    float* rstd1;
+    float* mean2;
+    float* rstd2;
+    const void* gate;    // null: ones
+    const void* gamma1;
+    const void* beta1;   // null: zeros
+    const void* gamma2;
+    const void* beta2;
+    int32_t rows, ldx, ldr, ldh, ldy, lds;
+};
+template <int S>
+struct ResNormPlan {
+    ResNormShard s[S];
+    int32_t cols, flags;
+    float alpha, eps1, eps2;
+};
+struct ResNormGradShard {
+    const void* x;
+    const void* h;       // pre only
+    const void* dh;      // RN_DH only
+    const void* dy;      // pre only
+    void* dx;
+    void* dr;
+    const float* mean1;
+    const float* rstd1;
+    const float* mean2;
+    const float* rstd2;
+    const void* gate;    // null: ones
+    const void* gamma1;
+    const void* gamma2;
+    float* part;         // [blocks][4][cols], null: no weight's gradient is wanted
+    int32_t rows, ldx, ldh, lddh, lddy, lddx, lddr, blocks;
+};
+template <int S>
+struct ResNormGradPlan {
+    ResNormGradShard s[S];
+    int32_t cols, flags;
+    float alpha;
+};
+struct ResNormJoinShard {
+    const float* part;
+    const void* gate;
+    const void* gamma1;
+    const void* beta1;
+    float* dgate;        // null: not wanted
+    float* dgamma1;
+    float* dbeta1;
+    float* dgamma2;
+    float* dbeta2;
+    int32_t blocks;
+};
+template <int S>
+struct ResNormJoin {
+    ResNormJoinShard s[S];
+    int32_t cols, flags;
+};
+// types of x, of the residual stream and of y (its gradient); n shards, 1 .. S
+template <int S>
+int32_t launch_residual_norm(const ResNormPlan<S>& plan, int n, int32_t x, int32_t r, int32_t y, hipStream_t stream);
+template <int S>
+int32_t launch_residual_norm_grad(const ResNormGradPlan<S>& plan, int n, int32_t x, int32_t r, int32_t y, hipStream_t stream);
+template <int S>
+int32_t launch_residual_norm_join(const ResNormJoin<S>& join, int n, hipStream_t stream);
+// workgroups that a shard of so many rows gets, each of which leaves one partial sum of the weights' gradients
+int32_t residual_norm_grad_blocks(int64_t rows, int64_t cols, int32_t k);
+
 }  // namespace sbp
