@@ -17,6 +17,7 @@ __global__ __launch_bounds__(NT) void linear_grad_kernel(LinearGradPlan<S> p) {
     constexpr int AHEAD = 4;   // rows of a lane on their way together
     const int lane = threadIdx.x & 31, side = threadIdx.x >> 5, c = blockIdx.x * COLS + lane * 8;
     const int step = s.blocks * SIDE;
+    const bool cut = s.cols % 8 != 0;   // some lane has fewer than eight elements
     float sum[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] = 0.0f;
@@ -41,10 +42,10 @@ __global__ __launch_bounds__(NT) void linear_grad_kernel(LinearGradPlan<S> p) {
             const int64_t row = first + (int64_t)u * step;
             const int upto = row < s.rows ? s.cols : 0;
             float d[8];
-            widen<YT>(settle8<YT>(raw[u], c, upto), 1.0f, d);
+            widen<YT>(cut ? settle8<YT>(raw[u], c, upto) : raw[u], 1.0f, d);
             if constexpr (GELU) {
                 float a[8];
-                widen<PT>(settle8<PT>(at[u], c, upto), scale_of(byte[u]), a);
+                widen<PT>(cut ? settle8<PT>(at[u], c, upto) : at[u], scale_of(byte[u]), a);
 #pragma unroll
                 for (int e = 0; e < 8; ++e) d[e] *= gelu_slope<YT == T_BF16>(a[e]);
                 store8<YT>(static_cast<char*>(s.da) + (row * s.ldda + c) * bytes_of<YT>, narrow<YT>(d), upto - c, p.streams & STREAM_OUT);
