@@ -13,6 +13,11 @@
 namespace sbp {
 namespace {
 
+// Past the caches: bf16 in rows of more than 2048.  16384 x 4096 158.5 us with it, 163 without, 1 device 1024 x 8192 32.1 / 36.2, 4096 x 8192 91.0 / 96.7, fp32 residual 8192 x 4096
+// 125.5 / 129 - but in fp32, whose eight elements are two loads of half a line each, 198 / 170, and in short rows whose inputs the memory-side cache
+// holds 24.6 / 22.1 (4096 x 1024).
+template <int T, int TPR> constexpr bool streamed = T == T_BF16 && TPR >= 512;
+
 template <int XT, int RT, int YT, int TPR, int V, int S>
 __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kernel(ResNormGradPlan<S> p) {
     constexpr int NT = TPR < 256 ? 256 : TPR, G = NT / TPR, NW = TPR / 64, N = V * 8, CAP = TPR * V * 8;
@@ -63,10 +68,10 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const int c = (v * TPR + t) * 8;
-            next_x[v] = load8<XT>(static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>, c, upto);
-            next_h[v] = load8<RT>(static_cast<const char*>(s.h) + row * s.ldh * bytes_of<RT>, c, pre ? upto : 0);
-            next_dy[v] = load8<YT>(static_cast<const char*>(s.dy) + row * s.lddy * bytes_of<YT>, c, pre ? upto : 0);
-            next_dh[v] = load8<RT>(static_cast<const char*>(s.dh) + row * s.lddh * bytes_of<RT>, c, with_dh ? upto : 0);
+            next_x[v] = load8<XT, streamed<XT, TPR>>(static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>, c, upto);
+            next_h[v] = load8<RT, streamed<RT, TPR>>(static_cast<const char*>(s.h) + row * s.ldh * bytes_of<RT>, c, pre ? upto : 0);
+            next_dy[v] = load8<YT, streamed<YT, TPR>>(static_cast<const char*>(s.dy) + row * s.lddy * bytes_of<YT>, c, pre ? upto : 0);
+            next_dh[v] = load8<RT, streamed<RT, TPR>>(static_cast<const char*>(s.dh) + row * s.lddh * bytes_of<RT>, c, with_dh ? upto : 0);
         }
         if (there && post) {
             next_mean1 = s.mean1 ? s.mean1[row] : 0.0f;
