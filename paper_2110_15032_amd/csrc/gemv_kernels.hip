@@ -21,6 +21,7 @@ template <int T, int M, int R, int WK, bool STREAM>
 __global__ __launch_bounds__(256) void gemv_rows_kernel(GemmBlockPlan p) {
     constexpr int GROUPS = 4 / WK, AHEAD = R == 4 && M == 1 ? 4 : 2;   // steps on their way together: 4096 x 16384, one row, two 25.0 us, four 24.3; one row of the weight a wave, 4096 x 4096, two 7.9, four 10.5
     const GemmShard& s = p.s[blockIdx.y];
+    if (s.m == 0) return;   // a device without rows, whose x need not be anywhere
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wk = wave % WK;
     const int64_t n0 = ((int64_t)blockIdx.x * GROUPS + wave / WK) * R;
     float acc[R][M];
@@ -96,7 +97,7 @@ __global__ __launch_bounds__(1024) void gemv_columns_kernel(GemmBlockPlan p) {
     constexpr int NW = 16, AHEAD = 4, STEP = NW * 8;
     const GemmShard& s = p.s[blockIdx.y];
     const int n0 = blockIdx.x * 64;
-    if (n0 >= s.n) return;
+    if (n0 >= s.n || s.m == 0) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = n0 + (lane & 7) * 8;
     float acc[8];
 #pragma unroll

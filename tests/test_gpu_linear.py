@@ -114,6 +114,14 @@ def test_one_row_with_many_columns():
     Layer(2, 4096, 16500, residual="f32", gelu=True).check()               # past the caches
 
 
+@pytest.mark.parametrize("m,k", [(3, 4), (1, 2), (5, 8), (2, 40)])
+@pytest.mark.parametrize("x", ["bf16", "f32"])
+def test_fewer_rows_than_devices(m, k, x):
+    """devices without rows, whose x, residual, pre and y are null"""
+    for w_trans, kk, n in ((1, 461, 1189), (1, 1500, 130), (1, 300, 9000), (0, 300, 20000), (0, 40, 64), (0, 777, 130)):
+        Layer(m, kk, n, k, "S0", x=x, residual="f32", pre="bf16", gelu=kk == 300, w_trans=w_trans, pitch=3).check()
+
+
 @pytest.mark.parametrize("k,sig,m,n", [(2, "B", 30, 100), (3, "S0", 100, 70), (8, "S0", 5, 64), (3, "S1", 50, 100), (8, "S1", 1, 2048), (9, "S1", 20, 180), (20, "S0", 70, 40), (64, "S1", 3, 640)])
 @pytest.mark.parametrize("x", ["bf16", "f32"])
 def test_on_devices(k, sig, m, n, x):

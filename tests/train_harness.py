@@ -31,7 +31,7 @@ class Buf:
         return typed.as_strided((self.rows, self.cols), (self.pitch, 1)) if self.used else typed.view(-1)[:0].reshape(0, self.cols) if not self.rows else typed.view(self.rows, 0)
 
     def data_ptr(self):
-        return self.raw.data_ptr()
+        return self.raw.data_ptr() if self.used else 0   # an empty local tensor need not be anywhere
 
     def host(self):
         """The rows in 64 bits (8 bits: as they are), after a look that nothing else was written."""
