@@ -275,36 +275,40 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
     }
 }
 
-// The workgroups' partial sums in order, and the weights' gradients from them: 32 columns a workgroup, eight runs of partial sums side by side.
+// The workgroups' partial sums in order, and the weights' gradients from them: 32 columns a workgroup, 32 runs of partial sums side by side.
+constexpr int RUNS = 32;
 template <int S>
-__global__ __launch_bounds__(256) void residual_norm_join_kernel(ResNormJoin<S> p) {
+__global__ __launch_bounds__(32 * RUNS) void residual_norm_join_kernel(ResNormJoin<S> p) {
     const ResNormJoinShard& s = p.s[S > 1 ? blockIdx.y : 0];
-    __shared__ float sums[4][8][33];
+    __shared__ float sums[4][RUNS][33], totals[4][32];
     const int lane = threadIdx.x & 31, run = threadIdx.x >> 5, c = blockIdx.x * 32 + lane;
     float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
     if (c < p.cols) {
-        for (int b = run; b < s.blocks; b += 16) {   // two on their way, past the end the last one again, which does not count
+        for (int b = run; b < s.blocks; b += 2 * RUNS) {   // two on their way, past the end the last one again, which does not count
             float v[2][4];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int which = 0; which < 4; ++which) v[u][which] = s.part[((int64_t)min(b + 8 * u, s.blocks - 1) * 4 + which) * p.cols + c];
+                for (int which = 0; which < 4; ++which) v[u][which] = s.part[((int64_t)min(b + RUNS * u, s.blocks - 1) * 4 + which) * p.cols + c];
 #pragma unroll
             for (int u = 0; u < 2; ++u)
 #pragma unroll
-                for (int which = 0; which < 4; ++which) a[which] += b + 8 * u < s.blocks ? v[u][which] : 0.0f;
+                for (int which = 0; which < 4; ++which) a[which] += b + RUNS * u < s.blocks ? v[u][which] : 0.0f;
         }
     }
 #pragma unroll
     for (int which = 0; which < 4; ++which) sums[which][run][lane] = a[which];
     __syncthreads();
+    if (run < 4) {
+        float total = 0.0f;
+#pragma unroll
+        for (int r = 0; r < RUNS; ++r) total += sums[run][r][lane];
+        totals[run][lane] = total;
+    }
+    __syncthreads();
     if (run != 0 || c >= p.cols) return;
 #pragma unroll
-    for (int which = 0; which < 4; ++which) {
-        a[which] = 0.0f;
-#pragma unroll
-        for (int r = 0; r < 8; ++r) a[which] += sums[which][r][lane];
-    }
+    for (int which = 0; which < 4; ++which) a[which] = totals[which][lane];
     auto weight = [&](const void* w, float otherwise) {
         return !w ? otherwise : p.flags & RN_BF16_WEIGHTS ? bf16_to_f32(static_cast<const uint16_t*>(w)[c]) : static_cast<const float*>(w)[c];
     };
@@ -321,12 +325,13 @@ int threads_of(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : co
 
 }  // namespace
 
-// One workgroup a CU, two where a row is short and there is much to do: more hide more, but each reads the weights and leaves four sums a column for the join.  us, 256 / 512 /
-// 1024 workgroups, bf16 on 8 devices: 65536 x 512 94.8 / 84.6 / 87.5, 32768 x 1024 129 / 88 / 90, 16384 x 2048 104 / 90 / 93, 16384 x 4096 163 / 179 / 180, 4096 x 8192
-// 96 / 108 / 133; one device 1024 x 1024 15.2 / 21.6 / 21.6.
+// One workgroup a CU, two or four where a row is short and there are enough rows: more hide more, but each reads the weights and leaves four sums a column for
+// the join.  us, 256 / 512 / 1024 workgroups, bf16: 31327 x 360 79 / 54 / 47, 16384 x 768 60.5 / 41.8 / 49.7, 4096 x 768 21.3 / 17.0, 32768 x 1024 129 / 88 / 90, 8192 x
+// 1537 67 / 48 / 56, but 1024 x 1024 11.3 / 13.2, 2000 x 1024 15.2 / 16.3; 8192 x 2560 58 / 62 / 72, 16384 x 4096 155 / 163 / 170, 4096 x 8192 96 / 108 / 133.
 int32_t residual_norm_grad_blocks(int64_t rows, int64_t cols, int32_t k) {
-    const int64_t g = std::max(1, 256 / threads_of(cols)), most = cols <= 2048 && rows * cols * k >= (int64_t)1 << 24 ? 512 : 256;
-    return (int32_t)std::max<int64_t>(1, std::min<int64_t>((rows + g - 1) / g, most / k));
+    const int64_t g = std::max(1, 256 / threads_of(cols)), turns = (rows + g - 1) / g;
+    const int64_t most = cols > 2048 || turns * k < 1280 ? 256 : cols > 512 || turns * k < 5120 ? 512 : 1024;
+    return (int32_t)std::max<int64_t>(1, std::min<int64_t>(turns, most / k));
 }
 
 template <int S>
@@ -368,7 +373,7 @@ int32_t launch_residual_norm_grad(const ResNormGradPlan<S>& given, int n, int32_
 
 template <int S>
 int32_t launch_residual_norm_join(const ResNormJoin<S>& join, int n, hipStream_t stream) {
-    hipLaunchKernelGGL(residual_norm_join_kernel<S>, dim3((uint32_t)((join.cols + 31) / 32), (uint32_t)n), dim3(256), 0, stream, join);
+    hipLaunchKernelGGL(residual_norm_join_kernel<S>, dim3((uint32_t)((join.cols + 31) / 32), (uint32_t)n), dim3(32 * RUNS), 0, stream, join);
     return launch_status(__func__);
 }
 template int32_t launch_residual_norm_grad<1>(const ResNormGradPlan<1>&, int, int32_t, int32_t, int32_t, hipStream_t);

@@ -61,13 +61,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
     for (int a = 0; a < AHEAD; ++a) fetch(a, row + a * step);
     auto work = [&](int a, int turn) __attribute__((always_inline)) {   // one row of every group, and the row AHEAD of it on its way
         float x[N], h[N];
-        const int there = row < s.rows ? cols : 0;
+        if (!part_of_row.even) {
+            asm volatile("");   // or all of it would be worked out, and chosen from
+            const int there = row < s.rows ? cols : 0;
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                next_x[a][v] = settle8<XT>(next_x[a][v], (v * TPR + t) * 8, there);
+                next_r[a][v] = settle8<RT>(next_r[a][v], (v * TPR + t) * 8, there);
+            }
+        }
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             float u[8], w[8];
-            const int c = (v * TPR + t) * 8;
-            widen<XT>(part_of_row.whole ? next_x[a][v] : settle8<XT>(next_x[a][v], c, there), 1.0f, u);
-            widen<RT>(part_of_row.whole ? next_r[a][v] : settle8<RT>(next_r[a][v], c, there), 1.0f, w);
+            widen<XT>(next_x[a][v], 1.0f, u);
+            widen<RT>(next_r[a][v], 1.0f, w);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
                 x[v * 8 + e] = u[e];
@@ -101,13 +108,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
         }
         if (!pre) return;
         if constexpr (!KEEP) load2();
-        if (!part_of_row.whole) {   // behind the row's end gate is 0, but x need not be finite there times it
-            asm volatile("");
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) h[v * 8 + e] = (v * TPR + t) * 8 + e < cols ? h[v * 8 + e] : 0.0f;
-        }
+        if (!part_of_row.whole) part_of_row.clear(h, cols);   // behind the row's end gate is 0, but x need not be finite there times it
         float mean, m2;
         part_of_row.spread(h, p.flags & RN_PRE_LAYER, part[turn][1][group], mean, m2);
         const float rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps2));

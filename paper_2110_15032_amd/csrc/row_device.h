@@ -57,6 +57,7 @@ struct RowPart {
     static constexpr int NW = TPR / 64;
     int t, cols;
     bool whole;        // no lane is without elements
+    bool even;         // no lane has fewer than eight of a vector without having none
     float of_wave, over_wave;   // elements of this lane's wave
     float elements;    // of wave t % NW
     float over;        // 1 / cols
@@ -65,12 +66,34 @@ struct RowPart {
 #pragma unroll
         for (int v = 0; v < V; ++v) have += min(max(cols - (v * TPR + t) * 8, 0), 8);
         whole = cols == TPR * V * 8;
+        even = cols % 8 == 0;
         of_wave = sum_wave((float)have);
         over_wave = of_wave > 0.0f ? 1.0f / of_wave : 0.0f;
         over = 1.0f / (float)cols;
         elements = 0.0f;
 #pragma unroll
         for (int v = 0; v < V; ++v) elements += (float)min(max(cols - (v * TPR + (t & (NW - 1)) * 64) * 8, 0), 512);
+    }
+
+    // 0 where no element is, which a row of `upto` elements ends in front of; not for `whole` ones.
+    __device__ inline void clear(float (&x)[V * 8], int upto) const {
+        if (even) {
+            asm volatile("");   // or both would be worked out, and one chosen
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const bool is = (v * TPR + t) * 8 < upto;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[v * 8 + e] = is ? x[v * 8 + e] : 0.0f;
+            }
+        } else {
+            asm volatile("");
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const int left = upto - (v * TPR + t) * 8;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[v * 8 + e] = e < left ? x[v * 8 + e] : 0.0f;
+            }
+        }
     }
 
     // Mean and sum of the squares of the distances to it (RMS, layer = false: 0 and the sum of squares), exact to fp32 sums whatever the row's
@@ -92,16 +115,12 @@ struct RowPart {
                 sq = fmaf(d, d, sq);
             }
         } else {
-            asm volatile("");   // or both would be worked out, and one chosen
+            float d[V * 8];
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int left = cols - (v * TPR + t) * 8;
+            for (int i = 0; i < V * 8; ++i) d[i] = x[i] - centre;
+            clear(d, cols);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const float d = e < left ? x[v * 8 + e] - centre : 0.0f;
-                    sq = fmaf(d, d, sq);
-                }
-            }
+            for (int i = 0; i < V * 8; ++i) sq = fmaf(d[i], d[i], sq);
         }
         sq = sum_wave(sq);
         mean = centre;
