@@ -2152,10 +2152,17 @@ bool gemv_pays(const GemmPlan& plan, int max_m, int max_n) {
     return plan.b_kc || (max_m == 1 && tiles_of(plan, 1, max_n, 1, 64) >= compute_units());
 }
 
+// Up to 32 rows whose 32 x 64 tiles leave half the chip without work.  us, such tiles, their waves splitting the reduction / gemm_few_kernel: 16384 x 4096, 8 rows
+// 73.9 / 35.0, 32 rows 90 / 57; 4096 x 4096, 16 rows 14.6 / 10.6; 2720 x 648, 10 rows 7.8 / 5.4; but 128 tiles, 8192 columns 16.3 / 19.3, 192 tiles 26.6 / 31.4.
+bool few_pays(const GemmPlan& plan, int max_m, int max_n) {
+    return plan.in_dtype == SBP_BF16 && plan.a_kc && plan.b_kc && max_m <= FEW_ROWS && longest_reduction(plan) > 0 && 2 * tiles_of(plan, max_m, max_n, 32, 64) < compute_units();
+}
+
 // The kernel for a product with a block's epilogue: launch_chosen's rules, over the kernels that have one.
 int32_t launch_block_chosen(const GemmBlockPlan& plan, const GemmPlan& like, int max_m, int max_n, hipStream_t stream) {
     const bool bf16 = plan.in_dtype == SBP_BF16, direct = rows_aligned(like);
     if (gemv_pays(like, max_m, max_n)) return launch_gemv(plan, max_m, max_n, stream);
+    if (few_pays(like, max_m, max_n)) return launch_gemm_few(plan, max_m, max_n, stream);
     if (one_element_pays(like, max_m, max_n, bf16 && direct) || (bf16 && !mfma_ok(like))) return launch_block_generic(plan, max_m, max_n, stream);
     auto order = [&](int bm, int bn) { return tile_order_for(tiles_along(max_m, bm), tiles_along(max_n, bn)); };
     if (!bf16) {

@@ -140,6 +140,75 @@ __global__ __launch_bounds__(1024) void gemv_columns_kernel(GemmBlockPlan p) {
     Ending<EPI_BLOCK>(p, blockIdx.y).finish<1>(s, 0, n0 + lane, v);
 }
 
+// Up to 32 rows in bf16, weights with the reduction index contiguous, few columns: a workgroup of 16 waves takes 16 of them, a wave every 16th piece of the reduction,
+// straight from memory into the operands of v_mfma_f32_16x16x32_bf16 (lane l: eight elements of row l % 16 from 8 (l / 16) on); the waves' sums meet in
+// LDS, in order.  The next piece is on its way while one is multiplied.  Any alignment.  Bound by how much of the weight is on its way; x comes from L2 for
+// every workgroup, as many bytes as the weight with 16 rows.
+template <int MT>   // 16 rows of x each
+__global__ __launch_bounds__(1024) void gemm_few_kernel(GemmBlockPlan p) {
+    constexpr int NW = 16, U = MT == 1 ? 6 : 4, STEP = 32 * U;   // what 128 registers hold; MT 1, 16384 x 4096, 8 rows, four 38.7 us, six 35.0
+    const GemmShard& s = p.s[blockIdx.y];
+    const int n0 = blockIdx.x * 16;
+    if (n0 >= s.n || s.m == 0) return;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), of = lane & 15, from = (lane >> 4) * 8;
+    // rows past the last one are the last one again, and stored nowhere
+    const char* const w = static_cast<const char*>(s.b) + (int64_t)min(n0 + of, s.n - 1) * s.ldb * 2;
+    const char* x[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) x[i] = static_cast<const char*>(s.a) + (int64_t)min(i * 16 + of, s.m - 1) * s.lda * 2;
+    f32x4 acc[MT];
+#pragma unroll
+    for (int i = 0; i < MT; ++i) acc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    Raw8<T_BF16> rw[U], rx[U][MT];
+    auto fetch = [&](int k0) __attribute__((always_inline)) {   // k0: uniform, not past the last piece's
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int c = min(k0 + u * 32 + from, s.kk);
+            rw[u] = load8<T_BF16>(w, c, s.kk);
+#pragma unroll
+            for (int i = 0; i < MT; ++i) rx[u][i] = load8<T_BF16>(x[i], c, s.kk);
+        }
+    };
+    if (wave * STEP < s.kk) fetch(wave * STEP);
+    for (int64_t k0 = wave * STEP; k0 < s.kk; k0 += NW * STEP) {
+        u32x4 b[U], a[U][MT];
+        if (k0 + STEP > s.kk) {
+            asm volatile("");   // or it would be done always, and chosen from
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int c = (int)min(k0 + u * 32 + from, (int64_t)s.kk);
+                rw[u] = settle8<T_BF16>(rw[u], c, s.kk);
+#pragma unroll
+                for (int i = 0; i < MT; ++i) rx[u][i] = settle8<T_BF16>(rx[u][i], c, s.kk);
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            b[u] = rw[u].w;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) a[u][i] = rx[u][i].w;
+        }
+        if (k0 + NW * STEP < s.kk) fetch((int)(k0 + NW * STEP));
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                acc[i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a[u][i]), __builtin_bit_cast(bf16x8, b[u]), acc[i], 0, 0, 0);
+    }
+    __shared__ float part[NW][MT * 256];   // [row][column]
+#pragma unroll
+    for (int i = 0; i < MT; ++i)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) part[wave][(i * 16 + (lane >> 4) * 4 + r) * 16 + of] = acc[i][r];
+    __syncthreads();
+    const int t = threadIdx.x;
+    if (t >= MT * 256) return;
+    float v[1] = {0.0f};
+#pragma unroll
+    for (int i = 0; i < NW; ++i) v[0] += part[i][t];
+    Ending<EPI_BLOCK>(p, blockIdx.y).finish<1>(s, t >> 4, n0 + (t & 15), v);
+}
+
 template <typename F>
 void with_rows(int m, F&& f) {
     if (m == 1) f(std::integral_constant<int, 1>{});
@@ -178,6 +247,14 @@ int32_t launch_gemv(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t
     };
     if (weight >= (int64_t)128 << 20) typed(std::true_type{});
     else typed(std::false_type{});
+    return launch_status(__func__);
+}
+
+// 1 .. FEW_ROWS rows, bf16, both operands with the reduction index contiguous
+int32_t launch_gemm_few(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream) {
+    const dim3 grid((uint32_t)tiles_along(max_n, 16), (uint32_t)plan.groups);
+    if (max_m <= 16) hipLaunchKernelGGL(gemm_few_kernel<1>, grid, dim3(1024), 0, stream, plan);
+    else hipLaunchKernelGGL(gemm_few_kernel<2>, grid, dim3(1024), 0, stream, plan);
     return launch_status(__func__);
 }
 

@@ -107,6 +107,9 @@ int32_t launch_linear(const GemmBlockPlan& plan, hipStream_t stream);
 constexpr int GEMV_ROWS = 4;
 // gemv_kernels.hip: 1 .. GEMV_ROWS rows of x, stored along the reduction
 int32_t launch_gemv(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream);
+// 1 .. FEW_ROWS rows in bf16, both operands stored along the reduction
+constexpr int FEW_ROWS = 32;
+int32_t launch_gemm_few(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream);
 
 // variant: SBP_KNOB_GEMM_VARIANT.  The launch_gemm_* functions below return SBP_ERR_UNSUPPORTED, with nothing enqueued, for a
 // grid that cannot be launched (grid_fits).

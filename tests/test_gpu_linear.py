@@ -107,6 +107,16 @@ def test_a_few_rows(m, kk, n, x):
         Layer(m, kk, n, x=x, residual="bf16" if m % 2 else "", pre="f32", gelu=m > 2, w_trans=w_trans, pitch=pitch).check()
 
 
+@pytest.mark.parametrize("m", [5, 15, 16, 17, 31, 32])
+@pytest.mark.parametrize("kk,n", [(1, 40), (7, 16), (8, 17), (127, 130), (128, 64), (2047, 300), (2048, 65), (2200, 1000), (4099, 15), (9000, 257)])
+def test_up_to_thirty_two_rows(m, kk, n):
+    """pieces of the reduction for some of the waves, for all, and for some again, whole and cut; rows at any alignment"""
+    for pitch in (0, 1, 8):
+        Layer(m, kk, n, residual="bf16" if m % 2 else "", pre="f32", gelu=m > 16, pitch=pitch).check()
+    Layer(m, kk, n, 3, "S1", pitch=5).check()
+    Layer(m, kk, n, 20, "S0", y="f32", residual="f32").check()
+
+
 def test_one_row_with_many_columns():
     for w_trans, pitch, x in ((0, 0, "bf16"), (0, 1, "bf16"), (1, 0, "f32"), (0, 0, "f32")):
         Layer(1, 300, 20000, x=x, residual="f32", gelu=True, w_trans=w_trans, pitch=pitch).check()
