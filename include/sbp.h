@@ -425,9 +425,10 @@ int32_t sbp_residual_norm_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_x
  * signatures, each S or B; SBP_F32 or SBP_BF16, any pitch, stored either way (trans).
  * sbp_square_sum: out [1,1] SBP_F32, P(sum): out_i = the sum of the squares of the elements that device i counts: its slice of
  *   an S tensor; of a B tensor, which every device has whole, its balanced share of the stored rows.  Squares are added in 64 bits
- *   in an order that depends on the sizes alone, and the sum is rounded once (a sum of 2^128 or more is infinity).  workspace: device
- *   memory of sbp_square_sum_workspace() bytes for the same list, 16-byte aligned, whose contents do not matter before or after the call;
- *   calls that may overlap in time need one each.
+ *   in an order that depends on the sizes and on which tensors lie back to back in memory (those are read as one), and the sum is
+ *   rounded once (a sum of 2^128 or more is infinity).  workspace: device memory of sbp_square_sum_workspace() bytes for the same list
+ *   (they depend on the sizes alone), 16-byte aligned, whose contents do not matter before or after the call; calls that may overlap
+ *   in time need one each.
  * sbp_clip: with norm = sqrt(squares), out = in * min(1, max_norm / norm) on every device (each writes its own copy of a B
  *   tensor), one rounding to out's type, SBP_F32 or SBP_BF16, of fp32 products.  squares [1,1] SBP_F32: sbp_square_sum's P(sum), whose parts
  *   every device then adds itself in the order of the devices, or B, boxed.  norm [1,1] SBP_F32, B, receives the norm

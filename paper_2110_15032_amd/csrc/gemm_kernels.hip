@@ -16,7 +16,8 @@
 //   gemm_mfma_persist16_kernel  the same on v_mfma_f32_16x16x32_bf16 (store_tile16): the default for
 //                             large shapes; under real operands the chip clocks this instruction higher.
 //   gemm_split_kernel         one fp32 operand (a P(sum) partial) split exactly into three bf16 terms.
-// Few output tiles and rows at any pitch: gemm_any_kernels.hip.  fp32 operands: gemm_f32_kernels.hip.
+// Few output tiles and rows at any pitch: gemm_any_kernels.hip.  fp32 operands: gemm_f32_kernels.hip.  A layer's epilogue (sbp_linear: bias, activation, residual): EPI_BLOCK
+// of gemm_generic, pipe16, persist16 and of the kernels in those two files, and gemv_kernels.hip for few rows.
 // All MFMA kernels share Tile (LDS images, swizzles, fragment reads) and store_tile (epilogue).
 //
 // Operand storage: "KC" = reduction index contiguous ([m][kk] for A, [n][kk] for B), otherwise the
@@ -631,7 +632,8 @@ __global__ __launch_bounds__(WM * WN * 64) void gemm_mfma_kernel(GemmPlan p, int
 // puts the four rows of a write on four groups of banks; a lane then owns eight consecutive columns of a row, whose bias stays in registers.  The residual of
 // the next strip is on its way while one is worked on.  What the edge leaves of a row's last eight columns is done element by element behind
 // each strip, and so is GeLU by erfc, whose code is long.  Loads of the persistent kernel's next tile are waited for here, all of them, so that its first steps
-// need not; stores are outside the compiler's bookkeeping, as in store_tile16.
+// need not; stores are outside the compiler's bookkeeping, as in store_tile16.  [8192, 4096] x [4096, 16384] with bias, GeLU and pre, 8 devices 835 .. 865 us (1.27 .. 1.32
+// PFLOP/s), [8192, 16384] x [16384, 4096] with bias onto a residual 886 .. 896.
 template <int TM, int TN>
 __device__ __attribute__((always_inline)) inline void store_block16(const f32x4 (&acc)[TM / 16][TN / 16], const GemmShard& s, const Ending<EPI_BLOCK>& end, int m_first, int n_first, int lane,
                                                                     char* win) {

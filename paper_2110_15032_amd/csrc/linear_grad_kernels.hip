@@ -2,7 +2,10 @@
 // the sum of dy alone.
 //
 // Bound by HBM.  32 lanes take 256 columns of a row, eight each, and eight rows side by side make a workgroup; it walks down its share of the
-// rows with the sums in registers, which meet in LDS at the end.  Its partial sums go to the caller's workspace and are joined in order.
+// rows with the sums in registers, which meet in LDS at the end.  Its partial sums go to the caller's workspace and are joined in order.  8192 x 16384 bf16 with
+// GeLU, 8 devices 145 us (141 + 5 for the join; 805 MB, 5.7 TB/s; GeLU's arithmetic is 89 of vector instructions); 1767 x 1001 fp32, 3 devices 12.3 (9.2 + 1.6).  Two rows
+// ahead instead of four 13.6 -> 12.3 at 2000 x 3001, but 12.4 -> 13.7 at 1767 x 1001; 1024 workgroups instead of 2048 31 -> 25 at 32768 x 300, and none at
+// the other sizes.
 #include "row_device.h"
 
 namespace sbp {

@@ -4,7 +4,8 @@
 //
 // Both are bound by HBM.  The argument block of a launch names local tensors (parts); their vectors of eight elements are numbered
 // through, a workgroup takes 1024 of them at a time (a chunk, of one part).  Where a part's chunks start is summed up over the lanes of every wave, so that the
-// argument block need not hold it.
+// argument block need not hold it.  2^28 elements from bf16 to fp32 on 8 devices: 80 us for the sum (537 MB, 6.7 TB/s), 265 for the clipping (1.61 GB, 6.1 TB/s), 353 in
+// all; 72 small tensors on two devices 22, of which the device works 11 in three launches.
 #include "block8_device.h"
 
 namespace sbp {

@@ -49,6 +49,7 @@ CASES = [
     (2, [(3, 8192, "bf16", "S0", 8, 0), (3, 8191, "bf16", "S0", 1, 0), (3, 8200, "f32", "S0", 8, 0), (300, 4, "f32", "S0", 1, 0)]),
     (8, [(3, 100, "f32", "S0", 0, 0), (1000, 1000, "bf16", "S0", 24, 0)]),             # devices without rows
     (1, [(700, 12289, "f32", "S0", 7, 0)]),                                              # rows of more vectors than a chunk, many chunks
+    (3, [(7, 9001, "bf16", "B", 0, 0), (50, 1001, "f32", "B", 0, 0), (5, 20000, "bf16", "B", 0, 1)]),   # shares of whole chunks from any element on
     (3, [(40 + i, 3 + 7 * i, "f32" if i % 3 else "bf16", ("S0", "S1", "B")[i % 3], i % 5, i % 2) for i in range(70)]),   # more than a launch takes
 ]
 
