@@ -28,23 +28,28 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
     const bool post = p.flags & RN_POST, pre = p.flags & RN_PRE, narrow_weights = p.flags & RN_BF16_WEIGHTS;
     __shared__ float2 part[2][2][G][NW];
     const RowPart<TPR, V> part_of_row(t, cols);
-    float gate[N], gamma1[N], beta1[N], gamma2[N], beta2[N];
-    auto load1 = [&]() {
-        load_column<V, TPR>(s.gate, narrow_weights, t, cols, 1.0f, gate);
+    float gate[8], gamma1[8], beta1[8], gamma2[8], beta2[8];   // of one vector
+    auto column = [&](int v) __attribute__((always_inline)) {   // not KEEP: opaque, or addresses would be held in registers from row to row
+        int c = (v * TPR + t) * 8;
+        if constexpr (!KEEP) asm volatile("" : "+v"(c));
+        return c;
+    };
+    auto load1 = [&](int v) __attribute__((always_inline)) {
+        const int c = column(v);
+        load_weight8(s.gate, narrow_weights, c, cols, 1.0f, gate);
         if (post) {
-            load_column<V, TPR>(s.gamma1, narrow_weights, t, cols, 1.0f, gamma1);
-            load_column<V, TPR>(s.beta1, narrow_weights, t, cols, 0.0f, beta1);
+            load_weight8(s.gamma1, narrow_weights, c, cols, 1.0f, gamma1);
+            load_weight8(s.beta1, narrow_weights, c, cols, 0.0f, beta1);
         }
     };
-    auto load2 = [&]() {
-        if (pre) {
-            load_column<V, TPR>(s.gamma2, narrow_weights, t, cols, 1.0f, gamma2);
-            load_column<V, TPR>(s.beta2, narrow_weights, t, cols, 0.0f, beta2);
-        }
+    auto load2 = [&](int v) __attribute__((always_inline)) {
+        const int c = column(v);
+        load_weight8(s.gamma2, narrow_weights, c, cols, 1.0f, gamma2);
+        load_weight8(s.beta2, narrow_weights, c, cols, 0.0f, beta2);
     };
     if constexpr (KEEP) {
-        load1();
-        load2();
+        load1(0);
+        if (pre) load2(0);
     }
 
     const int step = gridDim.x * G;
@@ -55,8 +60,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
         const char* const from_r = static_cast<const char*>(s.r) + row * s.ldr * bytes_of<RT>;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            next_x[a][v] = load8<XT>(from_x, (v * TPR + t) * 8, row < s.rows ? cols : 0);
-            next_r[a][v] = load8<RT>(from_r, (v * TPR + t) * 8, row < s.rows ? cols : 0);
+            const int c = column(v);
+            next_x[a][v] = load8<XT>(from_x, c, row < s.rows ? cols : 0);
+            next_r[a][v] = load8<RT>(from_r, c, row < s.rows ? cols : 0);
         }
     };
     int64_t row = (int64_t)blockIdx.x * G + group;
@@ -69,8 +75,9 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
             const int there = row < s.rows ? cols : 0;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                next_x[a][v] = settle8<XT>(next_x[a][v], (v * TPR + t) * 8, there);
-                next_r[a][v] = settle8<RT>(next_r[a][v], (v * TPR + t) * 8, there);
+                const int c = column(v);
+                next_x[a][v] = settle8<XT>(next_x[a][v], c, there);
+                next_r[a][v] = settle8<RT>(next_r[a][v], c, there);
             }
         }
 #pragma unroll
@@ -85,36 +92,35 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
             }
         }
         fetch(a, row + AHEAD * step);
-        if constexpr (!KEEP) load1();
+        float mean = 0.0f, rstd = 1.0f, m2;
         if (post) {
-            float mean, m2;
             part_of_row.spread(x, p.flags & RN_POST_LAYER, part[turn][0][group], mean, m2);
-            const float rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps1));
+            rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps1));
             if (t == 0 && row < s.rows) {
                 if (s.mean1) s.mean1[row] = mean;
                 if (s.rstd1) s.rstd1[row] = rstd;
             }
-#pragma unroll
-            for (int i = 0; i < N; ++i) x[i] = fmaf((x[i] - mean) * rstd, gamma1[i], beta1[i]);
         }
 #pragma unroll
-        for (int i = 0; i < N; ++i) h[i] = fmaf(gate[i], x[i], h[i]);
-        if (row < s.rows) {
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const int c = (v * TPR + t) * 8;
-                float u[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) u[e] = h[v * 8 + e];
-                store8<RT>(static_cast<char*>(s.h) + (row * s.ldh + c) * bytes_of<RT>, narrow<RT>(u), cols - c, p.flags & RN_STREAM_H);
+        for (int v = 0; v < V; ++v) {
+            const int c = column(v);
+            if constexpr (!KEEP) {
+                __builtin_amdgcn_sched_barrier(0);   // one vector's weights at a time, for their registers
+                load1(v);
             }
+            float u[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int i = v * 8 + e;
+                if (post) x[i] = fmaf((x[i] - mean) * rstd, gamma1[e], beta1[e]);
+                u[e] = h[i] = fmaf(gate[e], x[i], h[i]);
+            }
+            if (row < s.rows) store8<RT>(static_cast<char*>(s.h) + (row * s.ldh + c) * bytes_of<RT>, narrow<RT>(u), cols - c, p.flags & RN_STREAM_H);
         }
         if (!pre) return;
-        if constexpr (!KEEP) load2();
         if (!part_of_row.whole) part_of_row.clear(h, cols);   // behind the row's end gate is 0, but x need not be finite there times it
-        float mean, m2;
         part_of_row.spread(h, p.flags & RN_PRE_LAYER, part[turn][1][group], mean, m2);
-        const float rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps2));
+        rstd = inverse_root(fmaf(m2, part_of_row.over, p.eps2));
         if (row >= s.rows) return;
         if (t == 0) {
             if (s.mean2) s.mean2[row] = mean;
@@ -122,9 +128,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
         }
         float y[V][8];
 #pragma unroll
-        for (int v = 0; v < V; ++v)
+        for (int v = 0; v < V; ++v) {
+            if constexpr (!KEEP) {
+                __builtin_amdgcn_sched_barrier(0);
+                load2(v);
+            }
 #pragma unroll
-            for (int e = 0; e < 8; ++e) y[v][e] = fmaf((h[v * 8 + e] - mean) * rstd, gamma2[v * 8 + e], beta2[v * 8 + e]);
+            for (int e = 0; e < 8; ++e) y[v][e] = fmaf((h[v * 8 + e] - mean) * rstd, gamma2[e], beta2[e]);
+        }
         char* const to = static_cast<char*>(s.y) + row * s.ldy * bytes_of<YT>;
         if constexpr (bytes_of<YT> == 1) {
             if (!part_of_row.whole) {   // a block's largest magnitude is of elements alone
@@ -139,14 +150,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_kernel(Re
             narrow_blocks<true, YT>(y, q, byte);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int c = (v * TPR + t) * 8;
+                const int c = column(v);
                 store8<YT>(to + c, q[v], cols - c, p.flags & RN_STREAM_Y);
                 if ((t & 15) == 0 && c < cols) static_cast<uint8_t*>(s.y_scales)[row * s.lds + c / F8_BLOCK] = (uint8_t)byte[v];
             }
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int c = (v * TPR + t) * 8;
+                const int c = column(v);
                 store8<YT>(to + c * bytes_of<YT>, narrow<YT>(y[v]), cols - c, p.flags & RN_STREAM_Y);
             }
         }

@@ -6,21 +6,24 @@
 namespace sbp {
 namespace {
 
-// A weight's elements; `otherwise` where there is no weight.  bf16: its type (uniform, and read once a workgroup).
+// Eight elements of a weight from column c on; `otherwise` where there is no weight.  bf16: its type (uniform).
+__device__ inline void load_weight8(const void* w, bool bf16, int c, int cols, float otherwise, float (&out)[8]) {
+    if (!w) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) out[e] = c + e < cols ? otherwise : 0.0f;
+    } else if (bf16) {
+        widen<T_BF16>(settle8<T_BF16>(load8<T_BF16>(static_cast<const char*>(w), c, cols), c, cols), 1.0f, out);
+    } else {
+        widen<T_F32>(settle8<T_F32>(load8<T_F32>(static_cast<const char*>(w), c, cols), c, cols), 1.0f, out);
+    }
+}
+// all of a lane's
 template <int V, int TPR>
 __device__ inline void load_column(const void* w, bool bf16, int t, int cols, float otherwise, float (&out)[V * 8]) {
 #pragma unroll
     for (int v = 0; v < V; ++v) {
-        const int c = (v * TPR + t) * 8;
         float u[8];
-        if (!w) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) u[e] = c + e < cols ? otherwise : 0.0f;
-        } else if (bf16) {
-            widen<T_BF16>(settle8<T_BF16>(load8<T_BF16>(static_cast<const char*>(w), c, cols), c, cols), 1.0f, u);
-        } else {
-            widen<T_F32>(settle8<T_F32>(load8<T_F32>(static_cast<const char*>(w), c, cols), c, cols), 1.0f, u);
-        }
+        load_weight8(w, bf16, (v * TPR + t) * 8, cols, otherwise, u);
 #pragma unroll
         for (int e = 0; e < 8; ++e) out[v * 8 + e] = u[e];
     }
