@@ -8,8 +8,8 @@
 // so that five weights' gradients need four sums a column.  Without the first norm xhat is x, gamma1 1 and beta1 0.  Bound by HBM: the four inputs
 // of a row are read once.  Sums over rows stay in a workgroup's registers (rows of more than 8192: half of them in LDS), its partial sums go to the caller's workspace
 // and are joined in order.  A workgroup goes down its rows with one row ahead; what holds it is a row's chain (two sums over waves, behind one another).  16384 x
-// 4096 bf16, both norms layer, 8 devices 152 .. 162 us (154 + 7 for the join; 805 MB, 5.2 TB/s); 1767 x 1001 fp32, 3 devices 21 (18 + 4); rows of more than 8192 spill: 4532 x
-// 11752 254 us (2.5 TB/s).
+// 4096 bf16, both norms layer, 8 devices 152 .. 162 us (154 + 7 for the join; 805 MB, 5.2 TB/s); 1767 x 1001 fp32, 3 devices 21 (18 + 4); rows of more than 8192 keep two of
+// the sums in LDS and spill what the compute unit has no registers for: 4532 x 11752 210 us (3.0 TB/s), 4096 x 12288 156.
 #include "row_device.h"
 
 namespace sbp {
@@ -31,22 +31,26 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
     __shared__ float2 part[2][2][G][NW];
     __shared__ float sums[KEEP ? (G > 1 ? G * 4 * CAP : 4) : 2 * CAP];   // KEEP: the groups' sums at the end; else C and D
     const RowPart<TPR, V> part_of_row(t, cols);
-    float gamma2[N], through[N];   // through: gate gamma1
-    auto load1 = [&]() {
-        load_column<V, TPR>(s.gate, narrow_weights, t, cols, 1.0f, through);
+    float gamma2[8], through[8];   // of one vector; through: gate gamma1
+    auto column = [&](int v) __attribute__((always_inline)) {   // not KEEP: opaque, or addresses would be held in registers from row to row
+        int c = (v * TPR + t) * 8;
+        if constexpr (!KEEP) asm volatile("" : "+v"(c));
+        return c;
+    };
+    auto load1 = [&](int v) __attribute__((always_inline)) {
+        const int c = column(v);
+        load_weight8(s.gate, narrow_weights, c, cols, 1.0f, through);
         if (post) {
-            float w[N];
-            load_column<V, TPR>(s.gamma1, narrow_weights, t, cols, 1.0f, w);
+            float w[8];
+            load_weight8(s.gamma1, narrow_weights, c, cols, 1.0f, w);
 #pragma unroll
-            for (int i = 0; i < N; ++i) through[i] *= w[i];
+            for (int e = 0; e < 8; ++e) through[e] *= w[e];
         }
     };
-    auto load2 = [&]() {
-        if (pre) load_column<V, TPR>(s.gamma2, narrow_weights, t, cols, 1.0f, gamma2);
-    };
+    auto load2 = [&](int v) __attribute__((always_inline)) { load_weight8(s.gamma2, narrow_weights, column(v), cols, 1.0f, gamma2); };
     if constexpr (KEEP) {
-        load1();
-        load2();
+        load1(0);
+        if (pre) load2(0);
     }
     float sum_a[N], sum_b[N], sum_c[KEEP ? N : 1], sum_d[KEEP ? N : 1];
 #pragma unroll
@@ -69,7 +73,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
         const int upto = there ? cols : 0;
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int c = (v * TPR + t) * 8;
+            const int c = column(v);
             next_x[v] = load8<XT, streamed<XT, TPR>>(static_cast<const char*>(s.x) + row * s.ldx * bytes_of<XT>, c, upto);
             next_h[v] = load8<RT, streamed<RT, TPR>>(static_cast<const char*>(s.h) + row * s.ldh * bytes_of<RT>, c, pre ? upto : 0);
             next_dy[v] = load8<YT, streamed<YT, TPR>>(static_cast<const char*>(s.dy) + row * s.lddy * bytes_of<YT>, c, pre ? upto : 0);
@@ -151,19 +155,26 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
         }
         float s1 = 0.0f, s2 = 0.0f;
         if (pre) {
-            if constexpr (!KEEP) load2();
 #pragma unroll
-            for (int i = 0; i < N; ++i) {
-                if constexpr (KEEP) {
-                    sum_c[i] = fmaf(dy[i], hhat[i], sum_c[i]);
-                    sum_d[i] += dy[i];
-                } else {
-                    sums[i * TPR + t] = fmaf(dy[i], hhat[i], sums[i * TPR + t]);
-                    sums[CAP + i * TPR + t] += dy[i];
+            for (int v = 0; v < V; ++v) {
+                if constexpr (!KEEP) {
+                    __builtin_amdgcn_sched_barrier(0);   // one vector's weights at a time, for their registers
+                    load2(v);
                 }
-                dy[i] *= gamma2[i];
-                s1 += dy[i];
-                s2 = fmaf(dy[i], hhat[i], s2);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = v * 8 + e;
+                    if constexpr (KEEP) {
+                        sum_c[i] = fmaf(dy[i], hhat[i], sum_c[i]);
+                        sum_d[i] += dy[i];
+                    } else {
+                        sums[i * TPR + t] = fmaf(dy[i], hhat[i], sums[i * TPR + t]);
+                        sums[CAP + i * TPR + t] += dy[i];
+                    }
+                    dy[i] *= gamma2[e];
+                    s1 += dy[i];
+                    s2 = fmaf(dy[i], hhat[i], s2);
+                }
             }
             part_of_row.sums(s1, s2, part[turn][0][group]);
             s1 = p.flags & RN_PRE_LAYER ? s1 * part_of_row.over : 0.0f;
@@ -192,16 +203,22 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
         if (row < s.rows) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int c = (v * TPR + t) * 8;
+                const int c = column(v);
                 float u[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[e] = p.alpha * d[v * 8 + e];
                 store8<RT>(static_cast<char*>(s.dr) + (row * s.lddr + c) * bytes_of<RT>, narrow<RT>(u), cols - c, p.flags & RN_STREAM_H);
             }
         }
-        if constexpr (!KEEP) load1();
 #pragma unroll
-        for (int i = 0; i < N; ++i) d[i] *= through[i];
+        for (int v = 0; v < V; ++v) {
+            if constexpr (!KEEP) {
+                __builtin_amdgcn_sched_barrier(0);
+                load1(v);
+            }
+#pragma unroll
+            for (int e = 0; e < 8; ++e) d[v * 8 + e] *= through[e];
+        }
         if (post) {
             s1 = s2 = 0.0f;
 #pragma unroll
@@ -218,7 +235,7 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void residual_norm_grad_kern
         if (row < s.rows) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int c = (v * TPR + t) * 8;
+                const int c = column(v);
                 float u[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) u[e] = d[v * 8 + e];

@@ -7,7 +7,8 @@
 // elements each.  y is computed from h before its rounding.  A wave's lanes hold consecutive vectors, so that loads and stores are of consecutive bytes, and a
 // row never leaves its threads: one pass, two barriers a row (its two sums over waves).  8 devices, 8192 x 4096: bf16 around an fp32 residual 79 us (403 MB, 5.1
 // TB/s), all bf16 53 (268 MB); 1 x 4096 3.3 on the device.  One row ahead: two and three gained nothing, and loads past the caches 3 % where HBM has
-// the inputs and lost 13 % where the memory-side cache has (2048 x 4096, 13.9 / 15.7).  Rows of more than 8192 spill (16384: 2048 of them 77 us, 2.6 TB/s).
+// the inputs and lost 13 % where the memory-side cache has (2048 x 4096, 13.9 / 15.7).  Rows of more than 8192 read a vector's weights when they need them: 4096 x 12288
+// bf16 102 (3.9 TB/s; with all weights of a lane at a time, which spill, 146).
 #include "row_device.h"
 
 namespace sbp {
