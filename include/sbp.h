@@ -435,7 +435,7 @@ int32_t sbp_residual_norm_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_x
  *   (NULL: not wanted).  A norm that is NaN makes all results NaN, an infinite one makes finite values 0.  max_norm >= 0, not NaN.  out's
  *   shapes, signatures and trans are in's.  A local tensor of out may be that of in itself (the same address, type and pitch): in
  *   place; any other overlap is SBP_ERR_ALIAS.
- * An empty list has norm 0.  At most 2^31 - 1 rows and columns of a tensor, and 2^43 elements of a local one (SBP_ERR_UNSUPPORTED). */
+ * An empty list has norm 0.  At most 2^20 tensors, 2^31 - 1 rows and columns of a tensor, and 2^43 elements of a local one (SBP_ERR_UNSUPPORTED). */
 int32_t sbp_square_sum(const sbp_tensor_t* tensors, const sbp_t* sbp, int32_t n, const sbp_tensor_t* out, void* workspace,
                        int64_t workspace_bytes, int32_t k, void* stream);
 int32_t sbp_square_sum_workspace(const sbp_tensor_t* tensors, const sbp_t* sbp, int32_t n, int32_t k, int64_t* bytes);

@@ -231,23 +231,21 @@ int32_t launch_gemv(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t
     const uint32_t groups = (uint32_t)plan.groups;
     auto go = [&](auto t, auto past) {
         if (!plan.b_kc) {
+            if (!grid_fits(tiles_along(max_n, 64), 1024)) return (int32_t)SBP_ERR_UNSUPPORTED;
             hipLaunchKernelGGL((gemv_columns_kernel<t(), past()>), dim3((uint32_t)tiles_along(max_n, 64), groups), dim3(1024), 0, stream, plan);
-            return;
+            return launch_status("launch_gemv");
         }
+        if (!grid_fits(tiles_along(max_n, columns >= 8192 ? 16 : 1), 256)) return (int32_t)SBP_ERR_UNSUPPORTED;
         with_rows(max_m, [&](auto m) {
             // four rows a wave where that leaves a compute unit eight waves or more, else one, and the waves share a long reduction
             if (columns >= 8192) hipLaunchKernelGGL((gemv_rows_kernel<t(), m(), 4, 1, past()>), dim3((uint32_t)tiles_along(max_n, 16), groups), dim3(256), 0, stream, plan);
             else if (deepest > 1024) hipLaunchKernelGGL((gemv_rows_kernel<t(), m(), 1, 4, past()>), dim3((uint32_t)max_n, groups), dim3(256), 0, stream, plan);
             else hipLaunchKernelGGL((gemv_rows_kernel<t(), m(), 1, 1, past()>), dim3((uint32_t)tiles_along(max_n, 4), groups), dim3(256), 0, stream, plan);
         });
+        return launch_status("launch_gemv");
     };
-    auto typed = [&](auto past) {
-        if (f32) go(std::integral_constant<int, T_F32>{}, past);
-        else go(std::integral_constant<int, T_BF16>{}, past);
-    };
-    if (weight >= (int64_t)128 << 20) typed(std::true_type{});
-    else typed(std::false_type{});
-    return launch_status(__func__);
+    auto typed = [&](auto past) { return f32 ? go(std::integral_constant<int, T_F32>{}, past) : go(std::integral_constant<int, T_BF16>{}, past); };
+    return weight >= (int64_t)128 << 20 ? typed(std::true_type{}) : typed(std::false_type{});
 }
 
 // 1 .. FEW_ROWS rows, bf16, both operands with the reduction index contiguous

@@ -53,6 +53,7 @@ int32_t check_list(const sbp_tensor_t* t, const sbp_t* s, int32_t n, int32_t k, 
     if (k < 1 || k > SBP_MAX_K) return SBP_ERR_K;
     if (n < 0) return SBP_ERR_SHAPE;
     if (n && (!t || !s)) return SBP_ERR_NULL;
+    if (n > 1 << 20) return SBP_ERR_UNSUPPORTED;   // a device's launches are counted in 16 bits
     if (!locals.room(n, k)) return SBP_ERR_UNSUPPORTED;
     for (int32_t j = 0; j < n; ++j) {
         const int32_t st = check_one(t + j, s[j], k, locals.of + (int64_t)j * k);

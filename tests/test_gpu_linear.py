@@ -196,6 +196,19 @@ def test_results_past_two_to_the_31_elements():
     assert bool((pre[-2:, -3:] == 6).all()) and bool((y[-1, -3:] == 7).all()) and bool((y[-2, -3:] == 6).all())
 
 
+@pytest.mark.parametrize("w_trans", [0, 1])
+def test_one_row_with_more_columns_than_a_grid_of_the_fast_kernels(w_trans):
+    n = 2 ** 28 + 2 ** 12 + 37
+    x = torch.tensor([[1.0, 2.0]], dtype=torch.bfloat16, device="cuda")
+    w = (torch.arange(2 * n, device="cuda", dtype=torch.int32) % 61).to(torch.bfloat16)      # whole numbers, whose sums bf16 holds
+    w = w.view(n, 2) if w_trans else w.view(2, n)
+    y = torch.full((1, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    d = lambda t, r, c, tr=0: sbp.SbpTensor([t], r, c, sbp.BF16, tr)  # noqa: E731
+    sbp.sbp_linear(d(x, 1, 2), sbp.B, d(w, 2, n, w_trans), sbp.B, None, None, None, d(y, 1, n), sbp.AUTO, 1)
+    a, b = (w[:, 0], w[:, 1]) if w_trans else (w[0], w[1])
+    assert torch.equal(y[0], a + 2 * b)
+
+
 # ---- the epilogue's gradient ----------------------------------------------------------------------
 def check_grad(rows, cols, k=1, sig="B", y="bf16", pre="bf16", gelu=True, pitch=0, seed=0):
     dy = rounded(normal(rows, cols, seed=seed), y)

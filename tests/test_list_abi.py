@@ -67,6 +67,17 @@ def test_square_sum_refusals():
         sbp.SbpList([T(1, 8, 8)], [])
 
 
+def test_more_tensors_than_a_list_takes():
+    one = T(1, 1, 1, sbp.F32)
+    lst = sbp.SbpList([one], [sbp.B])
+    lst.n = (1 << 20) + 1                      # refused before any of them is looked at
+    with pytest.raises(sbp.SbpError) as e:
+        sbp.sbp_square_sum_workspace(lst, 1)
+    assert e.value.status == UNSUPPORTED
+    assert status(sbp.sbp_square_sum, lst, scalar(1, 5), Room(), 1) == UNSUPPORTED
+    assert status(sbp.sbp_clip, lst, scalar(1, 5), sbp.B, 1.0, lst, None, 1) == UNSUPPORTED
+
+
 def test_square_sum_raw_entries():
     L, out = sbp.lib(), ctypes.c_int64()
     s = (ctypes.c_int32 * 1)(sbp.B)
