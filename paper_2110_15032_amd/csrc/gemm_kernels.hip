@@ -2160,12 +2160,67 @@ bool few_pays(const GemmPlan& plan, int max_m, int max_n) {
     return plan.in_dtype == SBP_BF16 && plan.a_kc && plan.b_kc && max_m <= FEW_ROWS && longest_reduction(plan) > 0 && 2 * tiles_of(plan, max_m, max_n, 32, 64) < compute_units();
 }
 
+// Can the MFMA kernels with a block's epilogue count a shard's bytes in 32 bits?  An operand along the reduction from its start to its last row; else over the rows of
+// the reduction that offsets span, at most 256 (gemm_deep_kernel's touches), as the pointer itself moves from stage to stage.
+constexpr int LONG_ROW = 1 << 22;
+bool bytes_in_reach(int32_t kc, int64_t extent, int64_t ld, int64_t kk) { return (kc ? extent : ld <= LONG_ROW ? 0 : kk) * ld * 2 < (int64_t)1 << 32; }
+bool offsets_fit(const GemmPlan& plan) {
+    for (int g = 0; g < plan.groups; ++g) {
+        const GemmShard& s = plan.s[g];
+        if (s.m && s.n && s.kk && !(bytes_in_reach(plan.a_kc, s.m, s.lda, s.kk) && bytes_in_reach(plan.b_kc, s.n, s.ldb, s.kk))) return false;
+    }
+    return true;
+}
+// Rows of an operand along the reduction that are within reach, whole tiles where there are as many.
+int rows_in_reach(int64_t ld) {
+    const int64_t rows = 0xFFFFFFFFll / (2 * ld);
+    return (int)std::min<int64_t>(rows < 256 ? rows : rows / 256 * 256, INT32_MAX);
+}
+
+// Operands out of reach: the product in ranges of rows of x and of columns of w that are not, a launch each.  256 x 8192 x 262144 (w exactly 4 GiB), an element a lane / this:
+// w along the reduction 964 / 1.01 ms, along its columns 437 / 0.87.  Where ranges do not help (stored rows of more than 2^22 elements that are not along the reduction, 4 GiB of them; one
+// row of 4 GiB), an element a lane.
+int32_t launch_block_ranges(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream) {
+    int rows = INT32_MAX, cols = INT32_MAX;
+    for (int g = 0; g < plan.groups; ++g) {
+        const GemmShard& s = plan.s[g];
+        if (!s.m || !s.n || !s.kk) continue;
+        if (plan.a_kc) rows = std::min(rows, rows_in_reach(s.lda));
+        if (plan.b_kc) cols = std::min(cols, rows_in_reach(s.ldb));
+    }
+    if (rows == 0 || cols == 0 || (rows >= max_m && cols >= max_n)) return launch_block_generic(plan, max_m, max_n, stream);
+    auto size = [&](int32_t bf16) { return plan.flags & bf16 ? 2 : 4; };
+    auto behind = [](const void* p, int64_t elements, int bytes) { return p ? const_cast<char*>(static_cast<const char*>(p)) + elements * bytes : nullptr; };
+    for (int64_t m0 = 0; m0 < max_m; m0 += rows)
+        for (int64_t n0 = 0; n0 < max_n; n0 += cols) {
+            GemmBlockPlan part = plan;
+            for (int g = 0; g < plan.groups; ++g) {
+                const GemmShard& from = plan.s[g];
+                const GemmExtra& x = plan.x[g];
+                GemmShard& s = part.s[g];
+                s.m = (int32_t)std::min<int64_t>(std::max<int64_t>(from.m - m0, 0), rows);
+                s.n = (int32_t)std::min<int64_t>(std::max<int64_t>(from.n - n0, 0), cols);
+                if (s.m == 0 || s.n == 0) continue;
+                s.a = behind(from.a, plan.a_kc ? m0 * from.lda : m0, 2);
+                s.b = behind(from.b, plan.b_kc ? n0 * from.ldb : n0, 2);
+                s.c = behind(from.c, m0 * from.ldc + n0, size(GB_OUT_BF16));
+                part.x[g].bias = behind(x.bias, n0, size(GB_BIAS_BF16));
+                part.x[g].residual = behind(x.residual, m0 * x.ldr + n0, size(GB_RESIDUAL_BF16));
+                part.x[g].pre = behind(x.pre, m0 * x.ldp + n0, size(GB_PRE_BF16));
+            }
+            const int32_t st = launch_linear(part, stream);
+            if (st != SBP_OK) return st;
+        }
+    return SBP_OK;
+}
+
 // The kernel for a product with a block's epilogue: launch_chosen's rules, over the kernels that have one.
 int32_t launch_block_chosen(const GemmBlockPlan& plan, const GemmPlan& like, int max_m, int max_n, hipStream_t stream) {
     const bool bf16 = plan.in_dtype == SBP_BF16, direct = rows_aligned(like);
     if (gemv_pays(like, max_m, max_n)) return launch_gemv(plan, max_m, max_n, stream);
     if (few_pays(like, max_m, max_n)) return launch_gemm_few(plan, max_m, max_n, stream);
-    if (one_element_pays(like, max_m, max_n, bf16 && direct) || (bf16 && !mfma_ok(like))) return launch_block_generic(plan, max_m, max_n, stream);
+    if (one_element_pays(like, max_m, max_n, bf16 && direct)) return launch_block_generic(plan, max_m, max_n, stream);
+    if (bf16 && !offsets_fit(like)) return launch_block_ranges(plan, max_m, max_n, stream);
     auto order = [&](int bm, int bn) { return tile_order_for(tiles_along(max_m, bm), tiles_along(max_n, bn)); };
     if (!bf16) {
         const int tile = f32_tile(like, max_m, max_n), b = tile == F32_128 || tile == TERMS_128 ? 128 : tile == F32_64 || tile == TERMS_64 ? 64 : 32;
