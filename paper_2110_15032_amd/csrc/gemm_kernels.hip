@@ -55,25 +55,31 @@ __device__ inline void store_out(uint16_t* c, int64_t pos, float v) {
 template <bool A_BF16, bool B_BF16, typename OutT, int EPI>
 __global__ __launch_bounds__(256) void gemm_generic_kernel(PlanOf<EPI> p) {
     const GemmShard s = p.s[blockIdx.z];
-    const int m = blockIdx.y * 16 + threadIdx.y;
     const int n = blockIdx.x * 16 + threadIdx.x;
-    if (m >= s.m || n >= s.n) return;
-    float acc = 0.0f;
-    for (int kk = 0; kk < s.kk; ++kk) {
-        const int64_t ia = p.a_kc ? (int64_t)m * s.lda + kk : (int64_t)kk * s.lda + m;
-        const int64_t ib = p.b_kc ? (int64_t)n * s.ldb + kk : (int64_t)kk * s.ldb + n;
-        float a, b;
-        if constexpr (A_BF16) a = bf16_to_f32(static_cast<const uint16_t*>(s.a)[ia]);
-        else a = static_cast<const float*>(s.a)[ia];
-        if constexpr (B_BF16) b = bf16_to_f32(static_cast<const uint16_t*>(s.b)[ib]);
-        else b = static_cast<const float*>(s.b)[ib];
-        acc = fmaf(a, b, acc);
-    }
-    if constexpr (EPI == EPI_BLOCK) {
-        float v[1] = {acc};
-        Ending<EPI>(p, blockIdx.z).template finish<1>(s, m, n, v);
+    auto sum = [&](int m) {
+        float acc = 0.0f;
+        for (int kk = 0; kk < s.kk; ++kk) {
+            const int64_t ia = p.a_kc ? (int64_t)m * s.lda + kk : (int64_t)kk * s.lda + m;
+            const int64_t ib = p.b_kc ? (int64_t)n * s.ldb + kk : (int64_t)kk * s.ldb + n;
+            float a, b;
+            if constexpr (A_BF16) a = bf16_to_f32(static_cast<const uint16_t*>(s.a)[ia]);
+            else a = static_cast<const float*>(s.a)[ia];
+            if constexpr (B_BF16) b = bf16_to_f32(static_cast<const uint16_t*>(s.b)[ib]);
+            else b = static_cast<const float*>(s.b)[ib];
+            acc = fmaf(a, b, acc);
+        }
+        return acc;
+    };
+    if constexpr (EPI == EPI_BLOCK) {   // more rows than a grid has places for are gone through in turns
+        if (n >= s.n) return;
+        for (int64_t m = (int64_t)blockIdx.y * 16 + threadIdx.y; m < s.m; m += (int64_t)gridDim.y * 16) {
+            float v[1] = {sum((int)m)};
+            Ending<EPI>(p, blockIdx.z).template finish<1>(s, (int)m, n, v);
+        }
     } else {
-        store_out(static_cast<OutT*>(s.c), (int64_t)m * s.ldc + n, epilogue<EPI>(acc));
+        const int m = blockIdx.y * 16 + threadIdx.y;
+        if (m >= s.m || n >= s.n) return;
+        store_out(static_cast<OutT*>(s.c), (int64_t)m * s.ldc + n, epilogue<EPI>(sum(m)));
     }
 }
 
@@ -2139,8 +2145,7 @@ int32_t launch_block_persist16(const GemmBlockPlan& plan, int max_m, int max_n, 
     return launch_status(__func__);
 }
 int32_t launch_block_generic(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t stream) {
-    const dim3 grid((uint32_t)tiles_along(max_n, 16), (uint32_t)tiles_along(max_m, 16), (uint32_t)plan.groups);
-    if (grid.y > 65535) return SBP_ERR_UNSUPPORTED;
+    const dim3 grid((uint32_t)tiles_along(max_n, 16), (uint32_t)std::min(tiles_along(max_m, 16), 65535), (uint32_t)plan.groups);
     if (plan.in_dtype == SBP_BF16) hipLaunchKernelGGL((gemm_generic_kernel<true, true, uint16_t, EPI_BLOCK>), grid, dim3(16, 16), 0, stream, plan);
     else hipLaunchKernelGGL((gemm_generic_kernel<false, false, float, EPI_BLOCK>), grid, dim3(16, 16), 0, stream, plan);
     return launch_status(__func__);
