@@ -8,28 +8,150 @@ import pytest
 import torch
 
 import paper_2110_15032_amd as sbp
-from train_harness import CODE, TYPE, column, room
+from train_harness import CODE, POISON, SIG, SIZE, TYPE, U, close, column, normal, room, rounded, slices, split
 
 pytestmark = pytest.mark.gpu
 E = 2.0 ** -24
 
 
+class Bucket:
+    """Tensors of a list in one buffer a device, `gap` bytes behind each (a number, or one for every tensor; a negative one: 16 and what is missing to the next 16), rows `pad`
+    elements apart behind the longest.  specs: (rows, cols, type, signature); data: the global tensors, or None for outputs."""
+
+    def __init__(self, k, specs, gap, data=None, pad=0):
+        self.k, self.specs = k, specs
+        gaps = [gap] * len(specs) if isinstance(gap, int) else gap
+        self.shapes = [[tuple(t.shape) for t in slices(torch.empty(r, c, device="meta"), sig, k)] for r, c, _, sig in specs]
+        self.pitch = [max(c for _, c in shapes) + pad if pad else 0 for shapes in self.shapes]
+        self.at, ends = [], [0] * k                                # byte offsets
+        for j, (_, _, kind, _) in enumerate(specs):
+            assert all(e % 16 == 0 for e in ends), "a tensor starts at 16 bytes"
+            self.at.append(list(ends))
+            for i in range(k):
+                ends[i] += self.used(j, i) * SIZE[kind]
+                ends[i] += gaps[j] if gaps[j] >= 0 else 16 + -ends[i] % 16
+        raw = [torch.full((e + 64,), POISON, dtype=torch.uint8) for e in ends]
+        if data is not None:
+            for j, x in enumerate(data):
+                for i, t in enumerate(slices(x, specs[j][3], k)):
+                    self.view(raw, j, i).copy_(t)
+        self.raw = [b.cuda() for b in raw]
+        self.list = sbp.SbpList([sbp.SbpTensor([b.data_ptr() + self.at[j][i] for i, b in enumerate(self.raw)], r, c, CODE[kind], 0, self.pitch[j])
+                                 for j, (r, c, kind, _) in enumerate(specs)], [SIG[s[3]] for s in specs])
+
+    def used(self, j, i):
+        rows, cols = self.shapes[j][i]
+        return (rows - 1) * (self.pitch[j] or cols) + cols if rows and cols else 0
+
+    def view(self, raw, j, i):
+        kind, at = self.specs[j][2], self.at[j][i]
+        if not self.used(j, i):
+            return torch.empty(self.shapes[j][i], dtype=TYPE[kind])
+        return raw[i][at:at + self.used(j, i) * SIZE[kind]].view(TYPE[kind]).as_strided(self.shapes[j][i], (self.pitch[j] or self.shapes[j][i][1], 1))
+
+    def host(self):
+        """[tensor][device] in 64 bits, after a look that nothing else was written."""
+        raw = [b.cpu() for b in self.raw]
+        got = [[self.view(raw, j, i).double() for i in range(self.k)] for j in range(len(self.specs))]
+        for j, (_, _, kind, _) in enumerate(self.specs):
+            blank = torch.full((SIZE[kind],), POISON, dtype=torch.uint8).view(TYPE[kind])
+            for i in range(self.k):
+                self.view(raw, j, i).copy_(blank.expand(self.shapes[j][i]))
+        assert all(bool((b == POISON).all()) for b in raw), "bytes outside the tensors were written"
+        return got
+
+
+def square_sum(bucket, k):
+    """The parts, twice the same bits, and nothing behind the workspace written."""
+    size, got = sbp.sbp_square_sum_workspace(bucket.list, k), []
+    for _ in range(2):
+        out, work = column(1, "f32", "B", k), torch.full((size + 64,), 0xFF, dtype=torch.uint8, device="cuda")
+        sbp.sbp_square_sum(bucket.list, out.desc, work[:size], k)
+        got.append([float(t[0, 0]) for t in out.host()])
+        assert bool((work[size:] == 0xFF).all())
+    assert got[0] == got[1]
+    return out, got[0]
+
+
+def check(k, specs, in_gap, out_gap=None, kinds=None, pad=0, out_pad=0, seed=0, factor=0.37):
+    """Sums and clipping; out_gap None: in place, else results of `kinds` (one for every tensor) with such gaps."""
+    data = [rounded(normal(r, c, seed=seed + j, scale=10.0 ** (j % 3 - 1)), kind) for j, (r, c, kind, _) in enumerate(specs)]
+    b = Bucket(k, specs, in_gap, data, pad)
+    parts, got = square_sum(b, k)
+    for i in range(k):
+        want = 0.0
+        for x, (_, _, _, sig) in zip(data, specs):
+            local = slices(x, sig, k)[i]
+            if sig == "B":
+                begin, end = split(x.shape[0], k)[i]
+                local = local[begin:end]
+            want += float((local ** 2).sum())
+        assert abs(got[i] - want) <= 1.01 * E * want, (i, got[i], want)
+    norm = math.sqrt(sum(float((x ** 2).sum()) for x in data))
+    out = b if out_gap is None else Bucket(k, [(r, c, kind, sig) for (r, c, _, sig), kind in zip(specs, kinds)], out_gap, None, out_pad)
+    of = column(1, "f32", "B", k)
+    sbp.sbp_clip(b.list, parts.desc, sbp.P_SUM, factor * norm, out.list, of.desc, k)
+    for t in of.host():
+        assert abs(float(t[0, 0]) - norm) <= 1.01 * E * ((k + 1) / 2 + 1) * norm
+    for j, (locals_, x) in enumerate(zip(out.host(), data)):
+        u = U[out.specs[j][2]]
+        for y, part in zip(locals_, slices(x, specs[j][3], k)):
+            want = part * factor
+            close(y, want, (1.01 * ((k + 1) / 2 + 3) * E + 1.001 * u) * want.abs(), f"tensor {j}")
+    if out is not b:
+        assert all(torch.equal(p, q) for row, x, s in zip(b.host(), data, specs) for p, q in zip(row, slices(x, s[3], k)))
+
+
+# rows of whole 16 bytes, so that a device's part of a tensor ends where the next one may start; 8192 elements are a chunk
+SEAMS = [(1, 8), (3, 40), (5, 8192), (7, 1000), (2, 4104), (1, 16), (9, 2048), (4, 8200), (64, 72)]
+
+
+def seams(kinds, sigs):
+    return [(r, c, kinds[j % len(kinds)], sigs[j % len(sigs)]) for j, (r, c) in enumerate(SEAMS)]
+
+
+@pytest.mark.parametrize("k,sigs", [(1, ("B",)), (1, ("S0",)), (3, ("S0",)), (3, ("B",)), (2, ("B", "S0")), (9, ("S0", "B"))])
+@pytest.mark.parametrize("kinds", [("f32",), ("bf16",), ("bf16", "f32"), ("f32", "f32", "bf16")])
+def test_tensors_back_to_back(k, sigs, kinds):
+    """whole buckets, buckets whose type changes at a seam, and results that lie back to back where the inputs do not, or the other way round"""
+    specs = seams(kinds, sigs)
+    check(k, specs, 0)                                                           # in place
+    for out_kinds in (["f32"] * 9, ["bf16"] * 9, ["f32", "bf16", "bf16"] * 3):
+        check(k, specs, 0, 0, out_kinds)
+    check(k, specs, 0, 16, ["f32"] * 9)
+    check(k, specs, 16, 0, ["bf16"] * 9)
+    check(k, specs, [0, 16, 0, 0, 48, 0, 0, 16, 0], [0, 0, 16, 0, 0, 0, 32, 0, 0], ["bf16", "bf16", "f32"] * 3)
+
+
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-@pytest.mark.parametrize("short", [2, 4, 7])
-def test_rows_that_end_just_below_two_to_the_31(kind, short):
-    """the last columns of rows at a pitch, whose place plus eight is past 2^31"""
-    rows, pitch = 2, 2 ** 31 - 1
-    cols = 2 ** 31 - short
-    raw = torch.zeros((rows - 1) * pitch + cols, dtype=TYPE[kind], device="cuda")
-    x = raw.as_strided((rows, cols), (pitch, 1))
-    tail = torch.tensor([[3.0, 8, 1, 12, 5, 2, 7, 4, 9, 6, 11, 10], [2.0, 5, 9, 1, 7, 12, 3, 8, 10, 4, 6, 11]], device="cuda")
-    x[:, -12:] = tail
-    lst = sbp.SbpList([sbp.SbpTensor([raw], rows, cols, CODE[kind], 0, pitch)], [sbp.B])
-    out, norm = column(1, "f32", "B", 1), column(1, "f32", "B", 1)
-    sbp.sbp_square_sum(lst, out.desc, room(sbp.sbp_square_sum_workspace(lst, 1)), 1)
-    total = float((tail ** 2).sum())
-    assert float(out.host()[0][0, 0]) == total                                             # whole numbers
-    sbp.sbp_clip(lst, out.desc, sbp.B, 0.5 * math.sqrt(total), lst, norm.desc, 1)
-    got = x[:, -12:].float()
-    assert bool(((got - 0.5 * tail).abs() <= 4 * E * tail).all()), got
-    assert int(raw.count_nonzero()) == 24
+def test_one_long_bucket(kind):
+    """more chunks than the workgroups of a launch, most of them across seams"""
+    check(1, [(131, 1000, kind, "S0")] * 150, 0, 0, ["f32"] * 150)
+
+
+def test_back_to_back_past_a_launch():
+    """tensors that join, and between them more that do not than a launch has places for"""
+    specs = [(1, 8, "f32", "S0"), (1, 8, "f32", "B"), (2, 16, "bf16", "S0")] * 130
+    check(2, specs, [(0, 0, 16)[j % 3] for j in range(390)], 0, ["bf16"] * 390)
+
+
+# parts of a launch: up to 16, 64, 160 in one row each, up to 16, 80 with rows at a pitch
+@pytest.mark.parametrize("k,n", [(1, 65), (1, 160), (1, 161), (1, 700), (2, 81), (2, 350), (3, 107), (5, 33), (9, 40), (64, 1), (64, 5), (64, 11)])
+@pytest.mark.parametrize("pad", [0, 3])
+def test_many_parts(k, n, pad):
+    """one device in several launches, several devices in one, and both"""
+    specs = [(k + j % 5 if j % 7 else max(1, k - 3), 3 + 5 * j % 37, "f32" if j % 3 else "bf16", "B" if j % 4 == 1 else "S0") for j in range(n)]
+    check(k, specs, -1, pad=pad, seed=n)
+    check(k, specs, -1, -1, ["bf16" if j % 2 else "f32" for j in range(n)], pad=pad, out_pad=0 if pad else 2, seed=n)
+
+
+@pytest.mark.parametrize("k", [9, 64])
+def test_large_tensors_on_many_devices(k):
+    check(k, [(300, 1001, "bf16", "S0"), (70, 5000, "f32", "B"), (3, 9000, "f32", "B"), (129, 700, "f32", "S0")], -1, -1, ["f32", "bf16", "f32", "bf16"])
+    check(k, [(300, 1001, "bf16", "S0"), (70, 5000, "f32", "B"), (129, 700, "f32", "S1")], -1, -1, ["f32", "bf16", "f32"], pad=5, out_pad=8)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_shares_of_a_copy_that_start_at_any_element(kind):
+    """whole chunks from 1 to 7 elements behind a vector's start"""
+    check(8, [(8, 40001, kind, "B"), (8, 16387, kind, "B")], -1)
