@@ -117,20 +117,21 @@ __device__ inline void each_vector(const Shape& s, int chunk, F&& f) {
 }
 // all of the chunk's vectors are whole ones of one row
 __device__ inline bool whole_chunk(const Shape& s, int chunk) { return s.rows == 1 && ((int64_t)chunk + 1) * (LIST_CHUNK * 8) <= s.cols; }
-// Whole chunks: G consecutive elements a lane and load, so that the loads and stores of a wave are of consecutive bytes where the wider side has 16 of a lane.
+// Whole chunks: G consecutive elements a lane and load, so that the loads and stores of a wave are of consecutive bytes where the wider side has 16 of a lane.  At an element's
+// alignment: a device's share of a copy starts at any row.
 template <int T, int G>
 struct Group;   // G elements as they are stored
 template <>
 struct Group<T_F32, 4> {
-    typedef f32x4 type;
+    typedef f32x4_any type;
 };
 template <>
 struct Group<T_BF16, 4> {
-    typedef u32x2 type;
+    typedef u32x2_half type;
 };
 template <>
 struct Group<T_BF16, 8> {
-    typedef u32x4 type;
+    typedef u32x4_any type;
 };
 template <int T, int G>
 __device__ inline void widen_group(const typename Group<T, G>::type r, float (&v)[G]) {

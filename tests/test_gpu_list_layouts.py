@@ -155,3 +155,30 @@ def test_large_tensors_on_many_devices(k):
 def test_shares_of_a_copy_that_start_at_any_element(kind):
     """whole chunks from 1 to 7 elements behind a vector's start"""
     check(8, [(8, 40001, kind, "B"), (8, 16387, kind, "B")], -1)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+def test_shares_of_a_copy_that_start_at_any_element(kind):
+    """whole chunks from 1 to 7 elements behind a vector's start"""
+    check(8, [(8, 40001, kind, "B"), (8, 16387, kind, "B")], -1)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "f32"])
+@pytest.mark.parametrize("short", [2, 4, 7])
+def test_rows_that_end_just_below_two_to_the_31(kind, short):
+    """the last columns of rows at a pitch, whose place plus eight is past 2^31"""
+    rows, pitch = 2, 2 ** 31 - 1
+    cols = 2 ** 31 - short
+    raw = torch.zeros((rows - 1) * pitch + cols, dtype=TYPE[kind], device="cuda")
+    x = raw.as_strided((rows, cols), (pitch, 1))
+    tail = torch.tensor([[3.0, 8, 1, 12, 5, 2, 7, 4, 9, 6, 11, 10], [2.0, 5, 9, 1, 7, 12, 3, 8, 10, 4, 6, 11]], device="cuda")
+    x[:, -12:] = tail
+    lst = sbp.SbpList([sbp.SbpTensor([raw], rows, cols, CODE[kind], 0, pitch)], [sbp.B])
+    out, norm = column(1, "f32", "B", 1), column(1, "f32", "B", 1)
+    sbp.sbp_square_sum(lst, out.desc, room(sbp.sbp_square_sum_workspace(lst, 1)), 1)
+    total = float((tail ** 2).sum())
+    assert float(out.host()[0][0, 0]) == total                                             # whole numbers
+    sbp.sbp_clip(lst, out.desc, sbp.B, 0.5 * math.sqrt(total), lst, norm.desc, 1)
+    got = x[:, -12:].float()
+    assert bool(((got - 0.5 * tail).abs() <= 4 * E * tail).all()), got
+    assert int(raw.count_nonzero()) == 24
