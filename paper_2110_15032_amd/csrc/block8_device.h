@@ -73,9 +73,7 @@ __device__ inline Raw8<T> load8(const char* row, int c, int cols) {
     return r;
 }
 template <int T>
-__device__ inline Raw8<T> settle8(Raw8<T> r, int c, int cols) {
-    const int gone = c + 8 - cols;   // 1 .. 7: that many elements in front belong to the lane before
-    if (gone <= 0 || gone >= 8 || cols < 8) return r;
+__device__ inline Raw8<T> without_front(Raw8<T> r, int gone) {   // 1 .. 7 elements
     if constexpr (T == T_F32) {
         float v[8] = {r.a[0], r.a[1], r.a[2], r.a[3], r.b[0], r.b[1], r.b[2], r.b[3]};
 #pragma unroll
@@ -92,6 +90,12 @@ __device__ inline Raw8<T> settle8(Raw8<T> r, int c, int cols) {
         const uint64_t x = ((uint64_t)r.w[1] << 32 | r.w[0]) >> (gone * 8);
         return {u32x2{(uint32_t)x, (uint32_t)(x >> 32)}};
     }
+}
+// c: at most 2^31 - 9
+template <int T>
+__device__ inline Raw8<T> settle8(Raw8<T> r, int c, int cols) {
+    const int gone = c + 8 - cols;   // 1 .. 7: that many elements in front belong to the lane before
+    return gone <= 0 || gone >= 8 || cols < 8 ? r : without_front<T>(r, gone);
 }
 template <int T>
 __device__ inline void store8(void* at, const Raw8<T> r, int valid, bool stream = false) {

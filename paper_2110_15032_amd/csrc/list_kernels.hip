@@ -115,6 +115,12 @@ __device__ inline void each_vector(const Shape& s, int chunk, F&& f) {
         f(u, row, (int64_t)0, (int)v * 8, row < s.rows ? (int)s.cols : 0);
     }
 }
+// settle8 of rows that may be as long as 2^31 - 1
+template <int T>
+__device__ inline Raw8<T> settle_any8(const Raw8<T> r, int c, int cols) {
+    const int left = cols - c;
+    return left >= 8 || left <= 0 || cols < 8 ? r : without_front<T>(r, 8 - left);
+}
 // all of the chunk's vectors are whole ones of one row
 __device__ inline bool whole_chunk(const Shape& s, int chunk) { return s.rows == 1 && ((int64_t)chunk + 1) * (LIST_CHUNK * 8) <= s.cols; }
 // Whole chunks: G consecutive elements a lane and load, so that the loads and stores of a wave are of consecutive bytes where the wider side has 16 of a lane.  At an element's
@@ -202,7 +208,7 @@ __device__ inline void square_chunk(const void* in, const Shape& s, int chunk, d
     float v[8];
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) { raw[u] = load8<T>(static_cast<const char*>(in) + (row * s.ldi + from) * bytes_of<T>, c, cols); });
     each_vector(s, chunk, [&](int u, int64_t, int64_t, int c, int cols) {
-        widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
+        widen<T>(settle_any8<T>(raw[u], c, cols), 1.0f, v);
         add_squares(v, acc);
     });
 }
@@ -272,7 +278,7 @@ __device__ inline void clip_chunk(const void* in, void* out, const Shape& s, int
     float v[8];
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) { raw[u] = load8<T>(static_cast<const char*>(in) + (row * s.ldi + from) * bytes_of<T>, c, cols); });
     each_vector(s, chunk, [&](int u, int64_t row, int64_t from, int c, int cols) {
-        widen<T>(settle8<T>(raw[u], c, cols), 1.0f, v);
+        widen<T>(settle_any8<T>(raw[u], c, cols), 1.0f, v);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] *= factor;
         store8<U>(static_cast<char*>(out) + (row * s.ldo + from + c) * bytes_of<U>, narrow<U>(v), cols - c);   // none of them where cols - c is not positive

@@ -158,12 +158,6 @@ def test_shares_of_a_copy_that_start_at_any_element(kind):
 
 
 @pytest.mark.parametrize("kind", ["bf16", "f32"])
-def test_shares_of_a_copy_that_start_at_any_element(kind):
-    """whole chunks from 1 to 7 elements behind a vector's start"""
-    check(8, [(8, 40001, kind, "B"), (8, 16387, kind, "B")], -1)
-
-
-@pytest.mark.parametrize("kind", ["bf16", "f32"])
 @pytest.mark.parametrize("short", [2, 4, 7])
 def test_rows_that_end_just_below_two_to_the_31(kind, short):
     """the last columns of rows at a pitch, whose place plus eight is past 2^31"""
