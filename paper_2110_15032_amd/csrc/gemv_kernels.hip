@@ -15,8 +15,9 @@ __device__ inline void add8(const float (&x)[8], const float (&w)[8], float& acc
 
 // Weights with the reduction index contiguous.  A wave takes R rows of the weight and every WK-th 512 elements of them, eight a lane; where the waves of a
 // workgroup share rows (WK > 1) their sums meet in LDS, in order.
-// STREAM: the weight past the caches, where the memory-side cache would not keep it for the next token.  us, past them / cached: 4096 x 16384 on 8 devices (134 MB) 24.3 /
-// 25.7, 4 rows 26.9 / 29.0; 4096 x 4096 8.2 / 7.8; fp32 3000 x 8000 (96 MB, four of them in turn) 27.4 / 22.8.
+// STREAM: the weight past the caches: in bf16, where a token's weights do not stay in the memory-side cache.  us, past them / cached, four weights in turn: 4096 x 16384 (134 MB)
+// 23.8 / 25.7, 4 rows 26.8 / 28.7; 101 MB 19.3 / 20.8, 84 MB 17.5 / 18.7, 67 MB 14.1 / 14.1, 50 MB 10.8 / 10.2, 4 rows 18.4 / 16.1; columns contiguous 134 MB 27.4 / 29.4, 84 MB
+// 18.6 / 20.1, 67 MB 16.3 / 15.6.  Not in fp32, whose eight elements are two loads of half a line each: 134 MB 32.8 / 29.8, 101 MB 22.7 / 18.7, 403 MB 84.9 / 78.5.
 template <int T, int M, int R, int WK, bool STREAM>
 __global__ __launch_bounds__(256) void gemv_rows_kernel(GemmBlockPlan p) {
     constexpr int GROUPS = 4 / WK, AHEAD = R == 4 && M == 1 ? 4 : 2;   // steps on their way together: 4096 x 16384, one row, two 25.0 us, four 24.3; one row of the weight a wave, 4096 x 4096, two 7.9, four 10.5
@@ -244,8 +245,8 @@ int32_t launch_gemv(const GemmBlockPlan& plan, int max_m, int max_n, hipStream_t
         });
         return launch_status("launch_gemv");
     };
-    auto typed = [&](auto past) { return f32 ? go(std::integral_constant<int, T_F32>{}, past) : go(std::integral_constant<int, T_BF16>{}, past); };
-    return weight >= (int64_t)128 << 20 ? typed(std::true_type{}) : typed(std::false_type{});
+    if (f32) return go(std::integral_constant<int, T_F32>{}, std::false_type{});
+    return weight > (int64_t)64 << 20 ? go(std::integral_constant<int, T_BF16>{}, std::true_type{}) : go(std::integral_constant<int, T_BF16>{}, std::false_type{});   // see STREAM
 }
 
 // 1 .. FEW_ROWS rows, bf16, both operands with the reduction index contiguous
