@@ -91,9 +91,10 @@ typedef struct sbp_tensor {
                            125000-column logits shards: pitch 125056).  Accepted by sbp_matmul,
                            sbp_matmul_ex, sbp_matmul_rowmax, sbp_matmul_2d, sbp_row_max,
                            sbp_row_sumexp, sbp_xent_loss and sbp_xent_grad, and for the activations,
-                           their gradients and the matrices of the operators on 8-bit tensors and of
-                           layer normalisation; the boxing entry
-                           points take dense tensors only (SBP_ERR_UNSUPPORTED).                */
+                           their gradients and the matrices of the operators on 8-bit tensors, of
+                           layer normalisation, of layers and of the norms around a block, and for the
+                           tensors of a list; the boxing entry points and vectors [n, 1] next to such
+                           matrices are dense (SBP_ERR_UNSUPPORTED).                            */
 } sbp_tensor_t;
 
 /* ---- the scales of an 8-bit tensor ----------------------------------------
@@ -368,7 +369,7 @@ int32_t sbp_linear(const sbp_tensor_t* x, sbp_t sbp_x, const sbp_tensor_t* w, sb
  *   SBP_EPI_GELU: da = dy * gelu'(pre), as sbp_gelu_grad gives it, pre SBP_F32, SBP_BF16 or in 8 bits (with pre_scales; NULL else);
  *                 dbias = the sum of da, before its rounding, over the rows
  *   SBP_EPI_NONE: dbias = the sum of dy over the rows; pre, pre_scales and da are NULL (SBP_ERR_UNSUPPORTED)
- * dy, da SBP_F32 or SBP_BF16, one type; all S or B under one signature.  dbias [N,1] SBP_F32: for dy S(0) a whole vector on every
+ * dy, da SBP_F32 or SBP_BF16, one type; all S or B under one signature, trans = 0; at most 2^31 - 257 rows and columns (SBP_ERR_UNSUPPORTED).  dbias [N,1] SBP_F32: for dy S(0) a whole vector on every
  * device, P(sum); for S(1) S(0); for B B.  Sums are made in fp32 in an order that depends on the sizes alone.  workspace: device memory of
  * sbp_linear_grad_workspace() bytes, 16-byte aligned, whose contents do not matter before or after the call (NULL where that is 0;
  * SBP_ERR_SHAPE if workspace_bytes is too little).  Calls that may overlap in time need one each. */
@@ -382,9 +383,9 @@ int32_t sbp_linear_grad_workspace(int64_t rows, int64_t cols, sbp_t sbp_dy, int3
  *   t = post(x) (post NULL: x),  h = alpha * r + gate * t,  y = pre(h) (pre NULL: none, and y NULL)
  * A norm is (v - mean) * rstd * gamma + beta with the row's mean (SBP_NORM_RMS: 0, no beta, no mean) and rstd = 1 / sqrt(sum((v - mean)^2)
  * / C + eps).  x and the residual stream (r, h, one type) SBP_F32 or SBP_BF16; y in any of the two or in 8 bits (with
- * y_scales, NULL else); all under x's signature.  gate [C,1], B, or NULL (ones); gate and the norms' gamma and beta are of
+ * y_scales, NULL else); all under x's signature, trans = 0.  gate [C,1], B, or NULL (ones); gate and the norms' gamma and beta are of
  * one type, SBP_F32 or SBP_BF16.  Everything is computed in fp32 (the sums of a row's elements and of their squares have to be below 2^128),
- * y and the second norm's statistics from h before its rounding; h and y are rounded once.  At most 32 devices and rows of 16384
+ * y and the second norm's statistics from h before its rounding; h and y are rounded once.  At most 32 devices, 2^31 - 257 rows of 16384
  * elements, and no S(1) (SBP_ERR_UNSUPPORTED); a P tensor is SBP_ERR_SIGNATURE; rows of no elements have no statistics
  * (SBP_ERR_SHAPE where they are asked for). */
 enum {

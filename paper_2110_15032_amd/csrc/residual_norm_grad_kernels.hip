@@ -8,8 +8,9 @@
 // so that five weights' gradients need four sums a column.  Without the first norm xhat is x, gamma1 1 and beta1 0.  Bound by HBM: the four inputs
 // of a row are read once.  Sums over rows stay in a workgroup's registers (rows of more than 8192: half of them in LDS), its partial sums go to the caller's workspace
 // and are joined in order.  A workgroup goes down its rows with one row ahead; what holds it is a row's chain (two sums over waves, behind one another).  16384 x
-// 4096 bf16, both norms layer, 8 devices 152 .. 162 us (154 + 7 for the join; 805 MB, 5.2 TB/s); 1767 x 1001 fp32, 3 devices 21 (18 + 4); rows of more than 8192 keep two of
-// the sums in LDS and spill what the compute unit has no registers for: 4532 x 11752 210 us (3.0 TB/s), 4096 x 12288 156.
+// 4096 bf16, both norms layer, 8 devices 152 .. 162 us (154 + 7 for the join; 805 MB, 5.2 TB/s); 1767 x 1001 fp32, 3 devices 21 (18 + 4).  1024 threads have 128 registers each, and spill what does not
+// fit: in rows of 4097 to 8192 75 to 89 of them with an fp32 stream and another fp32 operand, 40 to 45 with an fp32 stream alone or fp32 x and dy around a bf16 one, at most 6
+// else; in rows of more than 8192, which keep two of the sums in LDS, 15 to 36: 4532 x 11752 210 us (3.0 TB/s), 4096 x 12288 156.
 #include "row_device.h"
 
 namespace sbp {
@@ -345,7 +346,7 @@ int threads_of(int64_t cols) { return cols <= 512 ? 64 : cols <= 1024 ? 128 : co
 }  // namespace
 
 // One workgroup a CU, two or four where a row is short and there are enough rows: more hide more, but each reads the weights and leaves four sums a column for
-// the join.  us, 256 / 512 / 1024 workgroups, bf16: 31327 x 360 79 / 54 / 47, 16384 x 768 60.5 / 41.8 / 49.7, 4096 x 768 21.3 / 17.0, 32768 x 1024 129 / 88 / 90, 8192 x
+// the join.  With 512 threads a row (130 to 141 registers; 128 in a launch for one device, all bf16) and with 1024 a CU holds one workgroup, so that what is more waits.  us, 256 / 512 / 1024 workgroups, bf16: 31327 x 360 79 / 54 / 47, 16384 x 768 60.5 / 41.8 / 49.7, 4096 x 768 21.3 / 17.0, 32768 x 1024 129 / 88 / 90, 8192 x
 // 1537 67 / 48 / 56, but 1024 x 1024 11.3 / 13.2, 2000 x 1024 15.2 / 16.3; 8192 x 2560 58 / 62 / 72, 16384 x 4096 155 / 163 / 170, 4096 x 8192 96 / 108 / 133.
 int32_t residual_norm_grad_blocks(int64_t rows, int64_t cols, int32_t k) {
     const int64_t g = std::max(1, 256 / threads_of(cols)), turns = (rows + g - 1) / g;

@@ -289,7 +289,7 @@ int32_t launch_gemm_f8(const GemmF8Plan& plan, hipStream_t stream);
 // ---------------------------------------------------------------------------------------------
 // An argument block costs about a microsecond a KB, so a launch has one of about its own size: places for CAP local tensors, S devices.
 constexpr int LIST_CHUNK = 1024;    // vectors of eight elements that a workgroup takes at a time, of one local tensor
-constexpr int LIST_BLOCKS = 2048;   // workgroups of a launch: eight a compute unit, as many as it holds
+constexpr int LIST_BLOCKS = 2048;   // most workgroups of a launch of the sum of squares: eight a compute unit, as many as it holds (clipping has one for every chunk)
 constexpr int LIST_DENSE = 160, LIST_PITCHED = 80, LIST_SOME = 64, LIST_FEW = 16;   // CAP, at most 192
 // A dense local tensor.  info: elements, from bit 48 on what of_list() says.
 template <bool OUT>
@@ -321,12 +321,13 @@ struct SquarePlan {
     int32_t parts, first_device, turns, first_turn, other_turn;
     int32_t stream;   // past the caches
 };
-// The partial sums of a device: `count` from its first place on, and those of tensors with a pitch, `pitched` from behind `dense_turns` turns on.
+// The partial sums of device d, `blocks` of them a turn: those of dense[d] turns from turn d * turns on, and those of tensors with a pitch, of pitched[d] turns from `dense_turns` turns
+// further on.  A device's turns: the launches that it has parts in.
 template <int S>
 struct SquareJoin {
     const double* partial;
     int32_t blocks, turns, dense_turns;
-    int16_t dense[S], pitched[S];   // turns
+    int16_t dense[S], pitched[S];
     float* out[S];
 };
 template <template <bool> class PART, int CAP, int S>
